@@ -139,7 +139,13 @@ typedef struct moe_gating {
 } moe_gating;
 
 /* Which entry point a workspace size refers to. */
-enum moe_entry { MOE_ENTRY_PERMUTE = 1, MOE_ENTRY_EXPERT_FFN = 2, MOE_ENTRY_FORWARD = 3 };
+enum moe_entry {
+    MOE_ENTRY_PERMUTE = 1,
+    MOE_ENTRY_EXPERT_FFN = 2,
+    MOE_ENTRY_FORWARD = 3,
+    MOE_ENTRY_EXPERT_FFN_I8 = 4,
+    MOE_ENTRY_FORWARD_I8 = 5
+};
 
 /* Stages of moe_forward, for the optional timing events of moe_taps. */
 enum moe_stage {
@@ -187,7 +193,7 @@ size_t moe_workspace_bytes(const moe_dims *dims, int entry);
 
 /*
  * Host-only check of dims against the limits of entry point `entry` (0: of
- * every entry point) and, when entry != 0, of ws_bytes against
+ * every bf16 entry point) and, when entry != 0, of ws_bytes against
  * moe_workspace_bytes(dims, entry).  Returns MOE_OK or the status the entry
  * point would return for these sizes.  Makes no HIP call.
  */
@@ -331,6 +337,124 @@ int moe_forward_noalloc(const moe_dims *dims, const moe_gating *gating,
                         const moe_bf16 *x, const int32_t *local_experts,
                         const moe_weights *weights, int64_t *counts,
                         moe_bf16 *out, const moe_taps *taps, void *stream);
+
+/*
+ * ---- 8-bit integer experts ------------------------------------------------
+ *
+ * The experts' matrices and their inputs in int8, one scale per output channel
+ * of a matrix and one per row (token) of an input: half the weight bytes that
+ * decode reads, and twice the matrix rate in prefill.  A value stands for
+ * q * scale.
+ *
+ * Rows of int8 lie a multiple of 16 bytes apart and start 16-byte aligned.  A
+ * row of K values that is not a multiple of 16 long goes on with zeros up to
+ * the next multiple, as moe_quantize_rows writes it.
+ */
+
+/*
+ * Symmetric quantisation of each row, for activations at every step and for
+ * weights once (a row of a weight matrix is an output channel):
+ *   a = max_c |x[r][c]|;  scale[r] = a / 127;  q[r][c] = 127 x[r][c] / a
+ * rounded to the nearest integer, ties to even, exactly (no result depends on
+ * how fp32 rounds the quotient); scale 0 and q 0 where a = 0.  A row that holds
+ * a NaN or an infinity gets scale NaN and q 0.
+ *   x      bf16, row r at x + r*ldx (ldx >= cols values, any alignment).
+ *   q      int8 out, row r at q + r*ldq (ldq >= cols, a multiple of 16),
+ *          written up to the next multiple of 16 of cols (zeros past cols).
+ *   scale  [rows] fp32 out.
+ * rows = 0 is a no-op.  x and q must not overlap.
+ */
+int moe_quantize_rows(int32_t rows, int32_t cols, const moe_bf16 *x, int64_t ldx,
+                      int8_t *q, int64_t ldq, float *scale, void *stream);
+
+/*
+ * Sizes of an 8-bit product.
+ *   M         rows of the result (grouped: the capacity of y; rows past
+ *             offsets[G] are left as they were).
+ *   N, K      output channels and inner dimension.
+ *   G         groups (experts) of moe_grouped_linear_i8, 1..1024.
+ *   X         rows of xq where they are read through x_rows.
+ *   ldx, ldw  row strides of xq and wq in bytes: multiples of 16, at least K
+ *             rounded up to 16, at most 2^21.
+ *   ldy       row stride of y in values, at least N.
+ * Limits (MOE_ERR_UNSUPPORTED beyond them): K < 2^17 (the int32 sums are then
+ * exact for any int8 values), N <= 2^24, ldy <= 2^21 and, with x_rows,
+ * X*ldx < 2^31.
+ */
+typedef struct moe_linear_dims {
+    int32_t M, N, K, G, X;
+    int64_t ldx, ldw, ldy;
+} moe_linear_dims;
+
+/*
+ * y[r][n] = (sum_c xq[r][c] wq[n][c]) * w_scale[n] * x_scale[r], the sum exact
+ * in int32, the products in fp32, one rounding to bf16.
+ *   xq [M] rows, x_scale [M], wq [N] rows, w_scale [N], y [M] rows out.
+ * Uses M, N, K and the strides.  M = 0 is a no-op.
+ */
+int moe_linear_i8(const moe_linear_dims *dims, const int8_t *xq, const float *x_scale,
+                  const int8_t *wq, const float *w_scale, moe_bf16 *y, void *stream);
+
+/*
+ * The same over ragged groups of rows, each with a weight matrix of its own
+ * (one expert's): for r in [offsets[g], offsets[g+1])
+ *   y[r][n] = (sum_c X[r][c] wq[g][n][c]) * w_scale[g][n] * (X's scale of r)
+ * with X[r] = xq[r], or xq[x_rows[r]] (and its scale) when x_rows is given.
+ *   offsets  [G+1] int32 device, not decreasing, in [0, M], as written by
+ *            moe_permute; offsets[0] > 0 and groups without rows are allowed.
+ *   x_rows   [M] int32 device, nullable (moe_permute's perm_token); an entry
+ *            outside [0, X) stands for a row of zeros.
+ *   wq       [G][N] rows, w_scale [G][N].
+ * M = 0 is a no-op.
+ */
+int moe_grouped_linear_i8(const moe_linear_dims *dims, const int8_t *xq, const float *x_scale,
+                          const int32_t *x_rows, const int32_t *offsets, const int8_t *wq,
+                          const float *w_scale, moe_bf16 *y, void *stream);
+
+/*
+ * Expert weights in int8, by output channel, stacked by local slot as in
+ * moe_weights.  Rows are dense but for the padding to 16: Hp, Ip and Wp are H,
+ * I and n_shared*I_shared rounded up to multiples of 16.
+ *   w_gate, w_up   [E_local][I][Hp]    w_down   [E_local][H][Ip]
+ *   s_gate, s_up   [E_local][I]        s_down   [E_local][H]     fp32 scales
+ * The shared experts are one FFN of width W = n_shared*I_shared (their sum is
+ * that FFN): gate and up stacked, the rows of down side by side, so that a
+ * channel of their sum has one scale.
+ *   sh_gate, sh_up [W][Hp]             sh_down  [H][Wp]
+ *   sh_s_gate, sh_s_up [W]             sh_s_down [H]
+ * The shared pointers may be NULL when n_shared == 0.
+ */
+typedef struct moe_weights_i8 {
+    const int8_t *w_gate, *w_up, *w_down;
+    const float *s_gate, *s_up, *s_down;
+    const int8_t *sh_gate, *sh_up, *sh_down;
+    const float *sh_s_gate, *sh_s_up, *sh_s_down;
+} moe_weights_i8;
+
+/*
+ * moe_expert_ffn on int8 experts: rows are quantised as by moe_quantize_rows,
+ * gate and up are products as above (in fp32, not rounded), h = silu(gate) * up
+ * is rounded to bf16 and quantised by row again, and y_perm is the product of
+ * that with down.  y_shared (bf16) is the shared FFN of x.
+ * Arguments as moe_expert_ffn's, x_perm and x in bf16; rows of y_perm past
+ * offsets[E_local] are left as they were.
+ *   ws  MOE_ENTRY_EXPERT_FFN_I8 workspace.
+ * Limits as there, and H, I, n_shared*I_shared < 2^17.
+ */
+int moe_expert_ffn_i8(const moe_dims *dims, const moe_bf16 *x_perm, const int32_t *offsets,
+                      const moe_weights_i8 *weights, const moe_bf16 *x, moe_bf16 *y_perm,
+                      moe_bf16 *y_shared, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * moe_forward on int8 experts: the layer as there, with moe_expert_ffn_i8's
+ * networks (x is quantised once per token).  Stage MOE_STAGE_FFN_UP includes
+ * the quantisation of x, MOE_STAGE_FFN_DOWN that of the hidden rows.
+ *   ws  MOE_ENTRY_FORWARD_I8 workspace.
+ */
+int moe_forward_i8(const moe_dims *dims, const moe_gating *gating, const float *logits,
+                   const int32_t *src, const moe_bf16 *x, const int32_t *local_experts,
+                   const moe_weights_i8 *weights, int64_t *counts, moe_bf16 *out,
+                   const moe_taps *taps, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * ---- Source-aware expert placement (Sec. 5.2 objective, Sec. 5.3 greedy) ---

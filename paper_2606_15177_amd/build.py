@@ -23,6 +23,8 @@ ARCH = "gfx950"
 
 SOURCES = ["route.hip", "permute.hip", "combine.hip", "ffn_skinny.hip", "ffn_mid.hip", "ffn_tiled.hip", "place.hip", "window.hip",
            "moe_abi.hip"]
+# the 8-bit experts
+SOURCES_I8 = ["quant.hip", "gemm_i8.hip"]
 
 CXXFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -65,8 +67,9 @@ def _check_resolved(lib: str) -> None:
 def build(verbose: bool = False) -> str:
     """Compile and link the library; returns its path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 1)) as ex:
-        objs = list(ex.map(_compile, SOURCES))
+    sources = SOURCES + SOURCES_I8
+    with cf.ThreadPoolExecutor(max_workers=min(len(sources), os.cpu_count() or 1)) as ex:
+        objs = list(ex.map(_compile, sources))
     tmp = LIB_PATH + ".tmp"
     cmd = [_hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -148,6 +148,45 @@ bool ffn_down_supported(const Segments& seg, const DownArgs& a);
 hipError_t launch_ffn_down2(const Segments& seg, const DownArgs& a, const Segments& sh_seg, const DownArgs& sh,
                             hipStream_t st);
 
+// ---- quant.hip -------------------------------------------------------------
+// q[r][c] = rint(127 x[r][c] / max_c |x[r][c]|) and scale[r] = that maximum /
+// 127 (see moe.h), for r < rows, or r < *n_rows (device) when that is fewer.
+struct QuantArgs {
+  const uint16_t* x;
+  int8_t* q;
+  float* scale;
+  const int32_t* n_rows;  // nullable
+  long long ldx, ldq;
+  int rows, cols;
+};
+// a, and b (nullable) in the same launch.
+hipError_t launch_quantize_rows(const QuantArgs& a, const QuantArgs* b, hipStream_t st);
+
+// ---- gemm_i8.hip -----------------------------------------------------------
+// out[r][n] = bf16((sum_c X[r][c] w0[g][n][c]) * ws0[g][n] * X's scale of r)
+// for the rows r of group g, or with w1, ws1 the gated pair silu(.0) * (.1).
+// X[r] = x[r], or x[x_rows[r]] (x_count rows of x; an entry outside them
+// counts as a row of zeros).  Rows are ldx and ldw bytes (multiples of 16) and
+// ldo values apart, and hold zeros from K to the next multiple of 16 in one
+// operand at least; groups of weights are N rows apart.
+struct GemmI8 {
+  const int8_t* x;
+  const float* x_scale;
+  const int32_t* x_rows;
+  int x_count;
+  const int32_t* offsets;
+  int static_rows;
+  int groups;
+  const int8_t *w0, *w1;
+  const float *ws0, *ws1;
+  uint16_t* out;
+  int K, N;
+  long long ldx, ldw, ldo;
+};
+// a over seg (as the expert GEMMs above); sh (nullable) over sh_seg, static rows.
+hipError_t launch_gemm_i8(const Segments& seg, const GemmI8& a, const Segments* sh_seg, const GemmI8* sh, bool gated,
+                          hipStream_t st);
+
 // ---- combine.hip -----------------------------------------------------------
 hipError_t launch_combine(int T, int k, int H, const uint16_t* y_perm, const int32_t* inv_pos,
                           const float* topk_w, const uint16_t* y_shared, uint16_t* out,

@@ -102,7 +102,7 @@ struct ForwardWs {
   size_t bytes;
 };
 
-ForwardWs carve_forward(const moe_dims* d, void* base) {
+ForwardWs carve_forward(const moe_dims* d, size_t ffn_bytes, void* base) {
   ForwardWs w{};
   unsigned char* p = static_cast<unsigned char*>(base);
   size_t off = 0;
@@ -121,10 +121,12 @@ ForwardWs carve_forward(const moe_dims* d, void* base) {
   w.y_shared = reinterpret_cast<uint16_t*>(
       take(d->n_shared > 0 ? static_cast<size_t>(d->T) * d->H * sizeof(uint16_t) : 0));
   w.permute_ws = take(moe::permute_ws_bytes(d->T, d->k, d->E_local, d->S, d->E));
-  w.ffn_ws = take(ffn_ws(d));
+  w.ffn_ws = take(ffn_bytes);
   w.bytes = off;
   return w;
 }
+
+size_t ffn_i8_ws(const moe_dims* d, bool one_x);
 
 size_t entry_ws(const moe_dims* d, int entry) {
   switch (entry) {
@@ -133,7 +135,11 @@ size_t entry_ws(const moe_dims* d, int entry) {
     case MOE_ENTRY_EXPERT_FFN:
       return ffn_ws(d);
     case MOE_ENTRY_FORWARD:
-      return carve_forward(d, nullptr).bytes;
+      return carve_forward(d, ffn_ws(d), nullptr).bytes;
+    case MOE_ENTRY_EXPERT_FFN_I8:
+      return ffn_i8_ws(d, false);
+    case MOE_ENTRY_FORWARD_I8:
+      return carve_forward(d, ffn_i8_ws(d, true), nullptr).bytes;
     default:
       return 0;
   }
@@ -209,11 +215,15 @@ int check_ffn_limits(const moe_dims* d, bool rows_indexed) {
   return MOE_OK;
 }
 
-// The limits of one entry point (0: of every entry point).
+int check_ffn_i8_limits(const moe_dims* d, bool one_x);
+
+// The limits of one entry point (0: of every bf16 entry point).
 int check_entry(const moe_dims* d, int entry) {
   int s = MOE_OK;
   if (entry == 0 || entry == MOE_ENTRY_EXPERT_FFN) s = check_ffn_limits(d, false);
   if (s == MOE_OK && (entry == 0 || entry == MOE_ENTRY_FORWARD)) s = check_ffn_limits(d, true);
+  if (entry == MOE_ENTRY_EXPERT_FFN_I8 || entry == MOE_ENTRY_FORWARD_I8)
+    s = check_ffn_i8_limits(d, entry == MOE_ENTRY_FORWARD_I8);
   return s;
 }
 
@@ -239,6 +249,209 @@ int run_ffn(const moe_dims* d, const uint16_t* x_perm, const int32_t* x_rows, co
     e = moe::launch_ffn_down(p.routed, p.dn, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   record(taps, 2 * MOE_STAGE_FFN_DOWN + 1, st);
+  return MOE_OK;
+}
+
+// ---- the same on int8 experts ----
+
+int64_t pad16(int64_t n) { return (n + 15) / 16 * 16; }
+constexpr int64_t kMaxI8K = (1 << 17) - 1;  // inner dimension: sums of int8 products stay within int32
+constexpr int64_t kMaxI8Stride = 1 << 21;   // 512 rows of a tile stay within 32-bit offsets
+constexpr int64_t kSpan = kIntMax;          // gathered rows: 32-bit offsets
+
+// Workspace of the int8 expert FFN: quantised inputs (x_rows_cap rows for the
+// routed experts, T for the shared ones unless they read the same rows),
+// hidden rows in bf16, and those quantised.
+struct FfnI8Ws {
+  int8_t *xq, *xq_sh, *hq, *hq_sh;
+  float *xs, *xs_sh, *hs, *hs_sh;
+  uint16_t *h, *h_sh;
+  size_t bytes;
+};
+FfnI8Ws carve_ffn_i8(const moe_dims* d, bool one_x, void* base) {
+  FfnI8Ws w{};
+  unsigned char* p = static_cast<unsigned char*>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    unsigned char* r = p ? p + off : nullptr;
+    off += align_up(bytes);
+    return r;
+  };
+  const size_t T = d->T, rows = T * d->k, hp = pad16(d->H), ip = pad16(d->I), shw = sh_width(d), wp = pad16(shw);
+  const size_t x_rows = one_x ? T : rows, sh_x = one_x || shw == 0 ? 0 : T, sh_h = shw == 0 ? 0 : T;
+  w.xq = reinterpret_cast<int8_t*>(take(x_rows * hp));
+  w.xs = reinterpret_cast<float*>(take(x_rows * sizeof(float)));
+  w.xq_sh = reinterpret_cast<int8_t*>(take(sh_x * hp));
+  w.xs_sh = reinterpret_cast<float*>(take(sh_x * sizeof(float)));
+  w.h = reinterpret_cast<uint16_t*>(take(rows * d->I * sizeof(uint16_t)));
+  w.hq = reinterpret_cast<int8_t*>(take(rows * ip));
+  w.hs = reinterpret_cast<float*>(take(rows * sizeof(float)));
+  w.h_sh = reinterpret_cast<uint16_t*>(take(sh_h * shw * sizeof(uint16_t)));
+  w.hq_sh = reinterpret_cast<int8_t*>(take(sh_h * wp));
+  w.hs_sh = reinterpret_cast<float*>(take(sh_h * sizeof(float)));
+  if (one_x) {
+    w.xq_sh = w.xq;
+    w.xs_sh = w.xs;
+  }
+  w.bytes = off;
+  return w;
+}
+
+size_t ffn_i8_ws(const moe_dims* d, bool one_x) { return carve_ffn_i8(d, one_x, nullptr).bytes; }
+
+int check_ffn_i8_limits(const moe_dims* d, bool one_x) {
+  if (d->H > kMaxI8K || d->I > kMaxI8K || sh_width(d) > kMaxI8K) return MOE_ERR_UNSUPPORTED;
+  if (one_x && static_cast<int64_t>(d->T) * pad16(d->H) > kSpan) return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+
+int weights_i8_ok(const moe_dims* d, const moe_weights_i8* w) {
+  if (w == nullptr) return MOE_ERR_NULL;
+  const void* routed[] = {w->w_gate, w->w_up, w->w_down, w->s_gate, w->s_up, w->s_down};
+  const void* shared[] = {w->sh_gate, w->sh_up, w->sh_down, w->sh_s_gate, w->sh_s_up, w->sh_s_down};
+  for (const void* p : routed)
+    if (p == nullptr) return MOE_ERR_NULL;
+  for (const void* p : shared)
+    if (d->n_shared > 0 && p == nullptr) return MOE_ERR_NULL;
+  for (int i = 0; i < 6; ++i) {
+    const uintptr_t mask = i < 3 ? 15 : 3;
+    if ((reinterpret_cast<uintptr_t>(routed[i]) & mask) != 0) return MOE_ERR_ALIGN;
+    if (d->n_shared > 0 && (reinterpret_cast<uintptr_t>(shared[i]) & mask) != 0) return MOE_ERR_ALIGN;
+  }
+  return MOE_OK;
+}
+
+// The experts' networks on int8: x quantised (rows rows, or *n_rows), gate/up
+// on it (through x_rows where x holds tokens), the hidden rows quantised, down.
+// x == x_sh: the shared experts read the rows quantised for the routed ones.
+int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, const int32_t* offsets,
+               const moe_weights_i8* w, const uint16_t* x_sh, uint16_t* y_perm, uint16_t* y_shared, void* ws,
+               const moe_taps* taps, hipStream_t st) {
+  const bool one_x = x_rows != nullptr;
+  const FfnI8Ws fw = carve_ffn_i8(d, one_x, ws);
+  const int shw = static_cast<int>(sh_width(d)), rows = d->T * d->k;
+  const long long hp = pad16(d->H), ip = pad16(d->I), wp = pad16(shw);
+  const int32_t* n_rows = offsets + d->E_local;
+  const int mean = static_cast<int>(static_cast<int64_t>(d->T) * d->k / d->E);
+  const int hit = static_cast<int>(std::ceil(d->E_local * (1.0 - std::pow(1.0 - static_cast<double>(d->k) / d->E, d->T))));
+  const moe::Segments routed{offsets, d->E_local, 0, d->T, rows, mean, hit};
+  const moe::Segments shared{nullptr, 1, d->T, d->T, d->T, d->T, 1};
+  const bool sh = d->n_shared > 0;
+  hipError_t e;
+
+  record(taps, 2 * MOE_STAGE_FFN_UP, st);
+  const moe::QuantArgs qx{x, fw.xq, fw.xs, one_x ? nullptr : n_rows, d->H, hp, one_x ? d->T : rows, d->H};
+  const moe::QuantArgs qx_sh{x_sh, fw.xq_sh, fw.xs_sh, nullptr, d->H, hp, d->T, d->H};
+  e = moe::launch_quantize_rows(qx, sh && !one_x ? &qx_sh : nullptr, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  const moe::GemmI8 up{fw.xq, fw.xs, x_rows, one_x ? d->T : 0, offsets, 0, d->E_local, w->w_gate, w->w_up,
+                       w->s_gate, w->s_up, fw.h, d->H, d->I, hp, hp, d->I};
+  const moe::GemmI8 sh_up{fw.xq_sh, fw.xs_sh, nullptr, 0, nullptr, d->T, 1, w->sh_gate, w->sh_up,
+                          w->sh_s_gate, w->sh_s_up, fw.h_sh, d->H, shw, hp, hp, shw};
+  e = moe::launch_gemm_i8(routed, up, sh ? &shared : nullptr, sh ? &sh_up : nullptr, true, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  record(taps, 2 * MOE_STAGE_FFN_UP + 1, st);
+
+  record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
+  const moe::QuantArgs qh{fw.h, fw.hq, fw.hs, n_rows, d->I, ip, rows, d->I};
+  const moe::QuantArgs qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, wp, d->T, shw};
+  e = moe::launch_quantize_rows(qh, sh ? &qh_sh : nullptr, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  const moe::GemmI8 dn{fw.hq, fw.hs, nullptr, 0, offsets, 0, d->E_local, w->w_down, nullptr,
+                       w->s_down, nullptr, y_perm, d->I, d->H, ip, ip, d->H};
+  const moe::GemmI8 sh_dn{fw.hq_sh, fw.hs_sh, nullptr, 0, nullptr, d->T, 1, w->sh_down, nullptr,
+                          w->sh_s_down, nullptr, y_shared, shw, d->H, wp, wp, d->H};
+  e = moe::launch_gemm_i8(routed, dn, sh ? &shared : nullptr, sh ? &sh_dn : nullptr, false, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  record(taps, 2 * MOE_STAGE_FFN_DOWN + 1, st);
+  return MOE_OK;
+}
+
+// The checks that the two 8-bit products share.
+int linear_ok(const moe_linear_dims* d, bool grouped, bool gathered, const void* xq, const void* x_scale,
+              const void* wq, const void* w_scale, const void* y) {
+  if (d == nullptr) return MOE_ERR_NULL;
+  if (d->M < 0 || d->N < 1 || d->K < 1 || (grouped && d->G < 1) || (gathered && d->X < 0)) return MOE_ERR_DIMS;
+  if (d->ldx < pad16(d->K) || d->ldw < pad16(d->K) || d->ldy < d->N) return MOE_ERR_DIMS;
+  if (d->K > kMaxI8K || d->N > (1 << 24) || d->ldx > kMaxI8Stride || d->ldw > kMaxI8Stride || d->ldy > kMaxI8Stride)
+    return MOE_ERR_UNSUPPORTED;
+  if (grouped && d->G > moe::kMaxExperts) return MOE_ERR_UNSUPPORTED;
+  if (gathered && d->X * d->ldx > kSpan) return MOE_ERR_UNSUPPORTED;
+  if (d->ldx % 16 != 0 || d->ldw % 16 != 0) return MOE_ERR_ALIGN;
+  if (d->M == 0) return MOE_OK;
+  if (!xq || !x_scale || !wq || !w_scale || !y) return MOE_ERR_NULL;
+  if (!aligned16(xq) || !aligned16(wq)) return MOE_ERR_ALIGN;
+  if (((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale)) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(y) & 1u) != 0)
+    return MOE_ERR_ALIGN;
+  return MOE_OK;
+}
+
+int forward_io_ok(const moe_dims* d, const float* logits, const int32_t* src, const moe_bf16* x,
+                  const int64_t* counts, const moe_bf16* out) {
+  if (d->T > 0 && (!logits || !x || !out)) return MOE_ERR_NULL;
+  if (counts && d->T > 0 && !src) return MOE_ERR_NULL;
+  if (d->T > 0 && (!aligned16(x) || !aligned16(out))) return MOE_ERR_ALIGN;
+  return MOE_OK;
+}
+
+// The layer's launches, ffn(x_rows, offsets) being the experts' networks.
+template <class Ffn>
+int run_forward(const moe_dims* d, const moe::RouteGating& rg, const float* logits, const int32_t* src,
+                const int32_t* local_experts, int64_t* counts, moe_bf16* out, const moe_taps* taps,
+                const ForwardWs& fw, hipStream_t st, Ffn ffn) {
+  int32_t* topk_idx = (taps && taps->topk_idx) ? taps->topk_idx : fw.topk_idx;
+  float* topk_w = (taps && taps->topk_w) ? taps->topk_w : fw.topk_w;
+  int32_t* offsets = (taps && taps->offsets) ? taps->offsets : fw.offsets;
+  int32_t* perm_token = (taps && taps->perm_token) ? taps->perm_token : fw.perm_token;
+  int32_t* inv_pos = (taps && taps->inv_pos) ? taps->inv_pos : fw.inv_pos;
+  int32_t* expert_load = taps ? taps->expert_load : nullptr;
+  hipError_t e;
+
+  record(taps, 2 * MOE_STAGE_ROUTE, st);
+  if (counts && expert_load) {
+    e = moe::launch_fill_i32(expert_load, d->E, 0, st);
+    if (e != hipSuccess) return MOE_ERR_DEVICE;
+  }
+  // decode-sized batches: the routing launch also writes the dispatch.
+  // Larger ones are dispatched by the permute passes, whose count pass then
+  // also takes the statistics: its blocks hold many more pairs than the
+  // router's, and their histograms are summed in two levels (see
+  // permute.hip) rather than by global atomics per bin and block.
+  const moe::DispatchArgs disp{local_experts, d->E_local, offsets, perm_token, inv_pos};
+  const bool stats_in_permute = counts != nullptr && static_cast<int64_t>(d->T) * d->k > moe::kDispatchPairs;
+  int64_t* route_counts = stats_in_permute ? nullptr : counts;
+  bool dispatched = false;
+  e = moe::launch_route(d->T, d->E, d->k, logits, topk_idx, topk_w, route_counts ? src : nullptr, d->S,
+                        route_counts, route_counts ? expert_load : nullptr, &rg, st, &disp, &dispatched);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  record(taps, 2 * MOE_STAGE_ROUTE + 1, st);
+
+  record(taps, 2 * MOE_STAGE_PERMUTE, st);
+  if (!dispatched) {
+    e = moe::launch_permute(d->T, d->k, d->E, d->E_local, local_experts, topk_idx, offsets, perm_token,
+                            inv_pos, fw.permute_ws, st, src, d->S, stats_in_permute ? counts : nullptr,
+                            stats_in_permute ? expert_load : nullptr);
+    if (e != hipSuccess) return MOE_ERR_DEVICE;
+  }
+  // no gathered copy of x: the gate/up GEMM reads its rows through perm_token
+  record(taps, 2 * MOE_STAGE_PERMUTE + 1, st);
+
+  if (d->T > 0) {
+    const int s = ffn(perm_token, offsets);
+    if (s != MOE_OK) return s;
+  } else {
+    record(taps, 2 * MOE_STAGE_FFN_UP, st);
+    record(taps, 2 * MOE_STAGE_FFN_UP + 1, st);
+    record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
+    record(taps, 2 * MOE_STAGE_FFN_DOWN + 1, st);
+  }
+
+  record(taps, 2 * MOE_STAGE_COMBINE, st);
+  e = moe::launch_combine(d->T, d->k, d->H, fw.y_perm, inv_pos, topk_w,
+                          d->n_shared > 0 ? fw.y_shared : nullptr, out, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  record(taps, 2 * MOE_STAGE_COMBINE + 1, st);
   return MOE_OK;
 }
 
@@ -387,69 +600,19 @@ int moe_forward(const moe_dims* d, const moe_gating* gating, const float* logits
   if (!local_experts && d->E_local != d->E) return MOE_ERR_DIMS;
   s = weights_ok(d, w);
   if (s != MOE_OK) return s;
-  if (d->T > 0 && (!logits || !x || !out)) return MOE_ERR_NULL;
-  if (counts && d->T > 0 && !src) return MOE_ERR_NULL;
-  if (d->T > 0 && (!aligned16(x) || !aligned16(out))) return MOE_ERR_ALIGN;
+  s = forward_io_ok(d, logits, src, x, counts, out);
+  if (s != MOE_OK) return s;
   s = check_entry(d, MOE_ENTRY_FORWARD);
   if (s != MOE_OK) return s;
   s = check_ws(d, MOE_ENTRY_FORWARD, ws, ws_bytes);
   if (s != MOE_OK) return s;
 
   hipStream_t st = static_cast<hipStream_t>(stream);
-  ForwardWs fw = carve_forward(d, ws);
-  int32_t* topk_idx = (taps && taps->topk_idx) ? taps->topk_idx : fw.topk_idx;
-  float* topk_w = (taps && taps->topk_w) ? taps->topk_w : fw.topk_w;
-  int32_t* offsets = (taps && taps->offsets) ? taps->offsets : fw.offsets;
-  int32_t* perm_token = (taps && taps->perm_token) ? taps->perm_token : fw.perm_token;
-  int32_t* inv_pos = (taps && taps->inv_pos) ? taps->inv_pos : fw.inv_pos;
-  int32_t* expert_load = taps ? taps->expert_load : nullptr;
-  hipError_t e;
-
-  record(taps, 2 * MOE_STAGE_ROUTE, st);
-  if (counts && expert_load) {
-    e = moe::launch_fill_i32(expert_load, d->E, 0, st);
-    if (e != hipSuccess) return MOE_ERR_DEVICE;
-  }
-  // decode-sized batches: the routing launch also writes the dispatch.
-  // Larger ones are dispatched by the permute passes, whose count pass then
-  // also takes the statistics: its blocks hold many more pairs than the
-  // router's, and their histograms are summed in two levels (see
-  // permute.hip) rather than by global atomics per bin and block.
-  const moe::DispatchArgs disp{local_experts, d->E_local, offsets, perm_token, inv_pos};
-  const bool stats_in_permute = counts != nullptr && static_cast<int64_t>(d->T) * d->k > moe::kDispatchPairs;
-  int64_t* route_counts = stats_in_permute ? nullptr : counts;
-  bool dispatched = false;
-  e = moe::launch_route(d->T, d->E, d->k, logits, topk_idx, topk_w, route_counts ? src : nullptr, d->S,
-                        route_counts, route_counts ? expert_load : nullptr, &rg, st, &disp, &dispatched);
-  if (e != hipSuccess) return MOE_ERR_DEVICE;
-  record(taps, 2 * MOE_STAGE_ROUTE + 1, st);
-
-  record(taps, 2 * MOE_STAGE_PERMUTE, st);
-  if (!dispatched) {
-    e = moe::launch_permute(d->T, d->k, d->E, d->E_local, local_experts, topk_idx, offsets, perm_token,
-                            inv_pos, fw.permute_ws, st, src, d->S, stats_in_permute ? counts : nullptr,
-                            stats_in_permute ? expert_load : nullptr);
-    if (e != hipSuccess) return MOE_ERR_DEVICE;
-  }
-  // no gathered copy of x: the gate/up GEMM reads its rows through perm_token
-  record(taps, 2 * MOE_STAGE_PERMUTE + 1, st);
-
-  if (d->T > 0) {
-    s = run_ffn(d, x, perm_token, offsets, w, x, fw.y_perm, fw.y_shared, fw.ffn_ws, taps, st);
-    if (s != MOE_OK) return s;
-  } else {
-    record(taps, 2 * MOE_STAGE_FFN_UP, st);
-    record(taps, 2 * MOE_STAGE_FFN_UP + 1, st);
-    record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
-    record(taps, 2 * MOE_STAGE_FFN_DOWN + 1, st);
-  }
-
-  record(taps, 2 * MOE_STAGE_COMBINE, st);
-  e = moe::launch_combine(d->T, d->k, d->H, fw.y_perm, inv_pos, topk_w,
-                          d->n_shared > 0 ? fw.y_shared : nullptr, out, st);
-  if (e != hipSuccess) return MOE_ERR_DEVICE;
-  record(taps, 2 * MOE_STAGE_COMBINE + 1, st);
-  return MOE_OK;
+  const ForwardWs fw = carve_forward(d, ffn_ws(d), ws);
+  return run_forward(d, rg, logits, src, local_experts, counts, out, taps, fw, st,
+                     [&](const int32_t* x_rows, const int32_t* offsets) {
+                       return run_ffn(d, x, x_rows, offsets, w, x, fw.y_perm, fw.y_shared, fw.ffn_ws, taps, st);
+                     });
 }
 
 int moe_forward_noalloc(const moe_dims* d, const moe_gating* gating, const float* logits, const int32_t* src,
@@ -471,6 +634,86 @@ int moe_forward_noalloc(const moe_dims* d, const moe_gating* gating, const float
   // before it is read within the call
   return moe_forward(d, gating, logits, src, x, local_experts, w, counts, out, taps, ws,
                      MOE_NOALLOC_SCRATCH_BYTES, stream);
+}
+
+int moe_quantize_rows(int32_t rows, int32_t cols, const moe_bf16* x, int64_t ldx, int8_t* q, int64_t ldq,
+                      float* scale, void* stream) {
+  if (rows < 0 || cols < 1 || ldx < cols || ldq < cols) return MOE_ERR_DIMS;
+  if (ldx > (int64_t{1} << 40) || ldq > (int64_t{1} << 40) || cols > kIntMax - 64) return MOE_ERR_UNSUPPORTED;
+  if (ldq % 16 != 0) return MOE_ERR_ALIGN;
+  if (rows == 0) return MOE_OK;
+  if (!x || !q || !scale) return MOE_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(x) & 1u) != 0 || !aligned16(q) || (reinterpret_cast<uintptr_t>(scale) & 3u) != 0)
+    return MOE_ERR_ALIGN;
+  const moe::QuantArgs a{x, q, scale, nullptr, ldx, ldq, rows, cols};
+  return status(moe::launch_quantize_rows(a, nullptr, static_cast<hipStream_t>(stream)));
+}
+
+int moe_linear_i8(const moe_linear_dims* d, const int8_t* xq, const float* x_scale, const int8_t* wq,
+                  const float* w_scale, moe_bf16* y, void* stream) {
+  const int s = linear_ok(d, false, false, xq, x_scale, wq, w_scale, y);
+  if (s != MOE_OK || d->M == 0) return s;
+  const moe::Segments seg{nullptr, 1, d->M, d->M, d->M, d->M, 1};
+  const moe::GemmI8 a{xq, x_scale, nullptr, 0, nullptr, d->M, 1, wq, nullptr, w_scale, nullptr, y,
+                      d->K, d->N, d->ldx, d->ldw, d->ldy};
+  return status(moe::launch_gemm_i8(seg, a, nullptr, nullptr, false, static_cast<hipStream_t>(stream)));
+}
+
+int moe_grouped_linear_i8(const moe_linear_dims* d, const int8_t* xq, const float* x_scale, const int32_t* x_rows,
+                          const int32_t* offsets, const int8_t* wq, const float* w_scale, moe_bf16* y, void* stream) {
+  const int s = linear_ok(d, true, x_rows != nullptr, xq, x_scale, wq, w_scale, y);
+  if (s != MOE_OK || d->M == 0) return s;
+  if (!offsets) return MOE_ERR_NULL;
+  if (((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(x_rows)) & 3u) != 0) return MOE_ERR_ALIGN;
+  const moe::Segments seg{offsets, d->G, 0, d->M, d->M, d->M / d->G, std::min(d->G, d->M)};
+  const moe::GemmI8 a{xq, x_scale, x_rows, x_rows ? d->X : 0, offsets, 0, d->G, wq, nullptr, w_scale, nullptr, y,
+                      d->K, d->N, d->ldx, d->ldw, d->ldy};
+  return status(moe::launch_gemm_i8(seg, a, nullptr, nullptr, false, static_cast<hipStream_t>(stream)));
+}
+
+int moe_expert_ffn_i8(const moe_dims* d, const moe_bf16* x_perm, const int32_t* offsets, const moe_weights_i8* w,
+                      const moe_bf16* x, moe_bf16* y_perm, moe_bf16* y_shared, void* ws, size_t ws_bytes,
+                      void* stream) {
+  int s = check_dims(d);
+  if (s != MOE_OK) return s;
+  s = weights_i8_ok(d, w);
+  if (s != MOE_OK) return s;
+  if (!x_perm || !offsets || !y_perm) return MOE_ERR_NULL;
+  if (d->n_shared > 0 && (!x || !y_shared)) return MOE_ERR_NULL;
+  if (!aligned16(x_perm) || !aligned16(y_perm)) return MOE_ERR_ALIGN;
+  if (d->n_shared > 0 && (!aligned16(x) || !aligned16(y_shared))) return MOE_ERR_ALIGN;
+  s = check_entry(d, MOE_ENTRY_EXPERT_FFN_I8);
+  if (s != MOE_OK) return s;
+  s = check_ws(d, MOE_ENTRY_EXPERT_FFN_I8, ws, ws_bytes);
+  if (s != MOE_OK) return s;
+  if (d->T == 0) return MOE_OK;
+  return run_ffn_i8(d, x_perm, nullptr, offsets, w, x, y_perm, y_shared, ws, nullptr, static_cast<hipStream_t>(stream));
+}
+
+int moe_forward_i8(const moe_dims* d, const moe_gating* gating, const float* logits, const int32_t* src,
+                   const moe_bf16* x, const int32_t* local_experts, const moe_weights_i8* w, int64_t* counts,
+                   moe_bf16* out, const moe_taps* taps, void* ws, size_t ws_bytes, void* stream) {
+  int s = check_dims(d);
+  if (s != MOE_OK) return s;
+  moe::RouteGating rg;
+  s = gating_ok(d, gating, &rg);
+  if (s != MOE_OK) return s;
+  if (!local_experts && d->E_local != d->E) return MOE_ERR_DIMS;
+  s = weights_i8_ok(d, w);
+  if (s != MOE_OK) return s;
+  s = forward_io_ok(d, logits, src, x, counts, out);
+  if (s != MOE_OK) return s;
+  s = check_entry(d, MOE_ENTRY_FORWARD_I8);
+  if (s != MOE_OK) return s;
+  s = check_ws(d, MOE_ENTRY_FORWARD_I8, ws, ws_bytes);
+  if (s != MOE_OK) return s;
+
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const ForwardWs fw = carve_forward(d, ffn_i8_ws(d, true), ws);
+  return run_forward(d, rg, logits, src, local_experts, counts, out, taps, fw, st,
+                     [&](const int32_t* x_rows, const int32_t* offsets) {
+                       return run_ffn_i8(d, x, x_rows, offsets, w, x, fw.y_perm, fw.y_shared, fw.ffn_ws, taps, st);
+                     });
 }
 
 // For the tests, which assert the kernel that a shape is meant for (not part

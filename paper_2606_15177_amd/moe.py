@@ -20,6 +20,7 @@ HEADER = os.path.join(os.path.dirname(_HERE), "include", "moe.h")
 MOE_OK, MOE_ERR_NULL, MOE_ERR_DIMS, MOE_ERR_UNSUPPORTED = 0, -1, -2, -3
 MOE_ERR_WORKSPACE, MOE_ERR_DEVICE, MOE_ERR_ALIGN = -4, -5, -6
 ENTRY_PERMUTE, ENTRY_EXPERT_FFN, ENTRY_FORWARD = 1, 2, 3
+ENTRY_EXPERT_FFN_I8, ENTRY_FORWARD_I8 = 4, 5
 GATE_SOFTMAX_TOPK, GATE_SOFTMAX, GATE_SIGMOID = 0, 1, 2   # moe_dims.flags
 STAGES = ("route", "permute", "ffn_up", "ffn_down", "combine")
 
@@ -42,6 +43,16 @@ class MoeTaps(C.Structure):
     _fields_ = [("topk_idx", C.c_void_p), ("topk_w", C.c_void_p), ("expert_load", C.c_void_p),
                 ("offsets", C.c_void_p), ("perm_token", C.c_void_p), ("inv_pos", C.c_void_p),
                 ("events", C.c_void_p * (2 * len(STAGES)))]
+
+
+class MoeLinearDims(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("M", "N", "K", "G", "X")] +
+                [(n, C.c_int64) for n in ("ldx", "ldw", "ldy")])
+
+
+class MoeWeightsI8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w_gate", "w_up", "w_down", "s_gate", "s_up", "s_down", "sh_gate", "sh_up",
+                                          "sh_down", "sh_s_gate", "sh_s_up", "sh_s_down")]
 
 
 class MoePlaceDims(C.Structure):
@@ -80,6 +91,12 @@ def _load() -> C.CDLL:
                          C.POINTER(MoeTaps), vp, sz, vp], i32),
         "moe_forward_noalloc": ([dp, C.POINTER(MoeGating), vp, vp, vp, vp, C.POINTER(MoeWeights), vp, vp,
                                  C.POINTER(MoeTaps), vp], i32),
+        "moe_quantize_rows": ([C.c_int32, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, vp], i32),
+        "moe_linear_i8": ([C.POINTER(MoeLinearDims), vp, vp, vp, vp, vp, vp], i32),
+        "moe_grouped_linear_i8": ([C.POINTER(MoeLinearDims), vp, vp, vp, vp, vp, vp, vp, vp], i32),
+        "moe_expert_ffn_i8": ([dp, vp, vp, C.POINTER(MoeWeightsI8), vp, vp, vp, vp, sz, vp], i32),
+        "moe_forward_i8": ([dp, C.POINTER(MoeGating), vp, vp, vp, vp, C.POINTER(MoeWeightsI8), vp, vp,
+                            C.POINTER(MoeTaps), vp, sz, vp], i32),
         "moe_place_slots": ([C.POINTER(MoePlaceDims), vp], sz),
         "moe_place_experts": ([C.POINTER(MoePlaceDims), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp], i32),
         "moe_window_stats": ([C.POINTER(MoeWindowDims), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp], i32),
@@ -98,7 +115,7 @@ def header_functions() -> list[str]:
     """Names of the functions include/moe.h declares."""
     with open(HEADER) as f:
         text = f.read()
-    return sorted(set(re.findall(r"\b(moe_[a-z_]+)\s*\(", text)))
+    return sorted(set(re.findall(r"\b(moe_[a-z0-9_]+)\s*\(", text)))
 
 
 def strerror(status: int) -> str:
@@ -236,6 +253,170 @@ def forward_noalloc(d, logits, src, x, local_experts, weights, counts, out, taps
            "moe_forward_noalloc")
 
 
+# ---- 8-bit integer experts ----
+
+_I8 = (torch.int8,)
+
+
+def _on_device(stream, *tensors):
+    """Context of the tensors' device and the stream to launch on: the given
+    one, or that device's current stream.  Tensors of two devices, or a stream
+    of another one, are refused."""
+    devs = {t.device for t in tensors if t is not None}
+    if any(d.type != "cuda" for d in devs):
+        raise ValueError("tensor must live on the GPU")
+    if len(devs) > 1:
+        raise ValueError(f"tensors live on different devices: {sorted(map(str, devs))}")
+    dev = next(iter(devs))
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif getattr(stream, "device", dev) != dev:
+        raise ValueError(f"stream of {stream.device}, tensors on {dev}")
+    return torch.cuda.device(dev), _stream(stream)
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _pad16(n: int) -> int:
+    return (n + 15) // 16 * 16
+
+
+def _rows(t, dtypes, cols: int, what: str):
+    """Pointer and row stride of a 2-D tensor of at least `cols` columns whose
+    rows are contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a torch tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what}: dtype {t.dtype} not in {dtypes}")
+    _need(t.dim() == 2 and t.shape[1] >= cols, f"{what}: expected rows of at least {cols} values, got {tuple(t.shape)}")
+    _need(t.shape[1] == 1 or t.stride(1) == 1, f"{what}: rows must be contiguous")
+    # one row has no stride to speak of
+    return t.data_ptr(), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vec(t, dtypes, n: int, what: str):
+    _need(isinstance(t, torch.Tensor) and t.numel() >= n, f"{what}: expected {n} values")
+    return _ptr(t, dtypes)
+
+
+def quantize_rows(x, q=None, scale=None, stream=None):
+    """moe_quantize_rows: int8 rows and their fp32 scales of x, bf16 [rows,
+    cols] (rows contiguous, any row stride).  q is int8 [rows, cols rounded up
+    to a multiple of 16], padded with zeros; both are allocated when not given.
+    Returns (q, scale)."""
+    xp, ldx = _rows(x, _BF16, 1, "x")
+    rows, cols = x.shape
+    ctx, st = _on_device(stream, x, q, scale)
+    with ctx:
+        if q is None or scale is None:
+            with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_stream()):
+                q = torch.empty((rows, _pad16(cols)), dtype=torch.int8, device=x.device) if q is None else q
+                scale = torch.empty((rows,), dtype=torch.float32, device=x.device) if scale is None else scale
+        qp, ldq = _rows(q, _I8, _pad16(cols), "q")
+        _need(q.shape[0] == rows, f"q: expected {rows} rows")
+        sp = _vec(scale, _F32, rows, "scale")
+        _check(_lib.moe_quantize_rows(rows, cols, xp, ldx, qp, ldq, sp, st), "moe_quantize_rows")
+    return q, scale
+
+
+def linear_i8(K, xq, x_scale, wq, w_scale, y, stream=None):
+    """moe_linear_i8: y [M, N] bf16 of xq [M, >= K padded to 16] and wq [N, the
+    same] int8 with fp32 scales [M] and [N], as quantize_rows makes them.  The
+    rows of xq, wq and y may lie apart."""
+    yp, ldy = _rows(y, _BF16, 1, "y")
+    M, N = y.shape
+    xp, ldx = _rows(xq, _I8, _pad16(K), "xq")
+    wp, ldw = _rows(wq, _I8, _pad16(K), "wq")
+    _need(xq.shape[0] == M and wq.shape[0] == N, f"expected {M} rows of xq and {N} of wq")
+    d = MoeLinearDims(M, N, K, 1, 0, ldx, ldw, ldy)
+    ctx, st = _on_device(stream, xq, x_scale, wq, w_scale, y)
+    with ctx:
+        _check(_lib.moe_linear_i8(C.byref(d), xp, _vec(x_scale, _F32, M, "x_scale"), wp,
+                                  _vec(w_scale, _F32, N, "w_scale"), yp, st), "moe_linear_i8")
+
+
+def grouped_linear_i8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stream=None):
+    """moe_grouped_linear_i8: rows offsets[g] .. offsets[g+1] of y [M, N] from
+    those of xq (or xq[x_rows[r]]) and wq[g]; wq int8 [G, N, >= K padded to 16],
+    w_scale fp32 [G, N], offsets int32 [G+1], x_rows int32 [M]."""
+    yp, ldy = _rows(y, _BF16, 1, "y")
+    M, N = y.shape
+    _need(isinstance(wq, torch.Tensor) and wq.dim() == 3 and wq.shape[1] == N, f"wq: expected [groups, {N}, ...]")
+    G = wq.shape[0]
+    xp, ldx = _rows(xq, _I8, _pad16(K), "xq")
+    wp, ldw = _rows(wq.flatten(0, 1), _I8, _pad16(K), "wq")
+    _need(wp == wq.data_ptr(), "wq: the groups must lie one behind the other")
+    _need(x_rows is not None or xq.shape[0] == M, f"expected {M} rows of xq")
+    d = MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy)
+    ctx, st = _on_device(stream, xq, x_scale, offsets, wq, w_scale, y, x_rows)
+    with ctx:
+        _check(_lib.moe_grouped_linear_i8(C.byref(d), xp, _vec(x_scale, _F32, xq.shape[0], "x_scale"),
+                                          None if x_rows is None else _vec(x_rows, _I32, M, "x_rows"),
+                                          _vec(offsets, _I32, G + 1, "offsets"), wp,
+                                          _vec(w_scale, _F32, G * N, "w_scale"), yp, st), "moe_grouped_linear_i8")
+
+
+def quantize_weights(d: MoeDims, w: dict) -> dict:
+    """The int8 weights of a layer (moe_weights_i8's layout) from its bf16 ones
+    (moe_weights' layout), a scale per output channel."""
+    EL, H, I = d.E_local, d.H, d.I
+    out = {}
+
+    def put(name, scale_name, t, shape):
+        q, s = quantize_rows(t)
+        out[name], out[scale_name] = q.view(*shape, -1), s.view(*shape)
+
+    put("w_gate", "s_gate", w["w_gate"].reshape(EL * I, H), (EL, I))
+    put("w_up", "s_up", w["w_up"].reshape(EL * I, H), (EL, I))
+    put("w_down", "s_down", w["w_down"].reshape(EL * H, I), (EL, H))
+    if d.n_shared:
+        width = d.n_shared * d.I_shared
+        put("sh_gate", "sh_s_gate", w["sh_gate"].reshape(width, H), (width,))
+        put("sh_up", "sh_s_up", w["sh_up"].reshape(width, H), (width,))
+        down = w["sh_down"].reshape(d.n_shared, H, d.I_shared).permute(1, 0, 2).reshape(H, width)
+        put("sh_down", "sh_s_down", down, (H,))
+    return out
+
+
+def make_weights_i8(d: MoeDims, w: dict) -> MoeWeightsI8:
+    """The handle of int8 weights (see quantize_weights); it holds the tensors."""
+    EL, H, I, width = d.E_local, d.H, d.I, d.n_shared * d.I_shared
+    hp, ip, wp = _pad16(H), _pad16(I), _pad16(width)
+    need = {"w_gate": (_I8, EL * I * hp), "w_up": (_I8, EL * I * hp), "w_down": (_I8, EL * H * ip),
+            "s_gate": (_F32, EL * I), "s_up": (_F32, EL * I), "s_down": (_F32, EL * H)}
+    if d.n_shared:
+        need.update({"sh_gate": (_I8, width * hp), "sh_up": (_I8, width * hp), "sh_down": (_I8, H * wp),
+                     "sh_s_gate": (_F32, width), "sh_s_up": (_F32, width), "sh_s_down": (_F32, H)})
+    h = MoeWeightsI8(**{n: _vec(w.get(n), t, size, n) for n, (t, size) in need.items()})
+    h.tensors = {n: w[n] for n in need}
+    return h
+
+
+def expert_ffn_i8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=None):
+    """moe_expert_ffn_i8; weights as make_weights_i8 returns them."""
+    rows = d.T * d.k
+    ctx, st = _on_device(stream, x_perm, offsets, x, y_perm, y_shared, ws, *weights.tensors.values())
+    with ctx:
+        _check(_lib.moe_expert_ffn_i8(C.byref(d), _vec(x_perm, _BF16, rows * d.H, "x_perm"),
+                                      _vec(offsets, _I32, d.E_local + 1, "offsets"), C.byref(weights), _ptr(x, _BF16),
+                                      _vec(y_perm, _BF16, rows * d.H, "y_perm"), _ptr(y_shared, _BF16), _ptr(ws),
+                                      0 if ws is None else ws.numel() * ws.element_size(), st), "moe_expert_ffn_i8")
+
+
+def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=None, stream=None, gating=None):
+    """moe_forward_i8; weights as make_weights_i8 returns them."""
+    ctx, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws, *weights.tensors.values())
+    with ctx:
+        _check(_lib.moe_forward_i8(C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"),
+                                   _ptr(src, _I32), _vec(x, _BF16, d.T * d.H, "x"), _ptr(local_experts, _I32),
+                                   C.byref(weights), _ptr(counts, _I64), _vec(out, _BF16, d.T * d.H, "out"),
+                                   None if taps is None else C.byref(taps), _ptr(ws),
+                                   0 if ws is None else ws.numel() * ws.element_size(), st), "moe_forward_i8")
+
+
 PAPER_PLACE_WEIGHTS = (1.0, 0.0025, 1.0)  # (alpha, beta, gamma), Sec. 6
 
 
@@ -297,4 +478,28 @@ class MoeLayer:
             out = torch.empty((self.d.T, self.d.H), dtype=torch.bfloat16, device=self.device)
         forward(self.d, logits, src, x, self.local_experts, self._w, counts, out, self.ws, taps, stream,
                 gating=self.gating)
+        return out
+
+
+class MoeLayerI8:
+    """MoeLayer on int8 experts: the weights are quantised once (bf16 ones, in
+    MoeLayer's layout) or taken as they are (quantize_weights' dict), and
+    forward calls moe_forward_i8.  Calls that may overlap (other streams, other
+    captured graphs replayed at the same time) each need a workspace of their
+    own: workspace(d, ENTRY_FORWARD_I8), given to forward as `ws`."""
+
+    def __init__(self, d: MoeDims, weights: dict, local_experts=None, device="cuda", gating=None):
+        self.d = d
+        self.gating = gating
+        self.local_experts = local_experts
+        self._w = make_weights_i8(d, weights if "s_gate" in weights else quantize_weights(d, weights))
+        self.ws = workspace(d, ENTRY_FORWARD_I8, device)
+        self.device = device
+
+    def forward(self, logits, src, x, counts=None, out=None, taps=None, stream=None, ws=None):
+        if out is None:
+            with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
+                out = torch.empty((self.d.T, self.d.H), dtype=torch.bfloat16, device=x.device)
+        forward_i8(self.d, logits, src, x, self.local_experts, self._w, counts, out, self.ws if ws is None else ws, taps,
+                   stream, gating=self.gating)
         return out

@@ -1,0 +1,172 @@
+"""The 8-bit entry points without a GPU: what they refuse, in which order and
+with which code, the workspaces they ask for, and the binding's own checks."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2606_15177_amd import workloads as W
+
+
+@pytest.fixture(scope="module")
+def moe():
+    from paper_2606_15177_amd import moe
+    return moe
+
+
+@pytest.mark.parametrize("rows,cols,x,ldx,q,ldq,scale,code", [
+    (-1, 8, 16, 8, 16, 16, 16, -2), (4, 0, 16, 8, 16, 16, 16, -2), (4, 8, 16, 7, 16, 16, 16, -2),
+    (4, 33, 16, 33, 16, 32, 16, -2),                       # ldq below cols
+    (4, 8, 16, 8, 16, 24, 16, -6), (4, 8, 17, 8, 16, 16, 16, -6), (4, 8, 16, 8, 24, 16, 16, -6),
+    (4, 8, 16, 8, 16, 16, 18, -6), (4, 8, None, 8, 16, 16, 16, -1), (4, 8, 16, 8, None, 16, 16, -1),
+    (4, 8, 16, 8, 16, 16, None, -1), (4, 8, 16, 2 ** 41, 16, 16, 16, -3), (4, 2 ** 31 - 1, 16, 2 ** 31, 16, 2 ** 31, 16, -3),
+    (0, 8, None, 8, None, 16, None, 0),                    # no rows: nothing to do
+])
+def test_quantize_rows_refusals(moe, rows, cols, x, ldx, q, ldq, scale, code):
+    assert moe._lib.moe_quantize_rows(rows, cols, x, ldx, q, ldq, scale, None) == code
+
+
+LIN = dict(M=4, N=8, K=40, G=2, X=4, ldx=48, ldw=48, ldy=8)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(M=-1), -2), (dict(N=0), -2), (dict(K=0), -2), (dict(ldx=32), -2), (dict(ldw=32), -2), (dict(ldy=7), -2),
+    (dict(ldx=56), -6), (dict(ldw=56), -6), (dict(K=2 ** 17, ldx=2 ** 17, ldw=2 ** 17), -3), (dict(ldx=2 ** 21 + 16), -3),
+    (dict(ldw=2 ** 21 + 16), -3), (dict(ldy=2 ** 21 + 1), -3), (dict(N=2 ** 24 + 1, ldy=2 ** 25), -3), (dict(M=0), 0),
+])
+def test_linear_refusals(moe, change, code):
+    d = moe.MoeLinearDims(**{**LIN, **change})
+    assert moe._lib.moe_linear_i8(C.byref(d), 16, 16, 16, 16, 16 if code else None, None) == code
+    assert moe._lib.moe_grouped_linear_i8(C.byref(d), 16, 16, None, 16, 16, 16, 16 if code else None, None) == code
+
+
+@pytest.mark.parametrize("ptrs,code", [
+    ((None, 16, 16, 16, 16), -1), ((16, None, 16, 16, 16), -1), ((16, 16, None, 16, 16), -1), ((16, 16, 16, None, 16), -1),
+    ((16, 16, 16, 16, None), -1), ((24, 16, 16, 16, 16), -6), ((16, 18, 16, 16, 16), -6), ((16, 16, 24, 16, 16), -6),
+    ((16, 16, 16, 18, 16), -6), ((16, 16, 16, 16, 17), -6),
+])
+def test_linear_pointers(moe, ptrs, code):
+    d = moe.MoeLinearDims(**LIN)
+    xq, xs, wq, ws, y = ptrs
+    assert moe._lib.moe_linear_i8(C.byref(d), xq, xs, wq, ws, y, None) == code
+    assert moe._lib.moe_grouped_linear_i8(C.byref(d), xq, xs, None, 16, wq, ws, y, None) == code
+    assert moe._lib.moe_linear_i8(None, xq, xs, wq, ws, y, None) == moe.MOE_ERR_NULL
+
+
+@pytest.mark.parametrize("change,x_rows,offsets,code", [
+    (dict(G=0), None, 16, -2), (dict(G=1025), None, 16, -3), (dict(X=-1), 16, 16, -2), (dict(), None, None, -1),
+    (dict(), 18, 16, -6), (dict(), 16, 18, -6), (dict(X=2 ** 26), 16, 16, -3),
+])
+def test_grouped_linear_refusals(moe, change, x_rows, offsets, code):
+    d = moe.MoeLinearDims(**{**LIN, **change})
+    assert moe._lib.moe_grouped_linear_i8(C.byref(d), 16, 16, x_rows, offsets, 16, 16, 16, None) == code
+
+
+def _i8_weights(moe, change=None, shared=True):
+    w = {n: 16 for n, _ in moe.MoeWeightsI8._fields_ if shared or not n.startswith("sh_")}
+    w.update(change or {})
+    return moe.MoeWeightsI8(**w)
+
+
+def test_layer_entry_points_refuse_before_launch(moe):
+    lib = moe._lib
+    d = moe.dims(T=4, H=64, E=8, k=2, I=64, S=2, E_local=8)
+    dsh = moe.dims(T=4, H=64, E=8, k=2, I=64, S=2, E_local=8, n_shared=1, I_shared=64)
+    ffn = lambda dd, w, x_perm=16, off=16, x=16, y=16, ysh=16, ws=256, n=1 << 20: lib.moe_expert_ffn_i8(  # noqa: E731
+        C.byref(dd), x_perm, off, C.byref(w), x, y, ysh, ws, n, None)
+    fwd = lambda dd, w, src=16, counts=16, local=None, ws=256, n=1 << 20, x=16: lib.moe_forward_i8(  # noqa: E731
+        C.byref(dd), None, 16, src, x, local, C.byref(w), counts, 16, None, ws, n, None)
+    for name, _ in moe.MoeWeightsI8._fields_:
+        shared = name.startswith("sh_")
+        for call in (ffn, fwd):
+            assert call(dsh, _i8_weights(moe, {name: None})) == moe.MOE_ERR_NULL, name
+            bad = 18 if name.removeprefix("sh_").startswith("s_") else 24   # scales to 4 bytes, matrices to 16
+            assert call(dsh, _i8_weights(moe, {name: bad})) == moe.MOE_ERR_ALIGN, name
+        if shared:   # not looked at without shared experts: the next check refuses
+            assert ffn(d, _i8_weights(moe, {name: None}), n=0) == moe.MOE_ERR_WORKSPACE
+    w = _i8_weights(moe)
+    assert lib.moe_expert_ffn_i8(C.byref(d), 16, 16, None, 16, 16, 16, 256, 1 << 20, None) == moe.MOE_ERR_NULL
+    assert ffn(d, w, x_perm=None) == moe.MOE_ERR_NULL and ffn(d, w, off=None) == moe.MOE_ERR_NULL
+    assert ffn(d, w, y=None) == moe.MOE_ERR_NULL and ffn(dsh, w, x=None) == moe.MOE_ERR_NULL
+    assert ffn(dsh, w, ysh=None) == moe.MOE_ERR_NULL and ffn(d, w, x_perm=24) == moe.MOE_ERR_ALIGN
+    assert ffn(dsh, w, x=24) == moe.MOE_ERR_ALIGN and ffn(d, w, ws=None) == moe.MOE_ERR_WORKSPACE
+    assert ffn(d, w, ws=128) == moe.MOE_ERR_ALIGN
+    assert fwd(d, w, src=None) == moe.MOE_ERR_NULL and fwd(d, w, x=24) == moe.MOE_ERR_ALIGN
+    assert fwd(moe.dims(T=4, H=64, E=8, k=2, I=64, S=2, E_local=4), w) == moe.MOE_ERR_DIMS   # no placement list
+    for call, entry in ((ffn, moe.ENTRY_EXPERT_FFN_I8), (fwd, moe.ENTRY_FORWARD_I8)):
+        for dd in (d, dsh):
+            need = moe.workspace_bytes(dd, entry)
+            assert call(dd, w, n=need - 1) == moe.MOE_ERR_WORKSPACE
+    # inner dimensions whose sums could pass int32
+    for change in (dict(H=2 ** 17), dict(I=2 ** 17), dict(n_shared=2, I_shared=2 ** 16)):
+        base = dict(T=4, H=64, E=8, k=2, I=64, S=2, E_local=8)
+        big = moe.dims(**{**base, **change})
+        assert ffn(big, w) == moe.MOE_ERR_UNSUPPORTED and fwd(big, w) == moe.MOE_ERR_UNSUPPORTED
+        for entry in (moe.ENTRY_EXPERT_FFN_I8, moe.ENTRY_FORWARD_I8):
+            assert moe.workspace_bytes(big, entry) == 0
+            assert moe.validate(big, entry, 1 << 62) == moe.MOE_ERR_UNSUPPORTED
+
+
+def test_large_batches_gather_limit(moe):
+    """forward_i8 reads token rows through 32-bit offsets: twice as many as moe_forward."""
+    base = dict(H=7168, E=256, k=1, I=2048, S=1, E_local=32)
+    assert moe.validate(moe.dims(T=299_000, **base), moe.ENTRY_FORWARD_I8, 1 << 62) == moe.MOE_OK
+    assert moe.validate(moe.dims(T=300_000, **base), moe.ENTRY_FORWARD_I8, 1 << 62) == moe.MOE_ERR_UNSUPPORTED
+    assert moe.validate(moe.dims(T=300_000, **base), moe.ENTRY_EXPERT_FFN_I8, 1 << 62) == moe.MOE_OK
+
+
+@pytest.mark.parametrize("name", W.CONFIG_ORDER)
+def test_workspaces_of_the_workloads(moe, name):
+    cfg = W.CONFIGS[name]
+    d = moe.dims_of(cfg)
+    rows = cfg.T * cfg.k
+    for entry in (moe.ENTRY_EXPERT_FFN_I8, moe.ENTRY_FORWARD_I8):
+        need = moe.workspace_bytes(d, entry)
+        assert need % 256 == 0
+        assert moe.validate(d, entry, need) == moe.MOE_OK
+        assert moe.validate(d, entry, need - 1) == moe.MOE_ERR_WORKSPACE
+    # hidden rows in bf16 and in int8, the input rows in int8
+    assert moe.workspace_bytes(d, moe.ENTRY_EXPERT_FFN_I8) >= rows * (3 * cfg.I + cfg.H)
+    # the layer quantises each token once
+    assert moe.workspace_bytes(d, moe.ENTRY_FORWARD_I8) >= rows * (3 * cfg.I + 2 * cfg.H) + cfg.T * cfg.H
+
+
+def test_binding_refuses_host_tensors_and_shapes(moe):
+    x = torch.zeros(4, 40, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU"):
+        moe.quantize_rows(x)
+    with pytest.raises(TypeError):
+        moe.quantize_rows(x.float())
+    with pytest.raises(ValueError, match="contiguous"):
+        moe.quantize_rows(x.t())
+    q, s, w, y = (torch.zeros(*n, dtype=t) for n, t in (((4, 48), torch.int8), ((4,), torch.float32), ((8, 48), torch.int8),
+                                                        ((4, 8), torch.bfloat16)))
+    ws = torch.zeros(8)
+    with pytest.raises(ValueError, match="GPU"):
+        moe.linear_i8(40, q, s, w, ws, y)
+    with pytest.raises(ValueError, match="at least 48"):
+        moe.linear_i8(40, q[:, :40], s, w, ws, y)
+    with pytest.raises(ValueError, match="rows of xq"):
+        moe.linear_i8(40, q[:3], s, w, ws, y)
+    with pytest.raises(ValueError, match="groups"):
+        moe.grouped_linear_i8(40, q, s, None, w, ws, y)
+    with pytest.raises(ValueError, match="one behind the other"):
+        moe.grouped_linear_i8(40, q, s, None, torch.zeros(2, 16, 48, dtype=torch.int8)[:, :8], ws, y)
+    d = moe.dims(T=4, H=64, E=8, k=2, I=64, S=2, E_local=8)
+    with pytest.raises(ValueError, match="w_gate"):
+        moe.make_weights_i8(d, {})
+
+
+def test_binding_checks_devices(moe):
+    """Tensors of two devices, or a stream of another device than theirs, are refused."""
+    class T:
+        def __init__(self, d):
+            self.device = torch.device(d)
+
+    class S:
+        device = torch.device("cuda:1")
+        cuda_stream = 0
+    with pytest.raises(ValueError, match="different devices"):
+        moe._on_device(S(), T("cuda:0"), None, T("cuda:1"))
+    with pytest.raises(ValueError, match="stream of"):
+        moe._on_device(S(), T("cuda:0"))
