@@ -1,0 +1,54 @@
+// Shared definitions of the 8-bit product kernels (gemm_i8.hip's launchers
+// choose among them).
+#pragma once
+
+#include "ffn_impl.h"
+
+namespace moe {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+// 16 bytes at any bf16 address: result rows of odd length start at odd
+// multiples of two bytes (global memory takes unaligned vector accesses on
+// this target)
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+
+constexpr uint32_t kPastEnd = 0x80000000u;  // an offset past a descriptor's range: reads zeros, no traffic
+constexpr int kXcds = 8;
+
+// Lane l holds A[row l % 32][16 (l / 32) ..] and B[col l % 32][16 (l / 32) ..]
+// (16 bytes), and C[8 (i / 4) + 4 (l / 32) + i % 4][l % 32] in element i.
+__device__ __forceinline__ i32x16 mfma_i8(i32x4 a, i32x4 b, i32x16 c) {
+  return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000);
+}
+
+// Row offsets as the kernels use them: whatever the array holds, they stay
+// within the rows that the caller's buffers have.
+__device__ __forceinline__ int row_at(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
+
+// Eight consecutive results, or those of them before N.
+__device__ __forceinline__ void store_cols(uint16_t* p, u32x4 v, int col, int N) {
+  if (col + 8 <= N) {
+    *reinterpret_cast<u32x4_a2*>(p) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i < N) p[i] = static_cast<uint16_t>(v[i / 2] >> (16 * (i & 1)));
+  }
+}
+
+// a over seg and sh (nullable, static rows) in one launch: 256-row tiles (K of
+// either past kTiledMinK), or items of up to 128 rows.
+constexpr int kTiledMinK = 384;
+hipError_t launch_tiled_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
+hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
+// Workgroups of launch_items_i8, and how many a grid dimension holds (2^32 - 1
+// threads).
+long long items_blocks(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
+constexpr long long kMaxItemBlocks = 0xffffffffll / (4 * kWave);
+
+}  // namespace moe

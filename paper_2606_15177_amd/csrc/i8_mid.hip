@@ -1,0 +1,421 @@
+// 8-bit products for decode and mid-sized batches: from one token to far fewer
+// rows per group than fill 256-row tiles.  Bound by reading the weights of the
+// groups that have rows once; groups of many rows add MFMA work.
+//
+// Items.  A workgroup of four waves takes up to 128 token rows of one group (a
+// chunk) times a block of weight rows: 128 of them for groups of up to 64 rows
+// (narrow items), 256 or 128 for larger ones (wide).  Two workgroups share a
+// CU.  A wave owns blocks of 32 weight rows (gated: 16 gate rows and the 16 up
+// rows of the same columns, which meet in one lane of the MFMA's result) and
+// all rows of the chunk.  Where a launch has few items, KP = 2 or 4 groups of
+// waves split K, over half or a quarter of the weight rows each, and add their
+// sums through LDS (integers: the order changes nothing).
+//
+// Pipeline.  buffer_load_dwordx4 ... lds into a ring of K stages in 80 KB of
+// LDS, D - 1 stages ahead, one barrier per stage.  16-byte chunk c of a row
+// sits at a slot rotated by the row, which spreads a fragment's rows over the
+// banks.  Each workgroup starts its walk along K elsewhere, so that rows that
+// lie a power of two apart spread over the memory channels.
+//
+// Order.  Items are numbered per kind (shared, wide, narrow) by group, column
+// block, chunk; an XCD owns a contiguous run of each kind, so that a group's
+// token rows and the weight block that its chunks share stay in one L2.  Within
+// an XCD heavy (shared and wide) and narrow items take turns of eight, a
+// multiple of its shader engines.
+#include <algorithm>
+#include <type_traits>
+
+#include "i8_impl.h"
+
+namespace moe {
+namespace {
+
+constexpr int kChunk = 128;         // token rows of a chunk
+constexpr int kWideRows = 64;       // groups of more rows take wide items
+constexpr int kItemRows = 128;      // weight rows of a narrow item
+constexpr int kFewWide = 128;       // fewer wide items than this take 128 weight rows: half the CUs' worth
+constexpr int kOneWide = 256;       // ... or fewer than this, one per CU, in a launch of fewer items than
+constexpr int kSlots = 512;         // workgroups fit the chip
+constexpr int kItemLds = 80 * 1024;
+constexpr int kTurn = 8;
+constexpr int kItemThreads = 4 * kWave;
+
+struct ItemsI8 {
+  GemmI8 g;   // groups with device offsets (groups 0: none)
+  GemmI8 sp;  // static rows (static_rows 0: none)
+  int rows;   // of g's result
+};
+
+__device__ __forceinline__ int run_start(int n, int x) { return static_cast<int>(static_cast<long long>(n) * x / kXcds); }
+
+template <bool GATED, int KP>
+__global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void items_i8_kernel(ItemsI8 ma) {
+  constexpr int FULL_COLS = GATED ? kItemRows / 2 : kItemRows;  // output columns of 128 weight rows
+  constexpr int OUT_COLS = FULL_COLS / KP;                      // ... of a narrow item
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+
+  // ---- which item ----
+  const int sp_m = ma.sp.static_rows;
+  const int sp_chunks = ceil_div(sp_m, kChunk);
+  // first row and rows of groups g0 + 64 i + lane
+  constexpr int kPasses = 4;
+  int first_row[kPasses], n_rows[kPasses];
+  auto load_groups = [&](int g0) {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      first_row[i] = n_rows[i] = 0;
+      if (g0 + i * kWave < ma.g.groups) {
+        const int gg = min(g0 + i * kWave + lane, ma.g.groups);  // past the last group: no rows
+        first_row[i] = ma.g.offsets[gg];
+        n_rows[i] = ma.g.offsets[min(gg + 1, ma.g.groups)];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      first_row[i] = min(max(first_row[i], 0), ma.rows);
+      n_rows[i] = max(min(n_rows[i], ma.rows) - first_row[i], 0);
+    }
+  };
+  int c_wide = 0, c_narrow = 0;  // chunks of the groups
+  for (int g0 = 0; g0 < ma.g.groups; g0 += kPasses * kWave) {
+    load_groups(g0);
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      c_wide += n_rows[i] > kWideRows ? ceil_div(n_rows[i], kChunk) : 0;
+      c_narrow += n_rows[i] > 0 && n_rows[i] <= kWideRows ? 1 : 0;
+    }
+  }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    c_wide += __shfl_xor(c_wide, off);
+    c_narrow += __shfl_xor(c_narrow, off);
+  }
+  c_wide = __builtin_amdgcn_readfirstlane(c_wide);
+  c_narrow = __builtin_amdgcn_readfirstlane(c_narrow);
+  const int narrow_blocks = ma.g.groups > 0 ? ceil_div(ma.g.N, OUT_COLS) : 0;
+  const int n_narrow = c_narrow * narrow_blocks;
+  auto shared_items = [&](int cols) { return sp_m > 0 ? sp_chunks * ceil_div(ma.sp.N, sp_m > kWideRows ? cols : OUT_COLS) : 0; };
+  int wide_cols = 2 * FULL_COLS;
+  const int heavy = shared_items(wide_cols) + c_wide * ceil_div(ma.g.N, wide_cols);
+  if (heavy < kFewWide || (heavy < kOneWide && heavy + n_narrow < kSlots)) wide_cols = FULL_COLS;
+  const int n_shared = shared_items(wide_cols);
+  const int wide_blocks = ceil_div(ma.g.N, wide_cols);
+  const int n_wide = c_wide * wide_blocks;
+  const int xcd = static_cast<int>(blockIdx.x) % kXcds, i = static_cast<int>(blockIdx.x) / kXcds;
+  const int s_lo = run_start(n_shared, xcd), w_lo = run_start(n_wide, xcd), n_lo = run_start(n_narrow, xcd);
+  const int my_shared = run_start(n_shared, xcd + 1) - s_lo;
+  const int my_heavy = my_shared + run_start(n_wide, xcd + 1) - w_lo;
+  const int my_narrow = run_start(n_narrow, xcd + 1) - n_lo;
+  if (i >= my_heavy + my_narrow) return;
+  const int turns = min(my_heavy, my_narrow) / kTurn;
+  bool narrow;
+  int idx;
+  if (i < 2 * turns * kTurn) {
+    narrow = (i / kTurn) & 1;
+    idx = i / (2 * kTurn) * kTurn + i % kTurn;
+  } else {
+    idx = i - turns * kTurn;
+    narrow = idx >= my_heavy;
+    idx = narrow ? i - my_heavy : idx;
+  }
+  const bool shared = !narrow && idx < my_shared;
+  const bool wide = shared ? sp_m > kWideRows : !narrow;
+  idx = narrow ? n_lo + idx : shared ? s_lo + idx : w_lo + idx - my_shared;
+  int g = 0, row_base = 0, m = sp_m, item = idx;
+  if (!shared) {
+    // the group of the kind's chunk `at`
+    const int blocks = wide ? wide_blocks : narrow_blocks;
+    const int at = idx / blocks;
+    bool found = false;
+    for (int g0 = 0, before = 0; !found && g0 < ma.g.groups; g0 += kPasses * kWave) {
+      if (ma.g.groups > kPasses * kWave) load_groups(g0);
+#pragma unroll
+      for (int q = 0; q < kPasses; ++q) {
+        if (found || g0 + q * kWave >= ma.g.groups) continue;
+        const int own = (n_rows[q] > kWideRows) == wide ? ceil_div(n_rows[q], kChunk) : 0;
+        int inc = own;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+          const int o = __shfl_up(inc, off);
+          if (lane >= off) inc += o;
+        }
+        const uint64_t past = __ballot(before + inc > at);
+        if (past) {
+          const int l = __ffsll(static_cast<long long>(past)) - 1;
+          g = g0 + q * kWave + l;
+          row_base = __builtin_amdgcn_readlane(first_row[q], l);
+          m = __builtin_amdgcn_readlane(n_rows[q], l);
+          item = idx - (before + __builtin_amdgcn_readlane(inc - own, l)) * blocks;
+          found = true;
+        } else {
+          before += __builtin_amdgcn_readlane(inc, kWave - 1);
+        }
+      }
+    }
+    if (!found) return;  // not reached: idx lies within the groups' items
+  }
+  const int n_chunks = ceil_div(m, kChunk);
+  int nblk = item / n_chunks;
+  int chunk = item - nblk * n_chunks;
+  g = __builtin_amdgcn_readfirstlane(g);
+  row_base = __builtin_amdgcn_readfirstlane(row_base);
+  m = __builtin_amdgcn_readfirstlane(m);
+  chunk = __builtin_amdgcn_readfirstlane(chunk);
+  nblk = __builtin_amdgcn_readfirstlane(nblk);
+
+  const GemmI8& p = shared ? ma.sp : ma.g;
+  const int N = p.N, bytes = ceil_div(p.K, 16) * 16;
+  const uint32_t ldx = static_cast<uint32_t>(p.ldx), ldw = static_cast<uint32_t>(p.ldw);
+  const int32_t* x_rows = p.x_rows;
+  // the group's rows in equal chunks of whole 32-row MFMA tiles
+  const int chunk_rows = ceil_div(ceil_div(m, n_chunks), 32) * 32;
+  const int m0 = chunk * chunk_rows;
+  const int rows = min(chunk_rows, m - m0);
+  const int n0 = nblk * (wide ? wide_cols : OUT_COLS);
+
+  const long long scales = static_cast<long long>(g) * N;
+  const int8_t* w0 = p.w0 + (scales + n0) * p.ldw;
+  const __amdgpu_buffer_rsrc_t rs_w0 = rsrc(w0);
+  const __amdgpu_buffer_rsrc_t rs_w1 = rsrc(GATED ? p.w1 + (scales + n0) * p.ldw : w0);
+  const __amdgpu_buffer_rsrc_t rs_x = rsrc(x_rows ? p.x : p.x + static_cast<long long>(row_base + m0) * p.ldx);
+  const int lrow = lane & 31, lhalf = lane >> 5;
+
+  auto body = [&](auto nsub_c, auto wb_c, auto kp_c, auto bk_c, auto depth_c) {
+    constexpr int NSUB = decltype(nsub_c)::value;  // 32-row tiles of tokens
+    constexpr int WB = decltype(wb_c)::value;      // 32-row blocks of weights per wave
+    constexpr int NK = decltype(kp_c)::value;      // K parts; waves WN apart take the same columns
+    constexpr int WN = 4 / NK;                     // waves along the weight rows
+    constexpr int BK = decltype(bk_c)::value;      // bytes of K per stage
+    constexpr int D = decltype(depth_c)::value;
+    constexpr int CPR = BK / 16;                   // 16-byte chunks per LDS row
+    constexpr int RPI = kWave / CPR;               // rows per load
+    constexpr int SWZ = 16 / CPR;                  // rows that share a rotation
+    constexpr int XPART = NSUB * 32 * BK;          // token rows of one K part
+    constexpr int STAGE = NK * XPART + 4 * WB * 32 * BK;
+    constexpr int XL = NSUB * 32 / RPI / WN;       // token loads per wave and stage
+    constexpr int WL = WB * 32 / RPI;              // weight loads per wave and stage
+    constexpr int LOADS = XL + WL;
+    constexpr int KS = BK / 32;                    // MFMA K-steps per stage
+    static_assert(D * STAGE <= kItemLds && XL * RPI * WN == NSUB * 32, "the ring fits, whole loads fill the token rows");
+    const int lr = lane / CPR;                     // row of a load
+    const int wn = wave % WN, wk = wave / WN;
+    // Scales: lane l holds that of weight row l of the wave's WB * 32, and
+    // those of the token rows of its results.
+    const int wr = lane % (WB * 32);
+    const int wcol = n0 + (GATED ? 16 * (WB * wn + wr / 32) + (wr & 15) : 32 * WB * wn + wr);
+    const float cs = (GATED && (wr & 16) ? p.ws1 : p.ws0)[scales + min(wcol, N - 1)];
+    float rsc[NSUB];
+#pragma unroll
+    for (int s = 0; s < NSUB; ++s) {
+      const int r = row_base + m0 + min(32 * s + lrow, rows - 1);
+      const int src = x_rows ? x_rows[r] : r;
+      const bool in = !x_rows || static_cast<unsigned>(src) < static_cast<unsigned>(p.x_count);
+      rsc[s] = p.x_scale[in ? src : 0];
+      if (!in) rsc[s] = 0.0f;
+    }
+    uint32_t woff[WL], xoff[XL];
+    int wpiece[WL], xpiece[XL];
+#pragma unroll
+    for (int i = 0; i < WL; ++i) {
+      const int r = RPI * i + lr;
+      const int b = WB * wn + r / 32;  // 32-row block of weights
+      const int col = GATED ? 16 * b + (r & 15) : 32 * b + r % 32;
+      woff[i] = n0 + col < N ? static_cast<uint32_t>(col) * ldw : kPastEnd;
+      wpiece[i] = (lane % CPR) ^ ((r / SWZ) % CPR);
+    }
+#pragma unroll
+    for (int q = 0; q < XL; ++q) {
+      const int r = RPI * (WN * q + wn) + lr;
+      int src = r;
+      if (x_rows) src = x_rows[row_base + m0 + min(r, rows - 1)];
+      const bool ok = r < rows && (!x_rows || static_cast<unsigned>(src) < static_cast<unsigned>(p.x_count));
+      xoff[q] = ok ? static_cast<uint32_t>(src) * ldx : kPastEnd;
+      xpiece[q] = (lane % CPR) ^ ((r / SWZ) % CPR);
+    }
+    const int nst = ceil_div(ceil_div(bytes, BK), NK);  // stages of a K part (the last part's may lie past K)
+    int s_ld = 0, slot_ld = 0;
+    int kb_ld = static_cast<int>((static_cast<unsigned>(nblk) * 7u + static_cast<unsigned>(g) * 3u) % static_cast<unsigned>(nst));
+    auto issue = [&]() {
+      unsigned char* st = smem + slot_ld * STAGE;
+      const int k0 = (wk * nst + kb_ld) * BK;
+      const uint32_t dead = s_ld < nst ? 0u : kPastEnd;
+#pragma unroll
+      for (int q = 0; q < XL; ++q) {
+        const int k = k0 + xpiece[q] * 16;
+        const uint32_t kill = dead | (k < bytes ? 0u : kPastEnd) | (xoff[q] & kPastEnd);
+        load_lds16(rs_x, st + wk * XPART + RPI * (WN * q + wn) * BK, (xoff[q] + static_cast<uint32_t>(k)) | kill);
+      }
+      unsigned char* wl = st + NK * XPART + wave * (WB * 32 * BK);
+#pragma unroll
+      for (int i = 0; i < WL; ++i) {
+        const int k = k0 + wpiece[i] * 16;
+        const uint32_t kill = dead | (k < bytes ? 0u : kPastEnd) | (woff[i] & kPastEnd);
+        load_lds16(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, (woff[i] + static_cast<uint32_t>(k)) | kill);
+      }
+      ++s_ld;
+      if (++slot_ld == D) slot_ld = 0;
+      if (++kb_ld == nst) kb_ld = 0;
+    };
+    i32x16 acc[WB][NSUB];
+#pragma unroll
+    for (int b = 0; b < WB; ++b)
+#pragma unroll
+      for (int s = 0; s < NSUB; ++s) acc[b][s] = i32x16{};
+#pragma unroll
+    for (int s = 0; s < D - 1; ++s) issue();
+    int slot = 0;
+    for (int j = 0; j < nst; ++j) {
+      __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * LOADS));  // own loads of stage j landed
+      phase_barrier();  // everyone's have, and everyone has read stage j - 1
+      issue();          // stage j + D - 1 into the slot of stage j - 1
+      const unsigned char* xp = smem + slot * STAGE + wk * XPART;
+      const unsigned char* wp = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
+      i32x4 wf[KS][WB], xf[KS][NSUB];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int at = ((2 * ks + lhalf) ^ ((lrow / SWZ) % CPR)) << 4;
+#pragma unroll
+        for (int b = 0; b < WB; ++b) wf[ks][b] = *reinterpret_cast<const i32x4*>(wp + (32 * b + lrow) * BK + at);
+#pragma unroll
+        for (int s = 0; s < NSUB; ++s) xf[ks][s] = *reinterpret_cast<const i32x4*>(xp + (32 * s + lrow) * BK + at);
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int b = 0; b < WB; ++b)
+#pragma unroll
+          for (int s = 0; s < NSUB; ++s) acc[b][s] = mfma_i8(wf[ks][b], xf[ks][s], acc[b][s]);
+      if (++slot == D) slot = 0;
+    }
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));  // the loads past the last stage: nothing may still write the LDS
+    if constexpr (NK > 1) {
+      static_assert((NK - 1) * WN * WB * NSUB * 16 * kWave * 4 <= kItemLds, "the partial sums fit the LDS");
+      int* red = reinterpret_cast<int*>(smem);
+      __syncthreads();  // every wave is past its last stage
+      if (wk > 0) {
+#pragma unroll
+        for (int b = 0; b < WB; ++b)
+#pragma unroll
+          for (int s = 0; s < NSUB; ++s)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              red[((((wk - 1) * WN + wn) * WB + b) * NSUB + s) * (16 * kWave) + v * kWave + lane] = acc[b][s][v];
+      }
+      __syncthreads();
+      if (wk > 0) return;
+#pragma unroll
+      for (int q = 0; q < NK - 1; ++q)
+#pragma unroll
+        for (int b = 0; b < WB; ++b)
+#pragma unroll
+          for (int s = 0; s < NSUB; ++s)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              acc[b][s][v] += red[(((q * WN + wn) * WB + b) * NSUB + s) * (16 * kWave) + v * kWave + lane];
+    }
+    // ---- results: lane holds C[n = 8 v4 + 4 lhalf + i][t = lrow] of each block ----
+    uint16_t* out = p.out + static_cast<long long>(row_base + m0) * p.ldo;
+#pragma unroll
+    for (int b = 0; b < WB; ++b) {
+      float sc[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        sc[v] = __int_as_float(__builtin_amdgcn_ds_bpermute(16 * lhalf + 4 * (32 * b + 8 * (v / 4) + v % 4), __float_as_int(cs)));
+#pragma unroll
+      for (int s = 0; s < NSUB; ++s) {
+        const int r = 32 * s + lrow;
+#pragma unroll
+        for (int h = 0; h < (GATED ? 1 : 2); ++h) {  // 16 columns each
+          uint32_t pk[2][2];
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            float o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int e = 8 * h + 4 * v + i;
+              o[i] = static_cast<float>(acc[b][s][e]) * sc[e] * rsc[s];
+              if constexpr (GATED) o[i] = silu(o[i]) * (static_cast<float>(acc[b][s][8 + e]) * sc[8 + e] * rsc[s]);
+            }
+            pk[v][0] = pack_bf16x2(o[0], o[1]);
+            pk[v][1] = pack_bf16x2(o[2], o[3]);
+          }
+          // lower lanes take columns 0..7, upper lanes 8..15
+          const auto a0 = __builtin_amdgcn_permlane32_swap(pk[0][0], pk[1][0], false, false);
+          const auto a1 = __builtin_amdgcn_permlane32_swap(pk[0][1], pk[1][1], false, false);
+          const int col = n0 + (GATED ? 16 * (WB * wn + b) : 32 * (WB * wn + b) + 16 * h) + 8 * lhalf;
+          if (r < rows && col < N) store_cols(out + r * p.ldo + col, u32x4{a0[0], a1[0], a0[1], a1[1]}, col, N);
+        }
+      }
+    }
+  };
+  using std::integral_constant;
+  using C1 = integral_constant<int, 1>;
+  using C2 = integral_constant<int, 2>;
+  using C3 = integral_constant<int, 3>;
+  using C4 = integral_constant<int, 4>;
+  using C5 = integral_constant<int, 5>;
+  using K64 = integral_constant<int, 64>;
+  using K128 = integral_constant<int, 128>;
+  if (wide && wide_cols > FULL_COLS)
+    body(C4{}, C2{}, C1{}, K64{}, C3{});
+  else if (wide)
+    body(C4{}, C1{}, C1{}, K64{}, C5{});
+  else if constexpr (KP == 1) {
+    if (rows > 32) body(C2{}, C1{}, C1{}, K128{}, C3{});
+    else body(C1{}, C1{}, C1{}, K128{}, C4{});
+  } else if constexpr (KP == 2) {
+    if (rows > 32) body(C2{}, C1{}, C2{}, K64{}, C5{});
+    else body(C1{}, C1{}, C2{}, K128{}, C3{});
+  } else {
+    if (rows > 32) body(C2{}, C1{}, C4{}, K64{}, C3{});
+    else body(C1{}, C1{}, C4{}, K64{}, C5{});
+  }
+}
+
+template <bool GATED, int KP>
+hipError_t launch_kp(long long blocks, const ItemsI8& ma, hipStream_t st) {
+  static unsigned long long lds_set = 0;  // devices with the LDS limit raised
+  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_i8_kernel<GATED, KP>), kItemLds, &lds_set);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((items_i8_kernel<GATED, KP>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), kItemLds, st, ma);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Narrow items that an evenly routed batch makes (undivided in K).
+long long narrow_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
+  const int cols = gated ? kItemRows / 2 : kItemRows;
+  return (a.offsets ? static_cast<long long>(seg.hit_groups) : 1) * ceil_div(a.N, cols) + (sh ? ceil_div(sh->N, cols) : 0);
+}
+
+int items_k_parts(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
+  if (seg.max_rows > kWideRows) return 1;
+  const long long items = narrow_items_i8(seg, a, sh, gated);
+  return items <= 64 ? 4 : items <= 128 ? 2 : 1;
+}
+
+long long items_blocks(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
+  const int cols = (gated ? kItemRows / 2 : kItemRows) / items_k_parts(seg, a, sh, gated);
+  // at most one partly filled chunk per group; wide items need fewer column blocks
+  const long long chunks = a.offsets ? seg.total_rows / kChunk + std::min(seg.groups, seg.total_rows) : ceil_div(a.static_rows, kChunk);
+  long long items = chunks * ceil_div(a.N, cols);
+  if (sh) items += static_cast<long long>(ceil_div(sh->static_rows, kChunk)) * ceil_div(sh->N, cols);
+  return items == 0 ? 0 : (items / kXcds + 3) * kXcds;  // each kind's run on an XCD rounds up by one
+}
+
+hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {
+  const long long blocks = items_blocks(seg, a, sh, gated);
+  if (blocks == 0) return hipSuccess;
+  ItemsI8 ma{a, sh ? *sh : GemmI8{}, seg.total_rows};
+  if (!a.offsets) ma = ItemsI8{GemmI8{}, a, 0};  // a product of static rows alone
+  switch (items_k_parts(seg, a, sh, gated)) {
+    case 4: return gated ? launch_kp<true, 4>(blocks, ma, st) : launch_kp<false, 4>(blocks, ma, st);
+    case 2: return gated ? launch_kp<true, 2>(blocks, ma, st) : launch_kp<false, 2>(blocks, ma, st);
+    default: return gated ? launch_kp<true, 1>(blocks, ma, st) : launch_kp<false, 1>(blocks, ma, st);
+  }
+}
+
+}  // namespace moe

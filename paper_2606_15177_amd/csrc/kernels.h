@@ -183,9 +183,12 @@ struct GemmI8 {
   int K, N;
   long long ldx, ldw, ldo;
 };
-// a over seg (as the expert GEMMs above); sh (nullable) over sh_seg, static rows.
-hipError_t launch_gemm_i8(const Segments& seg, const GemmI8& a, const Segments* sh_seg, const GemmI8* sh, bool gated,
-                          hipStream_t st);
+// a over seg (as the expert GEMMs above), and sh (nullable, static rows) in
+// the same launch.
+hipError_t launch_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
+// Host only: whether it accepts these sizes (the pointers are not looked at,
+// but for offsets being null or not).
+bool gemm_i8_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 
 // ---- combine.hip -----------------------------------------------------------
 hipError_t launch_combine(int T, int k, int H, const uint16_t* y_perm, const int32_t* inv_pos,

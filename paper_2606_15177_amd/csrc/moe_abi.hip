@@ -170,6 +170,13 @@ int weights_ok(const moe_dims* d, const moe_weights* w) {
   return MOE_OK;
 }
 
+// The routed rows; rows per expert and experts hit as if routing were even.
+moe::Segments routed_segments(const moe_dims* d, const int32_t* offsets) {
+  const int mean = static_cast<int>(static_cast<int64_t>(d->T) * d->k / d->E);
+  const int hit = static_cast<int>(std::ceil(d->E_local * (1.0 - std::pow(1.0 - static_cast<double>(d->k) / d->E, d->T))));
+  return moe::Segments{offsets, d->E_local, 0, d->T, d->T * d->k, mean, hit};
+}
+
 // The two grouped GEMMs of the experts (routed, then shared): their row
 // segments and arguments, built the same way for the host-side limit check
 // (null pointers; rows_indexed says whether the gate/up GEMM reads its rows
@@ -185,10 +192,7 @@ FfnPlan plan_ffn(const moe_dims* d, const uint16_t* x_perm, const int32_t* x_row
   const FfnWs fw = carve_ffn(d, ws);
   const int shw = static_cast<int>(sh_width(d));
   FfnPlan p{};
-  // rows per expert and experts hit, if routing were even
-  const int mean = static_cast<int>(static_cast<int64_t>(d->T) * d->k / d->E);
-  const int hit = static_cast<int>(std::ceil(d->E_local * (1.0 - std::pow(1.0 - static_cast<double>(d->k) / d->E, d->T))));
-  p.routed = moe::Segments{offsets, d->E_local, 0, d->T, d->T * d->k, mean, hit};
+  p.routed = routed_segments(d, offsets);
   p.shared = moe::Segments{nullptr, 1, d->T, d->T, d->T, d->T, 1};
   p.up = moe::UpArgs{x_perm, w ? w->w_gate : nullptr, w ? w->w_up : nullptr, fw.h, d->H, d->I, x_rows,
                      rows_indexed ? d->T : 0};
@@ -299,9 +303,39 @@ FfnI8Ws carve_ffn_i8(const moe_dims* d, bool one_x, void* base) {
 
 size_t ffn_i8_ws(const moe_dims* d, bool one_x) { return carve_ffn_i8(d, one_x, nullptr).bytes; }
 
+// The experts' products, built the same way for the limit check (null
+// pointers) and for the launches.
+struct FfnI8Plan {
+  moe::Segments routed;
+  moe::GemmI8 up, sh_up, dn, sh_dn;
+  bool sh;
+};
+FfnI8Plan plan_ffn_i8(const moe_dims* d, const FfnI8Ws& fw, const int32_t* x_rows, const int32_t* offsets,
+                      const moe_weights_i8& w, uint16_t* y_perm, uint16_t* y_shared) {
+  const int shw = static_cast<int>(sh_width(d));
+  const long long hp = pad16(d->H), ip = pad16(d->I), wp = pad16(shw);
+  FfnI8Plan p{};
+  p.routed = routed_segments(d, offsets);
+  p.up = moe::GemmI8{fw.xq, fw.xs, x_rows, x_rows ? d->T : 0, offsets, 0, d->E_local, w.w_gate, w.w_up, w.s_gate, w.s_up,
+                     fw.h, d->H, d->I, hp, hp, d->I};
+  p.sh_up = moe::GemmI8{fw.xq_sh, fw.xs_sh, nullptr, 0, nullptr, d->T, 1, w.sh_gate, w.sh_up, w.sh_s_gate, w.sh_s_up,
+                        fw.h_sh, d->H, shw, hp, hp, shw};
+  p.dn = moe::GemmI8{fw.hq, fw.hs, nullptr, 0, offsets, 0, d->E_local, w.w_down, nullptr, w.s_down, nullptr,
+                     y_perm, d->I, d->H, ip, ip, d->H};
+  p.sh_dn = moe::GemmI8{fw.hq_sh, fw.hs_sh, nullptr, 0, nullptr, d->T, 1, w.sh_down, nullptr, w.sh_s_down, nullptr,
+                        y_shared, shw, d->H, wp, wp, d->H};
+  p.sh = d->n_shared > 0;
+  return p;
+}
+
 int check_ffn_i8_limits(const moe_dims* d, bool one_x) {
   if (d->H > kMaxI8K || d->I > kMaxI8K || sh_width(d) > kMaxI8K) return MOE_ERR_UNSUPPORTED;
   if (one_x && static_cast<int64_t>(d->T) * pad16(d->H) > kSpan) return MOE_ERR_UNSUPPORTED;
+  static const int32_t some = 0;  // stands for device offsets
+  const FfnI8Plan p = plan_ffn_i8(d, FfnI8Ws{}, nullptr, &some, moe_weights_i8{}, nullptr, nullptr);
+  if (!moe::gemm_i8_supported(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true) ||
+      !moe::gemm_i8_supported(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false))
+    return MOE_ERR_UNSUPPORTED;
   return MOE_OK;
 }
 
@@ -329,39 +363,26 @@ int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, cons
                const moe_taps* taps, hipStream_t st) {
   const bool one_x = x_rows != nullptr;
   const FfnI8Ws fw = carve_ffn_i8(d, one_x, ws);
+  const FfnI8Plan p = plan_ffn_i8(d, fw, x_rows, offsets, *w, y_perm, y_shared);
   const int shw = static_cast<int>(sh_width(d)), rows = d->T * d->k;
-  const long long hp = pad16(d->H), ip = pad16(d->I), wp = pad16(shw);
   const int32_t* n_rows = offsets + d->E_local;
-  const int mean = static_cast<int>(static_cast<int64_t>(d->T) * d->k / d->E);
-  const int hit = static_cast<int>(std::ceil(d->E_local * (1.0 - std::pow(1.0 - static_cast<double>(d->k) / d->E, d->T))));
-  const moe::Segments routed{offsets, d->E_local, 0, d->T, rows, mean, hit};
-  const moe::Segments shared{nullptr, 1, d->T, d->T, d->T, d->T, 1};
-  const bool sh = d->n_shared > 0;
   hipError_t e;
 
   record(taps, 2 * MOE_STAGE_FFN_UP, st);
-  const moe::QuantArgs qx{x, fw.xq, fw.xs, one_x ? nullptr : n_rows, d->H, hp, one_x ? d->T : rows, d->H};
-  const moe::QuantArgs qx_sh{x_sh, fw.xq_sh, fw.xs_sh, nullptr, d->H, hp, d->T, d->H};
-  e = moe::launch_quantize_rows(qx, sh && !one_x ? &qx_sh : nullptr, st);
+  const moe::QuantArgs qx{x, fw.xq, fw.xs, one_x ? nullptr : n_rows, d->H, p.up.ldx, one_x ? d->T : rows, d->H};
+  const moe::QuantArgs qx_sh{x_sh, fw.xq_sh, fw.xs_sh, nullptr, d->H, p.up.ldx, d->T, d->H};
+  e = moe::launch_quantize_rows(qx, p.sh && !one_x ? &qx_sh : nullptr, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
-  const moe::GemmI8 up{fw.xq, fw.xs, x_rows, one_x ? d->T : 0, offsets, 0, d->E_local, w->w_gate, w->w_up,
-                       w->s_gate, w->s_up, fw.h, d->H, d->I, hp, hp, d->I};
-  const moe::GemmI8 sh_up{fw.xq_sh, fw.xs_sh, nullptr, 0, nullptr, d->T, 1, w->sh_gate, w->sh_up,
-                          w->sh_s_gate, w->sh_s_up, fw.h_sh, d->H, shw, hp, hp, shw};
-  e = moe::launch_gemm_i8(routed, up, sh ? &shared : nullptr, sh ? &sh_up : nullptr, true, st);
+  e = moe::launch_gemm_i8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   record(taps, 2 * MOE_STAGE_FFN_UP + 1, st);
 
   record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
-  const moe::QuantArgs qh{fw.h, fw.hq, fw.hs, n_rows, d->I, ip, rows, d->I};
-  const moe::QuantArgs qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, wp, d->T, shw};
-  e = moe::launch_quantize_rows(qh, sh ? &qh_sh : nullptr, st);
+  const moe::QuantArgs qh{fw.h, fw.hq, fw.hs, n_rows, d->I, p.dn.ldx, rows, d->I};
+  const moe::QuantArgs qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, p.sh_dn.ldx, d->T, shw};
+  e = moe::launch_quantize_rows(qh, p.sh ? &qh_sh : nullptr, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
-  const moe::GemmI8 dn{fw.hq, fw.hs, nullptr, 0, offsets, 0, d->E_local, w->w_down, nullptr,
-                       w->s_down, nullptr, y_perm, d->I, d->H, ip, ip, d->H};
-  const moe::GemmI8 sh_dn{fw.hq_sh, fw.hs_sh, nullptr, 0, nullptr, d->T, 1, w->sh_down, nullptr,
-                          w->sh_s_down, nullptr, y_shared, shw, d->H, wp, wp, d->H};
-  e = moe::launch_gemm_i8(routed, dn, sh ? &shared : nullptr, sh ? &sh_dn : nullptr, false, st);
+  e = moe::launch_gemm_i8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   record(taps, 2 * MOE_STAGE_FFN_DOWN + 1, st);
   return MOE_OK;
@@ -656,7 +677,8 @@ int moe_linear_i8(const moe_linear_dims* d, const int8_t* xq, const float* x_sca
   const moe::Segments seg{nullptr, 1, d->M, d->M, d->M, d->M, 1};
   const moe::GemmI8 a{xq, x_scale, nullptr, 0, nullptr, d->M, 1, wq, nullptr, w_scale, nullptr, y,
                       d->K, d->N, d->ldx, d->ldw, d->ldy};
-  return status(moe::launch_gemm_i8(seg, a, nullptr, nullptr, false, static_cast<hipStream_t>(stream)));
+  if (!moe::gemm_i8_supported(seg, a, nullptr, false)) return MOE_ERR_UNSUPPORTED;
+  return status(moe::launch_gemm_i8(seg, a, nullptr, false, static_cast<hipStream_t>(stream)));
 }
 
 int moe_grouped_linear_i8(const moe_linear_dims* d, const int8_t* xq, const float* x_scale, const int32_t* x_rows,
@@ -668,7 +690,8 @@ int moe_grouped_linear_i8(const moe_linear_dims* d, const int8_t* xq, const floa
   const moe::Segments seg{offsets, d->G, 0, d->M, d->M, d->M / d->G, std::min(d->G, d->M)};
   const moe::GemmI8 a{xq, x_scale, x_rows, x_rows ? d->X : 0, offsets, 0, d->G, wq, nullptr, w_scale, nullptr, y,
                       d->K, d->N, d->ldx, d->ldw, d->ldy};
-  return status(moe::launch_gemm_i8(seg, a, nullptr, nullptr, false, static_cast<hipStream_t>(stream)));
+  if (!moe::gemm_i8_supported(seg, a, nullptr, false)) return MOE_ERR_UNSUPPORTED;
+  return status(moe::launch_gemm_i8(seg, a, nullptr, false, static_cast<hipStream_t>(stream)));
 }
 
 int moe_expert_ffn_i8(const moe_dims* d, const moe_bf16* x_perm, const int32_t* offsets, const moe_weights_i8* w,
