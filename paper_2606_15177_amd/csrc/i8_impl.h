@@ -36,7 +36,7 @@ __device__ __forceinline__ void store_cols(uint16_t* p, u32x4 v, int col, int N)
     *reinterpret_cast<u32x4_a2*>(p) = v;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 7; ++i)
       if (col + i < N) p[i] = static_cast<uint16_t>(v[i / 2] >> (16 * (i & 1)));
   }
 }

@@ -1,11 +1,16 @@
 // 8-bit products for prefill-sized batches: persistent 256 x 256 tiles on
-// v_mfma_i32_32x32x32_i8, operands straight into LDS, two waves per SIMD.
+// v_mfma_i32_32x32x32_i8, operands straight into LDS, one wave per SIMD.
 //
-// Bound.  An MFMA takes 32 cycles for 32 x 32 x 32 products, 16 bytes per lane
-// of either operand: the same bytes per cycle as bf16 at twice the products.
-// A wave's 64 x 128 block needs six 1 KB fragment reads per eight MFMAs; with
-// the fills the LDS moves 64 KB per 512 cycles of MFMA time, near its 128
-// bytes a cycle.
+// Bound: the board's power.  An MFMA takes 32 cycles for 32 x 32 x 32 products,
+// 16 bytes per lane of either operand; back to back from registers alone they
+// run the chip at 1.9 GHz (3.9 POP/s), and what else moves costs clock: eight
+// waves that only read LDS at 112 bytes a cycle pull it down to 1.3 GHz.  So the
+// waves are few and their blocks as square as they come: four waves, 128 x 128
+// each, read eight 1 KB fragments per 16 MFMAs (eight waves of 64 x 128 read
+// twelve and issued four times the scalar instructions: dense 16384 x 4096 x
+// 7168 in 510 us where these take 466, in one sustained run).  Measured beside
+// the library's int8 product, in turn: 389 and 387 us there (2.47 POP/s), 434
+// and 433 us for 8192 x 8192 x 8192.
 //
 // Tiles.  256 token rows x 256 weight rows of one group.  Gated products take
 // 128 gate and the 128 up rows of the same columns, so that both sums of an
@@ -16,21 +21,19 @@
 // last partly filled one too.  The shared experts (static rows) are one more
 // group, first, with operands of its own.
 //
-// Rows past a group's end cost neither traffic (their loads lie past the
-// descriptor's range) nor MFMAs where they fill whole 64-row blocks: a wave
-// without rows only loads and waits.  Wave w on SIMD w % 4 takes rows 64 wm and
-// columns 128 wn with wm = (w % 4) / 2 + 2 (w / 4), wn = w % 2, so that the two
-// waves of a SIMD lie 128 rows apart: a group's last tile of up to 128 rows
-// keeps one wave busy on every SIMD and takes about half a tile's MFMA time.
+// A group's last tile: rows past its end cost no traffic (their loads lie past
+// the descriptor's range), and a tile of up to 128 or 64 rows takes half or a
+// quarter of the MFMAs, the four waves side by side along the weights.
 //
 // Stages and pipeline.  K advances by 128 bytes.  A stage is an X and a W part
-// [256 rows x 128 bytes], each in a slot of a ring of five (all 160 KB of
-// LDS): part P in slot P mod 5, X of stage s is P = 2 s, W 2 s + 1.  16-byte
-// chunk c of row r sits at slot c ^ ((r / 2) % 8), which spreads a fragment's
-// rows over the banks.  One barrier per stage, before its last K-step, once the
-// wave's loads of the next stage have landed and its LDS reads are done; past
-// it the two slots of the finished stage take W of stage + 2 and X of stage +
-// 3, two loads per wave and K-step among the MFMAs.  Stages run on across tiles.
+// [256 rows x 128 bytes]; rings of three X and two W parts take all 160 KB of
+// LDS.  16-byte chunk c of row r sits at slot c ^ ((r / 2) % 8), which spreads a
+// fragment's rows over the banks.  One barrier per stage, before its last
+// K-step, once the wave's loads of the next stage have landed and its LDS reads
+// are done; past it W of two stages on goes into the slot of this one, and X of
+// three on during the next stage.  Stages run on across tiles.  Within a K-step
+// the next one's fragment reads and the loads are spread over the MFMAs in the
+// order of their use.  The 256 accumulators fill the accumulation registers.
 #include <algorithm>
 #include <type_traits>
 
@@ -40,12 +43,12 @@ namespace moe {
 namespace {
 
 constexpr int kTile = 256;
-constexpr int kTiledThreads = 8 * kWave;
+constexpr int kTiledThreads = 4 * kWave;
 constexpr int kRow = 128;                 // bytes of an LDS row: K per stage
-constexpr int kPart = kTile * kRow;       // 32 KB
-constexpr int kParts = 5;
-constexpr int kTiledLds = kParts * kPart;
-constexpr int kLoads = 4;                 // per part and wave: 8 rows each
+constexpr int kPart = kTile * kRow;       // one operand of a stage: 32 KB
+constexpr int kXSlots = 3, kWSlots = 2;
+constexpr int kTiledLds = (kXSlots + kWSlots) * kPart;
+constexpr int kLoads = 8;                 // per part and wave: 8 rows each
 constexpr int kSteps = kRow / 32;         // MFMA K-steps of a stage
 constexpr int kBlockM = 8;
 constexpr int kWaitLds = 15 | (3 << 14) | (7 << 4);  // lgkmcnt(0)
@@ -71,14 +74,21 @@ __device__ __forceinline__ int load_scalar(const int* p, int i) { return ((Const
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// An accumulator element, read where it is used: the 256 accumulators fill the
+// accumulation registers, and left to itself the compiler copies all of them to
+// the other half of the register file at the end of the K loop.
+__device__ __forceinline__ float acc_value(int a) {
+  int v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
+  return static_cast<float>(v);
+}
+
 template <bool GATED, int PFX>
-__global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void tiled_i8_kernel(TiledI8 ta) {
+__global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void tiled_i8_kernel(TiledI8 ta) {
   constexpr int COLS = GATED ? kTile / 2 : kTile;  // output columns of a tile
-  constexpr int WCOLS = COLS / 2;                  // ... of a wave
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = lane_id();
   const int wave = uniform(static_cast<int>(threadIdx.x) / kWave);
-  const int wm = ((wave & 3) >> 1) + 2 * (wave >> 2), wn = wave & 1;
   const int lrow = lane & 31, lhalf = lane >> 5;
   const GemmI8& a = ta.g;
 
@@ -170,44 +180,42 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(2
   auto stages = [&](const TileInfo& ti) { return ceil_div(prob(ti).K, kRow); };
 
   // ---- loads ----
-  // Wave w fills rows 32 w .. 32 w + 31 of a part; load i writes rows 32 w + 8 i
+  // Wave w fills rows 64 w .. 64 w + 63 of a part; load i writes rows 64 w + 8 i
   // + lane / 8, slot lane % 8, with the chunk that belongs there.
-  auto load_row = [&](int i, int ln) { return 32 * wave + 8 * i + ln / 8; };
-  auto chunk_of = [&](int i, int ln) { return (ln % 8) ^ ((load_row(i, ln) / 2) % 8); };
-  auto part = [&](int P) { return smem + (P % kParts) * kPart; };
-  const bool w_up = GATED && ((wave >> 1) & 1);  // the wave's 32 weight rows are all gate or all up rows
+  auto chunk_of = [&](int i, int ln) { return (ln % 8) ^ ((4 * i + ln / 16) % 8); };
+  const bool w_up = GATED && (wave & 1);  // the wave's 64 weight rows are all gate or all up rows
   __amdgpu_buffer_rsrc_t rs_x, rs_w;
-  uint32_t xoff[kLoads], woff[kLoads], kx[2], kw[2];
-  int x_kb = 0, w_kb = 0, x_nkb = 0, w_nkb = 0, x_bytes = 0, w_bytes = 0;
-  int xr[kLoads];  // source rows of the next tile's loads, read a tile ahead
+  uint32_t xoff[kLoads], woff[kLoads];
+  // the stages to load next, of their tiles, and their slots
+  int x_kb = 0, w_kb = 0, x_nkb = 0, w_nkb = 0, x_bytes = 0, w_bytes = 0, x_slot = 0, w_slot = 0;
+  // First row of the wave's block of a tile (see place).
+  auto wave_row = [&](const TileInfo& ti) { return ti.rows > kTile / 2 ? 128 * (wave & 1) : 0; };
+  // Source rows of the next tile, read a tile ahead: of the wave's 64 rows of
+  // a part, and of rows l and 64 + l of its block of the results.
+  int xr = 0, src_row[2];
   auto x_rows_of = [&](const TileInfo& ti) {
     const GemmI8& p = prob(ti);
     const int ln = opaque_lane();
     if (p.x_rows) {
+      const int32_t* rows = p.x_rows + ti.row_base + ti.m0;
+      xr = rows[min(64 * wave + ln, ti.rows - 1)];
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) xr[i] = p.x_rows[ti.row_base + ti.m0 + min(load_row(i, ln), ti.rows - 1)];
+      for (int t = 0; t < 2; ++t) src_row[t] = rows[min(wave_row(ti) + 64 * t + ln, ti.rows - 1)];
     }
-  };
-  auto k_offsets = [&](uint32_t (&k)[2], int kb, int bytes) {
-    const int ln = opaque_lane();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) k[i] = static_cast<uint32_t>(kb * kRow) | (kb * kRow + chunk_of(i, ln) * 16 < bytes ? 0u : kPastEnd);
   };
   auto x_setup = [&](const TileInfo& ti, bool live) {
     const GemmI8& p = prob(ti);
     const int ln = opaque_lane();
     rs_x = rsrc(p.x_rows ? p.x : p.x + static_cast<long long>(ti.row_base + ti.m0) * p.ldx);
+    const int own = p.x_rows ? xr : 64 * wave + ln;
+    const bool in = live && 64 * wave + ln < ti.rows && (!p.x_rows || static_cast<unsigned>(own) < static_cast<unsigned>(p.x_count));
+    const int at = in ? own * static_cast<int>(p.ldx) : static_cast<int>(kPastEnd);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = load_row(i, ln);
-      const int src = p.x_rows ? xr[i] : r;
-      const bool ok = live && r < ti.rows && (!p.x_rows || static_cast<unsigned>(src) < static_cast<unsigned>(p.x_count));
-      xoff[i] = ok ? static_cast<uint32_t>(src) * static_cast<uint32_t>(p.ldx) + chunk_of(i, ln) * 16 : kPastEnd;
-    }
+    for (int i = 0; i < kLoads; ++i)
+      xoff[i] = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(4 * (8 * i + ln / 8), at)) + chunk_of(i, ln) * 16;
     x_kb = 0;
     x_nkb = stages(ti);
     x_bytes = ceil_div(p.K, 16) * 16;
-    k_offsets(kx, 0, x_bytes);
   };
   auto w_setup = [&](const TileInfo& ti, bool live) {
     const GemmI8& p = prob(ti);
@@ -216,112 +224,119 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(2
     rs_w = rsrc((w_up ? p.w1 : p.w0) + (static_cast<long long>(ti.g) * p.N + col0) * p.ldw);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = load_row(i, ln);
-      const int col = GATED ? (r >> 7) * 64 + (r & 63) : r;
+      const int r = 8 * i + ln / 8, col = GATED ? 64 * (wave >> 1) + r : 64 * wave + r;
       woff[i] = live && col0 + col < p.N ? static_cast<uint32_t>(col) * static_cast<uint32_t>(p.ldw) + chunk_of(i, ln) * 16 : kPastEnd;
     }
     w_kb = 0;
     w_nkb = stages(ti);
     w_bytes = ceil_div(p.K, 16) * 16;
-    k_offsets(kw, 0, w_bytes);
   };
-  auto load = [&](__amdgpu_buffer_rsrc_t rs, unsigned char* dst, const uint32_t (&off)[kLoads], const uint32_t (&k)[2], int i) {
-    load_lds16(rs, dst + wave * (32 * kRow) + i * 1024, (off[i] + k[i & 1]) | ((off[i] | k[i & 1]) & kPastEnd));
+  // (the range check looks at the lane's offset, not at the scalar one)
+  auto load = [&](__amdgpu_buffer_rsrc_t rs, int at, uint32_t off, int kb) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(smem + at), 16, off, kb * kRow, 0, 0);
   };
-  auto x_load = [&](int s, int i) { load(rs_x, part(2 * s), xoff, kx, i); };
-  auto w_load = [&](int s, int i) { load(rs_w, part(2 * s + 1), woff, kw, i); };
+  auto x_load = [&](int i) { load(rs_x, x_slot + wave * (64 * kRow) + i * 1024, xoff[i], x_kb); };
+  auto w_load = [&](int i) { load(rs_w, kXSlots * kPart + w_slot + wave * (64 * kRow) + i * 1024, woff[i], w_kb); };
+  // The stream's last stage: chunks past K (the offsets are not used again)
+  auto mask_tail = [&](uint32_t (&off)[kLoads], int kb, int bytes) {
+    const int ln = opaque_lane();
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      if (kb * kRow + chunk_of(i, ln) * 16 >= bytes) off[i] = kPastEnd;
+  };
 
   TileInfo cur = tile_info(0), nxt = cur;
   bool more = false;
-  // (a product has at least four stages here, so the loads, up to two stages
+  // (a product has at least four stages here, so the loads, up to three stages
   // ahead, are on the current tile or the next one)
   auto x_advance = [&]() {
+    x_slot = x_slot == (kXSlots - 1) * kPart ? 0 : x_slot + kPart;
     if (++x_kb == x_nkb) x_setup(nxt, more);
-    else k_offsets(kx, x_kb, x_bytes);
+    else if (x_kb == x_nkb - 1 && x_bytes % kRow != 0) mask_tail(xoff, x_kb, x_bytes);
   };
   auto w_advance = [&]() {
+    w_slot ^= kPart;
     if (++w_kb == w_nkb) w_setup(nxt, more);
-    else k_offsets(kw, w_kb, w_bytes);
+    else if (w_kb == w_nkb - 1 && w_bytes % kRow != 0) mask_tail(woff, w_kb, w_bytes);
   };
 
   // ---- products ----
-  i32x4 xf[2][2], wf[2][4];
-  i32x16 acc[4][2];
-  auto read_frags = [&](int s, int ks, int set) {
-    const unsigned char* xp = part(2 * s) + (64 * wm + lrow) * kRow;
-    const unsigned char* wp = part(2 * s + 1) + (128 * wn + lrow) * kRow;
-    const int slot = ((2 * ks + lhalf) ^ ((lrow / 2) % 8)) << 4;
+  // A wave's block of a tile, in 32 x 32 results: four tiles of weights by four
+  // of rows, the waves two by two; in a tile of up to 128 (64) rows two by four
+  // (two), all waves along the weights.
+  i32x4 xf[2][4], wf[2][4];
+  i32x16 acc[4][4];
+  int frag[kSteps];  // the lane's place in its row of a part, for K-step ks
 #pragma unroll
-    for (int t = 0; t < 4; ++t) wf[set][t] = *reinterpret_cast<const i32x4*>(wp + t * 32 * kRow + slot);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) xf[set][t] = *reinterpret_cast<const i32x4*>(xp + t * 32 * kRow + slot);
+  for (int ks = 0; ks < kSteps; ++ks) frag[ks] = lrow * kRow + (((2 * ks + lhalf) ^ ((lrow / 2) % 8)) << 4);
+  // bytes from a part's start to the block's rows, to its weight tiles and to
+  // the second half of them (gated: the up rows)
+  int x_at = 0, w_at[2] = {0, 0};
+  auto place = [&](const TileInfo& ti) {
+    const bool full = ti.rows > kTile / 2;
+    x_at = wave_row(ti) * kRow;
+    w_at[0] = kXSlots * kPart + kRow * (full ? 128 * (wave >> 1) : GATED ? 128 * (wave >> 1) + 32 * (wave & 1) : 64 * wave);
+    w_at[1] = w_at[0] + kRow * (full || GATED ? 64 : 32);
   };
-  auto mfma_set = [&](int set) {
-#pragma unroll
-    for (int tn = 0; tn < 4; ++tn)
-#pragma unroll
-      for (int tm = 0; tm < 2; ++tm) acc[tn][tm] = mfma_i8(wf[set][tn], xf[set][tm], acc[tn][tm]);
+  // Fragment q of a K-step, in the order of their first use.
+  auto read_frag = [&](auto tn, auto tm, int q, int xs, int ws, int ks, int set) {
+    constexpr int TN = decltype(tn)::value, TM = decltype(tm)::value;
+    if (q == 1 || q > TN) {
+      const int t = q == 1 ? 0 : q - TN;
+      if (t < TM) xf[set][t] = *reinterpret_cast<const i32x4*>(smem + xs + x_at + t * 32 * kRow + frag[ks]);
+    } else {
+      const int t = q == 0 ? 0 : q - 1;
+      wf[set][t] = *reinterpret_cast<const i32x4*>(smem + ws + w_at[t / (TN / 2)] + t % (TN / 2) * 32 * kRow + frag[ks]);
+    }
   };
 
-  // Scales of the wave's columns (lane l: column l, and column 64 + l or, gated,
-  // column l of up) and of the lane's two rows.
+  // Scales: of the block's weight rows (lane l: gate l and up l, or rows l and
+  // 64 + l), and of its rows l and 64 + l.
   float cs[2], rsc[2];
-  int src_row[2];
-  auto epilogue = [&](const TileInfo& ti, unsigned char* scr) {
+  int in_x = 0;  // bit t: row 64 t + l is a row of x (else zeros, whatever scale was read)
+  auto epilogue = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w, unsigned char* scr) {
+    constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
+    constexpr int TILES = GATED ? TN / 2 : TN;      // of 32 output columns
+    constexpr int PASS = TILES < 2 ? TILES : 2;     // ... stored at a time
+    constexpr int CH = 4 * PASS;                    // 16-byte chunks of a row of them
     const GemmI8& p = prob(ti);
-    const int ln = opaque_lane();
-    const int erow = ln & 31, eh = ln >> 5;
-    const int col_w = ti.nt * COLS + wn * WCOLS;
-    uint16_t* out = p.out + static_cast<long long>(ti.row_base + ti.m0 + 64 * wm) * p.ldo;
-    const int rows = ti.rows - 64 * wm;
-    // column scale of element 4 v + i of accumulator tile t of 32 columns
-    auto col_scale = [&](float c, int t, int v, int i) {
-      return __int_as_float(__builtin_amdgcn_ds_bpermute(16 * eh + 4 * (32 * t + 8 * v + i), __float_as_int(c)));
-    };
+    const int row_w = wave_row(ti);
+    uint16_t* out = p.out + static_cast<long long>(ti.row_base + ti.m0 + row_w) * p.ldo;
+    const int rows = ti.rows - row_w;
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");  // the last MFMAs' results are readable (acc_value)
 #pragma unroll
-    for (int tn = 0; tn < (GATED ? 2 : 4); ++tn) {
-      float s0[16], s1[16];
+    for (int tm = 0; tm < TM; ++tm) {
+      const int ln = opaque_lane();
+      const int erow = ln & 31, eh = ln >> 5;
+      auto from_lane = [&](float v, int l) { return __int_as_float(__builtin_amdgcn_ds_bpermute(4 * l, __float_as_int(v))); };
+      const float rs = from_lane((in_x >> (tm / 2)) & 1 ? rsc[tm / 2] : 0.0f, 32 * (tm % 2) + erow);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s0[v] = col_scale(GATED ? cs[0] : cs[tn / 2], tn % 2, v / 4, v % 4);
-        if constexpr (GATED) s1[v] = col_scale(cs[1], tn, v / 4, v % 4);
-      }
+      for (int pass = 0; pass < TILES / PASS; ++pass) {
+        // 32 rows of CH chunks, chunk c of row r rotated by the row
+        auto place = [&](int r, int c) { return scr + r * (16 * CH) + ((c ^ ((r / (8 / CH)) % CH)) << 4); };
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-      for (int tm = 0; tm < 2; ++tm) {
-        uint32_t pk[8];
+        for (int h = 0; h < PASS; ++h)
 #pragma unroll
-        for (int v = 0; v < 8; ++v) {
-          float o[2];
+          for (int v = 0; v < 4; ++v) {
+            const int tn = PASS * pass + h;
+            float o[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            o[i] = static_cast<float>(acc[tn][tm][2 * v + i]) * s0[2 * v + i] * rsc[tm];
-            if constexpr (GATED) o[i] = silu(o[i]) * (static_cast<float>(acc[tn + 2][tm][2 * v + i]) * s1[2 * v + i] * rsc[tm]);
+            for (int i = 0; i < 4; ++i) {
+              const int e = 4 * v + i, l = 32 * (tn % 2) + 8 * v + i;
+              o[i] = acc_value(acc[tn][tm][e]) * from_lane(GATED ? cs[0] : cs[tn / 2], l + 4 * eh) * rs;
+              if constexpr (GATED) o[i] = silu(o[i]) * (acc_value(acc[tn + TILES][tm][e]) * from_lane(cs[1], l + 4 * eh) * rs);
+            }
+            *reinterpret_cast<u32x2*>(place(erow, 4 * h + v) + 8 * eh) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
           }
-          pk[v] = pack_bf16x2(o[0], o[1]);
+#pragma unroll
+        for (int q = 0; q < CH / 2; ++q) {
+          const int rr = q * (kWave / CH) + ln / CH, c = ln % CH;
+          const u32x4 v = *reinterpret_cast<const u32x4*>(place(rr, c));
+          const int r = 32 * tm + rr, col = col_w + 32 * PASS * pass + 8 * c;
+          if (r < rows && col < p.N) store_cols(out + r * p.ldo + col, v, col, p.N);
         }
-        if constexpr (GATED) {
-          const int r = 32 * tm + erow;
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {  // columns 16 q ..: the lane halves swap to 8 consecutive ones each
-            const auto a0 = __builtin_amdgcn_permlane32_swap(pk[4 * q], pk[4 * q + 2], false, false);
-            const auto a1 = __builtin_amdgcn_permlane32_swap(pk[4 * q + 1], pk[4 * q + 3], false, false);
-            const int col = col_w + 32 * tn + 16 * q + 8 * eh;
-            if (r < rows && col < p.N) store_cols(out + r * p.ldo + col, u32x4{a0[0], a1[0], a0[1], a1[1]}, col, p.N);
-          }
-        } else {
-          // 32 rows x 64 bytes of this wave's LDS, chunk c of row r at c ^ ((r / 2) % 4)
-          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            *reinterpret_cast<u32x2*>(scr + erow * 64 + ((v ^ ((erow / 2) % 4)) << 4) + 8 * eh) = u32x2{pk[2 * v], pk[2 * v + 1]};
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int rr = 16 * q + (ln >> 2), c = ln & 3;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(scr + rr * 64 + ((c ^ ((rr / 2) % 4)) << 4));
-            const int r = 32 * tm + rr, col = col_w + 32 * tn + 8 * c;
-            if (r < rows && col < p.N) store_cols(out + r * p.ldo + col, v, col, p.N);
-          }
-        }
+        __builtin_amdgcn_sched_barrier(0);  // (accumulators are read a tile at a time)
       }
     }
   };
@@ -330,85 +345,105 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(2
   x_rows_of(cur);
   x_setup(cur, true);
   w_setup(cur, true);
-  for (int s = 0; s < 2; ++s) {
+  auto load_part = [&](bool x) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) x_load(s, i);
-    x_advance();
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      if (s == 0 || i < kLoads / 2) w_load(s, i);
-    if (s == 0) w_advance();
-  }
-  __builtin_amdgcn_s_waitcnt(wait_vm(kLoads + kLoads / 2));  // own stage-0 loads landed
+    for (int i = 0; i < kLoads; ++i) {
+      if (x) x_load(i);
+      else w_load(i);
+    }
+  };
+  load_part(true);
+  x_advance();
+  load_part(false);
+  w_advance();
+  load_part(true);
+  x_advance();
+  load_part(false);
+  w_advance();
+  __builtin_amdgcn_s_waitcnt(wait_vm(2 * kLoads));  // own stage-0 loads landed
   phase_barrier();
-  read_frags(0, 0, 0);
-  int j = 0;
+  int xs = 0, ws = 0;  // slots of the stage that is computed
   for (int i = 0; i < mine; ++i) {
+    const GemmI8& p = prob(cur);
+    const int nkb = stages(cur);
+    const bool full = cur.rows > kTile / 2;
+    const int col_w = cur.nt * COLS + (full ? 2 * (wave >> 1) : wave) * (COLS / 4);
+    {
+      const int ln = opaque_lane();
+      const long long sc = static_cast<long long>(cur.g) * p.N;
+      cs[0] = p.ws0[sc + min(col_w + ln, p.N - 1)];
+      cs[1] = GATED ? p.ws1[sc + min(col_w + ln, p.N - 1)] : p.ws0[sc + min(col_w + 64 + ln, p.N - 1)];
+      in_x = 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int src = p.x_rows ? src_row[t] : cur.row_base + cur.m0 + min(wave_row(cur) + 64 * t + ln, cur.rows - 1);
+        const bool in = !p.x_rows || static_cast<unsigned>(src) < static_cast<unsigned>(p.x_count);
+        rsc[t] = p.x_scale[in ? src : 0];
+        in_x |= in ? 1 << t : 0;
+      }
+    }
+    place(cur);
     more = i + 1 < mine;
     if (more) {
       nxt = tile_info(i + 1);
       x_rows_of(nxt);
     }
-    const GemmI8& p = prob(cur);
-    const int nkb = stages(cur);
-    {
-      const int ln = opaque_lane();
-      const long long sc = static_cast<long long>(cur.g) * p.N;
-      const int col = cur.nt * COLS + wn * WCOLS + ln;
-      cs[0] = p.ws0[sc + min(col, p.N - 1)];
-      cs[1] = GATED ? p.ws1[sc + min(col, p.N - 1)] : p.ws0[sc + min(col + 64, p.N - 1)];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int r = cur.row_base + cur.m0 + min(64 * wm + 32 * t + (ln & 31), cur.rows - 1);
-        src_row[t] = p.x_rows ? p.x_rows[r] : r;
-      }
-    }
 #pragma unroll
     for (int tn = 0; tn < 4; ++tn)
 #pragma unroll
-      for (int tm = 0; tm < 2; ++tm) acc[tn][tm] = i32x16{};
-    // (compiled twice: a wave without rows has neither reads nor MFMAs)
-    auto k_loop = [&](auto with_rows) {
-      constexpr bool kRows = decltype(with_rows)::value;
-      for (int kb = 0; kb < nkb; ++kb, ++j) {
+      for (int tm = 0; tm < 4; ++tm) acc[tn][tm] = i32x16{};
+    // Stage j: X of stage j + 2 goes out with its first two K-steps, W of stage
+    // j + 2 with its last one, past the barrier.
+    auto tile = [&](auto tn_c, auto tm_c) {
+      constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
+      constexpr int FRAGS = TN + TM, MFMAS = TN * TM;
 #pragma unroll
-        for (int ks = 0; ks < kSteps - 1; ++ks) {
-          if constexpr (kRows) read_frags(j, ks + 1, (ks + 1) & 1);
+      for (int q = 0; q < FRAGS; ++q) read_frag(tn_c, tm_c, q, xs, ws, 0, 0);
+      for (int kb = 0; kb < nkb; ++kb) {
+        const int xs1 = xs == (kXSlots - 1) * kPart ? 0 : xs + kPart, ws1 = ws ^ kPart;
 #pragma unroll
-          for (int l = 0; l < kLoads / 2; ++l) {
-            if (ks == 0) w_load(j + 1, kLoads / 2 + l);
-            else x_load(j + 2, (ks - 1) * (kLoads / 2) + l);
+        for (int ks = 0; ks < kSteps; ++ks) {
+          const bool last = ks == kSteps - 1;
+          if (last) {
+            x_advance();
+            __builtin_amdgcn_s_waitcnt(wait_vm(kLoads));  // own loads of stage j + 1 landed
+            __builtin_amdgcn_s_waitcnt(kWaitLds);
+            phase_barrier();
           }
-          if (ks == 0) w_advance();
-          if constexpr (kRows) mfma_set(ks & 1);
+          const int set = ks & 1, nx = last ? xs1 : xs, nw = last ? ws1 : ws, nk = last ? 0 : ks + 1;
+          // (the reads past the tile's last stage are not used)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            if (q < FRAGS) read_frag(tn_c, tm_c, q, nx, nw, nk, set ^ 1);
+            if (last) w_load(q);
+            else if (ks < 2 && q % 2 == 0) x_load(4 * ks + q / 2);
+#pragma unroll
+            for (int m = q * MFMAS / 8; m < (q + 1) * MFMAS / 8; ++m) {
+              const int tm = m / TN, tn = m % TN;
+              acc[tn][tm] = mfma_i8(wf[set][tn], xf[set][tm], acc[tn][tm]);
+            }
+          }
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            if (q < FRAGS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (last || (ks < 2 && q % 2 == 0)) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+            if (MFMAS >= 8 || q % 2 == 1) __builtin_amdgcn_sched_group_barrier(0x008, MFMAS == 16 ? 2 : 1, 0);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
-        x_advance();
-        __builtin_amdgcn_s_waitcnt(wait_vm(kLoads));  // own stage j + 1 landed
-        __builtin_amdgcn_s_waitcnt(kWaitLds);
-        phase_barrier();
-        if (kRows && kb == 0) {
-          // the rows' scales, through the rows just read (a row outside x is zeros)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const bool in = !p.x_rows || static_cast<unsigned>(src_row[t]) < static_cast<unsigned>(p.x_count);
-            rsc[t] = p.x_scale[in ? src_row[t] : 0];
-            if (!in) rsc[t] = 0.0f;
-          }
-        }
-        if (kRows || kb == nkb - 1) read_frags(j + 1, 0, 0);  // (past the last stage: a harmless stale read)
-#pragma unroll
-        for (int l = 0; l < kLoads / 2; ++l) w_load(j + 2, l);
-        if constexpr (kRows) mfma_set((kSteps - 1) & 1);
-        __builtin_amdgcn_sched_barrier(0);
+        w_advance();
+        xs = xs1;
+        ws = ws1;
       }
+      // The X part of the tile's last stage is free until this wave's next loads
+      // into its own 8 KB of it, with the next tile's first stage.
+      epilogue(tn_c, tm_c, cur, col_w, smem + (xs == 0 ? (kXSlots - 1) * kPart : xs - kPart) + wave * (64 * kRow));
     };
-    const bool active = 64 * wm < cur.rows;
-    if (active) k_loop(std::true_type{});
-    else k_loop(std::false_type{});
-    // The W part of the tile's last stage is free until this wave loads X of the
-    // stage three ahead into its own 4 KB of it.
-    if (active) epilogue(cur, part(2 * (j - 1) + 1) + wave * (32 * kRow));
+    using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
+    if (full) tile(Four{}, Four{});
+    else if (cur.rows > kTile / 4) tile(Two{}, Four{});
+    else tile(Two{}, Two{});
     cur = nxt;
   }
   __builtin_amdgcn_s_waitcnt(0);  // the dead loads past the last tile: nothing may still write the LDS
