@@ -72,6 +72,15 @@ __device__ __forceinline__ int opaque_lane() {
 typedef const int __attribute__((address_space(4)))* ConstIntPtr;
 __device__ __forceinline__ int load_scalar(const int* p, int i) { return ((ConstIntPtr)(uintptr_t)p)[i]; }
 
+// n / d for 0 <= n, 0 < d, n / d < 2^22 (tiles of a launch): the quotient in
+// fp32 is off by one at most.
+__device__ __forceinline__ int quotient(int n, int d) {
+  int q = static_cast<int>(static_cast<float>(n) * __builtin_amdgcn_rcpf(static_cast<float>(d)));
+  const int r = n - q * d;
+  q += r < 0 ? -1 : r >= d ? 1 : 0;
+  return q;
+}
+
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // An accumulator element, read where it is used: the 256 accumulators fill the
@@ -147,7 +156,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
       mg = total_mt;
     } else {
       local -= ta.sp_tiles;
-      const int at = local / tiles_n;  // row tile, of all groups
+      const int at = quotient(local, tiles_n);  // row tile, of all groups
       int cnt = 0, lo = 0;
 #pragma unroll
       for (int k = 0; k < PFX; ++k) {
@@ -163,9 +172,9 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
       local -= lo * tiles_n;
     }
     // blocks of kBlockM row tiles, the last block with the rest
-    const int b = local / (kBlockM * tn), r = local - b * (kBlockM * tn);
+    const int b = quotient(local, kBlockM * tn), r = local - b * (kBlockM * tn);
     const int bm = min(kBlockM, mg - b * kBlockM);
-    ti.nt = r / bm;
+    ti.nt = quotient(r, bm);
     ti.m0 = (b * kBlockM + r - ti.nt * bm) * kTile;
     ti.rows = min(kTile, m - ti.m0);
     ti.sp = uniform(ti.sp);
@@ -190,17 +199,23 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   int x_kb = 0, w_kb = 0, x_nkb = 0, w_nkb = 0, x_bytes = 0, w_bytes = 0, x_slot = 0, w_slot = 0;
   // First row of the wave's block of a tile (see place).
   auto wave_row = [&](const TileInfo& ti) { return ti.rows > kTile / 2 ? 128 * (wave & 1) : 0; };
-  // Source rows of the next tile, read a tile ahead: of the wave's 64 rows of
-  // a part, and of rows l and 64 + l of its block of the results.
-  int xr = 0, src_row[2];
+  // Source rows of a tile: of the wave's 64 rows of a part (read two tiles
+  // ahead: loads still in flight at the K loop's start, if it used them, would
+  // all be waited for there), and of rows l and 64 + l of its block of the
+  // results (read a tile ahead).
+  int xr = 0, xr_next = 0, src_row[2];
   auto x_rows_of = [&](const TileInfo& ti) {
+    const GemmI8& p = prob(ti);
+    int v = 0;
+    if (p.x_rows) v = p.x_rows[ti.row_base + ti.m0 + min(64 * wave + opaque_lane(), ti.rows - 1)];
+    return v;
+  };
+  auto result_rows_of = [&](const TileInfo& ti) {
     const GemmI8& p = prob(ti);
     const int ln = opaque_lane();
     if (p.x_rows) {
-      const int32_t* rows = p.x_rows + ti.row_base + ti.m0;
-      xr = rows[min(64 * wave + ln, ti.rows - 1)];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) src_row[t] = rows[min(wave_row(ti) + 64 * t + ln, ti.rows - 1)];
+      for (int t = 0; t < 2; ++t) src_row[t] = p.x_rows[ti.row_base + ti.m0 + min(wave_row(ti) + 64 * t + ln, ti.rows - 1)];
     }
   };
   auto x_setup = [&](const TileInfo& ti, bool live) {
@@ -245,7 +260,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
       if (kb * kRow + chunk_of(i, ln) * 16 >= bytes) off[i] = kPastEnd;
   };
 
-  TileInfo cur = tile_info(0), nxt = cur;
+  TileInfo cur = tile_info(0), nxt = cur, nn = cur;
   bool more = false;
   // (a product has at least four stages here, so the loads, up to three stages
   // ahead, are on the current tile or the next one)
@@ -303,46 +318,74 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     const int row_w = wave_row(ti);
     uint16_t* out = p.out + static_cast<long long>(ti.row_base + ti.m0 + row_w) * p.ldo;
     const int rows = ti.rows - row_w;
-    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");  // the last MFMAs' results are readable (acc_value)
+    auto from_lane = [&](float v, int l) { return __int_as_float(__builtin_amdgcn_ds_bpermute(4 * l, __float_as_int(v))); };
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const int ln = opaque_lane();
+    const int erow = ln & 31, eh = ln >> 5;
+    float rs[TM];
 #pragma unroll
-    for (int tm = 0; tm < TM; ++tm) {
-      const int ln = opaque_lane();
-      const int erow = ln & 31, eh = ln >> 5;
-      auto from_lane = [&](float v, int l) { return __int_as_float(__builtin_amdgcn_ds_bpermute(4 * l, __float_as_int(v))); };
-      const float rs = from_lane((in_x >> (tm / 2)) & 1 ? rsc[tm / 2] : 0.0f, 32 * (tm % 2) + erow);
+    for (int tm = 0; tm < TM; ++tm) rs[tm] = from_lane((in_x >> (tm / 2)) & 1 ? rsc[tm / 2] : 0.0f, 32 * (tm % 2) + erow);
+    // 32 rows of CH chunks in one of two buffers, chunk c of row r rotated by the row
+    auto place = [&](int buf, int r, int c) { return scr + buf * 4096 + r * (16 * CH) + ((c ^ ((r / (8 / CH)) % CH)) << 4); };
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");  // the last MFMAs' results are readable (acc_value)
+    auto emit = [&](auto inside) {
+      constexpr bool kInside = decltype(inside)::value;  // every row and column of the wave's block is a result
 #pragma unroll
       for (int pass = 0; pass < TILES / PASS; ++pass) {
-        // 32 rows of CH chunks, chunk c of row r rotated by the row
-        auto place = [&](int r, int c) { return scr + r * (16 * CH) + ((c ^ ((r / (8 / CH)) % CH)) << 4); };
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        float s0[16 * PASS], s1[16 * PASS];
 #pragma unroll
-        for (int h = 0; h < PASS; ++h)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const int tn = PASS * pass + h;
-            float o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int e = 4 * v + i, l = 32 * (tn % 2) + 8 * v + i;
-              o[i] = acc_value(acc[tn][tm][e]) * from_lane(GATED ? cs[0] : cs[tn / 2], l + 4 * eh) * rs;
-              if constexpr (GATED) o[i] = silu(o[i]) * (acc_value(acc[tn + TILES][tm][e]) * from_lane(cs[1], l + 4 * eh) * rs);
-            }
-            *reinterpret_cast<u32x2*>(place(erow, 4 * h + v) + 8 * eh) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
-          }
-#pragma unroll
-        for (int q = 0; q < CH / 2; ++q) {
-          const int rr = q * (kWave / CH) + ln / CH, c = ln % CH;
-          const u32x4 v = *reinterpret_cast<const u32x4*>(place(rr, c));
-          const int r = 32 * tm + rr, col = col_w + 32 * PASS * pass + 8 * c;
-          if (r < rows && col < p.N) store_cols(out + r * p.ldo + col, v, col, p.N);
+        for (int v = 0; v < 16 * PASS; ++v) {
+          const int tn = PASS * pass + v / 16, l = 32 * (tn % 2) + 8 * (v % 16 / 4) + v % 4;
+          s0[v] = from_lane(GATED ? cs[0] : cs[tn / 2], l + 4 * eh);
+          if constexpr (GATED) s1[v] = from_lane(cs[1], l + 4 * eh);
         }
-        __builtin_amdgcn_sched_barrier(0);  // (accumulators are read a tile at a time)
+        // a row tile's results go out while the next one's are computed
+        const int rr = ln / CH, cc = ln % CH;
+        const int col = col_w + 32 * PASS * pass + 8 * cc;
+        uint16_t* at = out + rr * p.ldo + col;
+        auto put = [&](int tm) {
+#pragma unroll
+          for (int q = 0; q < CH / 2; ++q) {
+            const int r = q * (kWave / CH) + rr;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(place(tm & 1, r, cc));
+            uint16_t* to = at + (32 * tm + q * (kWave / CH)) * p.ldo;
+            if constexpr (kInside) *reinterpret_cast<u32x4_a2*>(to) = v;
+            else if (32 * tm + r < rows && col < p.N) store_cols(to, v, col, p.N);
+          }
+        };
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) {
+#pragma unroll
+          for (int h = 0; h < PASS; ++h)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int tn = PASS * pass + h;
+              float o[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int e = 4 * v + i;
+                o[i] = acc_value(acc[tn][tm][e]) * s0[16 * h + e] * rs[tm];
+                if constexpr (GATED) o[i] = silu(o[i]) * (acc_value(acc[tn + TILES][tm][e]) * s1[16 * h + e] * rs[tm]);
+              }
+              *reinterpret_cast<u32x2*>(place(tm & 1, erow, 4 * h + v) + 8 * eh) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            }
+          if (tm > 0) put(tm - 1);
+          __builtin_amdgcn_sched_barrier(0);  // (accumulators are read a tile at a time)
+        }
+        put(TM - 1);
       }
-    }
+    };
+    if (rows >= 32 * TM && col_w + 32 * TILES <= p.N) emit(std::true_type{});
+    else emit(std::false_type{});
   };
 
   // ---- the workgroup's tiles ----
-  x_rows_of(cur);
+  xr = x_rows_of(cur);
+  result_rows_of(cur);
+  if (mine > 1) {
+    nxt = tile_info(1);
+    xr_next = x_rows_of(nxt);
+  }
   x_setup(cur, true);
   w_setup(cur, true);
   auto load_part = [&](bool x) {
@@ -384,9 +427,12 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     }
     place(cur);
     more = i + 1 < mine;
-    if (more) {
-      nxt = tile_info(i + 1);
-      x_rows_of(nxt);
+    xr = xr_next;
+    asm volatile("" : "+v"(xr));  // (waited for here, long after its load, not in the loop)
+    if (more) result_rows_of(nxt);
+    if (i + 2 < mine) {
+      nn = tile_info(i + 2);
+      xr_next = x_rows_of(nn);
     }
 #pragma unroll
     for (int tn = 0; tn < 4; ++tn)
@@ -445,6 +491,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     else if (cur.rows > kTile / 4) tile(Two{}, Four{});
     else tile(Two{}, Two{});
     cur = nxt;
+    nxt = nn;
   }
   __builtin_amdgcn_s_waitcnt(0);  // the dead loads past the last tile: nothing may still write the LDS
 }
