@@ -36,7 +36,7 @@ constexpr int kItemRows = 128;      // weight rows of a narrow item
 constexpr int kFewWide = 128;       // fewer wide items than this take 128 weight rows: half the CUs' worth
 constexpr int kOneWide = 256;       // ... or fewer than this, one per CU, in a launch of fewer items than
 constexpr int kSlots = 512;         // workgroups fit the chip
-constexpr int kItemLds = 80 * 1024;
+constexpr int kItemLds = 80 * 1024;   // two workgroups per CU
 constexpr int kTurn = 8;
 constexpr int kItemThreads = 4 * kWave;
 
@@ -47,6 +47,21 @@ struct ItemsI8 {
 };
 
 __device__ __forceinline__ int run_start(int n, int x) { return static_cast<int>(static_cast<long long>(n) * x / kXcds); }
+
+// The wave's loads of stage j have landed: of what was issued after them, the
+// token loads of the first stages (weights go out first there) and the whole
+// stages since may still be in flight.
+template <int D, int XL, int LOADS, int J = 0>
+__device__ __forceinline__ void wait_stage(int j) {
+  if constexpr (J == D - 1) {
+    __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * LOADS));
+  } else {
+    if (j == J)
+      __builtin_amdgcn_s_waitcnt(wait_vm((D - 2 - J) * XL + J * LOADS));
+    else
+      wait_stage<D, XL, LOADS, J + 1>(j);
+  }
+}
 
 template <bool GATED, int KP>
 __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void items_i8_kernel(ItemsI8 ma) {
@@ -78,22 +93,22 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
       n_rows[i] = max(min(n_rows[i], ma.rows) - first_row[i], 0);
     }
   };
-  int c_wide = 0, c_narrow = 0;  // chunks of the groups
+  // chunks of the groups (few groups are wide in the batches whose latency counts)
+  int c_wide = 0, c_narrow = 0;
   for (int g0 = 0; g0 < ma.g.groups; g0 += kPasses * kWave) {
     load_groups(g0);
+    int wide_here = 0;
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-      c_wide += n_rows[i] > kWideRows ? ceil_div(n_rows[i], kChunk) : 0;
-      c_narrow += n_rows[i] > 0 && n_rows[i] <= kWideRows ? 1 : 0;
+    for (int q = 0; q < kPasses; ++q) {
+      c_narrow += __popcll(__ballot(n_rows[q] > 0 && n_rows[q] <= kWideRows));
+      wide_here += n_rows[q] > kWideRows ? ceil_div(n_rows[q], kChunk) : 0;
+    }
+    if (__ballot(wide_here > 0) != 0) {
+#pragma unroll
+      for (int off = 1; off < kWave; off <<= 1) wide_here += __shfl_xor(wide_here, off);
+      c_wide += __builtin_amdgcn_readfirstlane(wide_here);
     }
   }
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    c_wide += __shfl_xor(c_wide, off);
-    c_narrow += __shfl_xor(c_narrow, off);
-  }
-  c_wide = __builtin_amdgcn_readfirstlane(c_wide);
-  c_narrow = __builtin_amdgcn_readfirstlane(c_narrow);
   const int narrow_blocks = ma.g.groups > 0 ? ceil_div(ma.g.N, OUT_COLS) : 0;
   const int n_narrow = c_narrow * narrow_blocks;
   auto shared_items = [&](int cols) { return sp_m > 0 ? sp_chunks * ceil_div(ma.sp.N, sp_m > kWideRows ? cols : OUT_COLS) : 0; };
@@ -134,12 +149,19 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
       for (int q = 0; q < kPasses; ++q) {
         if (found || g0 + q * kWave >= ma.g.groups) continue;
+        // chunks of the kind in the lane's group, and up to and with it
         const int own = (n_rows[q] > kWideRows) == wide ? ceil_div(n_rows[q], kChunk) : 0;
         int inc = own;
+        if (wide) {
 #pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-          const int o = __shfl_up(inc, off);
-          if (lane >= off) inc += o;
+          for (int off = 1; off < kWave; off <<= 1) {
+            const int o = __shfl_up(inc, off);
+            if (lane >= off) inc += o;
+          }
+        } else {
+          const uint64_t has = __ballot(own > 0);
+          inc += static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(has >> 32),
+                                                            __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(has), 0u)));
         }
         const uint64_t past = __ballot(before + inc > at);
         if (past) {
@@ -182,7 +204,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   const __amdgpu_buffer_rsrc_t rs_x = rsrc(x_rows ? p.x : p.x + static_cast<long long>(row_base + m0) * p.ldx);
   const int lrow = lane & 31, lhalf = lane >> 5;
 
-  auto body = [&](auto nsub_c, auto wb_c, auto kp_c, auto bk_c, auto depth_c) {
+  auto body = [&](auto nsub_c, auto wb_c, auto kp_c, auto bk_c, auto depth_c, auto few_c) {
     constexpr int NSUB = decltype(nsub_c)::value;  // 32-row tiles of tokens
     constexpr int WB = decltype(wb_c)::value;      // 32-row blocks of weights per wave
     constexpr int NK = decltype(kp_c)::value;      // K parts; waves WN apart take the same columns
@@ -192,29 +214,33 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int CPR = BK / 16;                   // 16-byte chunks per LDS row
     constexpr int RPI = kWave / CPR;               // rows per load
     constexpr int SWZ = 16 / CPR;                  // rows that share a rotation
-    constexpr int XPART = NSUB * 32 * BK;          // token rows of one K part
+    constexpr bool FEW = decltype(few_c)::value;   // up to 8 rows: the ring holds no more
+    constexpr int XR = FEW ? 8 : NSUB * 32;        // token rows of a stage
+    constexpr int XPART = XR * BK;                 // ... of one K part
     constexpr int STAGE = NK * XPART + 4 * WB * 32 * BK;
-    constexpr int XL = NSUB * 32 / RPI / WN;       // token loads per wave and stage
+    constexpr int XL = FEW ? 1 : XR / RPI / WN;    // token loads per wave and stage
     constexpr int WL = WB * 32 / RPI;              // weight loads per wave and stage
     constexpr int LOADS = XL + WL;
     constexpr int KS = BK / 32;                    // MFMA K-steps per stage
-    static_assert(D * STAGE <= kItemLds && XL * RPI * WN == NSUB * 32, "the ring fits, whole loads fill the token rows");
+    static_assert(D * STAGE <= kItemLds, "the ring fits");
+    static_assert(FEW ? RPI == 8 : XL * RPI * WN == XR, "whole loads fill the token rows");
     const int lr = lane / CPR;                     // row of a load
     const int wn = wave % WN, wk = wave / WN;
-    // Scales: lane l holds that of weight row l of the wave's WB * 32, and
-    // those of the token rows of its results.
-    const int wr = lane % (WB * 32);
-    const int wcol = n0 + (GATED ? 16 * (WB * wn + wr / 32) + (wr & 15) : 32 * WB * wn + wr);
-    const float cs = (GATED && (wr & 16) ? p.ws1 : p.ws0)[scales + min(wcol, N - 1)];
-    float rsc[NSUB];
+    // What waits for nothing goes out first: the source rows of the token loads
+    // and of the results, then the weights of the first stages; the rest follows.
+    auto x_row = [&](int q) { return FEW ? lr : RPI * (WN * q + wn) + lr; };  // (few rows: every wave of a K part loads them)
+    int xsrc[XL], src[NSUB];
+#pragma unroll
+    for (int q = 0; q < XL; ++q) xsrc[q] = x_rows ? x_rows[row_base + m0 + min(x_row(q), rows - 1)] : x_row(q);
 #pragma unroll
     for (int s = 0; s < NSUB; ++s) {
       const int r = row_base + m0 + min(32 * s + lrow, rows - 1);
-      const int src = x_rows ? x_rows[r] : r;
-      const bool in = !x_rows || static_cast<unsigned>(src) < static_cast<unsigned>(p.x_count);
-      rsc[s] = p.x_scale[in ? src : 0];
-      if (!in) rsc[s] = 0.0f;
+      src[s] = x_rows ? x_rows[r] : r;
     }
+    const int nst = ceil_div(ceil_div(bytes, BK), NK);  // stages of a K part (the last part's may lie past K)
+    const int rot = static_cast<int>((static_cast<unsigned>(nblk) * 7u + static_cast<unsigned>(g) * 3u) % static_cast<unsigned>(nst));
+    // first byte of stage s of the wave's K part
+    auto k_at = [&](int s) { return (wk * nst + (rot + s < nst ? rot + s : rot + s - nst)) * BK; };
     uint32_t woff[WL], xoff[XL];
     int wpiece[WL], xpiece[XL];
 #pragma unroll
@@ -225,61 +251,72 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
       woff[i] = n0 + col < N ? static_cast<uint32_t>(col) * ldw : kPastEnd;
       wpiece[i] = (lane % CPR) ^ ((r / SWZ) % CPR);
     }
+    auto load = [&](__amdgpu_buffer_rsrc_t rs, unsigned char* to, uint32_t off, int k, bool live) {
+      const uint32_t kill = (live && k < bytes ? 0u : kPastEnd) | (off & kPastEnd);
+      load_lds16(rs, to, (off + static_cast<uint32_t>(k)) | kill);
+    };
+    auto issue_w = [&](int s, int slot) {
+      unsigned char* wl = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
+      const int k0 = k_at(s);
+#pragma unroll
+      for (int i = 0; i < WL; ++i)
+        load(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, woff[i], k0 + wpiece[i] * 16, s < nst);
+    };
+    auto issue_x = [&](int s, int slot) {
+      unsigned char* xl = smem + slot * STAGE + wk * XPART;
+      const int k0 = k_at(s);
+#pragma unroll
+      for (int q = 0; q < XL; ++q)
+        load(rs_x, xl + (FEW ? 0 : RPI * (WN * q + wn) * BK), xoff[q], k0 + xpiece[q] * 16, s < nst);
+    };
+#pragma unroll 1
+    for (int s = 0; s < D - 1; ++s) issue_w(s, s);
 #pragma unroll
     for (int q = 0; q < XL; ++q) {
-      const int r = RPI * (WN * q + wn) + lr;
-      int src = r;
-      if (x_rows) src = x_rows[row_base + m0 + min(r, rows - 1)];
-      const bool ok = r < rows && (!x_rows || static_cast<unsigned>(src) < static_cast<unsigned>(p.x_count));
-      xoff[q] = ok ? static_cast<uint32_t>(src) * ldx : kPastEnd;
+      const int r = x_row(q);
+      const bool ok = r < rows && (!x_rows || static_cast<unsigned>(xsrc[q]) < static_cast<unsigned>(p.x_count));
+      xoff[q] = ok ? static_cast<uint32_t>(xsrc[q]) * ldx : kPastEnd;
       xpiece[q] = (lane % CPR) ^ ((r / SWZ) % CPR);
     }
-    const int nst = ceil_div(ceil_div(bytes, BK), NK);  // stages of a K part (the last part's may lie past K)
-    int s_ld = 0, slot_ld = 0;
-    int kb_ld = static_cast<int>((static_cast<unsigned>(nblk) * 7u + static_cast<unsigned>(g) * 3u) % static_cast<unsigned>(nst));
-    auto issue = [&]() {
-      unsigned char* st = smem + slot_ld * STAGE;
-      const int k0 = (wk * nst + kb_ld) * BK;
-      const uint32_t dead = s_ld < nst ? 0u : kPastEnd;
+#pragma unroll 1
+    for (int s = 0; s < D - 1; ++s) issue_x(s, s);
+    // Scales: lane l holds that of weight row l of the wave's WB * 32, and
+    // those of the token rows of its results.
+    const int wr = lane % (WB * 32);
+    const int wcol = n0 + (GATED ? 16 * (WB * wn + wr / 32) + (wr & 15) : 32 * WB * wn + wr);
+    const float cs = (GATED && (wr & 16) ? p.ws1 : p.ws0)[scales + min(wcol, N - 1)];
+    float rsc[NSUB];
+    bool in_x[NSUB];  // (else a row of zeros, whatever scale was read)
 #pragma unroll
-      for (int q = 0; q < XL; ++q) {
-        const int k = k0 + xpiece[q] * 16;
-        const uint32_t kill = dead | (k < bytes ? 0u : kPastEnd) | (xoff[q] & kPastEnd);
-        load_lds16(rs_x, st + wk * XPART + RPI * (WN * q + wn) * BK, (xoff[q] + static_cast<uint32_t>(k)) | kill);
-      }
-      unsigned char* wl = st + NK * XPART + wave * (WB * 32 * BK);
-#pragma unroll
-      for (int i = 0; i < WL; ++i) {
-        const int k = k0 + wpiece[i] * 16;
-        const uint32_t kill = dead | (k < bytes ? 0u : kPastEnd) | (woff[i] & kPastEnd);
-        load_lds16(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, (woff[i] + static_cast<uint32_t>(k)) | kill);
-      }
-      ++s_ld;
-      if (++slot_ld == D) slot_ld = 0;
-      if (++kb_ld == nst) kb_ld = 0;
-    };
+    for (int s = 0; s < NSUB; ++s) {
+      in_x[s] = !x_rows || static_cast<unsigned>(src[s]) < static_cast<unsigned>(p.x_count);
+      rsc[s] = p.x_scale[in_x[s] ? src[s] : 0];
+    }
     i32x16 acc[WB][NSUB];
 #pragma unroll
     for (int b = 0; b < WB; ++b)
 #pragma unroll
       for (int s = 0; s < NSUB; ++s) acc[b][s] = i32x16{};
-#pragma unroll
-    for (int s = 0; s < D - 1; ++s) issue();
     int slot = 0;
     for (int j = 0; j < nst; ++j) {
-      __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * LOADS));  // own loads of stage j landed
+      wait_stage<D, XL, LOADS>(j);  // own loads of stage j landed
       phase_barrier();  // everyone's have, and everyone has read stage j - 1
-      issue();          // stage j + D - 1 into the slot of stage j - 1
+      // stage j + D - 1 into the slot of stage j - 1
+      const int into = slot == 0 ? D - 1 : slot - 1;
+      issue_x(j + D - 1, into);
+      issue_w(j + D - 1, into);
       const unsigned char* xp = smem + slot * STAGE + wk * XPART;
       const unsigned char* wp = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
       i32x4 wf[KS][WB], xf[KS][NSUB];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const int at = ((2 * ks + lhalf) ^ ((lrow / SWZ) % CPR)) << 4;
+        const int xrow = FEW ? lrow % 8 : lrow;  // (few rows: columns past them are not results)
+        const int xat = ((2 * ks + lhalf) ^ ((xrow / SWZ) % CPR)) << 4;
 #pragma unroll
         for (int b = 0; b < WB; ++b) wf[ks][b] = *reinterpret_cast<const i32x4*>(wp + (32 * b + lrow) * BK + at);
 #pragma unroll
-        for (int s = 0; s < NSUB; ++s) xf[ks][s] = *reinterpret_cast<const i32x4*>(xp + (32 * s + lrow) * BK + at);
+        for (int s = 0; s < NSUB; ++s) xf[ks][s] = *reinterpret_cast<const i32x4*>(xp + (32 * s + xrow) * BK + xat);
       }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
@@ -315,6 +352,8 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
             for (int v = 0; v < 16; ++v)
               acc[b][s][v] += red[(((q * WN + wn) * WB + b) * NSUB + s) * (16 * kWave) + v * kWave + lane];
     }
+#pragma unroll
+    for (int s = 0; s < NSUB; ++s) rsc[s] = in_x[s] ? rsc[s] : 0.0f;
     // ---- results: lane holds C[n = 8 v4 + 4 lhalf + i][t = lrow] of each block ----
     uint16_t* out = p.out + static_cast<long long>(row_base + m0) * p.ldo;
 #pragma unroll
@@ -358,19 +397,23 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   using C5 = integral_constant<int, 5>;
   using K64 = integral_constant<int, 64>;
   using K128 = integral_constant<int, 128>;
+  constexpr std::false_type whole{};
+  constexpr std::true_type few{};
   if (wide && wide_cols > FULL_COLS)
-    body(C4{}, C2{}, C1{}, K64{}, C3{});
+    body(C4{}, C2{}, C1{}, K64{}, C3{}, whole);
   else if (wide)
-    body(C4{}, C1{}, C1{}, K64{}, C5{});
+    body(C4{}, C1{}, C1{}, K64{}, C5{}, whole);
   else if constexpr (KP == 1) {
-    if (rows > 32) body(C2{}, C1{}, C1{}, K128{}, C3{});
-    else body(C1{}, C1{}, C1{}, K128{}, C4{});
+    if (rows > 32) body(C2{}, C1{}, C1{}, K128{}, C3{}, whole);
+    else body(C1{}, C1{}, C1{}, K128{}, C4{}, whole);
   } else if constexpr (KP == 2) {
-    if (rows > 32) body(C2{}, C1{}, C2{}, K64{}, C5{});
-    else body(C1{}, C1{}, C2{}, K128{}, C3{});
+    if (rows > 32) body(C2{}, C1{}, C2{}, K64{}, C5{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, C3{}, whole);
+    else body(C1{}, C1{}, C2{}, K128{}, C4{}, few);
   } else {
-    if (rows > 32) body(C2{}, C1{}, C4{}, K64{}, C3{});
-    else body(C1{}, C1{}, C4{}, K64{}, C5{});
+    if (rows > 32) body(C2{}, C1{}, C4{}, K64{}, C3{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C4{}, K64{}, C5{}, whole);
+    else body(C1{}, C1{}, C4{}, K128{}, C4{}, few);
   }
 }
 

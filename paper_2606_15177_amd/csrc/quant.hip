@@ -80,63 +80,81 @@ __device__ __forceinline__ u32x2 quantize_vec(u32x4 v, float pre, float c) {
   return out;
 }
 
+// The largest of the 64 lanes' values, in all of them: within rows of 16 lanes
+// by data-parallel moves, then across the rows.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#define MOE_DPP_MAX(ctrl) v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), ctrl, 0xf, 0xf, true)))
+  MOE_DPP_MAX(0xB1);   // quad_perm [1 0 3 2]
+  MOE_DPP_MAX(0x4E);   // quad_perm [2 3 0 1]
+  MOE_DPP_MAX(0x141);  // row_half_mirror
+  MOE_DPP_MAX(0x140);  // row_mirror
+#undef MOE_DPP_MAX
+  const auto r16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(static_cast<uint32_t>(r16[0]), static_cast<uint32_t>(r16[1]));
+  const auto r32 = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(static_cast<uint32_t>(r32[0]), static_cast<uint32_t>(r32[1]));
+}
+
 // WPR waves per row, V vectors per lane held in registers (vectors past them
-// are read twice).
-template <int WPR, int V>
+// are read twice), R rows at a time per wave (WPR 1): short rows need several
+// in flight to cover the memory's latency.
+template <int WPR, int V, int R>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(QuantPair p) {
-  constexpr int RPB = kQuantWaves / WPR;  // rows of a block at a time
-  constexpr int STEP = WPR * kWave;       // vectors of a row at a time
+  static_assert(WPR == 1 || R == 1, "several rows at a time: one wave each");
+  constexpr int RPB = kQuantWaves / WPR * R;  // rows of a block at a time
+  constexpr int STEP = WPR * kWave;           // vectors of a row at a time
   __shared__ uint32_t part[kQuantWaves];
   const bool second = static_cast<int>(blockIdx.x) >= p.blocks_a;
   const QuantArgs& a = second ? p.b : p.a;
   const int block = static_cast<int>(blockIdx.x) - (second ? p.blocks_a : 0);
   const int blocks = second ? static_cast<int>(gridDim.x) - p.blocks_a : p.blocks_a;
-  const int wave = static_cast<int>(threadIdx.x) / kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
   const int at = static_cast<int>(threadIdx.x) % STEP;
   const int rows = a.n_rows ? min(a.rows, *a.n_rows) : a.rows;
   const int nvec = ceil_div(a.cols, 16) * 2;  // the padding to 16 values is written too, as zeros
-  for (long long r0 = static_cast<long long>(block) * RPB; r0 < rows; r0 += static_cast<long long>(blocks) * RPB) {
-    const long long r = r0 + wave / WPR;
-    const bool live = r < rows;
-    const uint16_t* row = a.x + (live ? r : 0) * a.ldx;
-    u32x4 v[V];
-    u16x2 m = {0, 0};
+  for (long long r0 = static_cast<long long>(block) * RPB + wave / WPR * R; r0 < rows; r0 += static_cast<long long>(blocks) * RPB) {
+    u32x4 v[R][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      v[i] = u32x4{0u, 0u, 0u, 0u};
-      if (live && at + i * STEP < nvec) v[i] = load_vec(row, at + i * STEP, a.cols);
-    }
+    for (int k = 0; k < R; ++k)
 #pragma unroll
-    for (int i = 0; i < V; ++i) m = max_bits(m, v[i]);
-    if (live)
+      for (int i = 0; i < V; ++i) {
+        v[k][i] = u32x4{0u, 0u, 0u, 0u};
+        if (r0 + k < rows && at + i * STEP < nvec) v[k][i] = load_vec(a.x + (r0 + k) * a.ldx, at + i * STEP, a.cols);
+      }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const long long r = r0 + k;
+      if (r >= rows) break;
+      const uint16_t* row = a.x + r * a.ldx;
+      u16x2 m = {0, 0};
+#pragma unroll
+      for (int i = 0; i < V; ++i) m = max_bits(m, v[k][i]);
       for (int i = at + V * STEP; i < nvec; i += STEP) m = max_bits(m, load_vec(row, i, a.cols));
-    uint32_t top = max(static_cast<uint32_t>(m[0]), static_cast<uint32_t>(m[1]));
+      uint32_t top = wave_max(max(static_cast<uint32_t>(m[0]), static_cast<uint32_t>(m[1])));
+      if constexpr (WPR > 1) {
+        if (lane_id() == 0) part[wave] = top;
+        __syncthreads();
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off)));
-    if constexpr (WPR > 1) {
-      if (lane_id() == 0) part[wave] = top;
-      __syncthreads();
+        for (int w = 0; w < kQuantWaves; ++w) top = max(top, part[w]);
+        __syncthreads();
+      }
+      const bool finite = top < 0x7f80u;
+      const float amax = __uint_as_float(top << 16);
+      // 127 / a leaves the range of fp32 for the smallest a: those rows are
+      // scaled by 2^80 first (exact)
+      const float pre = amax < 0x1p-60f ? 0x1p80f : 1.0f;
+      const float c = (finite && top != 0u) ? 127.0f / (amax * pre) : 0.0f;
+      if (at == 0) a.scale[r] = finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
+      int8_t* out = a.q + r * a.ldq;
+      // (a row that is not finite multiplies to NaN, whose bits are no integer)
+      auto put = [&](int i, u32x4 x) {
+        *reinterpret_cast<u32x2*>(out + static_cast<long long>(i) * kVec) = finite ? quantize_vec(x, pre, c) : u32x2{0u, 0u};
+      };
 #pragma unroll
-      for (int w = 0; w < kQuantWaves; ++w) top = max(top, part[w]);
-      __syncthreads();
+      for (int i = 0; i < V; ++i)
+        if (at + i * STEP < nvec) put(at + i * STEP, v[k][i]);
+      for (int i = at + V * STEP; i < nvec; i += STEP) put(i, load_vec(row, i, a.cols));
     }
-    const bool finite = top < 0x7f80u;
-    const float amax = __uint_as_float(top << 16);
-    // 127 / a leaves the range of fp32 for the smallest a: those rows are
-    // scaled by 2^80 first (exact)
-    const float pre = amax < 0x1p-60f ? 0x1p80f : 1.0f;
-    const float c = (finite && top != 0u) ? 127.0f / (amax * pre) : 0.0f;
-    if (!live) continue;
-    if (at == 0) a.scale[r] = finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
-    int8_t* out = a.q + r * a.ldq;
-    // (a row that is not finite multiplies to NaN, whose bits are no integer)
-    auto put = [&](int i, u32x4 x) {
-      *reinterpret_cast<u32x2*>(out + static_cast<long long>(i) * kVec) = finite ? quantize_vec(x, pre, c) : u32x2{0u, 0u};
-    };
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (at + i * STEP < nvec) put(at + i * STEP, v[i]);
-    for (int i = at + V * STEP; i < nvec; i += STEP) put(i, load_vec(row, i, a.cols));
   }
 }
 
@@ -148,21 +166,28 @@ int quant_blocks(const QuantArgs& a, int rows_per_block) {
   return static_cast<int>(std::min<long long>((static_cast<long long>(a.rows) + rows_per_block - 1) / rows_per_block, kMaxBlocks));
 }
 
+template <int WPR, int V, int R>
+hipError_t launch_rows(const QuantArgs& a, const QuantArgs* b, hipStream_t st) {
+  constexpr int RPB = kQuantWaves / WPR * R;
+  const QuantPair p{a, b ? *b : QuantArgs{}, quant_blocks(a, RPB)};
+  const int grid = p.blocks_a + (b ? quant_blocks(*b, RPB) : 0);
+  if (grid == 0) return hipSuccess;
+  hipLaunchKernelGGL((quantize_kernel<WPR, V, R>), dim3(grid), dim3(kQuantThreads), 0, st, p);
+  return hipGetLastError();
+}
+
 }  // namespace
 
-// A wave per row up to 2048 columns (four vectors per lane, no barrier), else
-// a workgroup per row, rows of up to 16384 columns in registers.
+// A wave per row up to 4096 columns, several rows of up to 1024; a workgroup
+// per row past that, and where there are no more rows than CUs (one row of
+// 2048: latency alone).
 hipError_t launch_quantize_rows(const QuantArgs& a, const QuantArgs* b, hipStream_t st) {
   const int cols = std::max(a.cols, b ? b->cols : 0);
-  const int rpb = cols <= 2048 ? kQuantWaves : 1;
-  const QuantPair p{a, b ? *b : QuantArgs{}, quant_blocks(a, rpb)};
-  const int grid = p.blocks_a + (b ? quant_blocks(*b, rpb) : 0);
-  if (grid == 0) return hipSuccess;
-  if (rpb > 1)
-    hipLaunchKernelGGL((quantize_kernel<1, 4>), dim3(grid), dim3(kQuantThreads), 0, st, p);
-  else
-    hipLaunchKernelGGL((quantize_kernel<kQuantWaves, 8>), dim3(grid), dim3(kQuantThreads), 0, st, p);
-  return hipGetLastError();
+  const long long rows = static_cast<long long>(a.rows) + (b ? b->rows : 0);
+  if (cols > 4096 || (cols > 512 && rows <= 256)) return launch_rows<kQuantWaves, 8, 1>(a, b, st);
+  if (cols > 2048) return launch_rows<1, 8, 1>(a, b, st);
+  if (cols > 1024) return launch_rows<1, 4, 1>(a, b, st);
+  return launch_rows<1, 2, 2>(a, b, st);
 }
 
 }  // namespace moe

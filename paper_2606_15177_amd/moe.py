@@ -258,21 +258,48 @@ def forward_noalloc(d, logits, src, x, local_experts, weights, counts, out, taps
 _I8 = (torch.int8,)
 
 
+# The handle of a device's current stream (torch.cuda.current_stream builds a
+# Stream object each time: 2.8 us of a call that launches in 4).
+_current_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _on_device(stream, *tensors):
-    """Context of the tensors' device and the stream to launch on: the given
-    one, or that device's current stream.  Tensors of two devices, or a stream
-    of another one, are refused."""
-    devs = {t.device for t in tensors if t is not None}
-    if any(d.type != "cuda" for d in devs):
-        raise ValueError("tensor must live on the GPU")
-    if len(devs) > 1:
-        raise ValueError(f"tensors live on different devices: {sorted(map(str, devs))}")
-    dev = next(iter(devs))
+    """The tensors' device index and the stream to launch on: the given one, or
+    that device's current stream.  Tensors of two devices, or a stream of another
+    one, are refused."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            d = t.get_device()
+            if d < 0:
+                raise ValueError("tensor must live on the GPU")
+            if dev is None:
+                dev = d
+            elif d != dev:
+                raise ValueError(f"tensors live on different devices: cuda:{dev}, cuda:{d}")
     if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    elif getattr(stream, "device", dev) != dev:
-        raise ValueError(f"stream of {stream.device}, tensors on {dev}")
-    return torch.cuda.device(dev), _stream(stream)
+        return dev, _current_handle(dev)
+    if getattr(stream, "device", None) is not None and stream.device.index != dev:
+        raise ValueError(f"stream of {stream.device}, tensors on cuda:{dev}")
+    return dev, _stream(stream)
+
+
+def _call(dev: int, where: str, *args) -> None:
+    """A library call with `dev` as the current device."""
+    f = getattr(_lib, where)
+    if torch.cuda.current_device() == dev:
+        status = f(*args)
+    else:
+        with torch.cuda.device(dev):
+            status = f(*args)
+    if status != MOE_OK:
+        raise MoeError(status, where)
+
+
+def _allocating_on(stream):
+    """Context in which tensors are allocated for use on `stream`."""
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None)
 
 
 def _need(ok: bool, what: str) -> None:
@@ -291,14 +318,18 @@ def _rows(t, dtypes, cols: int, what: str):
         raise TypeError(f"{what}: expected a torch tensor")
     if t.dtype not in dtypes:
         raise TypeError(f"{what}: dtype {t.dtype} not in {dtypes}")
-    _need(t.dim() == 2 and t.shape[1] >= cols, f"{what}: expected rows of at least {cols} values, got {tuple(t.shape)}")
-    _need(t.shape[1] == 1 or t.stride(1) == 1, f"{what}: rows must be contiguous")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] < cols:
+        raise ValueError(f"{what}: expected rows of at least {cols} values, got {tuple(shape)}")
+    if shape[1] != 1 and stride[1] != 1:
+        raise ValueError(f"{what}: rows must be contiguous")
     # one row has no stride to speak of
-    return t.data_ptr(), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]
 
 
 def _vec(t, dtypes, n: int, what: str):
-    _need(isinstance(t, torch.Tensor) and t.numel() >= n, f"{what}: expected {n} values")
+    if not isinstance(t, torch.Tensor) or t.numel() < n:
+        raise ValueError(f"{what}: expected {n} values")
     return _ptr(t, dtypes)
 
 
@@ -309,16 +340,14 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     Returns (q, scale)."""
     xp, ldx = _rows(x, _BF16, 1, "x")
     rows, cols = x.shape
-    ctx, st = _on_device(stream, x, q, scale)
-    with ctx:
-        if q is None or scale is None:
-            with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_stream()):
-                q = torch.empty((rows, _pad16(cols)), dtype=torch.int8, device=x.device) if q is None else q
-                scale = torch.empty((rows,), dtype=torch.float32, device=x.device) if scale is None else scale
-        qp, ldq = _rows(q, _I8, _pad16(cols), "q")
-        _need(q.shape[0] == rows, f"q: expected {rows} rows")
-        sp = _vec(scale, _F32, rows, "scale")
-        _check(_lib.moe_quantize_rows(rows, cols, xp, ldx, qp, ldq, sp, st), "moe_quantize_rows")
+    dev, st = _on_device(stream, x, q, scale)
+    if q is None or scale is None:
+        with _allocating_on(stream):
+            q = torch.empty((rows, _pad16(cols)), dtype=torch.int8, device=x.device) if q is None else q
+            scale = torch.empty((rows,), dtype=torch.float32, device=x.device) if scale is None else scale
+    qp, ldq = _rows(q, _I8, _pad16(cols), "q")
+    _need(q.shape[0] == rows, "q: expected as many rows as x has")
+    _call(dev, "moe_quantize_rows", rows, cols, xp, ldx, qp, ldq, _vec(scale, _F32, rows, "scale"), st)
     return q, scale
 
 
@@ -330,12 +359,10 @@ def linear_i8(K, xq, x_scale, wq, w_scale, y, stream=None):
     M, N = y.shape
     xp, ldx = _rows(xq, _I8, _pad16(K), "xq")
     wp, ldw = _rows(wq, _I8, _pad16(K), "wq")
-    _need(xq.shape[0] == M and wq.shape[0] == N, f"expected {M} rows of xq and {N} of wq")
-    d = MoeLinearDims(M, N, K, 1, 0, ldx, ldw, ldy)
-    ctx, st = _on_device(stream, xq, x_scale, wq, w_scale, y)
-    with ctx:
-        _check(_lib.moe_linear_i8(C.byref(d), xp, _vec(x_scale, _F32, M, "x_scale"), wp,
-                                  _vec(w_scale, _F32, N, "w_scale"), yp, st), "moe_linear_i8")
+    _need(xq.shape[0] == M and wq.shape[0] == N, "expected as many rows of xq and wq as y has rows and columns")
+    dev, st = _on_device(stream, xq, x_scale, wq, w_scale, y)
+    _call(dev, "moe_linear_i8", C.byref(MoeLinearDims(M, N, K, 1, 0, ldx, ldw, ldy)), xp, _vec(x_scale, _F32, M, "x_scale"),
+          wp, _vec(w_scale, _F32, N, "w_scale"), yp, st)
 
 
 def grouped_linear_i8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stream=None):
@@ -344,19 +371,17 @@ def grouped_linear_i8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stre
     w_scale fp32 [G, N], offsets int32 [G+1], x_rows int32 [M]."""
     yp, ldy = _rows(y, _BF16, 1, "y")
     M, N = y.shape
-    _need(isinstance(wq, torch.Tensor) and wq.dim() == 3 and wq.shape[1] == N, f"wq: expected [groups, {N}, ...]")
+    if not isinstance(wq, torch.Tensor) or wq.dim() != 3 or wq.shape[1] != N:
+        raise ValueError(f"wq: expected [groups, {N}, ...]")
     G = wq.shape[0]
     xp, ldx = _rows(xq, _I8, _pad16(K), "xq")
     wp, ldw = _rows(wq.flatten(0, 1), _I8, _pad16(K), "wq")
     _need(wp == wq.data_ptr(), "wq: the groups must lie one behind the other")
-    _need(x_rows is not None or xq.shape[0] == M, f"expected {M} rows of xq")
-    d = MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy)
-    ctx, st = _on_device(stream, xq, x_scale, offsets, wq, w_scale, y, x_rows)
-    with ctx:
-        _check(_lib.moe_grouped_linear_i8(C.byref(d), xp, _vec(x_scale, _F32, xq.shape[0], "x_scale"),
-                                          None if x_rows is None else _vec(x_rows, _I32, M, "x_rows"),
-                                          _vec(offsets, _I32, G + 1, "offsets"), wp,
-                                          _vec(w_scale, _F32, G * N, "w_scale"), yp, st), "moe_grouped_linear_i8")
+    _need(x_rows is not None or xq.shape[0] == M, "expected as many rows of xq as of y")
+    dev, st = _on_device(stream, xq, x_scale, offsets, wq, w_scale, y, x_rows)
+    _call(dev, "moe_grouped_linear_i8", C.byref(MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy)), xp,
+          _vec(x_scale, _F32, xq.shape[0], "x_scale"), None if x_rows is None else _vec(x_rows, _I32, M, "x_rows"),
+          _vec(offsets, _I32, G + 1, "offsets"), wp, _vec(w_scale, _F32, G * N, "w_scale"), yp, st)
 
 
 def quantize_weights(d: MoeDims, w: dict) -> dict:
@@ -392,29 +417,31 @@ def make_weights_i8(d: MoeDims, w: dict) -> MoeWeightsI8:
                      "sh_s_gate": (_F32, width), "sh_s_up": (_F32, width), "sh_s_down": (_F32, H)})
     h = MoeWeightsI8(**{n: _vec(w.get(n), t, size, n) for n, (t, size) in need.items()})
     h.tensors = {n: w[n] for n in need}
+    h.device_index = _on_device(None, *h.tensors.values())[0]
     return h
+
+
+def _bytes(ws) -> int:
+    return 0 if ws is None else ws.numel() * ws.element_size()
 
 
 def expert_ffn_i8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=None):
     """moe_expert_ffn_i8; weights as make_weights_i8 returns them."""
-    rows = d.T * d.k
-    ctx, st = _on_device(stream, x_perm, offsets, x, y_perm, y_shared, ws, *weights.tensors.values())
-    with ctx:
-        _check(_lib.moe_expert_ffn_i8(C.byref(d), _vec(x_perm, _BF16, rows * d.H, "x_perm"),
-                                      _vec(offsets, _I32, d.E_local + 1, "offsets"), C.byref(weights), _ptr(x, _BF16),
-                                      _vec(y_perm, _BF16, rows * d.H, "y_perm"), _ptr(y_shared, _BF16), _ptr(ws),
-                                      0 if ws is None else ws.numel() * ws.element_size(), st), "moe_expert_ffn_i8")
+    n = d.T * d.k * d.H
+    dev, st = _on_device(stream, x_perm, offsets, x, y_perm, y_shared, ws)
+    _need(dev == weights.device_index, "weights live on another device")
+    _call(dev, "moe_expert_ffn_i8", C.byref(d), _vec(x_perm, _BF16, n, "x_perm"), _vec(offsets, _I32, d.E_local + 1, "offsets"),
+          C.byref(weights), _ptr(x, _BF16), _vec(y_perm, _BF16, n, "y_perm"), _ptr(y_shared, _BF16), _ptr(ws), _bytes(ws), st)
 
 
 def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=None, stream=None, gating=None):
     """moe_forward_i8; weights as make_weights_i8 returns them."""
-    ctx, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws, *weights.tensors.values())
-    with ctx:
-        _check(_lib.moe_forward_i8(C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"),
-                                   _ptr(src, _I32), _vec(x, _BF16, d.T * d.H, "x"), _ptr(local_experts, _I32),
-                                   C.byref(weights), _ptr(counts, _I64), _vec(out, _BF16, d.T * d.H, "out"),
-                                   None if taps is None else C.byref(taps), _ptr(ws),
-                                   0 if ws is None else ws.numel() * ws.element_size(), st), "moe_forward_i8")
+    n = d.T * d.H
+    dev, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws)
+    _need(dev == weights.device_index, "weights live on another device")
+    _call(dev, "moe_forward_i8", C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"), _ptr(src, _I32),
+          _vec(x, _BF16, n, "x"), _ptr(local_experts, _I32), C.byref(weights), _ptr(counts, _I64), _vec(out, _BF16, n, "out"),
+          None if taps is None else C.byref(taps), _ptr(ws), _bytes(ws), st)
 
 
 PAPER_PLACE_WEIGHTS = (1.0, 0.0025, 1.0)  # (alpha, beta, gamma), Sec. 6
@@ -498,7 +525,7 @@ class MoeLayerI8:
 
     def forward(self, logits, src, x, counts=None, out=None, taps=None, stream=None, ws=None):
         if out is None:
-            with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None):
+            with _allocating_on(stream):
                 out = torch.empty((self.d.T, self.d.H), dtype=torch.bfloat16, device=x.device)
         forward_i8(self.d, logits, src, x, self.local_experts, self._w, counts, out, self.ws if ws is None else ws, taps,
                    stream, gating=self.gating)

@@ -161,12 +161,44 @@ def test_binding_checks_devices(moe):
     """Tensors of two devices, or a stream of another device than theirs, are refused."""
     class T:
         def __init__(self, d):
-            self.device = torch.device(d)
+            self.get_device = lambda: d
 
     class S:
         device = torch.device("cuda:1")
-        cuda_stream = 0
+        cuda_stream = 7
     with pytest.raises(ValueError, match="different devices"):
-        moe._on_device(S(), T("cuda:0"), None, T("cuda:1"))
+        moe._on_device(S(), T(0), None, T(1))
     with pytest.raises(ValueError, match="stream of"):
-        moe._on_device(S(), T("cuda:0"))
+        moe._on_device(S(), T(0))
+    with pytest.raises(ValueError, match="GPU"):
+        moe._on_device(None, T(-1))
+    assert moe._on_device(S(), None, T(1), T(1)) == (1, 7)
+
+
+def test_calls_run_on_the_tensors_device(moe, monkeypatch):
+    """With another device current, the call is made with the tensors' one as current."""
+    seen, current = [], [0]
+
+    class On:
+        def __init__(self, d):
+            self.d = d
+
+        def __enter__(self):
+            current[0] = self.d
+
+        def __exit__(self, *a):
+            current[0] = 0
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", On)
+
+    class Lib:
+        def moe_linear_i8(self, *a):
+            seen.append(current[0])
+            return a[0]
+    monkeypatch.setattr(moe, "_lib", Lib())
+    moe._call(1, "moe_linear_i8", 0)
+    moe._call(0, "moe_linear_i8", 0)
+    assert seen == [1, 0] and current == [0]
+    with pytest.raises(RuntimeError, match="moe_linear_i8"):
+        monkeypatch.setattr(moe, "strerror", lambda s: "text")
+        moe._call(1, "moe_linear_i8", -3)
