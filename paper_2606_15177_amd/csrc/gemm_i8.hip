@@ -6,24 +6,35 @@
 namespace moe {
 namespace {
 
-// Time of the tiles over that of the items (gate/up and down, kernel trace):
-// long K: Mixtral 1.04 and 1.34 at 200 tokens (a mean of 50 rows), 0.86 and
-// 0.90 at 300 (75); DSV3 share 1.19 and 1.11 at 1500 (47), 0.99 and 0.94 at
-// 2048 (64); shorter: DSV2-Lite 1.10 and 1.35 at 800 (75), 1.00 and 1.05 at
-// 1500 (140), 0.92 and 0.85 at 4096 (384); Qwen3 1.07 and 1.05 at 1500 (93),
-// 0.99 and 1.02 at 2048 (128).
-constexpr int kLongBytes = 4096, kMeanLong = 60, kMeanShort = 130;
+// 256-row tiles want rows that fill them and tiles for a good part of the CUs.
+// Over 160 random layers (65 to 8192 tokens, even to Zipf 1 routing; K 392 to
+// 14336) and 249 random products of static rows these lines choose the kernel
+// that is within 8 % of the faster one for all but 9 of 300 grouped products
+// (1.31 at worst, 0.7 % on average; another 160 layers 0.6 %) and all but 4 of
+// the others (1.44, 0.5 %).
+// Both sides, us (items, tiles):
+//   long K (kLongK bytes): Mixtral gate/up at a mean of 50 rows 180 and 190, at
+//     75 212 and 199; the DSV3 share's down at 62 rows 171 and 161;
+//   shorter: 122 rows of K 1416, N 3432 108 and 92, 97 rows of K 1656 35 and 39;
+//   many groups of short K, whose last tiles are mostly padding: Qwen3 gate/up
+//     at a mean of 309 rows 214 and 258, at 512 335 and 308, down at 315 149 and
+//     165, at 406 205 and 193;
+//   few tiles: 593 x 9972 x 1142 (117) 18.0 and 24.2, 11380 x 485 x 6294 (90)
+//     94 and 82, 3941 x 2301 x 2281 (144) 57 and 38.
+constexpr int kMeanLong = 60, kMeanShort = 110, kMeanMany = 350, kMeanManyGated = 420;
+constexpr int kMany = 64, kManyK = 2048;
+constexpr long long kFewTiles = 128, kFewStaticTiles = 96;
 
 bool takes_tiles(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   if (a.K <= kTiledMinK || (sh && sh->K <= kTiledMinK)) return false;
   if (items_blocks(seg, a, sh, gated) > kMaxItemBlocks) return true;
-  // few tiles leave CUs idle (16 experts of H 1024, I 512, 3000 tokens: 1.14
-  // and 1.12 with 128 tiles)
   const int cols = gated ? 128 : 256;
-  const long long tiles = (a.offsets ? static_cast<long long>(seg.groups) * ceil_div(seg.mean_rows, 256) : ceil_div(a.static_rows, 256)) *
-                          ceil_div(a.N, cols);
-  if (3 * tiles < 2 * device_cu_count()) return false;
-  return seg.mean_rows >= (a.K >= kLongBytes ? kMeanLong : kMeanShort);
+  auto tiles = [&](int rows, int N) { return static_cast<long long>(ceil_div(rows, 256)) * ceil_div(N, cols); };
+  if (!a.offsets) return tiles(a.static_rows, a.N) >= kFewStaticTiles;
+  if (seg.groups * tiles(seg.mean_rows, a.N) + (sh ? tiles(sh->static_rows, sh->N) : 0) < kFewTiles) return false;
+  if (a.K >= kLongK) return seg.mean_rows >= kMeanLong;
+  if (seg.groups < kMany || a.K > kManyK) return seg.mean_rows >= kMeanShort;
+  return seg.mean_rows >= (gated ? kMeanManyGated : kMeanMany);
 }
 
 }  // namespace

@@ -15,6 +15,7 @@ typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 
 constexpr uint32_t kPastEnd = 0x80000000u;  // an offset past a descriptor's range: reads zeros, no traffic
 constexpr int kXcds = 8;
+constexpr int kWaitLds = 15 | (3 << 14) | (7 << 4);  // s_waitcnt immediate (see wait_vm): LDS accesses done
 
 // Lane l holds A[row l % 32][16 (l / 32) ..] and B[col l % 32][16 (l / 32) ..]
 // (16 bytes), and C[8 (i / 4) + 4 (l / 32) + i % 4][l % 32] in element i.

@@ -30,13 +30,15 @@
 namespace moe {
 namespace {
 
-constexpr int kChunk = 128;         // token rows of a chunk
+constexpr int kChunk = 128;         // token rows of a chunk of a wide item
+constexpr int kSplitChunk = 64;     // ... of any item where K is split (32 where there are very few)
 constexpr int kWideRows = 64;       // groups of more rows take wide items
 constexpr int kItemRows = 128;      // weight rows of a narrow item
 constexpr int kFewWide = 128;       // fewer wide items than this take 128 weight rows: half the CUs' worth
 constexpr int kOneWide = 256;       // ... or fewer than this, one per CU, in a launch of fewer items than
 constexpr int kSlots = 512;         // workgroups fit the chip
 constexpr int kItemLds = 80 * 1024;   // two workgroups per CU
+constexpr int kDeepLds = 160 * 1024;  // one
 constexpr int kTurn = 8;
 constexpr int kItemThreads = 4 * kWave;
 
@@ -48,32 +50,33 @@ struct ItemsI8 {
 
 __device__ __forceinline__ int run_start(int n, int x) { return static_cast<int>(static_cast<long long>(n) * x / kXcds); }
 
-// The wave's loads of stage j have landed: of what was issued after them, the
-// token loads of the first stages (weights go out first there) and the whole
-// stages since may still be in flight.
-template <int D, int XL, int LOADS, int J = 0>
+// The wave's loads of stage j have landed.  After them were issued (with AHEAD
+// stages in flight behind it) the token loads of the first FIRST stages, whose
+// weights went out before, and whole stages.
+template <int FIRST, int AHEAD, int XL, int LOADS, int J = 0>
 __device__ __forceinline__ void wait_stage(int j) {
-  if constexpr (J == D - 1) {
-    __builtin_amdgcn_s_waitcnt(wait_vm((D - 2) * LOADS));
+  if constexpr (J == FIRST) {
+    __builtin_amdgcn_s_waitcnt(wait_vm(AHEAD * LOADS));
   } else {
     if (j == J)
-      __builtin_amdgcn_s_waitcnt(wait_vm((D - 2 - J) * XL + J * LOADS));
+      __builtin_amdgcn_s_waitcnt(wait_vm((FIRST - 1 - J) * XL + (AHEAD - (FIRST - 1 - J)) * LOADS));
     else
-      wait_stage<D, XL, LOADS, J + 1>(j);
+      wait_stage<FIRST, AHEAD, XL, LOADS, J + 1>(j);
   }
 }
 
-template <bool GATED, int KP>
+template <bool GATED, int KP, bool DEEP, int CHUNK>
 __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void items_i8_kernel(ItemsI8 ma) {
   constexpr int FULL_COLS = GATED ? kItemRows / 2 : kItemRows;  // output columns of 128 weight rows
   constexpr int OUT_COLS = FULL_COLS / KP;                      // ... of a narrow item
+  constexpr int WIDE_ROWS = KP > 1 ? 0x7fffffff : kWideRows;    // groups of more rows take wide items
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
 
   // ---- which item ----
   const int sp_m = ma.sp.static_rows;
-  const int sp_chunks = ceil_div(sp_m, kChunk);
+  const int sp_chunks = ceil_div(sp_m, CHUNK);
   // first row and rows of groups g0 + 64 i + lane
   constexpr int kPasses = 4;
   int first_row[kPasses], n_rows[kPasses];
@@ -93,25 +96,39 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
       n_rows[i] = max(min(n_rows[i], ma.rows) - first_row[i], 0);
     }
   };
-  // chunks of the groups (few groups are wide in the batches whose latency counts)
+  // Chunks of the groups, wide and narrow.  Where no group has more than one,
+  // they are counted by votes of the lanes.
   int c_wide = 0, c_narrow = 0;
+  bool several = false;
   for (int g0 = 0; g0 < ma.g.groups; g0 += kPasses * kWave) {
     load_groups(g0);
-    int wide_here = 0;
+    int wide_here = 0, narrow_here = 0, ones = 0;
+    bool more = false;
 #pragma unroll
     for (int q = 0; q < kPasses; ++q) {
-      c_narrow += __popcll(__ballot(n_rows[q] > 0 && n_rows[q] <= kWideRows));
-      wide_here += n_rows[q] > kWideRows ? ceil_div(n_rows[q], kChunk) : 0;
+      const int n = ceil_div(n_rows[q], CHUNK);
+      const bool w = n_rows[q] > WIDE_ROWS;
+      more |= n > 1 || w;
+      ones += __popcll(__ballot(n > 0));
+      wide_here += w ? n : 0;
+      narrow_here += w ? 0 : n;
     }
-    if (__ballot(wide_here > 0) != 0) {
+    if (__ballot(more) != 0) {
+      several = true;
 #pragma unroll
-      for (int off = 1; off < kWave; off <<= 1) wide_here += __shfl_xor(wide_here, off);
+      for (int off = 1; off < kWave; off <<= 1) {
+        wide_here += __shfl_xor(wide_here, off);
+        narrow_here += __shfl_xor(narrow_here, off);
+      }
       c_wide += __builtin_amdgcn_readfirstlane(wide_here);
+      c_narrow += __builtin_amdgcn_readfirstlane(narrow_here);
+    } else {
+      c_narrow += ones;
     }
   }
   const int narrow_blocks = ma.g.groups > 0 ? ceil_div(ma.g.N, OUT_COLS) : 0;
   const int n_narrow = c_narrow * narrow_blocks;
-  auto shared_items = [&](int cols) { return sp_m > 0 ? sp_chunks * ceil_div(ma.sp.N, sp_m > kWideRows ? cols : OUT_COLS) : 0; };
+  auto shared_items = [&](int cols) { return sp_m > 0 ? sp_chunks * ceil_div(ma.sp.N, sp_m > WIDE_ROWS ? cols : OUT_COLS) : 0; };
   int wide_cols = 2 * FULL_COLS;
   const int heavy = shared_items(wide_cols) + c_wide * ceil_div(ma.g.N, wide_cols);
   if (heavy < kFewWide || (heavy < kOneWide && heavy + n_narrow < kSlots)) wide_cols = FULL_COLS;
@@ -136,7 +153,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     idx = narrow ? i - my_heavy : idx;
   }
   const bool shared = !narrow && idx < my_shared;
-  const bool wide = shared ? sp_m > kWideRows : !narrow;
+  const bool wide = shared ? sp_m > WIDE_ROWS : !narrow;
   idx = narrow ? n_lo + idx : shared ? s_lo + idx : w_lo + idx - my_shared;
   int g = 0, row_base = 0, m = sp_m, item = idx;
   if (!shared) {
@@ -150,9 +167,9 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
       for (int q = 0; q < kPasses; ++q) {
         if (found || g0 + q * kWave >= ma.g.groups) continue;
         // chunks of the kind in the lane's group, and up to and with it
-        const int own = (n_rows[q] > kWideRows) == wide ? ceil_div(n_rows[q], kChunk) : 0;
+        const int own = (n_rows[q] > WIDE_ROWS) == wide ? ceil_div(n_rows[q], CHUNK) : 0;
         int inc = own;
-        if (wide) {
+        if (several) {
 #pragma unroll
           for (int off = 1; off < kWave; off <<= 1) {
             const int o = __shfl_up(inc, off);
@@ -178,7 +195,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     }
     if (!found) return;  // not reached: idx lies within the groups' items
   }
-  const int n_chunks = ceil_div(m, kChunk);
+  const int n_chunks = ceil_div(m, CHUNK);
   int nblk = item / n_chunks;
   int chunk = item - nblk * n_chunks;
   g = __builtin_amdgcn_readfirstlane(g);
@@ -222,7 +239,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int WL = WB * 32 / RPI;              // weight loads per wave and stage
     constexpr int LOADS = XL + WL;
     constexpr int KS = BK / 32;                    // MFMA K-steps per stage
-    static_assert(D * STAGE <= kItemLds, "the ring fits");
+    static_assert(D * STAGE <= (DEEP ? kDeepLds : kItemLds), "the ring fits");
     static_assert(FEW ? RPI == 8 : XL * RPI * WN == XR, "whole loads fill the token rows");
     const int lr = lane / CPR;                     // row of a load
     const int wn = wave % WN, wk = wave / WN;
@@ -297,34 +314,81 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     for (int b = 0; b < WB; ++b)
 #pragma unroll
       for (int s = 0; s < NSUB; ++s) acc[b][s] = i32x16{};
-    int slot = 0;
-    for (int j = 0; j < nst; ++j) {
-      wait_stage<D, XL, LOADS>(j);  // own loads of stage j landed
-      phase_barrier();  // everyone's have, and everyone has read stage j - 1
-      // stage j + D - 1 into the slot of stage j - 1
-      const int into = slot == 0 ? D - 1 : slot - 1;
-      issue_x(j + D - 1, into);
-      issue_w(j + D - 1, into);
+    constexpr bool OWN = NK == 4;                    // every wave reads only what it loads itself
+    constexpr bool PIPE = NK > 1;                    // a stage's fragments are read among the MFMAs of the one before
+    constexpr int SETS = PIPE ? 2 : 1;
+    i32x4 wf[SETS][KS][WB], xf[SETS][KS][NSUB];
+    auto read_frags = [&](int slot, auto set_c) {
+      constexpr int SET = decltype(set_c)::value;
       const unsigned char* xp = smem + slot * STAGE + wk * XPART;
       const unsigned char* wp = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
-      i32x4 wf[KS][WB], xf[KS][NSUB];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const int at = ((2 * ks + lhalf) ^ ((lrow / SWZ) % CPR)) << 4;
         const int xrow = FEW ? lrow % 8 : lrow;  // (few rows: columns past them are not results)
         const int xat = ((2 * ks + lhalf) ^ ((xrow / SWZ) % CPR)) << 4;
 #pragma unroll
-        for (int b = 0; b < WB; ++b) wf[ks][b] = *reinterpret_cast<const i32x4*>(wp + (32 * b + lrow) * BK + at);
+        for (int b = 0; b < WB; ++b) wf[SET][ks][b] = *reinterpret_cast<const i32x4*>(wp + (32 * b + lrow) * BK + at);
 #pragma unroll
-        for (int s = 0; s < NSUB; ++s) xf[ks][s] = *reinterpret_cast<const i32x4*>(xp + (32 * s + xrow) * BK + xat);
+        for (int s = 0; s < NSUB; ++s) xf[SET][ks][s] = *reinterpret_cast<const i32x4*>(xp + (32 * s + xrow) * BK + xat);
       }
+    };
+    auto multiply = [&](auto set_c) {
+      constexpr int SET = decltype(set_c)::value;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int b = 0; b < WB; ++b)
 #pragma unroll
-          for (int s = 0; s < NSUB; ++s) acc[b][s] = mfma_i8(wf[ks][b], xf[ks][s], acc[b][s]);
-      if (++slot == D) slot = 0;
+          for (int s = 0; s < NSUB; ++s) acc[b][s] = mfma_i8(wf[SET][ks][b], xf[SET][ks][s], acc[b][s]);
+    };
+    // Stage j has landed, for this wave and (unless it reads its own loads
+    // alone) for all; its LDS reads of the stage before are done.
+    auto arrive = [&](int j) {
+      wait_stage<D - 1, D - 2, XL, LOADS>(j);
+      if constexpr (PIPE) __builtin_amdgcn_s_waitcnt(kWaitLds);
+      if constexpr (OWN) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        phase_barrier();
+      }
+    };
+    auto next_slot = [](int slot) { return slot == D - 1 ? 0 : slot + 1; };
+    using S0 = std::integral_constant<int, 0>;
+    using S1 = std::integral_constant<int, SETS - 1>;
+    int slot = 0;
+    if constexpr (PIPE) {
+      // stage j + D goes into the slot of stage j, whose fragments are in registers
+      issue_x(D - 1, D - 1);
+      issue_w(D - 1, D - 1);
+      arrive(0);
+      read_frags(0, S0{});
+      auto step = [&](int j, auto cur, auto nxt) {
+        const int next = next_slot(slot);
+        arrive(j + 1);
+        issue_x(j + D, slot);
+        issue_w(j + D, slot);
+        read_frags(next, nxt);  // (past the last stage: not used)
+        multiply(cur);
+        slot = next;
+      };
+      for (int j = 0; j < nst; j += 2) {
+        step(j, S0{}, S1{});
+        if (j + 1 < nst) step(j + 1, S1{}, S0{});
+      }
+    } else {
+      for (int j = 0; j < nst; ++j) {
+        arrive(j);
+        // stage j + D - 1 into the slot of stage j - 1
+        const int into = slot == 0 ? D - 1 : slot - 1;
+        issue_x(j + D - 1, into);
+        issue_w(j + D - 1, into);
+        read_frags(slot, S0{});
+        multiply(S0{});
+        slot = next_slot(slot);
+      }
     }
     __builtin_amdgcn_s_waitcnt(wait_vm(0));  // the loads past the last stage: nothing may still write the LDS
     if constexpr (NK > 1) {
@@ -399,54 +463,80 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   using K128 = integral_constant<int, 128>;
   constexpr std::false_type whole{};
   constexpr std::true_type few{};
-  if (wide && wide_cols > FULL_COLS)
-    body(C4{}, C2{}, C1{}, K64{}, C3{}, whole);
-  else if (wide)
-    body(C4{}, C1{}, C1{}, K64{}, C5{}, whole);
-  else if constexpr (KP == 1) {
-    if (rows > 32) body(C2{}, C1{}, C1{}, K128{}, C3{}, whole);
+  if constexpr (KP == 1) {
+    if (wide && wide_cols > FULL_COLS) body(C4{}, C2{}, C1{}, K64{}, C3{}, whole);
+    else if (wide) body(C4{}, C1{}, C1{}, K64{}, C5{}, whole);
+    else if (rows > 32) body(C2{}, C1{}, C1{}, K128{}, C3{}, whole);
     else body(C1{}, C1{}, C1{}, K128{}, C4{}, whole);
   } else if constexpr (KP == 2) {
-    if (rows > 32) body(C2{}, C1{}, C2{}, K64{}, C5{}, whole);
-    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, C3{}, whole);
+    if (rows > 32) body(C2{}, C1{}, C2{}, integral_constant<int, DEEP ? 128 : 64>{}, C5{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, integral_constant<int, DEEP ? 6 : 3>{}, whole);
     else body(C1{}, C1{}, C2{}, K128{}, C4{}, few);
   } else {
-    if (rows > 32) body(C2{}, C1{}, C4{}, K64{}, C3{}, whole);
-    else if (rows > 8) body(C1{}, C1{}, C4{}, K64{}, C5{}, whole);
+    if (CHUNK > 32 && rows > 32) body(C2{}, C1{}, C4{}, integral_constant<int, DEEP ? 128 : 64>{}, C3{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C4{}, integral_constant<int, DEEP ? 128 : 64>{}, C5{}, whole);
     else body(C1{}, C1{}, C4{}, K128{}, C4{}, few);
   }
 }
 
-template <bool GATED, int KP>
+template <bool GATED, int KP, bool DEEP, int CHUNK>
 hipError_t launch_kp(long long blocks, const ItemsI8& ma, hipStream_t st) {
+  constexpr int lds = DEEP ? kDeepLds : kItemLds;
   static unsigned long long lds_set = 0;  // devices with the LDS limit raised
-  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_i8_kernel<GATED, KP>), kItemLds, &lds_set);
+  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_i8_kernel<GATED, KP, DEEP, CHUNK>), lds, &lds_set);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((items_i8_kernel<GATED, KP>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), kItemLds, st, ma);
+  hipLaunchKernelGGL((items_i8_kernel<GATED, KP, DEEP, CHUNK>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), lds, st, ma);
   return hipGetLastError();
+}
+
+// How a launch cuts its products: K in `parts`, chunks of `rows` rows where
+// that is more than one, and whether one workgroup has all of a CU's LDS.
+struct Cut {
+  int parts, rows;
+  bool deep;
+};
+
+// With the sums of few items (64 rows x 128 weight rows each, of an evenly
+// routed batch) most CUs would idle, and an item runs through its whole K
+// alone.  Time with K undivided, in 2 and in 4 parts, us (products of static
+// rows): 64 items, 64 x 8192 x 4096 19.9, 14.8, 12.7; 112, 64 x 14336 x 4096
+// 22.8, 17.2, 23.8; 189, 396 x 3391 x 12416 78, 55, 67; 256 of short K, 1000 x
+// 2048 x 768 10.6, 12.8, 22.4; 392, 849 x 3534 x 4367 35, 52, 71.
+Cut items_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
+  const int cols = gated ? kItemRows / 2 : kItemRows;
+  auto chunks = [](int rows) { return std::max(1, ceil_div(rows, kSplitChunk)); };
+  const long long items =
+      (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +
+      (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
+  Cut c{1, kChunk, false};
+  if (items <= 64) c.parts = 4;
+  else if (items <= 128 || (items <= 256 && a.K >= 4096)) c.parts = 2;
+  if (c.parts > 1) {
+    c.rows = items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
+    c.deep = seg.max_rows > 8;
+  }
+  return c;
 }
 
 }  // namespace
 
-// Narrow items that an evenly routed batch makes (undivided in K).
-long long narrow_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
-  const int cols = gated ? kItemRows / 2 : kItemRows;
-  return (a.offsets ? static_cast<long long>(seg.hit_groups) : 1) * ceil_div(a.N, cols) + (sh ? ceil_div(sh->N, cols) : 0);
-}
-
-int items_k_parts(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
-  if (seg.max_rows > kWideRows) return 1;
-  const long long items = narrow_items_i8(seg, a, sh, gated);
-  return items <= 64 ? 4 : items <= 128 ? 2 : 1;
-}
-
 long long items_blocks(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
-  const int cols = (gated ? kItemRows / 2 : kItemRows) / items_k_parts(seg, a, sh, gated);
+  const Cut c = items_cut(seg, a, sh, gated);
+  const int cols = (gated ? kItemRows / 2 : kItemRows) / c.parts;
   // at most one partly filled chunk per group; wide items need fewer column blocks
-  const long long chunks = a.offsets ? seg.total_rows / kChunk + std::min(seg.groups, seg.total_rows) : ceil_div(a.static_rows, kChunk);
+  const long long chunks = a.offsets ? seg.total_rows / c.rows + std::min(seg.groups, seg.total_rows) : ceil_div(a.static_rows, c.rows);
   long long items = chunks * ceil_div(a.N, cols);
-  if (sh) items += static_cast<long long>(ceil_div(sh->static_rows, kChunk)) * ceil_div(sh->N, cols);
+  if (sh) items += static_cast<long long>(ceil_div(sh->static_rows, c.rows)) * ceil_div(sh->N, cols);
   return items == 0 ? 0 : (items / kXcds + 3) * kXcds;  // each kind's run on an XCD rounds up by one
+}
+
+template <bool GATED>
+static hipError_t launch_cut(const Cut& c, long long blocks, const ItemsI8& ma, hipStream_t st) {
+  if (c.parts == 1) return launch_kp<GATED, 1, false, kChunk>(blocks, ma, st);
+  if (c.parts == 2)
+    return c.deep ? launch_kp<GATED, 2, true, kSplitChunk>(blocks, ma, st) : launch_kp<GATED, 2, false, kSplitChunk>(blocks, ma, st);
+  if (c.rows == 32) return launch_kp<GATED, 4, true, 32>(blocks, ma, st);
+  return c.deep ? launch_kp<GATED, 4, true, kSplitChunk>(blocks, ma, st) : launch_kp<GATED, 4, false, kSplitChunk>(blocks, ma, st);
 }
 
 hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {
@@ -454,11 +544,8 @@ hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* s
   if (blocks == 0) return hipSuccess;
   ItemsI8 ma{a, sh ? *sh : GemmI8{}, seg.total_rows};
   if (!a.offsets) ma = ItemsI8{GemmI8{}, a, 0};  // a product of static rows alone
-  switch (items_k_parts(seg, a, sh, gated)) {
-    case 4: return gated ? launch_kp<true, 4>(blocks, ma, st) : launch_kp<false, 4>(blocks, ma, st);
-    case 2: return gated ? launch_kp<true, 2>(blocks, ma, st) : launch_kp<false, 2>(blocks, ma, st);
-    default: return gated ? launch_kp<true, 1>(blocks, ma, st) : launch_kp<false, 1>(blocks, ma, st);
-  }
+  const Cut c = items_cut(seg, a, sh, gated);
+  return gated ? launch_cut<true>(c, blocks, ma, st) : launch_cut<false>(c, blocks, ma, st);
 }
 
 }  // namespace moe

@@ -51,7 +51,6 @@ constexpr int kTiledLds = (kXSlots + kWSlots) * kPart;
 constexpr int kLoads = 8;                 // per part and wave: 8 rows each
 constexpr int kSteps = kRow / 32;         // MFMA K-steps of a stage
 constexpr int kBlockM = 8;
-constexpr int kWaitLds = 15 | (3 << 14) | (7 << 4);  // lgkmcnt(0)
 
 struct TiledI8 {
   GemmI8 g, sp;
