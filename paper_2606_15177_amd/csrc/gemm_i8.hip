@@ -6,35 +6,33 @@
 namespace moe {
 namespace {
 
-// 256-row tiles want rows that fill them and tiles for a good part of the CUs.
-// Over 160 random layers (65 to 8192 tokens, even to Zipf 1 routing; K 392 to
-// 14336) and 249 random products of static rows these lines choose the kernel
-// that is within 8 % of the faster one for all but 9 of 300 grouped products
-// (1.31 at worst, 0.7 % on average; another 160 layers 0.6 %) and all but 4 of
-// the others (1.44, 0.5 %).
-// Both sides, us (items, tiles):
-//   long K (kLongK bytes): Mixtral gate/up at a mean of 50 rows 180 and 190, at
-//     75 212 and 199; the DSV3 share's down at 62 rows 171 and 161;
-//   shorter: 122 rows of K 1416, N 3432 108 and 92, 97 rows of K 1656 35 and 39;
+// 256-row tiles want rows that fill them and tiles for a good part of the CUs;
+// fewer on short K, where an item's turnaround is short too.  Over 400 random
+// layers (65 to 8192 tokens, even to Zipf 1 routing, K 392 to 14336) these lines
+// choose the faster kernel within 8 % for all but 31 of 760 grouped products
+// (1.29 at worst, 0.7 % on average), and over 297 random products of static rows
+// for all but 5 (1.38, 0.4 %).  Both sides, us (items, tiles):
+//   rows: Qwen3 of 3000 tokens (a mean of 187, 128 groups) gate/up 143 and 136,
+//     1500 tokens 115 and 123; DSV2-Lite of 3000 (281) 210 and 187, of 1500 126
+//     and 132; 8 experts of K 14336, N 4096 at a mean of 84 110 and 148;
 //   many groups of short K, whose last tiles are mostly padding: Qwen3 gate/up
-//     at a mean of 309 rows 214 and 258, at 512 335 and 308, down at 315 149 and
-//     165, at 406 205 and 193;
-//   few tiles: 593 x 9972 x 1142 (117) 18.0 and 24.2, 11380 x 485 x 6294 (90)
-//     94 and 82, 3941 x 2301 x 2281 (144) 57 and 38.
-constexpr int kMeanLong = 60, kMeanShort = 110, kMeanMany = 350, kMeanManyGated = 420;
+//     at a mean of 358, Zipf 1, 241 and 281, at 312, Zipf 0.6, 203 and 170;
+//   few tiles, grouped: 150 of K 896 17 and 23, 85 of K 2960 53 and 47; static:
+//     84 of K 5033 72 and 60, 117 of K 1142 18 and 25, 264 of K 796 29 and 34.
+constexpr int kMeanRows = 85, kMeanMany = 300;
 constexpr int kMany = 64, kManyK = 2048;
-constexpr long long kFewTiles = 128, kFewStaticTiles = 96;
+constexpr int kShortK = 1500;
+constexpr long long kFewTiles = 110, kFewShort = 300, kFewStatic = 80, kFewStaticShort = 128;
 
 bool takes_tiles(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   if (a.K <= kTiledMinK || (sh && sh->K <= kTiledMinK)) return false;
   if (items_blocks(seg, a, sh, gated) > kMaxItemBlocks) return true;
   const int cols = gated ? 128 : 256;
+  const bool brief = a.K < kShortK;
   auto tiles = [&](int rows, int N) { return static_cast<long long>(ceil_div(rows, 256)) * ceil_div(N, cols); };
-  if (!a.offsets) return tiles(a.static_rows, a.N) >= kFewStaticTiles;
-  if (seg.groups * tiles(seg.mean_rows, a.N) + (sh ? tiles(sh->static_rows, sh->N) : 0) < kFewTiles) return false;
-  if (a.K >= kLongK) return seg.mean_rows >= kMeanLong;
-  if (seg.groups < kMany || a.K > kManyK) return seg.mean_rows >= kMeanShort;
-  return seg.mean_rows >= (gated ? kMeanManyGated : kMeanMany);
+  if (!a.offsets) return tiles(a.static_rows, a.N) >= (brief ? kFewStaticShort : kFewStatic);
+  if (seg.groups * tiles(seg.mean_rows, a.N) + (sh ? tiles(sh->static_rows, sh->N) : 0) < (brief ? kFewShort : kFewTiles)) return false;
+  return seg.mean_rows >= (seg.groups >= kMany && a.K <= kManyK ? kMeanMany : kMeanRows);
 }
 
 }  // namespace

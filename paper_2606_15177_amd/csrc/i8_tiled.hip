@@ -21,6 +21,10 @@
 // last partly filled one too.  The shared experts (static rows) are one more
 // group, first, with operands of its own.
 //
+// Last round.  Where the tiles past the last whole round of the grid are at most
+// half (a quarter) of the workgroups, each is run in two (four) parts of its
+// rows on as many CUs.
+//
 // A group's last tile: rows past its end cost no traffic (their loads lie past
 // the descriptor's range), and a tile of up to 128 or 64 rows takes half or a
 // quarter of the MFMAs, the four waves side by side along the weights.
@@ -130,16 +134,18 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   const int n_wg = static_cast<int>(gridDim.x);  // a multiple of the XCDs
   const int xcd = static_cast<int>(blockIdx.x) % kXcds, in_xcd = static_cast<int>(blockIdx.x) / kXcds;
   const int rounds = total / n_wg, rest = total - rounds * n_wg;
-  const int rest_lo = static_cast<int>(static_cast<long long>(rest) * xcd / kXcds);
-  const int rest_hi = static_cast<int>(static_cast<long long>(rest) * (xcd + 1) / kXcds);
-  const int mine = rounds + (in_xcd < rest_hi - rest_lo ? 1 : 0);  // tiles of this workgroup
-  if (mine == 0) return;
+  // the last round's tiles in `split` parts of 256 / split rows
+  const int split = 4 * rest <= n_wg ? 4 : 2 * rest <= n_wg ? 2 : 1;
+  const int rest_lo = static_cast<int>(static_cast<long long>(rest) * split * xcd / kXcds);
+  const int rest_hi = static_cast<int>(static_cast<long long>(rest) * split * (xcd + 1) / kXcds);
+  int mine = rounds + (in_xcd < rest_hi - rest_lo ? 1 : 0);  // tiles of this workgroup
 
   struct TileInfo {
     int sp, g, row_base, m0, rows, nt;  // rows of the tile: m0 .. m0 + rows - 1 of the group
   };
   auto tile_info = [&](int i) {
-    const int id = i < rounds ? i * n_wg + xcd * (n_wg / kXcds) + in_xcd : rounds * n_wg + rest_lo + in_xcd;
+    const int part = rest_lo + in_xcd;  // (in the last round)
+    const int id = i < rounds ? i * n_wg + xcd * (n_wg / kXcds) + in_xcd : rounds * n_wg + part / split;
     TileInfo ti;
     ti.sp = id < ta.sp_tiles ? 1 : 0;
     int local = id, mg, m, tn = tiles_n;
@@ -176,6 +182,11 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     ti.nt = quotient(r, bm);
     ti.m0 = (b * kBlockM + r - ti.nt * bm) * kTile;
     ti.rows = min(kTile, m - ti.m0);
+    if (i == rounds && split > 1) {
+      const int at = part % split * (kTile / split);
+      ti.m0 += at;
+      ti.rows = min(kTile / split, ti.rows - at);
+    }
     ti.sp = uniform(ti.sp);
     ti.g = uniform(ti.g);
     ti.row_base = uniform(ti.row_base);
@@ -186,6 +197,10 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   };
   auto prob = [&](const TileInfo& ti) -> const GemmI8& { return ti.sp ? ta.sp : ta.g; };
   auto stages = [&](const TileInfo& ti) { return ceil_div(prob(ti).K, kRow); };
+
+  // (a part past the tile's rows is none)
+  if (mine > rounds && split > 1 && tile_info(rounds).rows <= 0) --mine;
+  if (mine == 0) return;
 
   // ---- loads ----
   // Wave w fills rows 64 w .. 64 w + 63 of a part; load i writes rows 64 w + 8 i
