@@ -24,7 +24,7 @@ ARCH = "gfx950"
 SOURCES = ["route.hip", "permute.hip", "combine.hip", "ffn_skinny.hip", "ffn_mid.hip", "ffn_tiled.hip", "place.hip", "window.hip",
            "moe_abi.hip"]
 # the 8-bit experts
-SOURCES_I8 = ["quant.hip", "gemm_i8.hip", "i8_mid.hip", "i8_tiled.hip"]
+SOURCES_I8 = ["quant.hip", "gemm_i8.hip", "i8_few.hip", "i8_mid.hip", "i8_tiled.hip"]
 
 CXXFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",

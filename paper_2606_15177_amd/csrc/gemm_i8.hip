@@ -38,11 +38,16 @@ bool takes_tiles(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool ga
 }  // namespace
 
 hipError_t launch_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {
+  if (a.xb) return launch_few_i8(seg, a, sh, gated, st);
   return takes_tiles(seg, a, sh, gated) ? launch_tiled_i8(seg, a, sh, gated, st) : launch_items_i8(seg, a, sh, gated, st);
 }
 
 bool gemm_i8_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   return items_blocks(seg, a, sh, gated) <= kMaxItemBlocks || takes_tiles(seg, a, sh, gated);
+}
+
+bool gemm_i8_quantizes(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
+  return seg.max_rows <= kFewRows && (!sh || sh->static_rows <= kFewRows) && few_supported(seg, a, sh, gated);
 }
 
 }  // namespace moe

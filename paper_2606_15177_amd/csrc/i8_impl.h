@@ -3,16 +3,12 @@
 #pragma once
 
 #include "ffn_impl.h"
+#include "quant_impl.h"
 
 namespace moe {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
-// 16 bytes at any bf16 address: result rows of odd length start at odd
-// multiples of two bytes (global memory takes unaligned vector accesses on
-// this target)
-typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
-
 constexpr uint32_t kPastEnd = 0x80000000u;  // an offset past a descriptor's range: reads zeros, no traffic
 constexpr int kXcds = 8;
 constexpr int kWaitLds = 15 | (3 << 14) | (7 << 4);  // s_waitcnt immediate (see wait_vm): LDS accesses done
@@ -31,6 +27,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p) {
 // within the rows that the caller's buffers have.
 __device__ __forceinline__ int row_at(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
 
+// A scalar load: its wait leaves the vector-memory counter, and so the tile
+// loads in flight, alone.
+typedef const int __attribute__((address_space(4)))* ConstIntPtr;
+__device__ __forceinline__ int load_scalar(const int* p, int i) { return ((ConstIntPtr)(uintptr_t)p)[i]; }
+
 // Eight consecutive results, or those of them before N.
 __device__ __forceinline__ void store_cols(uint16_t* p, u32x4 v, int col, int N) {
   if (col + 8 <= N) {
@@ -47,6 +48,11 @@ __device__ __forceinline__ void store_cols(uint16_t* p, u32x4 v, int col, int N)
 constexpr int kTiledMinK = 384;
 hipError_t launch_tiled_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
 hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
+// Bf16 rows (xb), few of them per group (any number is computed): each
+// workgroup quantises the rows that it multiplies.
+constexpr int kFewRows = 8;
+bool few_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
+hipError_t launch_few_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
 // Workgroups of launch_items_i8, and how many a grid dimension holds (2^32 - 1
 // threads).
 long long items_blocks(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);

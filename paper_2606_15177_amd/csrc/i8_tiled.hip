@@ -70,11 +70,6 @@ __device__ __forceinline__ int opaque_lane() {
   return ln & 63;  // (known to be small and not negative)
 }
 
-// A scalar load: its wait leaves the vector-memory counter, and so the tile
-// loads in flight, alone.
-typedef const int __attribute__((address_space(4)))* ConstIntPtr;
-__device__ __forceinline__ int load_scalar(const int* p, int i) { return ((ConstIntPtr)(uintptr_t)p)[i]; }
-
 // n / d for 0 <= n, 0 < d, n / d < 2^22 (tiles of a launch): the quotient in
 // fp32 is off by one at most.
 __device__ __forceinline__ int quotient(int n, int d) {

@@ -168,7 +168,9 @@ hipError_t launch_quantize_rows(const QuantArgs& a, const QuantArgs* b, hipStrea
 // X[r] = x[r], or x[x_rows[r]] (x_count rows of x; an entry outside them
 // counts as a row of zeros).  Rows are ldx and ldw bytes (multiples of 16) and
 // ldo values apart, and hold zeros from K to the next multiple of 16 in one
-// operand at least; groups of weights are N rows apart.
+// operand at least; groups of weights are N rows apart.  With xb the rows are
+// bf16, ldxb values apart, and the product quantises them itself (x and x_scale
+// are not read); only where gemm_i8_quantizes.
 struct GemmI8 {
   const int8_t* x;
   const float* x_scale;
@@ -182,6 +184,8 @@ struct GemmI8 {
   uint16_t* out;
   int K, N;
   long long ldx, ldw, ldo;
+  const uint16_t* xb = nullptr;
+  long long ldxb = 0;
 };
 // a over seg (as the expert GEMMs above), and sh (nullable, static rows) in
 // the same launch.
@@ -189,6 +193,9 @@ hipError_t launch_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh
 // Host only: whether it accepts these sizes (the pointers are not looked at,
 // but for offsets being null or not).
 bool gemm_i8_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
+// Host only: whether these sizes take bf16 rows, and run faster so than after
+// a launch that quantises them.
+bool gemm_i8_quantizes(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 
 // ---- combine.hip -----------------------------------------------------------
 hipError_t launch_combine(int T, int k, int H, const uint16_t* y_perm, const int32_t* inv_pos,

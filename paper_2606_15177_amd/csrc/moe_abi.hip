@@ -357,30 +357,39 @@ int weights_i8_ok(const moe_dims* d, const moe_weights_i8* w) {
 
 // The experts' networks on int8: x quantised (rows rows, or *n_rows), gate/up
 // on it (through x_rows where x holds tokens), the hidden rows quantised, down.
+// Where there are few rows the products quantise them.
 // x == x_sh: the shared experts read the rows quantised for the routed ones.
 int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, const int32_t* offsets,
                const moe_weights_i8* w, const uint16_t* x_sh, uint16_t* y_perm, uint16_t* y_shared, void* ws,
                const moe_taps* taps, hipStream_t st) {
   const bool one_x = x_rows != nullptr;
   const FfnI8Ws fw = carve_ffn_i8(d, one_x, ws);
-  const FfnI8Plan p = plan_ffn_i8(d, fw, x_rows, offsets, *w, y_perm, y_shared);
+  FfnI8Plan p = plan_ffn_i8(d, fw, x_rows, offsets, *w, y_perm, y_shared);
   const int shw = static_cast<int>(sh_width(d)), rows = d->T * d->k;
   const int32_t* n_rows = offsets + d->E_local;
   hipError_t e;
 
   record(taps, 2 * MOE_STAGE_FFN_UP, st);
+  if (moe::gemm_i8_quantizes(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true)) {
+    p.up.xb = x, p.sh_up.xb = x_sh;
+    p.up.ldxb = p.sh_up.ldxb = d->H;
+  }
   const moe::QuantArgs qx{x, fw.xq, fw.xs, one_x ? nullptr : n_rows, d->H, p.up.ldx, one_x ? d->T : rows, d->H};
   const moe::QuantArgs qx_sh{x_sh, fw.xq_sh, fw.xs_sh, nullptr, d->H, p.up.ldx, d->T, d->H};
-  e = moe::launch_quantize_rows(qx, p.sh && !one_x ? &qx_sh : nullptr, st);
+  e = p.up.xb ? hipSuccess : moe::launch_quantize_rows(qx, p.sh && !one_x ? &qx_sh : nullptr, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   e = moe::launch_gemm_i8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   record(taps, 2 * MOE_STAGE_FFN_UP + 1, st);
 
   record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
+  if (moe::gemm_i8_quantizes(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false)) {
+    p.dn.xb = fw.h, p.sh_dn.xb = fw.h_sh;
+    p.dn.ldxb = d->I, p.sh_dn.ldxb = shw;
+  }
   const moe::QuantArgs qh{fw.h, fw.hq, fw.hs, n_rows, d->I, p.dn.ldx, rows, d->I};
   const moe::QuantArgs qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, p.sh_dn.ldx, d->T, shw};
-  e = moe::launch_quantize_rows(qh, p.sh ? &qh_sh : nullptr, st);
+  e = p.dn.xb ? hipSuccess : moe::launch_quantize_rows(qh, p.sh ? &qh_sh : nullptr, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   e = moe::launch_gemm_i8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;

@@ -488,3 +488,54 @@ def test_no_tokens(moe):
                                        torch.empty((0, 64), **e), counts=counts)
     torch.cuda.synchronize()
     assert out.shape == (0, 64) and (counts == 1).all()
+
+
+# Few tokens: the products quantise the rows themselves, K in four, two and one
+# parts (gate/up: 1 to 2, 5, and 24 or more items of 128 weight rows times the
+# experts hit), rows longer than the registers hold (down, 9000), rows of the
+# last case too long for it at 8 tokens, and a shared expert of its own width.
+FEW = [dict(H=512, E=16, k=2, I=256, E_local=16), dict(H=2048, E=32, k=4, I=768, E_local=24),
+       dict(H=1000, E=6, k=3, I=1544, E_local=6, n_shared=1, I_shared=344), dict(H=136, E=8, k=8, I=40, E_local=8),
+       dict(H=256, E=4, k=2, I=9000, E_local=4, n_shared=2, I_shared=1000)]
+
+
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_few_tokens_are_those_of_a_batch(moe, case):
+    """Up to 9 tokens: bit for bit the rows of a batch of 40, whose rows are
+    quantised by a launch; one row is zero and one not finite."""
+    big = moe.dims(T=40, S=1, **FEW[case])
+    _, q = layer_weights(moe, big, case)
+    local = None if big.E_local == big.E else torch.arange(big.E_local, dtype=torch.int32, device="cuda")
+    logits, x = torch.randn((40, big.E), generator=gen(case), device="cuda"), randn((40, big.H), case)
+    x[1], x[4, 3] = 0.0, float("nan")
+    ref = moe.MoeLayerI8(big, q, local).forward(logits, None, x)
+    for T in (1, 2, 3, 5, 8, 9):
+        d = moe.dims(T=T, S=1, **FEW[case])
+        layer = moe.MoeLayerI8(d, q, local)
+        layer.ws.fill_(0xff)
+        out = layer.forward(logits[:T], None, x[:T])
+        assert torch.equal(out.view(torch.int16), ref[:T].view(torch.int16)), T
+
+
+@pytest.mark.parametrize("sizes", [[24, 0, 0], [0, 9, 15], [17, 0, 1], [0, 0, 0], [1, 1, 1]])
+def test_few_tokens_in_any_groups(moe, sizes):
+    """expert_ffn_i8 of 8 tokens, however their rows lie; rows behind the last
+    group stay as they were."""
+    d = moe.dims(T=8, S=1, H=264, E=3, k=3, I=200, E_local=3, n_shared=1, I_shared=88)
+    _, q = layer_weights(moe, d, 5)
+    w = moe.make_weights_i8(d, q)
+    o = np.concatenate([[0], np.cumsum(sizes)]).tolist()
+    x_perm, x = randn((24, d.H), 1), randn((8, d.H), 2)
+    y = torch.full((24, d.H), 3.0, dtype=torch.bfloat16, device="cuda")
+    ysh = torch.empty((8, d.H), dtype=torch.bfloat16, device="cuda")
+    ws = moe.workspace(d, moe.ENTRY_EXPERT_FFN_I8).fill_(0xff)
+    moe.expert_ffn_i8(d, x_perm, torch.tensor(o, dtype=torch.int32, device="cuda"), w, x, y, ysh, ws)
+    for e in range(3):
+        if o[e] < o[e + 1]:
+            ref, bound = ffn_and_bound(x_perm[o[e]:o[e + 1]].double(), deq(q["w_gate"][e], q["s_gate"][e], d.H),
+                                       deq(q["w_up"][e], q["s_up"][e], d.H), deq(q["w_down"][e], q["s_down"][e], d.I))
+            assert ((y[o[e]:o[e + 1]].double() - ref).abs() <= bound).all(), e
+    assert (y[o[-1]:] == 3.0).all()
+    ref, bound = ffn_and_bound(x.double(), deq(q["sh_gate"], q["sh_s_gate"], d.H), deq(q["sh_up"], q["sh_s_up"], d.H),
+                               deq(q["sh_down"], q["sh_s_down"], 88))
+    assert ((ysh.double() - ref).abs() <= bound).all()
