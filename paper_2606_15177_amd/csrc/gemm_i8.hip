@@ -50,4 +50,10 @@ bool gemm_i8_quantizes(const Segments& seg, const GemmI8& a, const GemmI8* sh, b
   return seg.max_rows <= kFewRows && (!sh || sh->static_rows <= kFewRows) && few_supported(seg, a, sh, gated);
 }
 
+GemmI8Plan plan_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
+  if (!a.xb && takes_tiles(seg, a, sh, gated)) return {1, 1, 256};
+  const Cut c = a.xb ? few_cut(seg, a, sh, gated) : items_cut(seg, a, sh, gated);
+  return {a.xb ? 2 : 0, c.parts, c.rows};
+}
+
 }  // namespace moe

@@ -312,13 +312,18 @@ bool few_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool 
 // (us, one part and two, gate/up: 288 items of K 7168 97.6 and 89.7, 344 of K
 // 4096 82.6 and 80.2, 96 of K 2048 28.1 and 27.0, 384 of K 2048 47.8 and 49.9;
 // down, two and four: 64 of K 11008 72.1 and 67.2).
-hipError_t launch_few_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {
+Cut few_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   const int cols = gated ? 64 : 128;
   const long long hit = static_cast<long long>(seg.hit_groups) * ceil_div(a.N, cols) + (sh ? ceil_div(sh->N, cols) : 0);
-  const int parts = hit <= 64 ? 4 : hit <= 128 || (hit <= 512 && a.K >= 4096) ? 2 : 1;
+  return {hit <= 64 ? 4 : hit <= 128 || (hit <= 512 && a.K >= 4096) ? 2 : 1, chunk_rows(seg, sh)};
+}
+
+hipError_t launch_few_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {
+  const Cut c = few_cut(seg, a, sh, gated);
+  const int parts = c.parts;
   const int blocks = static_cast<int>((parts * few_items(seg, a, sh, gated) / kXcds + 1) * kXcds);
   const int lds = few_lds(seg, a, sh);
-  const FewI8 ma{a, sh ? *sh : GemmI8{}, seg.total_rows, chunk_rows(seg, sh)};
+  const FewI8 ma{a, sh ? *sh : GemmI8{}, seg.total_rows, c.rows};
   if (parts == 4) return gated ? launch_few_kp<true, 4>(blocks, lds, ma, st) : launch_few_kp<false, 4>(blocks, lds, ma, st);
   if (parts == 2) return gated ? launch_few_kp<true, 2>(blocks, lds, ma, st) : launch_few_kp<false, 2>(blocks, lds, ma, st);
   return gated ? launch_few_kp<true, 1>(blocks, lds, ma, st) : launch_few_kp<false, 1>(blocks, lds, ma, st);

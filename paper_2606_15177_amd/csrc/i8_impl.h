@@ -48,10 +48,16 @@ __device__ __forceinline__ void store_cols(uint16_t* p, u32x4 v, int col, int N)
 constexpr int kTiledMinK = 384;
 hipError_t launch_tiled_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
 hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
+// How a launch of items cuts its products: K in `parts`, chunks of `rows` rows.
+struct Cut {
+  int parts, rows;
+};
+Cut items_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 // Bf16 rows (xb), few of them per group (any number is computed): each
 // workgroup quantises the rows that it multiplies.
 constexpr int kFewRows = 8;
 bool few_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
+Cut few_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 hipError_t launch_few_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
 // Workgroups of launch_items_i8, and how many a grid dimension holds (2^32 - 1
 // threads).

@@ -32,6 +32,7 @@ namespace {
 
 constexpr int kChunk = 128;         // token rows of a chunk of a wide item
 constexpr int kSplitChunk = 64;     // ... of any item where K is split (32 where there are very few)
+constexpr int kBriefChunk = 8;      // ... where no group has more rows
 constexpr int kWideRows = 64;       // groups of more rows take wide items
 constexpr int kItemRows = 128;      // weight rows of a narrow item
 constexpr int kFewWide = 128;       // fewer wide items than this take 128 weight rows: half the CUs' worth
@@ -41,6 +42,8 @@ constexpr int kItemLds = 80 * 1024;   // two workgroups per CU
 constexpr int kDeepLds = 160 * 1024;  // one
 constexpr int kTurn = 8;
 constexpr int kItemThreads = 4 * kWave;
+
+constexpr int item_lds(int parts, int chunk) { return parts > 1 && chunk > kBriefChunk ? kDeepLds : kItemLds; }
 
 struct ItemsI8 {
   GemmI8 g;   // groups with device offsets (groups 0: none)
@@ -65,7 +68,7 @@ __device__ __forceinline__ void wait_stage(int j) {
   }
 }
 
-template <bool GATED, int KP, bool DEEP, int CHUNK>
+template <bool GATED, int KP, int CHUNK>
 __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void items_i8_kernel(ItemsI8 ma) {
   constexpr int FULL_COLS = GATED ? kItemRows / 2 : kItemRows;  // output columns of 128 weight rows
   constexpr int OUT_COLS = FULL_COLS / KP;                      // ... of a narrow item
@@ -209,7 +212,8 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   const uint32_t ldx = static_cast<uint32_t>(p.ldx), ldw = static_cast<uint32_t>(p.ldw);
   const int32_t* x_rows = p.x_rows;
   // the group's rows in equal chunks of whole 32-row MFMA tiles
-  const int chunk_rows = ceil_div(ceil_div(m, n_chunks), 32) * 32;
+  constexpr int UNIT = CHUNK < 32 ? CHUNK : 32;
+  const int chunk_rows = ceil_div(ceil_div(m, n_chunks), UNIT) * UNIT;
   const int m0 = chunk * chunk_rows;
   const int rows = min(chunk_rows, m - m0);
   const int n0 = nblk * (wide ? wide_cols : OUT_COLS);
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int WL = WB * 32 / RPI;              // weight loads per wave and stage
     constexpr int LOADS = XL + WL;
     constexpr int KS = BK / 32;                    // MFMA K-steps per stage
-    static_assert(D * STAGE <= (DEEP ? kDeepLds : kItemLds), "the ring fits");
+    static_assert(D * STAGE <= item_lds(KP, CHUNK), "the ring fits");
     static_assert(FEW ? RPI == 8 : XL * RPI * WN == XR, "whole loads fill the token rows");
     const int lr = lane / CPR;                     // row of a load
     const int wn = wave % WN, wk = wave / WN;
@@ -468,33 +472,30 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     else if (wide) body(C4{}, C1{}, C1{}, K64{}, C5{}, whole);
     else if (rows > 32) body(C2{}, C1{}, C1{}, K128{}, C3{}, whole);
     else body(C1{}, C1{}, C1{}, K128{}, C4{}, whole);
+  } else if constexpr (CHUNK == kBriefChunk) {
+    body(C1{}, C1{}, integral_constant<int, KP>{}, K128{}, C4{}, few);
   } else if constexpr (KP == 2) {
-    if (rows > 32) body(C2{}, C1{}, C2{}, integral_constant<int, DEEP ? 128 : 64>{}, C5{}, whole);
-    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, integral_constant<int, DEEP ? 6 : 3>{}, whole);
+    if (rows > 32) body(C2{}, C1{}, C2{}, K128{}, C5{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, integral_constant<int, 6>{}, whole);
     else body(C1{}, C1{}, C2{}, K128{}, C4{}, few);
   } else {
-    if (CHUNK > 32 && rows > 32) body(C2{}, C1{}, C4{}, integral_constant<int, DEEP ? 128 : 64>{}, C3{}, whole);
-    else if (rows > 8) body(C1{}, C1{}, C4{}, integral_constant<int, DEEP ? 128 : 64>{}, C5{}, whole);
+    if (CHUNK > 32 && rows > 32) body(C2{}, C1{}, C4{}, K128{}, C3{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C4{}, K128{}, C5{}, whole);
     else body(C1{}, C1{}, C4{}, K128{}, C4{}, few);
   }
 }
 
-template <bool GATED, int KP, bool DEEP, int CHUNK>
+template <bool GATED, int KP, int CHUNK>
 hipError_t launch_kp(long long blocks, const ItemsI8& ma, hipStream_t st) {
-  constexpr int lds = DEEP ? kDeepLds : kItemLds;
+  constexpr int lds = item_lds(KP, CHUNK);
   static unsigned long long lds_set = 0;  // devices with the LDS limit raised
-  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_i8_kernel<GATED, KP, DEEP, CHUNK>), lds, &lds_set);
+  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_i8_kernel<GATED, KP, CHUNK>), lds, &lds_set);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((items_i8_kernel<GATED, KP, DEEP, CHUNK>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), lds, st, ma);
+  hipLaunchKernelGGL((items_i8_kernel<GATED, KP, CHUNK>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), lds, st, ma);
   return hipGetLastError();
 }
 
-// How a launch cuts its products: K in `parts`, chunks of `rows` rows where
-// that is more than one, and whether one workgroup has all of a CU's LDS.
-struct Cut {
-  int parts, rows;
-  bool deep;
-};
+}  // namespace
 
 // With the sums of few items (64 rows x 128 weight rows each, of an evenly
 // routed batch) most CUs would idle, and an item runs through its whole K
@@ -508,17 +509,12 @@ Cut items_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated
   const long long items =
       (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +
       (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
-  Cut c{1, kChunk, false};
+  Cut c{1, kChunk};
   if (items <= 64) c.parts = 4;
   else if (items <= 128 || (items <= 256 && a.K >= 4096)) c.parts = 2;
-  if (c.parts > 1) {
-    c.rows = items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
-    c.deep = seg.max_rows > 8;
-  }
+  if (c.parts > 1) c.rows = seg.max_rows <= kBriefChunk ? kBriefChunk : items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
   return c;
 }
-
-}  // namespace
 
 long long items_blocks(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   const Cut c = items_cut(seg, a, sh, gated);
@@ -532,11 +528,11 @@ long long items_blocks(const Segments& seg, const GemmI8& a, const GemmI8* sh, b
 
 template <bool GATED>
 static hipError_t launch_cut(const Cut& c, long long blocks, const ItemsI8& ma, hipStream_t st) {
-  if (c.parts == 1) return launch_kp<GATED, 1, false, kChunk>(blocks, ma, st);
+  if (c.parts == 1) return launch_kp<GATED, 1, kChunk>(blocks, ma, st);
   if (c.parts == 2)
-    return c.deep ? launch_kp<GATED, 2, true, kSplitChunk>(blocks, ma, st) : launch_kp<GATED, 2, false, kSplitChunk>(blocks, ma, st);
-  if (c.rows == 32) return launch_kp<GATED, 4, true, 32>(blocks, ma, st);
-  return c.deep ? launch_kp<GATED, 4, true, kSplitChunk>(blocks, ma, st) : launch_kp<GATED, 4, false, kSplitChunk>(blocks, ma, st);
+    return c.rows == kBriefChunk ? launch_kp<GATED, 2, kBriefChunk>(blocks, ma, st) : launch_kp<GATED, 2, kSplitChunk>(blocks, ma, st);
+  if (c.rows == kBriefChunk) return launch_kp<GATED, 4, kBriefChunk>(blocks, ma, st);
+  return c.rows == 32 ? launch_kp<GATED, 4, 32>(blocks, ma, st) : launch_kp<GATED, 4, kSplitChunk>(blocks, ma, st);
 }
 
 hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {

@@ -196,6 +196,12 @@ bool gemm_i8_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, b
 // Host only: whether these sizes take bf16 rows, and run faster so than after
 // a launch that quantises them.
 bool gemm_i8_quantizes(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
+// Host only: how a launch runs.  The kernel (0 items, 1 tiles, 2 items that
+// quantise their rows), the parts of K, the rows of a tile or a chunk.
+struct GemmI8Plan {
+  int kernel, parts, rows;
+};
+GemmI8Plan plan_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 
 // ---- combine.hip -----------------------------------------------------------
 hipError_t launch_combine(int T, int k, int H, const uint16_t* y_perm, const int32_t* inv_pos,

@@ -355,9 +355,20 @@ int weights_i8_ok(const moe_dims* d, const moe_weights_i8* w) {
   return MOE_OK;
 }
 
+// Where there are few rows the products quantise them.
+void quantize_in_products(const moe_dims* d, const FfnI8Ws& fw, const uint16_t* x, const uint16_t* x_sh, FfnI8Plan* p) {
+  if (moe::gemm_i8_quantizes(p->routed, p->up, p->sh ? &p->sh_up : nullptr, true)) {
+    p->up.xb = x, p->sh_up.xb = x_sh;
+    p->up.ldxb = p->sh_up.ldxb = d->H;
+  }
+  if (moe::gemm_i8_quantizes(p->routed, p->dn, p->sh ? &p->sh_dn : nullptr, false)) {
+    p->dn.xb = fw.h, p->sh_dn.xb = fw.h_sh;
+    p->dn.ldxb = d->I, p->sh_dn.ldxb = p->sh_dn.K;
+  }
+}
+
 // The experts' networks on int8: x quantised (rows rows, or *n_rows), gate/up
 // on it (through x_rows where x holds tokens), the hidden rows quantised, down.
-// Where there are few rows the products quantise them.
 // x == x_sh: the shared experts read the rows quantised for the routed ones.
 int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, const int32_t* offsets,
                const moe_weights_i8* w, const uint16_t* x_sh, uint16_t* y_perm, uint16_t* y_shared, void* ws,
@@ -365,15 +376,12 @@ int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, cons
   const bool one_x = x_rows != nullptr;
   const FfnI8Ws fw = carve_ffn_i8(d, one_x, ws);
   FfnI8Plan p = plan_ffn_i8(d, fw, x_rows, offsets, *w, y_perm, y_shared);
+  quantize_in_products(d, fw, x, x_sh, &p);
   const int shw = static_cast<int>(sh_width(d)), rows = d->T * d->k;
   const int32_t* n_rows = offsets + d->E_local;
   hipError_t e;
 
   record(taps, 2 * MOE_STAGE_FFN_UP, st);
-  if (moe::gemm_i8_quantizes(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true)) {
-    p.up.xb = x, p.sh_up.xb = x_sh;
-    p.up.ldxb = p.sh_up.ldxb = d->H;
-  }
   const moe::QuantArgs qx{x, fw.xq, fw.xs, one_x ? nullptr : n_rows, d->H, p.up.ldx, one_x ? d->T : rows, d->H};
   const moe::QuantArgs qx_sh{x_sh, fw.xq_sh, fw.xs_sh, nullptr, d->H, p.up.ldx, d->T, d->H};
   e = p.up.xb ? hipSuccess : moe::launch_quantize_rows(qx, p.sh && !one_x ? &qx_sh : nullptr, st);
@@ -383,10 +391,6 @@ int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, cons
   record(taps, 2 * MOE_STAGE_FFN_UP + 1, st);
 
   record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
-  if (moe::gemm_i8_quantizes(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false)) {
-    p.dn.xb = fw.h, p.sh_dn.xb = fw.h_sh;
-    p.dn.ldxb = d->I, p.sh_dn.ldxb = shw;
-  }
   const moe::QuantArgs qh{fw.h, fw.hq, fw.hs, n_rows, d->I, p.dn.ldx, rows, d->I};
   const moe::QuantArgs qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, p.sh_dn.ldx, d->T, shw};
   e = p.dn.xb ? hipSuccess : moe::launch_quantize_rows(qh, p.sh ? &qh_sh : nullptr, st);
@@ -395,6 +399,11 @@ int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, cons
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   record(taps, 2 * MOE_STAGE_FFN_DOWN + 1, st);
   return MOE_OK;
+}
+
+moe::Segments linear_segments(const moe_linear_dims* d, const int32_t* offsets, bool grouped) {
+  return grouped ? moe::Segments{offsets, d->G, 0, d->M, d->M, d->M / d->G, std::min(d->G, d->M)}
+                 : moe::Segments{nullptr, 1, d->M, d->M, d->M, d->M, 1};
 }
 
 // The checks that the two 8-bit products share.
@@ -683,7 +692,7 @@ int moe_linear_i8(const moe_linear_dims* d, const int8_t* xq, const float* x_sca
                   const float* w_scale, moe_bf16* y, void* stream) {
   const int s = linear_ok(d, false, false, xq, x_scale, wq, w_scale, y);
   if (s != MOE_OK || d->M == 0) return s;
-  const moe::Segments seg{nullptr, 1, d->M, d->M, d->M, d->M, 1};
+  const moe::Segments seg = linear_segments(d, nullptr, false);
   const moe::GemmI8 a{xq, x_scale, nullptr, 0, nullptr, d->M, 1, wq, nullptr, w_scale, nullptr, y,
                       d->K, d->N, d->ldx, d->ldw, d->ldy};
   if (!moe::gemm_i8_supported(seg, a, nullptr, false)) return MOE_ERR_UNSUPPORTED;
@@ -696,7 +705,7 @@ int moe_grouped_linear_i8(const moe_linear_dims* d, const int8_t* xq, const floa
   if (s != MOE_OK || d->M == 0) return s;
   if (!offsets) return MOE_ERR_NULL;
   if (((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(x_rows)) & 3u) != 0) return MOE_ERR_ALIGN;
-  const moe::Segments seg{offsets, d->G, 0, d->M, d->M, d->M / d->G, std::min(d->G, d->M)};
+  const moe::Segments seg = linear_segments(d, offsets, true);
   const moe::GemmI8 a{xq, x_scale, x_rows, x_rows ? d->X : 0, offsets, 0, d->G, wq, nullptr, w_scale, nullptr, y,
                       d->K, d->N, d->ldx, d->ldw, d->ldy};
   if (!moe::gemm_i8_supported(seg, a, nullptr, false)) return MOE_ERR_UNSUPPORTED;
@@ -764,6 +773,44 @@ int moe_test_ffn_plan(const moe_dims* d, int rows_indexed, int64_t out[2][7]) {
   for (int i = 0; i < 2; ++i) {
     const int64_t v[7] = {g[i].kernel, g[i].tail, g[i].split_k, g[i].merged, g[i].blocks, g[i].sh_kernel, g[i].sh_blocks};
     std::copy(v, v + 7, out[i]);
+  }
+  return MOE_OK;
+}
+
+// For the tests: how the 8-bit products run (moe::GemmI8Plan: kernel, parts,
+// rows), of moe_linear_i8 or moe_grouped_linear_i8, and of
+// moe_forward_i8's or moe_expert_ffn_i8's gate/up and down.
+int moe_test_linear_i8_plan(const moe_linear_dims* d, int grouped, int64_t out[3]) {
+  static const int32_t some = 0;  // stands for device offsets
+  if (d == nullptr || d->M < 1 || d->N < 1 || d->K < 1 || (grouped && d->G < 1)) return MOE_ERR_DIMS;
+  const moe::Segments seg = linear_segments(d, grouped ? &some : nullptr, grouped != 0);
+  moe::GemmI8 a{};
+  a.offsets = seg.offsets;
+  a.static_rows = grouped ? 0 : d->M;
+  a.groups = seg.groups;
+  a.K = d->K, a.N = d->N;
+  const moe::GemmI8Plan p = moe::plan_gemm_i8(seg, a, nullptr, false);
+  const int64_t v[3] = {p.kernel, p.parts, p.rows};
+  std::copy(v, v + 3, out);
+  return MOE_OK;
+}
+
+int moe_test_ffn_i8_plan(const moe_dims* d, int64_t out[2][3]) {
+  const int s = check_dims(d);
+  if (s != MOE_OK) return s;
+  if (d->T == 0 || check_ffn_i8_limits(d, false) != MOE_OK) return MOE_ERR_UNSUPPORTED;
+  static const int32_t some = 0;     // stands for device offsets
+  static const uint16_t row = 0;     // ... and rows
+  FfnI8Ws fw{};
+  uint16_t h = 0;
+  fw.h = fw.h_sh = &h;
+  FfnI8Plan p = plan_ffn_i8(d, fw, nullptr, &some, moe_weights_i8{}, nullptr, nullptr);
+  quantize_in_products(d, fw, &row, &row, &p);
+  const moe::GemmI8Plan g[2] = {moe::plan_gemm_i8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true),
+                                moe::plan_gemm_i8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false)};
+  for (int i = 0; i < 2; ++i) {
+    const int64_t v[3] = {g[i].kernel, g[i].parts, g[i].rows};
+    std::copy(v, v + 3, out[i]);
   }
   return MOE_OK;
 }

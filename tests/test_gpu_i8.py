@@ -4,7 +4,9 @@ Products: the int32 sums are exact, so the result is a fixed fp32 expression of
 an integer; it is compared bit for bit with that expression (and, through it,
 to half a bf16 step of the exact value, asserted once).  Quantisation: integers
 and scales bit for bit.  The experts' networks: within the bound that rounding
-of the hidden rows leaves (see hidden_bound)."""
+of the hidden rows leaves (see ffn_and_bound)."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -539,3 +541,97 @@ def test_few_tokens_in_any_groups(moe, sizes):
     ref, bound = ffn_and_bound(x.double(), deq(q["sh_gate"], q["sh_s_gate"], d.H), deq(q["sh_up"], q["sh_s_up"], d.H),
                                deq(q["sh_down"], q["sh_s_down"], 88))
     assert ((ysh.double() - ref).abs() <= bound).all()
+
+
+# ------------------------------------------ shapes that reach each kernel ----
+
+
+ITEMS, TILES, FEW_ROWS = 0, 1, 2
+
+
+def linear_plan(moe, M, N, K, G=0):
+    """(kernel, parts of K, rows of a tile or chunk)."""
+    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), (C.c_int64 * 3)()
+    assert moe._lib.moe_test_linear_i8_plan(C.byref(d), int(G > 0), out) == 0
+    return tuple(out)
+
+
+def ffn_plan(moe, d):
+    out = (C.c_int64 * 6)()
+    assert moe._lib.moe_test_ffn_i8_plan(C.byref(d), out) == 0
+    return tuple(out[:3]), tuple(out[3:])
+
+
+# Items: few rows with K in 2 and 4 parts, chunks of 64 and 32; undivided, with
+# 256 weight rows per item.  Tiles: 90 (their only round in 2 parts per tile),
+# 300 (44 past a round of 256: 4 parts), 220 (whole), K a byte past the items'.
+KERNELS = [(7, 9001, 130, (ITEMS, 2, 8)), (8, 517, 1003, (ITEMS, 4, 8)), (50, 1003, 517, (ITEMS, 4, 32)),
+           (50, 5003, 517, (ITEMS, 4, 64)), (60, 12003, 4100, (ITEMS, 2, 64)), (4200, 2051, 380, (ITEMS, 1, 128)),
+           (2500, 2100, 1700, (TILES, 1, 256)), (5003, 3801, 1501, (TILES, 1, 256)), (5003, 2803, 1501, (TILES, 1, 256)),
+           (16000, 1027, 385, (TILES, 1, 256))]
+
+
+@pytest.mark.parametrize("M,N,K,plan", KERNELS)
+def test_linear_kernels(moe, M, N, K, plan):
+    assert linear_plan(moe, M, N, K) == plan
+    xq, xs, wq, ws = operands(M, N, K, M + N + K)
+    y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    moe.linear_i8(K, xq, xs, wq, ws, y)
+    assert torch.equal(y, exact_product(xq, xs, wq, ws, K))
+
+
+# Groups: tiles of up to 64, 256 and 1024 groups with the last tiles of groups
+# in halves and quarters, empty groups and one that has most rows; items.
+GROUP_KERNELS = [(ragged(8, 350, 1), 2000, 1600, (TILES, 1, 256)), ([0, 64, 65, 128, 129, 256, 2800, 0], 1999, 1603, (TILES, 1, 256)),
+                 (ragged(100, 120, 2, 1500), 513, 2100, (TILES, 1, 256)), (ragged(300, 120, 3), 260, 2100, (TILES, 1, 256)),
+                 (ragged(1000, 110, 4), 70, 2052, (TILES, 1, 256)), (ragged(30, 16, 5, 600), 1003, 900, (ITEMS, 1, 128)),
+                 ([5, 0, 70, 3], 3000, 700, (ITEMS, 2, 64)), ([2, 0, 1], 1000, 700, (ITEMS, 4, 8)), ([3, 0, 4, 1], 2500, 500, (ITEMS, 2, 8))]
+
+
+@pytest.mark.parametrize("case", range(len(GROUP_KERNELS)))
+@pytest.mark.parametrize("gather", [False, True])
+def test_grouped_kernels(moe, case, gather):
+    sizes, N, K, plan = GROUP_KERNELS[case]
+    M = sum(sizes)
+    assert linear_plan(moe, M, N, K, len(sizes)) == plan
+    check_grouped(moe, sizes, N, K, case, spare=0, gather=max(1, M // 3) if gather else None)
+
+
+FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=904, E_local=4, n_shared=1, I_shared=520), (TILES, 1, 256), (ITEMS, 1, 128)),
+               (dict(T=3300, H=2104, E=80, k=3, I=136, E_local=70), (TILES, 1, 256), (ITEMS, 1, 128)),
+               (dict(T=7200, H=2104, E=300, k=4, I=136, E_local=300), (TILES, 1, 256), (ITEMS, 1, 128)),
+               (dict(T=3000, H=256, E=4, k=2, I=1536, E_local=4), (ITEMS, 1, 128), (ITEMS, 1, 128)),
+               (dict(T=2000, H=2048, E=4, k=2, I=1544, E_local=4, n_shared=1, I_shared=1600), (TILES, 1, 256), (TILES, 1, 256))]
+
+
+@pytest.mark.parametrize("case", range(len(FFN_KERNELS)))
+def test_ffn_kernels(moe, case):
+    """The layers that tiles and wide items are for, and their bits from one
+    entry point to the other."""
+    conf, up, down = FFN_KERNELS[case]
+    d = moe.dims(S=1, **conf)
+    assert ffn_plan(moe, d) == (up, down)
+    _, q = layer_weights(moe, d, case)
+    w = moe.make_weights_i8(d, q)
+    local = None if d.E_local == d.E else torch.arange(d.E_local, dtype=torch.int32, device="cuda")
+    logits, x = torch.randn((d.T, d.E), generator=gen(case), device="cuda"), randn((d.T, d.H), case)
+    out = moe.MoeLayerI8(d, q, local).forward(logits, None, x)
+    src, counts = torch.zeros(d.T, dtype=torch.int32, device="cuda"), torch.zeros((1, d.E), dtype=torch.int64, device="cuda")
+    assert torch.equal(out, run_steps(moe, d, logits, src, x, local, w, None, counts))
+    # and the experts' rows against 64 bits
+    o = dispatch(moe, d, case)
+    x_perm = randn((d.T * d.k, d.H), case + 50)
+    y = torch.full((d.T * d.k, d.H), 3.0, dtype=torch.bfloat16, device="cuda")
+    ysh = torch.empty((d.T, d.H), dtype=torch.bfloat16, device="cuda") if d.n_shared else None
+    moe.expert_ffn_i8(d, x_perm, torch.tensor(o, dtype=torch.int32, device="cuda"), w, x, y, ysh,
+                      moe.workspace(d, moe.ENTRY_EXPERT_FFN_I8).fill_(0xff))
+    for e in range(0, d.E_local, max(1, d.E_local // 8)):
+        if o[e] < o[e + 1]:
+            ref, bound = ffn_and_bound(x_perm[o[e]:o[e + 1]].double(), deq(q["w_gate"][e], q["s_gate"][e], d.H),
+                                       deq(q["w_up"][e], q["s_up"][e], d.H), deq(q["w_down"][e], q["s_down"][e], d.I))
+            assert ((y[o[e]:o[e + 1]].double() - ref).abs() <= bound).all(), e
+    assert (y[o[-1]:] == 3.0).all()
+    if d.n_shared:
+        ref, bound = ffn_and_bound(x.double(), deq(q["sh_gate"], q["sh_s_gate"], d.H), deq(q["sh_up"], q["sh_s_up"], d.H),
+                                   deq(q["sh_down"], q["sh_s_down"], d.I_shared))
+        assert ((ysh.double() - ref).abs() <= bound).all()

@@ -202,3 +202,41 @@ def test_calls_run_on_the_tensors_device(moe, monkeypatch):
     with pytest.raises(RuntimeError, match="moe_linear_i8"):
         monkeypatch.setattr(moe, "strerror", lambda s: "text")
         moe._call(1, "moe_linear_i8", -3)
+
+
+def linear_plan(moe, M, N, K, G=0):
+    """(kernel, parts of K, rows of a tile or chunk) of a product."""
+    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), (C.c_int64 * 3)()
+    assert moe._lib.moe_test_linear_i8_plan(C.byref(d), int(G > 0), out) == 0
+    return tuple(out)
+
+
+ITEMS, TILES, FEW = 0, 1, 2
+
+
+@pytest.mark.parametrize("M,N,K,G,plan", [
+    (1, 2048, 7168, 0, (ITEMS, 4, 8)), (8, 8192, 512, 0, (ITEMS, 4, 8)), (8, 8193, 512, 0, (ITEMS, 2, 8)),
+    (8, 16385, 512, 0, (ITEMS, 1, 128)), (9, 8192, 512, 0, (ITEMS, 4, 64)), (33, 4096, 512, 0, (ITEMS, 4, 32)),
+    (33, 4097, 512, 0, (ITEMS, 4, 64)), (64, 16384, 512, 0, (ITEMS, 2, 64)), (64, 16385, 512, 0, (ITEMS, 1, 128)),
+    (64, 16385, 4096, 0, (ITEMS, 2, 64)), (64, 32769, 4096, 0, (TILES, 1, 256)),
+    (2560, 2048, 1500, 0, (TILES, 1, 256)), (2560, 1792, 1500, 0, (ITEMS, 1, 128)), (2560, 2048, 1499, 0, (ITEMS, 1, 128)),
+    (4096, 2048, 1499, 0, (TILES, 1, 256)), (16384, 4096, 384, 0, (ITEMS, 1, 128)), (16384, 4096, 385, 0, (TILES, 1, 256)),
+    (8 * 85, 3584, 1500, 8, (TILES, 1, 256)), (8 * 84, 3584, 1500, 8, (ITEMS, 1, 128)), (8 * 85, 3328, 1500, 8, (ITEMS, 1, 128)),
+    (64 * 300, 1024, 2048, 64, (TILES, 1, 256)), (64 * 299, 1024, 2048, 64, (ITEMS, 1, 128)), (64 * 85, 1024, 2049, 64, (TILES, 1, 256)),
+])
+def test_products_take_the_kernel_of_their_sizes(moe, M, N, K, G, plan):
+    assert linear_plan(moe, M, N, K, G) == plan
+
+
+@pytest.mark.parametrize("change,up,down", [
+    (dict(T=1), (FEW, 2, 1), (FEW, 2, 1)), (dict(T=8), (FEW, 1, 8), (FEW, 1, 8)), (dict(T=9), (ITEMS, 1, 128), (ITEMS, 1, 128)),
+    (dict(T=1, I=64), (FEW, 4, 1), (FEW, 2, 1)), (dict(T=1, H=512, I=512), (FEW, 4, 1), (FEW, 4, 1)),
+    # rows past half a CU's LDS are quantised by a launch of their own
+    (dict(T=4, H=7168), (FEW, 2, 4), (FEW, 1, 4)), (dict(T=8, H=8000), (ITEMS, 1, 128), (FEW, 1, 8)),
+    (dict(T=4096, H=2304, E=32, E_local=32, I=1536), (TILES, 1, 256), (TILES, 1, 256)),
+])
+def test_layers_take_the_kernel_of_their_sizes(moe, change, up, down):
+    d = moe.dims(**{**dict(T=1, S=1, H=2048, E=128, k=8, I=768, E_local=128), **change})
+    out = (C.c_int64 * 6)()
+    assert moe._lib.moe_test_ffn_i8_plan(C.byref(d), out) == 0
+    assert (tuple(out[:3]), tuple(out[3:])) == (up, down)
