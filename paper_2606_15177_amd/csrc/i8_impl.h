@@ -27,6 +27,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p) {
 // within the rows that the caller's buffers have.
 __device__ __forceinline__ int row_at(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
 
+// load_lds16 of data that no other workgroup reads: its lines leave the L2
+// first, and what is shared stays.  Only for whole 128-byte lines.
+__device__ __forceinline__ void load_lds16_once(__amdgpu_buffer_rsrc_t rs, unsigned char* lds, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)lds, 16, off, 0, 0, 2);
+}
+
 // A scalar load: its wait leaves the vector-memory counter, and so the tile
 // loads in flight, alone.
 typedef const int __attribute__((address_space(4)))* ConstIntPtr;

@@ -224,6 +224,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   const __amdgpu_buffer_rsrc_t rs_w1 = rsrc(GATED ? p.w1 + (scales + n0) * p.ldw : w0);
   const __amdgpu_buffer_rsrc_t rs_x = rsrc(x_rows ? p.x : p.x + static_cast<long long>(row_base + m0) * p.ldx);
   const int lrow = lane & 31, lhalf = lane >> 5;
+  const bool once = n_chunks == 1;  // this workgroup alone reads its weights
 
   auto body = [&](auto nsub_c, auto wb_c, auto kp_c, auto bk_c, auto depth_c, auto few_c) {
     constexpr int NSUB = decltype(nsub_c)::value;  // 32-row tiles of tokens
@@ -272,23 +273,30 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
       woff[i] = n0 + col < N ? static_cast<uint32_t>(col) * ldw : kPastEnd;
       wpiece[i] = (lane % CPR) ^ ((r / SWZ) % CPR);
     }
-    auto load = [&](__amdgpu_buffer_rsrc_t rs, unsigned char* to, uint32_t off, int k, bool live) {
+    // offset `off` of rows of K at byte k, or past the end
+    auto at_k = [&](uint32_t off, int k, bool live) {
       const uint32_t kill = (live && k < bytes ? 0u : kPastEnd) | (off & kPastEnd);
-      load_lds16(rs, to, (off + static_cast<uint32_t>(k)) | kill);
+      return (off + static_cast<uint32_t>(k)) | kill;
     };
     auto issue_w = [&](int s, int slot) {
       unsigned char* wl = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
       const int k0 = k_at(s);
+      if (KP == 1 && BK == 128 && once) {
 #pragma unroll
-      for (int i = 0; i < WL; ++i)
-        load(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, woff[i], k0 + wpiece[i] * 16, s < nst);
+        for (int i = 0; i < WL; ++i)
+          load_lds16_once(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, at_k(woff[i], k0 + wpiece[i] * 16, s < nst));
+      } else {
+#pragma unroll
+        for (int i = 0; i < WL; ++i)
+          load_lds16(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, at_k(woff[i], k0 + wpiece[i] * 16, s < nst));
+      }
     };
     auto issue_x = [&](int s, int slot) {
       unsigned char* xl = smem + slot * STAGE + wk * XPART;
       const int k0 = k_at(s);
 #pragma unroll
       for (int q = 0; q < XL; ++q)
-        load(rs_x, xl + (FEW ? 0 : RPI * (WN * q + wn) * BK), xoff[q], k0 + xpiece[q] * 16, s < nst);
+        load_lds16(rs_x, xl + (FEW ? 0 : RPI * (WN * q + wn) * BK), at_k(xoff[q], k0 + xpiece[q] * 16, s < nst));
     };
 #pragma unroll 1
     for (int s = 0; s < D - 1; ++s) issue_w(s, s);
