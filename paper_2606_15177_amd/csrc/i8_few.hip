@@ -3,8 +3,8 @@
 // tokens is bound by the latency of its launches and by reading the weights of
 // the experts that it hits; this leaves out two of six launches (us, with the
 // rows quantised by launches of their own and by the products: Qwen3 layer of 1
-// token 32.7 and 26.8, of 4 55.9 and 48.2, of 8 82 and 74; DSV2-Lite of 1 37.0
-// and 30.9; DSV3's 32 local experts of 1 106 and 90, of 4 200 and 190).
+// token 32.7 and 26.0, of 4 55.9 and 45.0, of 8 82 and 65; DSV2-Lite of 1 37.0
+// and 30.0; DSV3's 32 local experts of 1 106 and 82, of 4 200 and 169).
 //
 // A workgroup of four waves takes up to 8 rows of one group times 128 / KP
 // weight rows, K in KP parts.  A wave streams its own 32 weight rows (gated: 16
@@ -15,6 +15,9 @@
 // in LDS over the whole K, rows 32 bytes past a multiple of 256 apart, which
 // spreads the 16 chunks that a fragment reads over the banks.  The MFMA's
 // columns past the rows repeat the last one; no result is taken of them.
+//
+// Weights are read once, but where a group has more rows than expected, and leave
+// the L2 first (Qwen3 of 8 tokens 71.8 us without the hint, 65.1 with it).
 //
 // Two workgroups share a CU.  Rows that leave room for one only lose what the
 // launches cost (8 rows of 7168: 250 us before, 257 here), as does a ring of
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int i = 0; i < kLoads; ++i) {
       const int k = k0 + piece[i] * 16;
       const uint32_t kill = (s < nst && k < bytes ? 0u : kPastEnd) | (woff[i] & kPastEnd);
-      load_lds16(GATED && i >= kLoads / 2 ? rs_w1 : rs_w0, ring + slot * kStage + i * 1024, (woff[i] + static_cast<uint32_t>(k)) | kill);
+      load_lds16_once(GATED && i >= kLoads / 2 ? rs_w1 : rs_w0, ring + slot * kStage + i * 1024, (woff[i] + static_cast<uint32_t>(k)) | kill);
     }
   };
 #pragma unroll 1

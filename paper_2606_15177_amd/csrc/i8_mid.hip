@@ -2,26 +2,42 @@
 // rows per group than fill 256-row tiles.  Bound by reading the weights of the
 // groups that have rows once; groups of many rows add MFMA work.
 //
-// Items.  A workgroup of four waves takes up to 128 token rows of one group (a
-// chunk) times a block of weight rows: 128 of them for groups of up to 64 rows
-// (narrow items), 256 or 128 for larger ones (wide).  Two workgroups share a
-// CU.  A wave owns blocks of 32 weight rows (gated: 16 gate rows and the 16 up
-// rows of the same columns, which meet in one lane of the MFMA's result) and
+// Items.  A workgroup of four waves takes a chunk of the token rows of one group
+// times a block of weight rows.  K undivided: up to 128 token rows, 128 weight
+// rows for groups of up to 64 rows (narrow items), 256 or 128 for larger ones
+// (wide).  A wave owns blocks of 32 weight rows (gated: 16 gate rows and the 16
+// up rows of the same columns, which meet in one lane of the MFMA's result) and
 // all rows of the chunk.  Where a launch has few items, KP = 2 or 4 groups of
-// waves split K, over half or a quarter of the weight rows each, and add their
-// sums through LDS (integers: the order changes nothing).
+// waves split K, over half or a quarter of 128 weight rows each and chunks of 64,
+// 32 or 8 token rows, and add their sums through LDS (integers: the order changes
+// nothing).  At 256 tokens the gate product of Qwen3 reads 201 MB in 43 us (4.7
+// TB/s); 1 x 2048 x 7168 takes 8.2 us, of which a launch of nothing is 2.
 //
-// Pipeline.  buffer_load_dwordx4 ... lds into a ring of K stages in 80 KB of
-// LDS, D - 1 stages ahead, one barrier per stage.  16-byte chunk c of a row
-// sits at a slot rotated by the row, which spreads a fragment's rows over the
-// banks.  Each workgroup starts its walk along K elsewhere, so that rows that
-// lie a power of two apart spread over the memory channels.
+// Pipeline.  buffer_load_dwordx4 ... lds into a ring of K stages, D - 1 stages
+// ahead: 80 KB of LDS and two workgroups per CU, or, with K divided and chunks of
+// more than 8 rows, all 160 KB (the launch has less than one workgroup per CU
+// anyway).  One barrier per stage, none where a wave reads its own loads alone
+// (KP 4).  With K divided the next stage's fragments are read among the MFMAs of
+// one, since then a SIMD has no other wave to run.  Chunks of up to 8 rows hold no
+// more in the ring.  16-byte chunk c of a row sits at a slot rotated by the row,
+// which spreads a fragment's rows over the banks.  Each workgroup starts its walk
+// along K elsewhere, so that rows that lie a power of two apart spread over the
+// memory channels.
 //
 // Order.  Items are numbered per kind (shared, wide, narrow) by group, column
 // block, chunk; an XCD owns a contiguous run of each kind, so that a group's
 // token rows and the weight block that its chunks share stay in one L2.  Within
 // an XCD heavy (shared and wide) and narrow items take turns of eight, a
 // multiple of its shader engines.
+//
+// Caches.  Weights that one workgroup alone reads, in whole 128-byte lines, leave
+// the L2 first: layers of 16 to 256 tokens are 5 to 11 % faster (us, without the
+// hint and with it: Qwen3 of 256 150 and 138, DSV2-Lite of 128 149 and 132, DSV3's
+// 32 local experts of 32 290 and 261).  Not where chunks share weights or a stage
+// takes half a line (DSV2-Lite of 1021, gate/up: 119 and 160), and not in the
+// small launches that divide K, whose weights a program may find in the cache
+// behind the L2 again: 1 x 2048 x 7168 from HBM 9.9 and 9.5, from that cache 8.2
+// and 8.8, 32 x 4096 x 14336 24.1 and 23.8, 15.2 and 23.0.
 #include <algorithm>
 #include <type_traits>
 
@@ -281,7 +297,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     auto issue_w = [&](int s, int slot) {
       unsigned char* wl = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
       const int k0 = k_at(s);
-      if (KP == 1 && BK == 128 && once) {
+      if (KP == 1 && BK == 128 && once) {  // (see Caches above)
 #pragma unroll
         for (int i = 0; i < WL; ++i)
           load_lds16_once(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, at_k(woff[i], k0 + wpiece[i] * 16, s < nst));

@@ -23,6 +23,13 @@ struct QuantPair {
   int blocks_a;
 };
 
+// Vector v of a row that is not read again: its lines leave the caches first
+// (16384 x 7168: 65.3 us without the hint, 62.3 with it, 5.66 TB/s).
+__device__ __forceinline__ u32x4 load_once(const uint16_t* row, int v, int cols) {
+  const int c = v * kVec;
+  return c + kVec <= cols ? __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2*>(row + c)) : load_vec(row, v, cols);
+}
+
 // WPR waves per row, V vectors per lane held in registers (vectors past them
 // are read twice), R rows at a time per wave (WPR 1): short rows need several
 // in flight to cover the memory's latency.
@@ -47,7 +54,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(QuantPair p) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         v[k][i] = u32x4{0u, 0u, 0u, 0u};
-        if (r0 + k < rows && at + i * STEP < nvec) v[k][i] = load_vec(a.x + (r0 + k) * a.ldx, at + i * STEP, a.cols);
+        if (r0 + k < rows && at + i * STEP < nvec) v[k][i] = load_once(a.x + (r0 + k) * a.ldx, at + i * STEP, a.cols);
       }
 #pragma unroll
     for (int k = 0; k < R; ++k) {
