@@ -100,7 +100,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (!shared) {
     const int at = (id - n_shared) / blocks;  // chunk, of all groups
     int before = 0;
-    for (int g0 = 0; g0 < ma.g.groups; g0 += kWave) {
+    bool found = false;
+    for (int g0 = 0; !found && g0 < ma.g.groups; g0 += kWave) {
       int first, own;
       const int n = group_rows(g0 + lane, first);
       const int inc = scan(n, own);
@@ -111,11 +112,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         row_base = __builtin_amdgcn_readlane(first, l);
         m = __builtin_amdgcn_readlane(n, l);
         item = id - n_shared - (before + __builtin_amdgcn_readlane(inc - own, l)) * blocks;
-        break;
+        found = true;
       }
       before += __builtin_amdgcn_readlane(inc, kWave - 1);
     }
+    if (!found) return;  // not reached: the chunk lies within the groups' chunks
   }
+  g = __builtin_amdgcn_readfirstlane(g);
+  row_base = __builtin_amdgcn_readfirstlane(row_base);
+  m = __builtin_amdgcn_readfirstlane(m);
   const GemmI8& p = shared ? ma.sp : ma.g;
   const int n_chunks = ceil_div(m, ma.chunk);
   const int nblk = __builtin_amdgcn_readfirstlane(item / n_chunks);
