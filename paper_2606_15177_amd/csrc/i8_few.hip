@@ -317,9 +317,9 @@ bool few_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool 
 }
 
 // K in parts where the items are few, and further on long K, whose items last
-// (us, one part and two, gate/up: 288 items of K 7168 97.6 and 89.7, 344 of K
-// 4096 82.6 and 80.2, 96 of K 2048 28.1 and 27.0, 384 of K 2048 47.8 and 49.9;
-// down, two and four: 64 of K 11008 72.1 and 67.2).
+// (us of a layer with one part and two, gate/up: 288 items of K 7168 86.4 and
+// 79.4, 344 of K 4096 75.6 and 73.6, 96 of K 2048 29.7 and 27.6, 384 of K 2048
+// 43.2 and 46.5; with two and four, down: 64 of K 11008 65.5 and 60.8).
 Cut few_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   const int cols = gated ? 64 : 128;
   const long long hit = static_cast<long long>(seg.hit_groups) * ceil_div(a.N, cols) + (sh ? ceil_div(sh->N, cols) : 0);
