@@ -30,11 +30,12 @@
 // quarter of the MFMAs, the four waves side by side along the weights.
 //
 // Stages and pipeline.  K advances by 128 bytes.  A stage is an X and a W part
-// [256 rows x 128 bytes]; rings of three X and two W parts take all 160 KB of
-// LDS.  16-byte chunk c of row r sits at slot c ^ ((r / 2) % 8), which spreads a
+// [256 rows x 128 bytes]; rings of two X and three W parts take all 160 KB of
+// LDS (weights come from HBM, rows mostly from the L2: three X and two W parts
+// were up to 5 % slower, 1024 tokens of 16 experts of K 5120 217 us, 206 here).  16-byte chunk c of row r sits at slot c ^ ((r / 2) % 8), which spreads a
 // fragment's rows over the banks.  One barrier per stage, before its last
 // K-step, once the wave's loads of the next stage have landed and its LDS reads
-// are done; past it W of two stages on goes into the slot of this one, and X of
+// are done; past it X of two stages on goes into the slot of this one, and W of
 // three on during the next stage.  Stages run on across tiles.  Within a K-step
 // the next one's fragment reads and the loads are spread over the MFMAs in the
 // order of their use.  The 256 accumulators fill the accumulation registers.
@@ -50,7 +51,7 @@ constexpr int kTile = 256;
 constexpr int kTiledThreads = 4 * kWave;
 constexpr int kRow = 128;                 // bytes of an LDS row: K per stage
 constexpr int kPart = kTile * kRow;       // one operand of a stage: 32 KB
-constexpr int kXSlots = 3, kWSlots = 2;
+constexpr int kXSlots = 2, kWSlots = 3;
 constexpr int kTiledLds = (kXSlots + kWSlots) * kPart;
 constexpr int kLoads = 8;                 // per part and wave: 8 rows each
 constexpr int kSteps = kRow / 32;         // MFMA K-steps of a stage
@@ -274,12 +275,12 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   // (a product has at least four stages here, so the loads, up to three stages
   // ahead, are on the current tile or the next one)
   auto x_advance = [&]() {
-    x_slot = x_slot == (kXSlots - 1) * kPart ? 0 : x_slot + kPart;
+    x_slot ^= kPart;
     if (++x_kb == x_nkb) x_setup(nxt, more);
     else if (x_kb == x_nkb - 1 && x_bytes % kRow != 0) mask_tail(xoff, x_kb, x_bytes);
   };
   auto w_advance = [&]() {
-    w_slot ^= kPart;
+    w_slot = w_slot == (kWSlots - 1) * kPart ? 0 : w_slot + kPart;
     if (++w_kb == w_nkb) w_setup(nxt, more);
     else if (w_kb == w_nkb - 1 && w_bytes % kRow != 0) mask_tail(woff, w_kb, w_bytes);
   };
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     for (int tn = 0; tn < 4; ++tn)
 #pragma unroll
       for (int tm = 0; tm < 4; ++tm) acc[tn][tm] = i32x16{};
-    // Stage j: X of stage j + 2 goes out with its first two K-steps, W of stage
+    // Stage j: W of stage j + 2 goes out with its first two K-steps, X of stage
     // j + 2 with its last one, past the barrier.
     auto tile = [&](auto tn_c, auto tm_c) {
       constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
@@ -455,12 +456,12 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
 #pragma unroll
       for (int q = 0; q < FRAGS; ++q) read_frag(tn_c, tm_c, q, xs, ws, 0, 0);
       for (int kb = 0; kb < nkb; ++kb) {
-        const int xs1 = xs == (kXSlots - 1) * kPart ? 0 : xs + kPart, ws1 = ws ^ kPart;
+        const int xs1 = xs ^ kPart, ws1 = ws == (kWSlots - 1) * kPart ? 0 : ws + kPart;
 #pragma unroll
         for (int ks = 0; ks < kSteps; ++ks) {
           const bool last = ks == kSteps - 1;
           if (last) {
-            x_advance();
+            w_advance();
             __builtin_amdgcn_s_waitcnt(wait_vm(kLoads));  // own loads of stage j + 1 landed
             __builtin_amdgcn_s_waitcnt(kWaitLds);
             phase_barrier();
@@ -470,8 +471,8 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
             if (q < FRAGS) read_frag(tn_c, tm_c, q, nx, nw, nk, set ^ 1);
-            if (last) w_load(q);
-            else if (ks < 2 && q % 2 == 0) x_load(4 * ks + q / 2);
+            if (last) x_load(q);
+            else if (ks < 2 && q % 2 == 0) w_load(4 * ks + q / 2);
 #pragma unroll
             for (int m = q * MFMAS / 8; m < (q + 1) * MFMAS / 8; ++m) {
               const int tm = m / TN, tn = m % TN;
@@ -486,13 +487,13 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        w_advance();
+        x_advance();
         xs = xs1;
         ws = ws1;
       }
-      // The X part of the tile's last stage is free until this wave's next loads
+      // The W part of the tile's last stage is free until this wave's next loads
       // into its own 8 KB of it, with the next tile's first stage.
-      epilogue(tn_c, tm_c, cur, col_w, smem + (xs == 0 ? (kXSlots - 1) * kPart : xs - kPart) + wave * (64 * kRow));
+      epilogue(tn_c, tm_c, cur, col_w, smem + kXSlots * kPart + (ws == 0 ? (kWSlots - 1) * kPart : ws - kPart) + wave * (64 * kRow));
     };
     using Two = std::integral_constant<int, 2>;
     using Four = std::integral_constant<int, 4>;
