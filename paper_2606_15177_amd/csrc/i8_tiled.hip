@@ -31,14 +31,17 @@
 //
 // Stages and pipeline.  K advances by 128 bytes.  A stage is an X and a W part
 // [256 rows x 128 bytes]; rings of two X and three W parts take all 160 KB of
-// LDS (weights come from HBM, rows mostly from the L2: three X and two W parts
-// were up to 5 % slower, 1024 tokens of 16 experts of K 5120 217 us, 206 here).  16-byte chunk c of row r sits at slot c ^ ((r / 2) % 8), which spreads a
-// fragment's rows over the banks.  One barrier per stage, before its last
-// K-step, once the wave's loads of the next stage have landed and its LDS reads
-// are done; past it X of two stages on goes into the slot of this one, and W of
-// three on during the next stage.  Stages run on across tiles.  Within a K-step
-// the next one's fragment reads and the loads are spread over the MFMAs in the
-// order of their use.  The 256 accumulators fill the accumulation registers.
+// LDS.  (Weights come from HBM, rows mostly from the L2: with three X and two W
+// parts 1024 tokens of 16 experts of K 5120 took 217 us, 206 here, DSV3's 32 local
+// experts with 512 tokens 434 and 417.  Telling the L2 that weights are read once,
+// as the items do, gained up to 6 % where every group has one row tile and lost
+// up to 5 % elsewhere.)  16-byte chunk c of row r sits at slot c ^ ((r / 2) % 8),
+// which spreads a fragment's rows over the banks.  One barrier per stage, before
+// its last K-step, once the wave's loads of the next stage have landed and its LDS
+// reads are done; past it X of two stages on goes into the slot of this one, and
+// W of three on during the next stage.  Stages run on across tiles.  Within a
+// K-step the next one's fragment reads and the loads are spread over the MFMAs in
+// the order of their use.  The 256 accumulators fill the accumulation registers.
 #include <algorithm>
 #include <type_traits>
 
