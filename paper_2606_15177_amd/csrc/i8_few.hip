@@ -17,7 +17,8 @@
 // columns past the rows repeat the last one; no result is taken of them.
 //
 // Weights are read once, but where a group has more rows than expected, and leave
-// the L2 first (Qwen3 of 8 tokens 71.8 us without the hint, 65.1 with it).
+// the L2 first where a stage takes whole lines (Qwen3 of 8 tokens 71.8 us without
+// the hint, 65.1 with it; 16 experts of 4104 x 3600, 1 token: 32 and 40).
 //
 // Two workgroups share a CU.  Rows that leave room for one only lose what the
 // launches cost (8 rows of 7168: 250 us before, 257 here), as does a ring of
@@ -52,7 +53,7 @@ constexpr int kHead = 4 * kFewRows * 4 + kFewRows * 4;
 
 __device__ __forceinline__ int run_start(int n, int x) { return static_cast<int>(static_cast<long long>(n) * x / kXcds); }
 
-template <bool GATED, int KP>
+template <bool GATED, int KP, bool ONCE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void few_i8_kernel(FewI8 ma) {
   constexpr int OUT_COLS = (GATED ? 64 : 128) / KP;  // output columns of an item
   constexpr int WN = 4 / KP;                         // waves along the weight rows
@@ -153,7 +154,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int i = 0; i < kLoads; ++i) {
       const int k = k0 + piece[i] * 16;
       const uint32_t kill = (s < nst && k < bytes ? 0u : kPastEnd) | (woff[i] & kPastEnd);
-      load_lds16_once(GATED && i >= kLoads / 2 ? rs_w1 : rs_w0, ring + slot * kStage + i * 1024, (woff[i] + static_cast<uint32_t>(k)) | kill);
+      const uint32_t at = (woff[i] + static_cast<uint32_t>(k)) | kill;
+      if constexpr (ONCE) load_lds16_once(GATED && i >= kLoads / 2 ? rs_w1 : rs_w0, ring + slot * kStage + i * 1024, at);
+      else load_lds16(GATED && i >= kLoads / 2 ? rs_w1 : rs_w0, ring + slot * kStage + i * 1024, at);
     }
   };
 #pragma unroll 1
@@ -284,13 +287,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
 }
 
-template <bool GATED, int KP>
+template <bool GATED, int KP, bool ONCE>
 hipError_t launch_few_kp(int blocks, int lds, const FewI8& ma, hipStream_t st) {
   static unsigned long long lds_set = 0;  // devices with the LDS limit raised
-  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&few_i8_kernel<GATED, KP>), kMaxLds, &lds_set);
+  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&few_i8_kernel<GATED, KP, ONCE>), kMaxLds, &lds_set);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((few_i8_kernel<GATED, KP>), dim3(blocks), dim3(kThreads), lds, st, ma);
+  hipLaunchKernelGGL((few_i8_kernel<GATED, KP, ONCE>), dim3(blocks), dim3(kThreads), lds, st, ma);
   return hipGetLastError();
+}
+
+template <bool ONCE>
+hipError_t launch_few_once(bool gated, int parts, int blocks, int lds, const FewI8& ma, hipStream_t st) {
+  if (parts == 4) return gated ? launch_few_kp<true, 4, ONCE>(blocks, lds, ma, st) : launch_few_kp<false, 4, ONCE>(blocks, lds, ma, st);
+  if (parts == 2) return gated ? launch_few_kp<true, 2, ONCE>(blocks, lds, ma, st) : launch_few_kp<false, 2, ONCE>(blocks, lds, ma, st);
+  return gated ? launch_few_kp<true, 1, ONCE>(blocks, lds, ma, st) : launch_few_kp<false, 1, ONCE>(blocks, lds, ma, st);
 }
 
 // Rows of an item: no more than any group is expected to have.
@@ -332,9 +342,8 @@ hipError_t launch_few_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh,
   const int blocks = static_cast<int>((parts * few_items(seg, a, sh, gated) / kXcds + 1) * kXcds);
   const int lds = few_lds(seg, a, sh);
   const FewI8 ma{a, sh ? *sh : GemmI8{}, seg.total_rows, c.rows};
-  if (parts == 4) return gated ? launch_few_kp<true, 4>(blocks, lds, ma, st) : launch_few_kp<false, 4>(blocks, lds, ma, st);
-  if (parts == 2) return gated ? launch_few_kp<true, 2>(blocks, lds, ma, st) : launch_few_kp<false, 2>(blocks, lds, ma, st);
-  return gated ? launch_few_kp<true, 1>(blocks, lds, ma, st) : launch_few_kp<false, 1>(blocks, lds, ma, st);
+  const bool once = whole_lines(a.w0, a.ldw) && whole_lines(a.w1, 0) && (!sh || (whole_lines(sh->w0, sh->ldw) && whole_lines(sh->w1, 0)));
+  return once ? launch_few_once<true>(gated, parts, blocks, lds, ma, st) : launch_few_once<false>(gated, parts, blocks, lds, ma, st);
 }
 
 }  // namespace moe

@@ -28,7 +28,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p) {
 __device__ __forceinline__ int row_at(const int32_t* offsets, int g, int rows) { return min(max(offsets[g], 0), rows); }
 
 // load_lds16 of data that no other workgroup reads: its lines leave the L2
-// first, and what is shared stays.  Only for whole 128-byte lines.
+// first, and what is shared stays.  Only for whole lines: of a line that two
+// loads share the second fetches it again.
+constexpr int kLine = 128;
+__host__ __device__ __forceinline__ bool whole_lines(const int8_t* rows, long long stride) {
+  return ((reinterpret_cast<uintptr_t>(rows) | static_cast<uintptr_t>(stride)) & (kLine - 1)) == 0;
+}
 __device__ __forceinline__ void load_lds16_once(__amdgpu_buffer_rsrc_t rs, unsigned char* lds, uint32_t off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)lds, 16, off, 0, 0, 2);
 }

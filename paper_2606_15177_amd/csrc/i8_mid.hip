@@ -34,10 +34,11 @@
 // the L2 first: layers of 16 to 256 tokens are 5 to 11 % faster (us, without the
 // hint and with it: Qwen3 of 256 150 and 138, DSV2-Lite of 128 149 and 132, DSV3's
 // 32 local experts of 32 290 and 261).  Not where chunks share weights or a stage
-// takes half a line (DSV2-Lite of 1021, gate/up: 119 and 160), and not in the
-// small launches that divide K, whose weights a program may find in the cache
-// behind the L2 again: 1 x 2048 x 7168 from HBM 9.9 and 9.5, from that cache 8.2
-// and 8.8, 32 x 4096 x 14336 24.1 and 23.8, 15.2 and 23.0.
+// takes half a line (DSV2-Lite of 1021, gate/up: 119 and 160) or parts of two (16
+// experts of 4104 x 3600, 16 tokens: 155 and 176), and not in the small launches
+// that divide K, whose weights a program may find in the cache behind the L2 again:
+// 1 x 2048 x 7168 from HBM 9.9 and 9.5, from that cache 8.2 and 8.8, 32 x 4096 x
+// 14336 24.1 and 23.8, 15.2 and 23.0.
 #include <algorithm>
 #include <type_traits>
 
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   const __amdgpu_buffer_rsrc_t rs_w1 = rsrc(GATED ? p.w1 + (scales + n0) * p.ldw : w0);
   const __amdgpu_buffer_rsrc_t rs_x = rsrc(x_rows ? p.x : p.x + static_cast<long long>(row_base + m0) * p.ldx);
   const int lrow = lane & 31, lhalf = lane >> 5;
-  const bool once = n_chunks == 1;  // this workgroup alone reads its weights
+  const bool once = n_chunks == 1 && whole_lines(p.w0, p.ldw);  // this workgroup alone reads its weights
 
   auto body = [&](auto nsub_c, auto wb_c, auto kp_c, auto bk_c, auto depth_c, auto few_c) {
     constexpr int NSUB = decltype(nsub_c)::value;  // 32-row tiles of tokens
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     auto issue_w = [&](int s, int slot) {
       unsigned char* wl = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
       const int k0 = k_at(s);
-      if (KP == 1 && BK == 128 && once) {  // (see Caches above)
+      if (KP == 1 && BK == kLine && once) {  // (see Caches above)
 #pragma unroll
         for (int i = 0; i < WL; ++i)
           load_lds16_once(GATED && ((RPI * i) & 16) ? rs_w1 : rs_w0, wl + i * 1024, at_k(woff[i], k0 + wpiece[i] * 16, s < nst));
