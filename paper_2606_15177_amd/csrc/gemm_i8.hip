@@ -6,23 +6,24 @@
 namespace moe {
 namespace {
 
-// 256-row tiles want rows that fill them and tiles for a good part of the CUs;
-// fewer on short K, where an item's turnaround is short too.  Over 400 random
-// layers (65 to 8192 tokens, even to Zipf 1 routing, K 392 to 14336) these lines
-// choose the faster kernel within 8 % for all but 31 of 760 grouped products
-// (1.29 at worst, 0.7 % on average), and over 297 random products of static rows
-// for all but 5 (1.38, 0.4 %).  Both sides, us (items, tiles):
-//   rows: Qwen3 of 3000 tokens (a mean of 187, 128 groups) gate/up 143 and 136,
-//     1500 tokens 115 and 123; DSV2-Lite of 3000 (281) 210 and 187, of 1500 126
-//     and 132; 8 experts of K 14336, N 4096 at a mean of 84 110 and 148;
-//   many groups of short K, whose last tiles are mostly padding: Qwen3 gate/up
-//     at a mean of 358, Zipf 1, 241 and 281, at 312, Zipf 0.6, 203 and 170;
-//   few tiles, grouped: 150 of K 896 17 and 23, 85 of K 2960 53 and 47; static:
-//     84 of K 5033 72 and 60, 117 of K 1142 18 and 25, 264 of K 796 29 and 34.
-constexpr int kMeanRows = 85, kMeanMany = 300;
+// 256-row tiles want rows that fill them and tiles for half of the CUs; more on
+// short K, where an item's turnaround is short too.  Over 800 random layers (65 to
+// 8192 tokens, even to Zipf 1 routing, K 392 to 14336) these lines choose the
+// faster kernel within 8 % for all but 75 of 1600 grouped products (1.39 at worst,
+// 0.9 % on average), and over 297 random products of static rows for all but 5
+// (1.38, 0.4 %).  Both sides, us (items, tiles):
+//   rows: 8 experts of K 4096, N 14336 at a mean of 67 178 and 186, of 81 225 and
+//     196; K 3128, N 904, 34 groups of 80 54 and 40;
+//   many groups of short K, whose last tiles are mostly padding: Qwen3 gate/up at a
+//     mean of 193 147 and 163, of 252 172 and 206; DSV2-Lite's at 281 216 and 247,
+//     at 308 235 and 235, its down at 381 168 and 152;
+//   few tiles, grouped: 116 of K 2936 26 and 39, 126 of K 2408 37 and 29; short K:
+//     384 of K 712 28 and 38, 435 of K 1296 86 and 81; static: 84 of K 5033 72 and
+//     60, 117 of K 1142 18 and 25, 264 of K 796 29 and 34.
+constexpr int kMeanRows = 75, kMeanMany = 300;
 constexpr int kMany = 64, kManyK = 2048;
 constexpr int kShortK = 1500;
-constexpr long long kFewTiles = 110, kFewShort = 300, kFewStatic = 80, kFewStaticShort = 128;
+constexpr long long kFewTiles = 128, kFewShort = 400, kFewStatic = 80, kFewStaticShort = 128;
 
 bool takes_tiles(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   if (a.K <= kTiledMinK || (sh && sh->K <= kTiledMinK)) return false;

@@ -597,7 +597,7 @@ def test_grouped_kernels(moe, case, gather):
     check_grouped(moe, sizes, N, K, case, spare=0, gather=max(1, M // 3) if gather else None)
 
 
-FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=904, E_local=4, n_shared=1, I_shared=520), (TILES, 1, 256), (ITEMS, 1, 128)),
+FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_shared=520), (TILES, 1, 256), (ITEMS, 1, 128)),
                (dict(T=3300, H=2104, E=80, k=3, I=136, E_local=70), (TILES, 1, 256), (ITEMS, 1, 128)),
                (dict(T=7200, H=2104, E=300, k=4, I=136, E_local=300), (TILES, 1, 256), (ITEMS, 1, 128)),
                (dict(T=3000, H=256, E=4, k=2, I=1536, E_local=4), (ITEMS, 1, 128), (ITEMS, 1, 128)),

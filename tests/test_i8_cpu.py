@@ -221,8 +221,9 @@ ITEMS, TILES, FEW = 0, 1, 2
     (64, 16385, 4096, 0, (ITEMS, 2, 64)), (64, 32769, 4096, 0, (TILES, 1, 256)),
     (2560, 2048, 1500, 0, (TILES, 1, 256)), (2560, 1792, 1500, 0, (ITEMS, 1, 128)), (2560, 2048, 1499, 0, (ITEMS, 1, 128)),
     (4096, 2048, 1499, 0, (TILES, 1, 256)), (16384, 4096, 384, 0, (ITEMS, 1, 128)), (16384, 4096, 385, 0, (TILES, 1, 256)),
-    (8 * 85, 3584, 1500, 8, (TILES, 1, 256)), (8 * 84, 3584, 1500, 8, (ITEMS, 1, 128)), (8 * 85, 3328, 1500, 8, (ITEMS, 1, 128)),
-    (64 * 300, 1024, 2048, 64, (TILES, 1, 256)), (64 * 299, 1024, 2048, 64, (ITEMS, 1, 128)), (64 * 85, 1024, 2049, 64, (TILES, 1, 256)),
+    (8 * 75, 4096, 1500, 8, (TILES, 1, 256)), (8 * 74, 4096, 1500, 8, (ITEMS, 1, 128)), (8 * 75, 3840, 1500, 8, (ITEMS, 1, 128)),
+    (8 * 300, 6400, 1499, 8, (TILES, 1, 256)), (8 * 300, 6144, 1499, 8, (ITEMS, 1, 128)),
+    (64 * 300, 1024, 2048, 64, (TILES, 1, 256)), (64 * 299, 1024, 2048, 64, (ITEMS, 1, 128)), (64 * 75, 1024, 2049, 64, (TILES, 1, 256)),
 ])
 def test_products_take_the_kernel_of_their_sizes(moe, M, N, K, G, plan):
     assert linear_plan(moe, M, N, K, G) == plan
