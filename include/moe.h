@@ -373,7 +373,7 @@ int moe_quantize_rows(int32_t rows, int32_t cols, const moe_bf16 *x, int64_t ldx
  *             offsets[G] are left as they were).
  *   N, K      output channels and inner dimension.
  *   G         groups (experts) of moe_grouped_linear_i8, 1..1024.
- *   X         rows of xq where they are read through x_rows.
+ *   X         rows of xq where they are read through x_rows, at least 1.
  *   ldx, ldw  row strides of xq and wq in bytes: multiples of 16, at least K
  *             rounded up to 16, at most 2^21.
  *   ldy       row stride of y in values, at least N.

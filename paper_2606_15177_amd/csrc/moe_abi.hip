@@ -410,7 +410,8 @@ moe::Segments linear_segments(const moe_linear_dims* d, const int32_t* offsets, 
 int linear_ok(const moe_linear_dims* d, bool grouped, bool gathered, const void* xq, const void* x_scale,
               const void* wq, const void* w_scale, const void* y) {
   if (d == nullptr) return MOE_ERR_NULL;
-  if (d->M < 0 || d->N < 1 || d->K < 1 || (grouped && d->G < 1) || (gathered && d->X < 0)) return MOE_ERR_DIMS;
+  if (d->M < 0 || d->N < 1 || d->K < 1 || (grouped && d->G < 1) || (gathered && d->X < (d->M > 0 ? 1 : 0)))
+    return MOE_ERR_DIMS;
   if (d->ldx < pad16(d->K) || d->ldw < pad16(d->K) || d->ldy < d->N) return MOE_ERR_DIMS;
   if (d->K > kMaxI8K || d->N > (1 << 24) || d->ldx > kMaxI8Stride || d->ldw > kMaxI8Stride || d->ldy > kMaxI8Stride)
     return MOE_ERR_UNSUPPORTED;

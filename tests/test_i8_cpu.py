@@ -241,3 +241,12 @@ def test_layers_take_the_kernel_of_their_sizes(moe, change, up, down):
     out = (C.c_int64 * 6)()
     assert moe._lib.moe_test_ffn_i8_plan(C.byref(d), out) == 0
     assert (tuple(out[:3]), tuple(out[3:])) == (up, down)
+
+
+@pytest.mark.parametrize("change,code", [(dict(X=0), -2), (dict(X=-1), -2), (dict(X=0, M=0), 0), (dict(X=1, M=0), 0)])
+def test_grouped_linear_needs_a_row_to_gather(moe, change, code):
+    """x_rows' entries outside [0, X) are rows of zeros, but some row has to be there."""
+    d = moe.MoeLinearDims(**{**LIN, **change})
+    assert moe._lib.moe_grouped_linear_i8(C.byref(d), 16, 16, 16, 16, 16, 16, 16, None) == code
+    if code == 0:
+        assert moe._lib.moe_grouped_linear_i8(C.byref(d), None, None, 16, 16, None, None, None, None) == 0
