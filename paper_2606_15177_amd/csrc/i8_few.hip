@@ -333,7 +333,7 @@ bool few_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool 
 Cut few_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   const int cols = gated ? 64 : 128;
   const long long hit = static_cast<long long>(seg.hit_groups) * ceil_div(a.N, cols) + (sh ? ceil_div(sh->N, cols) : 0);
-  return {hit <= 64 ? 4 : hit <= 128 || (hit <= 512 && a.K >= 4096) ? 2 : 1, chunk_rows(seg, sh)};
+  return {hit <= 64 ? 4 : hit <= 128 || (hit <= 512 && a.K >= 4096) ? 2 : 1, chunk_rows(seg, sh), false};
 }
 
 hipError_t launch_few_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {

@@ -62,6 +62,7 @@ hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* s
 // How a launch of items cuts its products: K in `parts`, chunks of `rows` rows.
 struct Cut {
   int parts, rows;
+  bool half;  // 16 weight rows per wave, not 32
 };
 Cut items_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 // Bf16 rows (xb), few of them per group (any number is computed): each

@@ -49,6 +49,7 @@ namespace {
 
 constexpr int kChunk = 128;         // token rows of a chunk of a wide item
 constexpr int kSplitChunk = 64;     // ... of any item where K is split (32 where there are very few)
+constexpr int kFewHalf = 32;        // items (of 128 weight rows) up to which they are halved once more, K in 4 parts
 constexpr int kBriefChunk = 8;      // ... where no group has more rows
 constexpr int kWideRows = 64;       // groups of more rows take wide items
 constexpr int kItemRows = 128;      // weight rows of a narrow item
@@ -85,10 +86,10 @@ __device__ __forceinline__ void wait_stage(int j) {
   }
 }
 
-template <bool GATED, int KP, int CHUNK>
+template <bool GATED, int KP, int CHUNK, bool HALF>
 __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void items_i8_kernel(ItemsI8 ma) {
   constexpr int FULL_COLS = GATED ? kItemRows / 2 : kItemRows;  // output columns of 128 weight rows
-  constexpr int OUT_COLS = FULL_COLS / KP;                      // ... of a narrow item
+  constexpr int OUT_COLS = FULL_COLS / KP / (HALF ? 2 : 1);     // ... of a narrow item
   constexpr int WIDE_ROWS = KP > 1 ? 0x7fffffff : kWideRows;    // groups of more rows take wide items
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = lane_id();
@@ -256,9 +257,10 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     constexpr bool FEW = decltype(few_c)::value;   // up to 8 rows: the ring holds no more
     constexpr int XR = FEW ? 8 : NSUB * 32;        // token rows of a stage
     constexpr int XPART = XR * BK;                 // ... of one K part
-    constexpr int STAGE = NK * XPART + 4 * WB * 32 * BK;
+    constexpr int WR = HALF ? 16 : 32;             // weight rows of a block
+    constexpr int STAGE = NK * XPART + 4 * WB * WR * BK;
     constexpr int XL = FEW ? 1 : XR / RPI / WN;    // token loads per wave and stage
-    constexpr int WL = WB * 32 / RPI;              // weight loads per wave and stage
+    constexpr int WL = WB * WR / RPI;              // weight loads per wave and stage
     constexpr int LOADS = XL + WL;
     constexpr int KS = BK / 32;                    // MFMA K-steps per stage
     static_assert(D * STAGE <= item_lds(KP, CHUNK), "the ring fits");
@@ -285,8 +287,8 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
       const int r = RPI * i + lr;
-      const int b = WB * wn + r / 32;  // 32-row block of weights
-      const int col = GATED ? 16 * b + (r & 15) : 32 * b + r % 32;
+      const int b = WB * wn + r / WR;  // block of weights
+      const int col = GATED ? 16 * b + (r & 15) : WR * b + r % WR;
       woff[i] = n0 + col < N ? static_cast<uint32_t>(col) * ldw : kPastEnd;
       wpiece[i] = (lane % CPR) ^ ((r / SWZ) % CPR);
     }
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
       return (off + static_cast<uint32_t>(k)) | kill;
     };
     auto issue_w = [&](int s, int slot) {
-      unsigned char* wl = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
+      unsigned char* wl = smem + slot * STAGE + NK * XPART + wave * (WB * WR * BK);
       const int k0 = k_at(s);
       if (KP == 1 && BK == kLine && once) {  // (see Caches above)
 #pragma unroll
@@ -329,7 +331,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     // Scales: lane l holds that of weight row l of the wave's WB * 32, and
     // those of the token rows of its results.
     const int wr = lane % (WB * 32);
-    const int wcol = n0 + (GATED ? 16 * (WB * wn + wr / 32) + (wr & 15) : 32 * WB * wn + wr);
+    const int wcol = n0 + (GATED ? 16 * (WB * wn + wr / 32) + (wr & 15) : WR * WB * wn + wr);
     const float cs = (GATED && (wr & 16) ? p.ws1 : p.ws0)[scales + min(wcol, N - 1)];
     float rsc[NSUB];
     bool in_x[NSUB];  // (else a row of zeros, whatever scale was read)
@@ -350,14 +352,14 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     auto read_frags = [&](int slot, auto set_c) {
       constexpr int SET = decltype(set_c)::value;
       const unsigned char* xp = smem + slot * STAGE + wk * XPART;
-      const unsigned char* wp = smem + slot * STAGE + NK * XPART + wave * (WB * 32 * BK);
+      const unsigned char* wp = smem + slot * STAGE + NK * XPART + wave * (WB * WR * BK);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const int at = ((2 * ks + lhalf) ^ ((lrow / SWZ) % CPR)) << 4;
+        const int at = ((2 * ks + lhalf) ^ ((lrow % WR / SWZ) % CPR)) << 4;
         const int xrow = FEW ? lrow % 8 : lrow;  // (few rows: columns past them are not results)
         const int xat = ((2 * ks + lhalf) ^ ((xrow / SWZ) % CPR)) << 4;
 #pragma unroll
-        for (int b = 0; b < WB; ++b) wf[SET][ks][b] = *reinterpret_cast<const i32x4*>(wp + (32 * b + lrow) * BK + at);
+        for (int b = 0; b < WB; ++b) wf[SET][ks][b] = *reinterpret_cast<const i32x4*>(wp + (WR * b + lrow % WR) * BK + at);
 #pragma unroll
         for (int s = 0; s < NSUB; ++s) xf[SET][ks][s] = *reinterpret_cast<const i32x4*>(xp + (32 * s + xrow) * BK + xat);
       }
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
       for (int s = 0; s < NSUB; ++s) {
         const int r = 32 * s + lrow;
 #pragma unroll
-        for (int h = 0; h < (GATED ? 1 : 2); ++h) {  // 16 columns each
+        for (int h = 0; h < (GATED || HALF ? 1 : 2); ++h) {  // 16 columns each
           uint32_t pk[2][2];
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
@@ -476,7 +478,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
           // lower lanes take columns 0..7, upper lanes 8..15
           const auto a0 = __builtin_amdgcn_permlane32_swap(pk[0][0], pk[1][0], false, false);
           const auto a1 = __builtin_amdgcn_permlane32_swap(pk[0][1], pk[1][1], false, false);
-          const int col = n0 + (GATED ? 16 * (WB * wn + b) : 32 * (WB * wn + b) + 16 * h) + 8 * lhalf;
+          const int col = n0 + (GATED ? 16 * (WB * wn + b) : WR * (WB * wn + b) + 16 * h) + 8 * lhalf;
           if (r < rows && col < N) store_cols(out + r * p.ldo + col, u32x4{a0[0], a1[0], a0[1], a1[1]}, col, N);
         }
       }
@@ -498,7 +500,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     else if (rows > 32) body(C2{}, C1{}, C1{}, K128{}, C3{}, whole);
     else body(C1{}, C1{}, C1{}, K128{}, C4{}, whole);
   } else if constexpr (CHUNK == kBriefChunk) {
-    body(C1{}, C1{}, integral_constant<int, KP>{}, K128{}, C4{}, few);
+    body(C1{}, C1{}, integral_constant<int, KP>{}, K128{}, integral_constant<int, HALF ? 6 : 4>{}, few);
   } else if constexpr (KP == 2) {
     if (rows > 32) body(C2{}, C1{}, C2{}, K128{}, C5{}, whole);
     else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, integral_constant<int, 6>{}, whole);
@@ -510,13 +512,13 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   }
 }
 
-template <bool GATED, int KP, int CHUNK>
+template <bool GATED, int KP, int CHUNK, bool HALF = false>
 hipError_t launch_kp(long long blocks, const ItemsI8& ma, hipStream_t st) {
   constexpr int lds = item_lds(KP, CHUNK);
   static unsigned long long lds_set = 0;  // devices with the LDS limit raised
-  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_i8_kernel<GATED, KP, CHUNK>), lds, &lds_set);
+  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_i8_kernel<GATED, KP, CHUNK, HALF>), lds, &lds_set);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((items_i8_kernel<GATED, KP, CHUNK>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), lds, st, ma);
+  hipLaunchKernelGGL((items_i8_kernel<GATED, KP, CHUNK, HALF>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), lds, st, ma);
   return hipGetLastError();
 }
 
@@ -534,16 +536,17 @@ Cut items_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated
   const long long items =
       (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +
       (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
-  Cut c{1, kChunk};
+  Cut c{1, kChunk, false};
   if (items <= 64) c.parts = 4;
   else if (items <= 128 || (items <= 256 && a.K >= 4096)) c.parts = 2;
   if (c.parts > 1) c.rows = seg.max_rows <= kBriefChunk ? kBriefChunk : items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
+  c.half = !gated && c.parts == 4 && c.rows == kBriefChunk && items <= kFewHalf;
   return c;
 }
 
 long long items_blocks(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   const Cut c = items_cut(seg, a, sh, gated);
-  const int cols = (gated ? kItemRows / 2 : kItemRows) / c.parts;
+  const int cols = (gated ? kItemRows / 2 : kItemRows) / c.parts / (c.half ? 2 : 1);
   // at most one partly filled chunk per group; wide items need fewer column blocks
   const long long chunks = a.offsets ? seg.total_rows / c.rows + std::min(seg.groups, seg.total_rows) : ceil_div(a.static_rows, c.rows);
   long long items = chunks * ceil_div(a.N, cols);
@@ -556,6 +559,8 @@ static hipError_t launch_cut(const Cut& c, long long blocks, const ItemsI8& ma, 
   if (c.parts == 1) return launch_kp<GATED, 1, kChunk>(blocks, ma, st);
   if (c.parts == 2)
     return c.rows == kBriefChunk ? launch_kp<GATED, 2, kBriefChunk>(blocks, ma, st) : launch_kp<GATED, 2, kSplitChunk>(blocks, ma, st);
+  if constexpr (!GATED)
+    if (c.half) return launch_kp<false, 4, kBriefChunk, true>(blocks, ma, st);
   if (c.rows == kBriefChunk) return launch_kp<GATED, 4, kBriefChunk>(blocks, ma, st);
   return c.rows == 32 ? launch_kp<GATED, 4, 32>(blocks, ma, st) : launch_kp<GATED, 4, kSplitChunk>(blocks, ma, st);
 }
