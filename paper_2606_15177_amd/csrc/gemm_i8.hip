@@ -52,9 +52,9 @@ bool gemm_i8_quantizes(const Segments& seg, const GemmI8& a, const GemmI8* sh, b
 }
 
 GemmI8Plan plan_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
-  if (!a.xb && takes_tiles(seg, a, sh, gated)) return {1, 1, 256};
+  if (!a.xb && takes_tiles(seg, a, sh, gated)) return {1, 1, 256, 0};
   const Cut c = a.xb ? few_cut(seg, a, sh, gated) : items_cut(seg, a, sh, gated);
-  return {a.xb ? 2 : 0, c.parts, c.rows};
+  return {a.xb ? 2 : 0, c.parts, c.rows, c.half};
 }
 
 }  // namespace moe

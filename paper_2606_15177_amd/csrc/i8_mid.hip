@@ -8,21 +8,20 @@
 // (wide).  A wave owns blocks of 32 weight rows (gated: 16 gate rows and the 16
 // up rows of the same columns, which meet in one lane of the MFMA's result) and
 // all rows of the chunk.  Where a launch has few items, KP = 2 or 4 groups of
-// waves split K, over half or a quarter of 128 weight rows each and chunks of 64,
-// 32 or 8 token rows, and add their sums through LDS (integers: the order changes
-// nothing).  At 256 tokens the gate product of Qwen3 reads 201 MB in 43 us (4.7
-// TB/s); 1 x 2048 x 7168 takes 8.2 us, of which a launch of nothing is 2.
+// waves split K, over a half, a quarter or (KP 4, HALF) an eighth of 128 weight
+// rows each and chunks of 64, 32 or 8 token rows, and add their sums through LDS
+// (integers: the order changes nothing).  At 256 tokens the gate product of Qwen3
+// reads 201 MB in 43 us (4.7 TB/s); 1 x 2048 x 7168 takes 7.1 us with its weights
+// in the cache behind the L2, of which a launch of nothing is 2.
 //
 // Pipeline.  buffer_load_dwordx4 ... lds into a ring of K stages, D - 1 stages
-// ahead: 80 KB of LDS and two workgroups per CU, or, with K divided and chunks of
-// more than 8 rows, all 160 KB (the launch has less than one workgroup per CU
-// anyway).  One barrier per stage, none where a wave reads its own loads alone
-// (KP 4).  With K divided the next stage's fragments are read among the MFMAs of
-// one, since then a SIMD has no other wave to run.  Chunks of up to 8 rows hold no
-// more in the ring.  16-byte chunk c of a row sits at a slot rotated by the row,
-// which spreads a fragment's rows over the banks.  Each workgroup starts its walk
-// along K elsewhere, so that rows that lie a power of two apart spread over the
-// memory channels.
+// ahead (its size: item_lds).  One barrier per stage, none where a wave reads its
+// own loads alone (KP 4).  With K divided the next stage's fragments are read among
+// the MFMAs of one, since then a SIMD has no other wave to run.  Chunks of up to 8
+// rows hold no more in the ring.  16-byte chunk c of a row sits at a slot rotated
+// by the row, which spreads a fragment's rows over the banks.  Each workgroup
+// starts its walk along K elsewhere, so that rows that lie a power of two apart
+// spread over the memory channels.
 //
 // Order.  Items are numbered per kind (shared, wide, narrow) by group, column
 // block, chunk; an XCD owns a contiguous run of each kind, so that a group's
@@ -49,19 +48,24 @@ namespace {
 
 constexpr int kChunk = 128;         // token rows of a chunk of a wide item
 constexpr int kSplitChunk = 64;     // ... of any item where K is split (32 where there are very few)
-constexpr int kFewHalf = 32;        // items (of 128 weight rows) up to which they are halved once more, K in 4 parts
+constexpr int kFewHalf = 32;        // items (of 32 token rows) up to which they are halved once more, K in 4 parts
 constexpr int kBriefChunk = 8;      // ... where no group has more rows
 constexpr int kWideRows = 64;       // groups of more rows take wide items
 constexpr int kItemRows = 128;      // weight rows of a narrow item
 constexpr int kFewWide = 128;       // fewer wide items than this take 128 weight rows: half the CUs' worth
 constexpr int kOneWide = 256;       // ... or fewer than this, one per CU, in a launch of fewer items than
 constexpr int kSlots = 512;         // workgroups fit the chip
-constexpr int kItemLds = 80 * 1024;   // two workgroups per CU
-constexpr int kDeepLds = 160 * 1024;  // one
 constexpr int kTurn = 8;
 constexpr int kItemThreads = 4 * kWave;
 
-constexpr int item_lds(int parts, int chunk) { return parts > 1 && chunk > kBriefChunk ? kDeepLds : kItemLds; }
+// LDS of a workgroup, and so workgroups per CU: two, or one where K is divided
+// over chunks of more than 8 rows (the launch has hardly more than one per CU).
+// More than the ring is worth keeps the next launch waiting: 80 KB and rings of
+// four stages against 160 KB and seven, 1 x 2048 x 7168 8.2 and 9.5 us; 96 against
+// 160, 256 x 1024 x 1024 5.1 and 5.4; 128 against 160, 777 x 1003 x 528 6.2 and 6.5.
+constexpr int item_lds(int parts, int chunk) {
+  return 1024 * (parts == 1 || chunk == kBriefChunk ? 80 : chunk == 32 ? 96 : parts == 2 ? 128 : 160);
+}
 
 struct ItemsI8 {
   GemmI8 g;   // groups with device offsets (groups 0: none)
@@ -423,7 +427,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     }
     __builtin_amdgcn_s_waitcnt(wait_vm(0));  // the loads past the last stage: nothing may still write the LDS
     if constexpr (NK > 1) {
-      static_assert((NK - 1) * WN * WB * NSUB * 16 * kWave * 4 <= kItemLds, "the partial sums fit the LDS");
+      static_assert((NK - 1) * WN * WB * NSUB * 16 * kWave * 4 <= item_lds(KP, CHUNK), "the partial sums fit the LDS");
       int* red = reinterpret_cast<int*>(smem);
       __syncthreads();  // every wave is past its last stage
       if (wk > 0) {
@@ -502,13 +506,15 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   } else if constexpr (CHUNK == kBriefChunk) {
     body(C1{}, C1{}, integral_constant<int, KP>{}, K128{}, integral_constant<int, HALF ? 6 : 4>{}, few);
   } else if constexpr (KP == 2) {
-    if (rows > 32) body(C2{}, C1{}, C2{}, K128{}, C5{}, whole);
-    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, integral_constant<int, 6>{}, whole);
+    if (rows > 32) body(C2{}, C1{}, C2{}, K128{}, C4{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, C5{}, whole);
     else body(C1{}, C1{}, C2{}, K128{}, C4{}, few);
   } else {
-    if (CHUNK > 32 && rows > 32) body(C2{}, C1{}, C4{}, K128{}, C3{}, whole);
-    else if (rows > 8) body(C1{}, C1{}, C4{}, K128{}, C5{}, whole);
-    else body(C1{}, C1{}, C4{}, K128{}, C4{}, few);
+    if constexpr (CHUNK > 32) {
+      if (rows > 32) return body(C2{}, C1{}, C4{}, K128{}, C3{}, whole);
+    }
+    if (rows > 8) body(C1{}, C1{}, C4{}, K128{}, integral_constant<int, HALF ? 4 : CHUNK == 32 ? 3 : 5>{}, whole);
+    else body(C1{}, C1{}, C4{}, K128{}, integral_constant<int, HALF ? 6 : 4>{}, few);
   }
 }
 
@@ -530,17 +536,27 @@ hipError_t launch_kp(long long blocks, const ItemsI8& ma, hipStream_t st) {
 // rows): 64 items, 64 x 8192 x 4096 19.9, 14.8, 12.7; 112, 64 x 14336 x 4096
 // 22.8, 17.2, 23.8; 189, 396 x 3391 x 12416 78, 55, 67; 256 of short K, 1000 x
 // 2048 x 768 10.6, 12.8, 22.4; 392, 849 x 3534 x 4367 35, 52, 71.
+//
+// In 4 parts and still at most half a chip of workgroups, a wave takes 16 weight
+// rows instead of 32: half of an MFMA's rows go unused, twice as many CUs read.
+// Weights from HBM, us, 32 rows and 16: 1 x 2048 x 7168 9.9 and 8.2, 16 x 4096 x
+// 14336 22.4 and 17.0, 128 x 1024 x 4096 8.8 and 7.4; with more workgroups than CUs
+// (1 x 5120 x 4096) 8.7 and 9.1.
 Cut items_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
   const int cols = gated ? kItemRows / 2 : kItemRows;
-  auto chunks = [](int rows) { return std::max(1, ceil_div(rows, kSplitChunk)); };
-  const long long items =
-      (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +
-      (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
+  // items of 128 weight rows and so many token rows
+  auto count = [&](int rows) {
+    auto chunks = [&](int n) { return std::max(1, ceil_div(n, rows)); };
+    return (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +
+           (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
+  };
+  const long long items = count(kSplitChunk);
   Cut c{1, kChunk, false};
   if (items <= 64) c.parts = 4;
   else if (items <= 128 || (items <= 256 && a.K >= 4096)) c.parts = 2;
   if (c.parts > 1) c.rows = seg.max_rows <= kBriefChunk ? kBriefChunk : items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
-  c.half = !gated && c.parts == 4 && c.rows == kBriefChunk && items <= kFewHalf;
+  c.half = !gated && c.parts == 4 && count(32) <= kFewHalf;
+  if (c.half && c.rows > 32) c.rows = 32;
   return c;
 }
 
@@ -560,7 +576,9 @@ static hipError_t launch_cut(const Cut& c, long long blocks, const ItemsI8& ma, 
   if (c.parts == 2)
     return c.rows == kBriefChunk ? launch_kp<GATED, 2, kBriefChunk>(blocks, ma, st) : launch_kp<GATED, 2, kSplitChunk>(blocks, ma, st);
   if constexpr (!GATED)
-    if (c.half) return launch_kp<false, 4, kBriefChunk, true>(blocks, ma, st);
+    if (c.half) {
+      return c.rows == kBriefChunk ? launch_kp<false, 4, kBriefChunk, true>(blocks, ma, st) : launch_kp<false, 4, 32, true>(blocks, ma, st);
+    }
   if (c.rows == kBriefChunk) return launch_kp<GATED, 4, kBriefChunk>(blocks, ma, st);
   return c.rows == 32 ? launch_kp<GATED, 4, 32>(blocks, ma, st) : launch_kp<GATED, 4, kSplitChunk>(blocks, ma, st);
 }

@@ -197,9 +197,10 @@ bool gemm_i8_supported(const Segments& seg, const GemmI8& a, const GemmI8* sh, b
 // a launch that quantises them.
 bool gemm_i8_quantizes(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 // Host only: how a launch runs.  The kernel (0 items, 1 tiles, 2 items that
-// quantise their rows), the parts of K, the rows of a tile or a chunk.
+// quantise their rows), the parts of K, the rows of a tile or a chunk, and
+// whether a wave takes 16 weight rows instead of 32.
 struct GemmI8Plan {
-  int kernel, parts, rows;
+  int kernel, parts, rows, half;
 };
 GemmI8Plan plan_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 

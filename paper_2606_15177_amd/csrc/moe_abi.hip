@@ -779,9 +779,9 @@ int moe_test_ffn_plan(const moe_dims* d, int rows_indexed, int64_t out[2][7]) {
 }
 
 // For the tests: how the 8-bit products run (moe::GemmI8Plan: kernel, parts,
-// rows), of moe_linear_i8 or moe_grouped_linear_i8, and of
+// rows, half), of moe_linear_i8 or moe_grouped_linear_i8, and of
 // moe_forward_i8's or moe_expert_ffn_i8's gate/up and down.
-int moe_test_linear_i8_plan(const moe_linear_dims* d, int grouped, int64_t out[3]) {
+int moe_test_linear_i8_plan(const moe_linear_dims* d, int grouped, int64_t out[4]) {
   static const int32_t some = 0;  // stands for device offsets
   if (d == nullptr || d->M < 1 || d->N < 1 || d->K < 1 || (grouped && d->G < 1)) return MOE_ERR_DIMS;
   const moe::Segments seg = linear_segments(d, grouped ? &some : nullptr, grouped != 0);
@@ -791,12 +791,12 @@ int moe_test_linear_i8_plan(const moe_linear_dims* d, int grouped, int64_t out[3
   a.groups = seg.groups;
   a.K = d->K, a.N = d->N;
   const moe::GemmI8Plan p = moe::plan_gemm_i8(seg, a, nullptr, false);
-  const int64_t v[3] = {p.kernel, p.parts, p.rows};
-  std::copy(v, v + 3, out);
+  const int64_t v[4] = {p.kernel, p.parts, p.rows, p.half};
+  std::copy(v, v + 4, out);
   return MOE_OK;
 }
 
-int moe_test_ffn_i8_plan(const moe_dims* d, int64_t out[2][3]) {
+int moe_test_ffn_i8_plan(const moe_dims* d, int64_t out[2][4]) {
   const int s = check_dims(d);
   if (s != MOE_OK) return s;
   if (d->T == 0 || check_ffn_i8_limits(d, false) != MOE_OK) return MOE_ERR_UNSUPPORTED;
@@ -810,8 +810,8 @@ int moe_test_ffn_i8_plan(const moe_dims* d, int64_t out[2][3]) {
   const moe::GemmI8Plan g[2] = {moe::plan_gemm_i8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true),
                                 moe::plan_gemm_i8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false)};
   for (int i = 0; i < 2; ++i) {
-    const int64_t v[3] = {g[i].kernel, g[i].parts, g[i].rows};
-    std::copy(v, v + 3, out[i]);
+    const int64_t v[4] = {g[i].kernel, g[i].parts, g[i].rows, g[i].half};
+    std::copy(v, v + 4, out[i]);
   }
   return MOE_OK;
 }

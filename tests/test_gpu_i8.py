@@ -546,26 +546,30 @@ def test_few_tokens_in_any_groups(moe, sizes):
 # ------------------------------------------ shapes that reach each kernel ----
 
 
-ITEMS, TILES, FEW_ROWS = 0, 1, 2
+ITEMS, TILES, HALF = 0, 1, "half"
 
 
 def linear_plan(moe, M, N, K, G=0):
-    """(kernel, parts of K, rows of a tile or chunk)."""
-    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), (C.c_int64 * 3)()
+    """(kernel, parts of K, rows of a tile or chunk), and HALF where a wave
+    takes 16 weight rows."""
+    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), (C.c_int64 * 4)()
     assert moe._lib.moe_test_linear_i8_plan(C.byref(d), int(G > 0), out) == 0
-    return tuple(out)
+    return tuple(out[:3]) + ((HALF,) if out[3] else ())
 
 
 def ffn_plan(moe, d):
-    out = (C.c_int64 * 6)()
+    out = (C.c_int64 * 8)()
     assert moe._lib.moe_test_ffn_i8_plan(C.byref(d), out) == 0
-    return tuple(out[:3]), tuple(out[3:])
+    return tuple(out[:3]), tuple(out[4:7])
 
 
-# Items: few rows with K in 2 and 4 parts, chunks of 64 and 32; undivided, with
+# Items: few rows with K in 2 and 4 parts, chunks of 64 and 32, a wave with 32
+# and 16 weight rows; undivided, with
 # 256 weight rows per item.  Tiles: 90 (their only round in 2 parts per tile),
 # 300 (44 past a round of 256: 4 parts), 220 (whole), K a byte past the items'.
-KERNELS = [(7, 9001, 130, (ITEMS, 2, 8)), (8, 517, 1003, (ITEMS, 4, 8)), (50, 1003, 517, (ITEMS, 4, 32)),
+KERNELS = [(7, 9001, 130, (ITEMS, 2, 8)), (8, 517, 1003, (ITEMS, 4, 8, HALF)), (50, 1003, 517, (ITEMS, 4, 32, HALF)),
+           (7, 5001, 1003, (ITEMS, 4, 8)), (50, 4001, 517, (ITEMS, 4, 32)), (30, 1999, 1700, (ITEMS, 4, 32, HALF)),
+           (260, 300, 3001, (ITEMS, 4, 32, HALF)),
            (50, 5003, 517, (ITEMS, 4, 64)), (60, 12003, 4100, (ITEMS, 2, 64)), (4200, 2051, 380, (ITEMS, 1, 128)),
            (2500, 2100, 1700, (TILES, 1, 256)), (5003, 3801, 1501, (TILES, 1, 256)), (5003, 2803, 1501, (TILES, 1, 256)),
            (16000, 1027, 385, (TILES, 1, 256))]
@@ -585,7 +589,8 @@ def test_linear_kernels(moe, M, N, K, plan):
 GROUP_KERNELS = [(ragged(8, 350, 1), 2000, 1600, (TILES, 1, 256)), ([0, 64, 65, 128, 129, 256, 2800, 0], 1999, 1603, (TILES, 1, 256)),
                  (ragged(100, 120, 2, 1500), 513, 2100, (TILES, 1, 256)), (ragged(300, 120, 3), 260, 2100, (TILES, 1, 256)),
                  (ragged(1000, 110, 4), 70, 2052, (TILES, 1, 256)), (ragged(30, 16, 5, 600), 1003, 900, (ITEMS, 1, 128)),
-                 ([5, 0, 70, 3], 3000, 700, (ITEMS, 2, 64)), ([2, 0, 1], 1000, 700, (ITEMS, 4, 8)), ([3, 0, 4, 1], 2500, 500, (ITEMS, 2, 8))]
+                 ([5, 0, 70, 3], 3000, 700, (ITEMS, 2, 64)), ([2, 0, 1], 1000, 700, (ITEMS, 4, 8, HALF)), ([2, 30, 0, 9], 600, 900, (ITEMS, 4, 32, HALF)),
+                 ([2, 70, 0, 9, 33, 32, 8], 100, 900, (ITEMS, 4, 32, HALF)), ([3, 0, 4, 1], 2500, 500, (ITEMS, 2, 8))]
 
 
 @pytest.mark.parametrize("case", range(len(GROUP_KERNELS)))

@@ -205,17 +205,20 @@ def test_calls_run_on_the_tensors_device(moe, monkeypatch):
 
 
 def linear_plan(moe, M, N, K, G=0):
-    """(kernel, parts of K, rows of a tile or chunk) of a product."""
-    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), (C.c_int64 * 3)()
+    """(kernel, parts of K, rows of a tile or chunk) of a product, and HALF
+    where a wave takes 16 weight rows."""
+    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), (C.c_int64 * 4)()
     assert moe._lib.moe_test_linear_i8_plan(C.byref(d), int(G > 0), out) == 0
-    return tuple(out)
+    return tuple(out[:3]) + ((HALF,) if out[3] else ())
 
 
-ITEMS, TILES, FEW = 0, 1, 2
+ITEMS, TILES, FEW, HALF = 0, 1, 2, "half"
 
 
 @pytest.mark.parametrize("M,N,K,G,plan", [
-    (1, 2048, 7168, 0, (ITEMS, 4, 8)), (8, 8192, 512, 0, (ITEMS, 4, 8)), (8, 8193, 512, 0, (ITEMS, 2, 8)),
+    (1, 2048, 7168, 0, (ITEMS, 4, 8, HALF)), (8, 4096, 512, 0, (ITEMS, 4, 8, HALF)), (8, 4097, 512, 0, (ITEMS, 4, 8)),
+    (32, 4096, 512, 0, (ITEMS, 4, 32, HALF)), (32, 4097, 512, 0, (ITEMS, 4, 64)), (64, 2048, 512, 0, (ITEMS, 4, 32, HALF)),
+    (64, 2049, 512, 0, (ITEMS, 4, 32)), (3, 128, 512, 8, (ITEMS, 4, 8, HALF)), (8, 8192, 512, 0, (ITEMS, 4, 8)), (8, 8193, 512, 0, (ITEMS, 2, 8)),
     (8, 16385, 512, 0, (ITEMS, 1, 128)), (9, 8192, 512, 0, (ITEMS, 4, 64)), (33, 4096, 512, 0, (ITEMS, 4, 32)),
     (33, 4097, 512, 0, (ITEMS, 4, 64)), (64, 16384, 512, 0, (ITEMS, 2, 64)), (64, 16385, 512, 0, (ITEMS, 1, 128)),
     (64, 16385, 4096, 0, (ITEMS, 2, 64)), (64, 32769, 4096, 0, (TILES, 1, 256)),
@@ -238,9 +241,9 @@ def test_products_take_the_kernel_of_their_sizes(moe, M, N, K, G, plan):
 ])
 def test_layers_take_the_kernel_of_their_sizes(moe, change, up, down):
     d = moe.dims(**{**dict(T=1, S=1, H=2048, E=128, k=8, I=768, E_local=128), **change})
-    out = (C.c_int64 * 6)()
+    out = (C.c_int64 * 8)()
     assert moe._lib.moe_test_ffn_i8_plan(C.byref(d), out) == 0
-    assert (tuple(out[:3]), tuple(out[3:])) == (up, down)
+    assert (tuple(out[:3]), tuple(out[4:7])) == (up, down) and not (out[3] or out[7])
 
 
 @pytest.mark.parametrize("change,code", [(dict(X=0), -2), (dict(X=-1), -2), (dict(X=0, M=0), 0), (dict(X=1, M=0), 0)])
