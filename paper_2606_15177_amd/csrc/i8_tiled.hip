@@ -9,8 +9,8 @@
 // each, read eight 1 KB fragments per 16 MFMAs (eight waves of 64 x 128 read
 // twelve and issued four times the scalar instructions: dense 16384 x 4096 x
 // 7168 in 510 us where these take 466, in one sustained run).  Measured beside
-// the library's int8 product, in turn: 389 and 387 us there (2.47 POP/s), 434
-// and 433 us for 8192 x 8192 x 8192.
+// the library's int8 product, in turn: 378 us there and 371 (2.59 POP/s), 425 and
+// 418 for 8192 x 8192 x 8192, 241 and 220 for 16384 x 7168 x 2048.
 //
 // Tiles.  256 token rows x 256 weight rows of one group.  Gated products take
 // 128 gate and the 128 up rows of the same columns, so that both sums of an
