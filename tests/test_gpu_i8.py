@@ -640,3 +640,68 @@ def test_ffn_kernels(moe, case):
         ref, bound = ffn_and_bound(x.double(), deq(q["sh_gate"], q["sh_s_gate"], d.H), deq(q["sh_up"], q["sh_s_up"], d.H),
                                    deq(q["sh_down"], q["sh_s_down"], d.I_shared))
         assert ((ysh.double() - ref).abs() <= bound).all()
+
+
+# --------------------------------------------- far offsets, calls at once ----
+
+
+@pytest.mark.parametrize("K,kernel", [(32, ITEMS), (400, TILES)])
+def test_linear_past_32_bit_offsets(moe, K, kernel):
+    """More than 2^31 results: 4 GB of them, rows of the first, a middle and the last tile."""
+    M, N = 66003, 33001
+    assert linear_plan(moe, M, N, K)[0] == kernel
+    g = gen(K)
+    xq = torch.randint(-127, 128, (M, pad16(K)), generator=g, device="cuda", dtype=torch.int8)
+    wq = torch.randint(-127, 128, (N, pad16(K)), generator=g, device="cuda", dtype=torch.int8)
+    xs, ws = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+    y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    moe.linear_i8(K, xq, xs, wq, ws, y)
+    for r in (slice(0, 3), slice(32767, 32770), slice(M - 3, M)):
+        assert torch.equal(y[r], exact_product(xq[r], xs[r], wq, ws, K))
+
+
+@pytest.mark.parametrize("rows,plan", [(1, ITEMS), (90, TILES)])
+def test_grouped_past_32_bit_offsets(moe, rows, plan):
+    """2.6 GB of weights; the first, a middle and the last group."""
+    G, N, K = 320, 1000, 8200
+    M = G * rows
+    assert linear_plan(moe, M, N, K, G)[0] == plan
+    g = gen(rows)
+    xq = torch.randint(-127, 128, (M, pad16(K)), generator=g, device="cuda", dtype=torch.int8)
+    wq = torch.randint(-127, 128, (G, N, pad16(K)), generator=g, device="cuda", dtype=torch.int8)
+    xq[:, K:], wq[:, :, K:] = 0, 0  # rows go on with zeros
+    xs, ws = torch.rand(M, generator=g, device="cuda"), torch.rand((G, N), generator=g, device="cuda")
+    y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    offsets = torch.arange(0, M + 1, rows, dtype=torch.int32, device="cuda")
+    moe.grouped_linear_i8(K, xq, xs, offsets, wq, ws, y)
+    for e in (0, 261, 262, G - 1):
+        r = slice(e * rows, e * rows + rows)
+        assert torch.equal(y[r], exact_product(xq[r], xs[r], wq[e], ws[e], K)), e
+
+
+def test_quantize_past_32_bit_offsets(moe):
+    rows, cols = 70001, 16400
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(5))
+    q, scale = moe.quantize_rows(x)
+    for r in (slice(0, 2), slice(65484, 65487), slice(rows - 2, rows)):
+        ref, ref_s = quantized_exactly(x[r])
+        assert np.array_equal(q[r].cpu().numpy(), ref) and np.array_equal(scale[r].cpu().numpy(), ref_s)
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_two_streams_at_once(moe, T):
+    """One layer on two streams, each with a workspace of its own."""
+    d = moe.dims(T=T, S=1, H=1024, E=16, k=2, I=520, E_local=16, n_shared=1, I_shared=264)
+    _, q = layer_weights(moe, d, 2)
+    layer = moe.MoeLayerI8(d, q)
+    data = [(torch.randn((T, 16), generator=gen(s), device="cuda"), randn((T, 1024), s)) for s in range(2)]
+    ref = [layer.forward(lg, None, x) for lg, x in data]
+    streams, ws = [torch.cuda.Stream() for _ in range(2)], [moe.workspace(d, moe.ENTRY_FORWARD_I8) for _ in range(2)]
+    out = [[torch.empty_like(ref[0]) for _ in range(20)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s in range(2):
+            layer.forward(data[s][0], None, data[s][1], out=out[s][i], stream=streams[s], ws=ws[s])
+    torch.cuda.synchronize()
+    for s in range(2):
+        assert all(torch.equal(o, ref[s]) for o in out[s])
