@@ -378,8 +378,9 @@ int moe_quantize_rows(int32_t rows, int32_t cols, const moe_bf16 *x, int64_t ldx
  *             rounded up to 16, at most 2^21.
  *   ldy       row stride of y in values, at least N.
  * Limits (MOE_ERR_UNSUPPORTED beyond them): K < 2^17 (the int32 sums are then
- * exact for any int8 values), N <= 2^24, ldy <= 2^21 and, with x_rows,
- * X*ldx < 2^31.
+ * exact for any int8 values), ldy (and so N) <= 2^21, M <= 2^31 - 256 and, with
+ * x_rows, X*ldx < 2^31.  A product of short rows may need more workgroups than
+ * a launch holds before M gets there, and is refused the same way.
  */
 typedef struct moe_linear_dims {
     int32_t M, N, K, G, X;
@@ -439,7 +440,7 @@ typedef struct moe_weights_i8 {
  * Arguments as moe_expert_ffn's, x_perm and x in bf16; rows of y_perm past
  * offsets[E_local] are left as they were.
  *   ws  MOE_ENTRY_EXPERT_FFN_I8 workspace.
- * Limits as there, and H, I, n_shared*I_shared < 2^17.
+ * Limits as there, and H, I, n_shared*I_shared < 2^17, T*k <= 2^31 - 256.
  */
 int moe_expert_ffn_i8(const moe_dims *dims, const moe_bf16 *x_perm, const int32_t *offsets,
                       const moe_weights_i8 *weights, const moe_bf16 *x, moe_bf16 *y_perm,

@@ -262,6 +262,7 @@ int64_t pad16(int64_t n) { return (n + 15) / 16 * 16; }
 constexpr int64_t kMaxI8K = (1 << 17) - 1;  // inner dimension: sums of int8 products stay within int32
 constexpr int64_t kMaxI8Stride = 1 << 21;   // 512 rows of a tile stay within 32-bit offsets
 constexpr int64_t kSpan = kIntMax;          // gathered rows: 32-bit offsets
+constexpr int64_t kMaxI8Rows = kIntMax - 255;  // a last tile or chunk, up to 256 rows, ends within int32
 
 // Workspace of the int8 expert FFN: quantised inputs (x_rows_cap rows for the
 // routed experts, T for the shared ones unless they read the same rows),
@@ -330,6 +331,7 @@ FfnI8Plan plan_ffn_i8(const moe_dims* d, const FfnI8Ws& fw, const int32_t* x_row
 
 int check_ffn_i8_limits(const moe_dims* d, bool one_x) {
   if (d->H > kMaxI8K || d->I > kMaxI8K || sh_width(d) > kMaxI8K) return MOE_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(d->T) * d->k > kMaxI8Rows) return MOE_ERR_UNSUPPORTED;
   if (one_x && static_cast<int64_t>(d->T) * pad16(d->H) > kSpan) return MOE_ERR_UNSUPPORTED;
   static const int32_t some = 0;  // stands for device offsets
   const FfnI8Plan p = plan_ffn_i8(d, FfnI8Ws{}, nullptr, &some, moe_weights_i8{}, nullptr, nullptr);
@@ -413,7 +415,7 @@ int linear_ok(const moe_linear_dims* d, bool grouped, bool gathered, const void*
   if (d->M < 0 || d->N < 1 || d->K < 1 || (grouped && d->G < 1) || (gathered && d->X < (d->M > 0 ? 1 : 0)))
     return MOE_ERR_DIMS;
   if (d->ldx < pad16(d->K) || d->ldw < pad16(d->K) || d->ldy < d->N) return MOE_ERR_DIMS;
-  if (d->K > kMaxI8K || d->N > (1 << 24) || d->ldx > kMaxI8Stride || d->ldw > kMaxI8Stride || d->ldy > kMaxI8Stride)
+  if (d->M > kMaxI8Rows || d->K > kMaxI8K || d->ldx > kMaxI8Stride || d->ldw > kMaxI8Stride || d->ldy > kMaxI8Stride)
     return MOE_ERR_UNSUPPORTED;
   if (grouped && d->G > moe::kMaxExperts) return MOE_ERR_UNSUPPORTED;
   if (gathered && d->X * d->ldx > kSpan) return MOE_ERR_UNSUPPORTED;

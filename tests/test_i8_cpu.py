@@ -253,3 +253,18 @@ def test_grouped_linear_needs_a_row_to_gather(moe, change, code):
     assert moe._lib.moe_grouped_linear_i8(C.byref(d), 16, 16, 16, 16, 16, 16, 16, None) == code
     if code == 0:
         assert moe._lib.moe_grouped_linear_i8(C.byref(d), None, None, 16, 16, None, None, None, None) == 0
+
+
+@pytest.mark.parametrize("M", [2 ** 31 - 255, 2 ** 31 - 127, 2 ** 31 - 1])
+def test_rows_at_the_end_of_32_bits(moe, M):
+    """A last tile or chunk of rows would end past int32: refused as a size, not as a failed launch."""
+    for change in (dict(), dict(K=400, ldx=400, ldw=400), dict(N=1, ldy=1, K=1, ldx=16, ldw=16)):
+        d = moe.MoeLinearDims(**{**LIN, "M": M, **change})
+        assert moe._lib.moe_linear_i8(C.byref(d), 16, 16, 16, 16, 16, None) == moe.MOE_ERR_UNSUPPORTED
+        for x_rows in (None, 16):
+            assert moe._lib.moe_grouped_linear_i8(C.byref(d), 16, 16, x_rows, 16, 16, 16, 16, None) == moe.MOE_ERR_UNSUPPORTED
+    for k in (1, 8):
+        d = moe.dims(T=-(-M // k), H=8, E=8, k=k, I=8, S=1, E_local=8, n_shared=1, I_shared=8)
+        for entry in (moe.ENTRY_EXPERT_FFN_I8, moe.ENTRY_FORWARD_I8):
+            assert moe.validate(d, entry, 1 << 62) == moe.MOE_ERR_UNSUPPORTED
+            assert moe.workspace_bytes(d, entry) == 0
