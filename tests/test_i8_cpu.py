@@ -268,3 +268,20 @@ def test_rows_at_the_end_of_32_bits(moe, M):
         for entry in (moe.ENTRY_EXPERT_FFN_I8, moe.ENTRY_FORWARD_I8):
             assert moe.validate(d, entry, 1 << 62) == moe.MOE_ERR_UNSUPPORTED
             assert moe.workspace_bytes(d, entry) == 0
+
+
+def test_binding_refuses_sizes_past_32_bits(moe):
+    """Sizes that the C structs cannot hold are refused, not cut to their low 32 bits."""
+    def rows(n, cols, dtype=torch.int8):   # (of one row's memory)
+        return torch.zeros((1, cols), dtype=dtype).expand(n, cols)
+    many = 2 ** 32 + 4
+    q, y, s = rows(4, 48), rows(4, 8, torch.bfloat16), torch.zeros(8)
+    w, x_rows = torch.zeros((2, 8, 48), dtype=torch.int8), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: moe.quantize_rows(rows(many, 40, torch.bfloat16)),
+                 lambda: moe.linear_i8(40, rows(many, 48), s, rows(8, 48), s, rows(many, 8, torch.bfloat16)),
+                 lambda: moe.grouped_linear_i8(40, rows(many, 48), s, s, w, s, rows(many, 8, torch.bfloat16)),
+                 lambda: moe.grouped_linear_i8(40, rows(many, 48), s, s, w, s, y, x_rows=x_rows),
+                 lambda: moe.grouped_linear_i8(40, q, s, s, torch.zeros((1, 1, 48), dtype=torch.int8).expand(many, 8, 48), s, y)):
+        with pytest.raises(moe.MoeError, match="limits") as e:
+            call()
+        assert e.value.status == moe.MOE_ERR_UNSUPPORTED
