@@ -339,6 +339,11 @@ def _vec(t, dtypes, n: int, what: str):
     return _ptr(t, dtypes)
 
 
+def _opt(t, dtypes, n: int, what: str):
+    """_vec of a tensor that may be left out."""
+    return None if t is None else _vec(t, dtypes, n, what)
+
+
 def quantize_rows(x, q=None, scale=None, stream=None):
     """moe_quantize_rows: int8 rows and their fp32 scales of x, bf16 [rows,
     cols] (rows contiguous, any row stride).  q is int8 [rows, cols rounded up
@@ -436,11 +441,12 @@ def _bytes(ws) -> int:
 
 def expert_ffn_i8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=None):
     """moe_expert_ffn_i8; weights as make_weights_i8 returns them."""
-    n = d.T * d.k * d.H
+    n, n_shared = d.T * d.k * d.H, d.T * d.H if d.n_shared else 0
     dev, st = _on_device(stream, x_perm, offsets, x, y_perm, y_shared, ws)
     _need(dev == weights.device_index, "weights live on another device")
     _call(dev, "moe_expert_ffn_i8", C.byref(d), _vec(x_perm, _BF16, n, "x_perm"), _vec(offsets, _I32, d.E_local + 1, "offsets"),
-          C.byref(weights), _ptr(x, _BF16), _vec(y_perm, _BF16, n, "y_perm"), _ptr(y_shared, _BF16), _ptr(ws), _bytes(ws), st)
+          C.byref(weights), _opt(x, _BF16, n_shared, "x"), _vec(y_perm, _BF16, n, "y_perm"),
+          _opt(y_shared, _BF16, n_shared, "y_shared"), _ptr(ws), _bytes(ws), st)
 
 
 def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=None, stream=None, gating=None):
@@ -448,8 +454,10 @@ def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=
     n = d.T * d.H
     dev, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws)
     _need(dev == weights.device_index, "weights live on another device")
-    _call(dev, "moe_forward_i8", C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"), _ptr(src, _I32),
-          _vec(x, _BF16, n, "x"), _ptr(local_experts, _I32), C.byref(weights), _ptr(counts, _I64), _vec(out, _BF16, n, "out"),
+    _call(dev, "moe_forward_i8", C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"),
+          _opt(src, _I32, 0 if counts is None else d.T, "src"), _vec(x, _BF16, n, "x"),
+          _opt(local_experts, _I32, d.E_local, "local_experts"), C.byref(weights), _opt(counts, _I64, d.S * d.E, "counts"),
+          _vec(out, _BF16, n, "out"),
           None if taps is None else C.byref(taps), _ptr(ws), _bytes(ws), st)
 
 

@@ -285,3 +285,73 @@ def test_binding_refuses_sizes_past_32_bits(moe):
         with pytest.raises(moe.MoeError, match="limits") as e:
             call()
         assert e.value.status == moe.MOE_ERR_UNSUPPORTED
+
+
+@pytest.fixture
+def recorded(moe, monkeypatch):
+    """The binding's calls on host tensors: the library's arguments are recorded, nothing is launched."""
+    calls = []
+    monkeypatch.setattr(moe, "_on_device", lambda stream, *t: (0, 0))
+    monkeypatch.setattr(moe, "_ptr", lambda t, dtypes=None: None if t is None else t.data_ptr())
+    monkeypatch.setattr(moe, "_call", lambda dev, where, *args: calls.append((where, args)))
+    return calls
+
+
+def _host_layer(moe, T, n_shared):
+    """Dims, every tensor argument of the two layer entries at exactly its size, and int8 weights."""
+    d = moe.dims(T=T, H=40, E=8, k=2, I=24, S=3, E_local=5, n_shared=n_shared, I_shared=16)
+    bf = dict(dtype=torch.bfloat16)
+    t = dict(x_perm=torch.zeros((T * 2, 40), **bf), offsets=torch.zeros(6, dtype=torch.int32), x=torch.zeros((T, 40), **bf),
+             y_perm=torch.zeros((T * 2, 40), **bf), y_shared=torch.zeros((T, 40), **bf), logits=torch.zeros((T, 8)),
+             src=torch.zeros(T, dtype=torch.int32), local_experts=torch.zeros(5, dtype=torch.int32),
+             counts=torch.zeros((3, 8), dtype=torch.int64), out=torch.zeros((T, 40), **bf))
+    return d, t
+
+
+def _host_weights(moe, EL=5, H=40, I=24, width=0):
+    p = lambda n: (n + 15) // 16 * 16   # noqa: E731
+    q, s = dict(dtype=torch.int8), dict(dtype=torch.float32)
+    w = dict(w_gate=torch.zeros((EL, I, p(H)), **q), w_up=torch.zeros((EL, I, p(H)), **q), w_down=torch.zeros((EL, H, p(I)), **q),
+             s_gate=torch.zeros((EL, I), **s), s_up=torch.zeros((EL, I), **s), s_down=torch.zeros((EL, H), **s))
+    if width:
+        w.update(sh_gate=torch.zeros((width, p(H)), **q), sh_up=torch.zeros((width, p(H)), **q), sh_down=torch.zeros((H, p(width)), **q),
+                 sh_s_gate=torch.zeros(width, **s), sh_s_up=torch.zeros(width, **s), sh_s_down=torch.zeros(H, **s))
+    return w
+
+
+FFN_ARGS = ("x_perm", "offsets", "x", "y_perm", "y_shared")
+FORWARD_ARGS = ("logits", "src", "x", "local_experts", "counts", "out")
+
+
+def _ffn_call(moe, d, t, weights):
+    moe.expert_ffn_i8(d, t["x_perm"], t["offsets"], weights, t["x"], t["y_perm"], t["y_shared"], None)
+
+
+def _forward_call(moe, d, t, weights):
+    moe.forward_i8(d, t["logits"], t["src"], t["x"], t["local_experts"], weights, t["counts"], t["out"], None)
+
+
+@pytest.mark.parametrize("T", [1, 7])
+@pytest.mark.parametrize("call,names", [(_ffn_call, FFN_ARGS), (_forward_call, FORWARD_ARGS)])
+def test_layer_binding_refuses_short_tensors(moe, recorded, T, call, names):
+    """Every tensor that the library reads or writes is as long as it will be read or written."""
+    d, t = _host_layer(moe, T, 1)
+    w = moe.make_weights_i8(d, _host_weights(moe, width=16))
+    call(moe, d, t, w)
+    assert len(recorded) == 1
+    for name in names:
+        short = {**t, name: t[name].flatten()[:-1]}
+        with pytest.raises(ValueError, match=name):
+            call(moe, d, short, w)
+    assert len(recorded) == 1
+    # left out: the library decides
+    for name in ("x", "y_shared", "src", "local_experts", "counts"):
+        if name in names and not (name == "x" and call is _forward_call):
+            call(moe, d, {**t, name: None}, w)
+    # not looked at by the library: no size to keep to
+    d, t = _host_layer(moe, T, 0)
+    w = moe.make_weights_i8(d, _host_weights(moe))
+    if call is _ffn_call:
+        call(moe, d, {**t, "x": t["x"][:0], "y_shared": t["y_shared"][:0]}, w)
+    else:
+        call(moe, d, {**t, "counts": None, "src": t["src"][:0]}, w)
