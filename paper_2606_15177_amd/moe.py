@@ -53,6 +53,8 @@ class MoeLinearDims(C.Structure):
 class MoeWeightsI8(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w_gate", "w_up", "w_down", "s_gate", "s_up", "s_down", "sh_gate", "sh_up",
                                           "sh_down", "sh_s_gate", "sh_s_up", "sh_s_down")]
+    # of a handle that make_weights_i8 made: its device, and its experts, H, I and shared width
+    device_index = sizes = None
 
 
 class MoePlaceDims(C.Structure):
@@ -432,7 +434,19 @@ def make_weights_i8(d: MoeDims, w: dict) -> MoeWeightsI8:
     h = MoeWeightsI8(**{n: _vec(w.get(n), t, size, n) for n, (t, size) in need.items()})
     h.tensors = {n: w[n] for n in need}
     h.device_index = _on_device(None, *h.tensors.values())[0]
+    h.sizes = (EL, H, I, width)
     return h
+
+
+def _weights_i8(d: MoeDims, w: MoeWeightsI8, dev: int) -> MoeWeightsI8:
+    """The handle, refused where it was made for another device or other sizes
+    (more experts, or shared ones that d does not have, are none)."""
+    if w.sizes is not None:
+        _need(w.device_index == dev, "weights live on another device")
+        EL, H, I, width = w.sizes
+        _need(EL >= d.E_local and H == d.H and I == d.I and (not d.n_shared or width == d.n_shared * d.I_shared),
+              "weights were made for other sizes")
+    return w
 
 
 def _bytes(ws) -> int:
@@ -443,7 +457,7 @@ def expert_ffn_i8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=N
     """moe_expert_ffn_i8; weights as make_weights_i8 returns them."""
     n, n_shared = d.T * d.k * d.H, d.T * d.H if d.n_shared else 0
     dev, st = _on_device(stream, x_perm, offsets, x, y_perm, y_shared, ws)
-    _need(dev == weights.device_index, "weights live on another device")
+    weights = _weights_i8(d, weights, dev)
     _call(dev, "moe_expert_ffn_i8", C.byref(d), _vec(x_perm, _BF16, n, "x_perm"), _vec(offsets, _I32, d.E_local + 1, "offsets"),
           C.byref(weights), _opt(x, _BF16, n_shared, "x"), _vec(y_perm, _BF16, n, "y_perm"),
           _opt(y_shared, _BF16, n_shared, "y_shared"), _ptr(ws), _bytes(ws), st)
@@ -453,7 +467,7 @@ def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=
     """moe_forward_i8; weights as make_weights_i8 returns them."""
     n = d.T * d.H
     dev, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws)
-    _need(dev == weights.device_index, "weights live on another device")
+    weights = _weights_i8(d, weights, dev)
     _call(dev, "moe_forward_i8", C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"),
           _opt(src, _I32, 0 if counts is None else d.T, "src"), _vec(x, _BF16, n, "x"),
           _opt(local_experts, _I32, d.E_local, "local_experts"), C.byref(weights), _opt(counts, _I64, d.S * d.E, "counts"),

@@ -355,3 +355,26 @@ def test_layer_binding_refuses_short_tensors(moe, recorded, T, call, names):
         call(moe, d, {**t, "x": t["x"][:0], "y_shared": t["y_shared"][:0]}, w)
     else:
         call(moe, d, {**t, "counts": None, "src": t["src"][:0]}, w)
+
+
+@pytest.mark.parametrize("call", [_ffn_call, _forward_call])
+def test_layer_binding_refuses_weights_of_other_sizes(moe, recorded, call):
+    """A handle of int8 weights knows the sizes that it was made for."""
+    d, t = _host_layer(moe, 3, 1)
+    for change in (dict(EL=4), dict(H=32), dict(H=48), dict(I=16), dict(I=32), dict(width=0), dict(width=8), dict(width=24)):
+        sizes = {**dict(EL=5, H=40, I=24, width=16), **change}
+        other = moe.dims(T=9, H=sizes["H"], E=8, k=2, I=sizes["I"], S=1, E_local=sizes["EL"], n_shared=int(sizes["width"] > 0),
+                         I_shared=sizes["width"])
+        w = moe.make_weights_i8(other, _host_weights(moe, **sizes))
+        with pytest.raises(ValueError, match="other sizes"):
+            call(moe, d, t, w)
+    assert not recorded
+    # another batch, one expert more than hosted, shared experts that the layer does not use, a struct filled by hand
+    call(moe, d, t, moe.make_weights_i8(_host_layer(moe, 50, 1)[0], _host_weights(moe, width=16)))
+    more = moe.dims(T=3, H=40, E=8, k=2, I=24, S=3, E_local=6, n_shared=1, I_shared=16)
+    w = moe.make_weights_i8(more, _host_weights(moe, EL=6, width=16))
+    call(moe, d, t, w)
+    call(moe, _host_layer(moe, 3, 0)[0], t, w)
+    by_hand = moe.MoeWeightsI8(**{n: 16 for n, _ in moe.MoeWeightsI8._fields_})
+    call(moe, d, t, by_hand)
+    assert len(recorded) == 4
