@@ -438,9 +438,14 @@ def make_weights_i8(d: MoeDims, w: dict) -> MoeWeightsI8:
     return h
 
 
-def _weights_i8(d: MoeDims, w: MoeWeightsI8, dev: int) -> MoeWeightsI8:
-    """The handle, refused where it was made for another device or other sizes
-    (more experts, or shared ones that d does not have, are none)."""
+def _weights_i8(d: MoeDims, w, dev: int) -> MoeWeightsI8:
+    """The handle w, or that of the dict w; refused where it was made for another
+    device or other sizes (more experts, or shared ones that d does not have, are
+    none)."""
+    if isinstance(w, dict):
+        w = make_weights_i8(d, w)
+    elif not isinstance(w, MoeWeightsI8):
+        raise TypeError(f"weights: expected int8 ones (make_weights_i8, quantize_weights), not a {type(w).__name__} or bf16 ones")
     if w.sizes is not None:
         _need(w.device_index == dev, "weights live on another device")
         EL, H, I, width = w.sizes
@@ -454,7 +459,7 @@ def _bytes(ws) -> int:
 
 
 def expert_ffn_i8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=None):
-    """moe_expert_ffn_i8; weights as make_weights_i8 returns them."""
+    """moe_expert_ffn_i8; weights as make_weights_i8 returns them, or its dict."""
     n, n_shared = d.T * d.k * d.H, d.T * d.H if d.n_shared else 0
     dev, st = _on_device(stream, x_perm, offsets, x, y_perm, y_shared, ws)
     weights = _weights_i8(d, weights, dev)
@@ -464,7 +469,7 @@ def expert_ffn_i8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=N
 
 
 def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=None, stream=None, gating=None):
-    """moe_forward_i8; weights as make_weights_i8 returns them."""
+    """moe_forward_i8; weights as make_weights_i8 returns them, or its dict."""
     n = d.T * d.H
     dev, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws)
     weights = _weights_i8(d, weights, dev)

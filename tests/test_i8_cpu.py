@@ -378,3 +378,18 @@ def test_layer_binding_refuses_weights_of_other_sizes(moe, recorded, call):
     by_hand = moe.MoeWeightsI8(**{n: 16 for n, _ in moe.MoeWeightsI8._fields_})
     call(moe, d, t, by_hand)
     assert len(recorded) == 4
+
+
+@pytest.mark.parametrize("call", [_ffn_call, _forward_call])
+def test_layer_binding_takes_a_dict_of_weights(moe, recorded, call):
+    """As expert_ffn and forward do."""
+    d, t = _host_layer(moe, 3, 1)
+    tensors = _host_weights(moe, width=16)
+    call(moe, d, t, tensors)
+    call(moe, d, t, moe.make_weights_i8(d, tensors))
+    seen = [next(a._obj for a in args if isinstance(getattr(a, "_obj", None), moe.MoeWeightsI8)) for _, args in recorded]
+    assert all(getattr(seen[0], n) == tensors[n].data_ptr() == getattr(seen[1], n) for n in tensors)
+    with pytest.raises(ValueError, match="w_down"):
+        call(moe, d, t, {**tensors, "w_down": tensors["w_down"][:4]})
+    with pytest.raises(TypeError, match="bf16"):
+        call(moe, d, t, moe.MoeWeights())
