@@ -299,9 +299,14 @@ def _call(dev: int, where: str, *args) -> None:
         raise MoeError(status, where)
 
 
-def _allocating_on(stream):
-    """Context in which tensors are allocated for use on `stream`."""
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else None)
+def _allocating_on(stream, dev: int):
+    """Context in which tensors are allocated for use on `stream` of device dev,
+    which may be a raw handle (0, and HIP's 1, stand for the default stream)."""
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        handle = getattr(handle, "value", handle) or 0
+        stream = torch.cuda.ExternalStream(handle, device=dev) if handle > 1 else torch.cuda.default_stream(dev)
+    return torch.cuda.stream(stream)
 
 
 def _need(ok: bool, what: str) -> None:
@@ -356,7 +361,7 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     _fits("moe_quantize_rows", rows, cols)
     dev, st = _on_device(stream, x, q, scale)
     if q is None or scale is None:
-        with _allocating_on(stream):
+        with _allocating_on(stream, dev):
             q = torch.empty((rows, _pad16(cols)), dtype=torch.int8, device=x.device) if q is None else q
             scale = torch.empty((rows,), dtype=torch.float32, device=x.device) if scale is None else scale
     qp, ldq = _rows(q, _I8, _pad16(cols), "q")
@@ -561,7 +566,7 @@ class MoeLayerI8:
 
     def forward(self, logits, src, x, counts=None, out=None, taps=None, stream=None, ws=None):
         if out is None:
-            with _allocating_on(stream):
+            with _allocating_on(stream, _on_device(stream, x)[0]):
                 out = torch.empty((self.d.T, self.d.H), dtype=torch.bfloat16, device=x.device)
         forward_i8(self.d, logits, src, x, self.local_experts, self._w, counts, out, self.ws if ws is None else ws, taps,
                    stream, gating=self.gating)

@@ -705,3 +705,27 @@ def test_two_streams_at_once(moe, T):
     torch.cuda.synchronize()
     for s in range(2):
         assert all(torch.equal(o, ref[s]) for o in out[s])
+
+
+def test_outputs_on_a_raw_stream_handle(moe):
+    """Allocated outputs belong to the stream that writes them, given as a handle
+    too: freed, their block (12 and 14 MB, each one of its own) goes to that
+    stream's next allocations and to no other stream's."""
+    d = moe.dims(T=6000, S=1, H=1048, E=4, k=2, I=64, E_local=4)
+    _, q = layer_weights(moe, d, 1)
+    layer, side = moe.MoeLayerI8(d, q), torch.cuda.Stream()
+    logits, x, wide = torch.randn((6000, 4), generator=gen(1), device="cuda"), randn((6000, 1048), 3), randn((6000, 2100), 4)
+    eager, (eq, es) = layer.forward(logits, None, x), moe.quantize_rows(wide)
+    for handle in (side.cuda_stream, C.c_void_p(side.cuda_stream)):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        out, (xq, xs) = layer.forward(logits, None, x, stream=handle), moe.quantize_rows(wide, stream=handle)
+        side.synchronize()
+        assert torch.equal(out, eager) and torch.equal(xq, eq) and torch.equal(xs, es)
+        blocks = {out.data_ptr(), xq.data_ptr()}
+        torch.cuda.synchronize()   # (the comparisons read them on the current stream)
+        del out, xq, xs
+        other = [torch.empty(12 << 20, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        with torch.cuda.stream(side):
+            own = [torch.empty(12 << 20, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        assert blocks <= {t.data_ptr() for t in own} and not blocks & {t.data_ptr() for t in other}

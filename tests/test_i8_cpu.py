@@ -393,3 +393,49 @@ def test_layer_binding_takes_a_dict_of_weights(moe, recorded, call):
         call(moe, d, t, {**tensors, "w_down": tensors["w_down"][:4]})
     with pytest.raises(TypeError, match="bf16"):
         call(moe, d, t, moe.MoeWeights())
+
+
+@pytest.mark.parametrize("kind", ["none", "torch", "int", "pointer", "object", "null", "legacy"])
+def test_outputs_belong_to_the_stream_they_are_written_on(moe, recorded, monkeypatch, kind):
+    """What quantize_rows and MoeLayerI8.forward allocate is that stream's in
+    torch's allocator, a raw handle's too: freed early, it is not handed out to
+    the current stream while the launch may still write it."""
+    entered = []
+
+    class Stream:
+        def __init__(self, name):
+            self.name = name
+            self.cuda_stream = 48
+
+    class External(Stream):
+        def __init__(self, handle, device):
+            super().__init__(("external", handle, device))
+
+    class On:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            entered.append(self.s and self.s.name)
+
+        def __exit__(self, *a):
+            pass
+    for name, fake in (("Stream", Stream), ("ExternalStream", External), ("stream", On), ("default_stream", lambda dev: Stream(("default", dev)))):
+        monkeypatch.setattr(torch.cuda, name, fake)
+
+    class Handle:
+        cuda_stream = 64
+    stream, where = {"none": (None, None), "torch": (Stream("torch"), "torch"), "int": (48, ("external", 48, 0)),
+                     "pointer": (C.c_void_p(48), ("external", 48, 0)), "object": (Handle(), ("external", 64, 0)),
+                     "null": (C.c_void_p(None), ("default", 0)), "legacy": (1, ("default", 0))}[kind]
+    x = torch.zeros((3, 40), dtype=torch.bfloat16)
+    moe.quantize_rows(x, stream=stream)
+    assert entered == [where]
+    d, t = _host_layer(moe, 3, 0)
+    layer = moe.MoeLayerI8(d, _host_weights(moe), t["local_experts"], device="cpu")
+    layer.forward(t["logits"], None, t["x"], stream=stream)
+    assert entered == [where, where] and [c[0] for c in recorded] == ["moe_quantize_rows", "moe_forward_i8"]
+    # given ones are the caller's
+    moe.quantize_rows(x, torch.zeros((3, 48), dtype=torch.int8), torch.zeros(3), stream=stream)
+    layer.forward(t["logits"], None, t["x"], out=t["out"], stream=stream)
+    assert len(entered) == 2
