@@ -336,8 +336,8 @@ def _rows(t, dtypes, cols: int, what: str):
         raise ValueError(f"{what}: expected rows of at least {cols} values, got {tuple(shape)}")
     if shape[1] != 1 and stride[1] != 1:
         raise ValueError(f"{what}: rows must be contiguous")
-    # one row has no stride to speak of
-    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]
+    # one row has no stride to speak of: int8 rows are asked for in whole 16s
+    return t.data_ptr(), stride[0] if shape[0] > 1 else cols if t.dtype == torch.int8 else shape[1]
 
 
 def _vec(t, dtypes, n: int, what: str):

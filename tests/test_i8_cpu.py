@@ -439,3 +439,25 @@ def test_outputs_belong_to_the_stream_they_are_written_on(moe, recorded, monkeyp
     moe.quantize_rows(x, torch.zeros((3, 48), dtype=torch.int8), torch.zeros(3), stream=stream)
     layer.forward(t["logits"], None, t["x"], out=t["out"], stream=stream)
     assert len(entered) == 2
+
+
+def test_one_row_has_no_stride(moe, recorded):
+    """A single row may be cut from a longer one at any length: the stride that
+    goes to the library is one that it takes, whatever the row's tensor says."""
+    row = torch.zeros((1, 2 ** 21 + 100), dtype=torch.int8)
+    bf, s = torch.zeros((1, 90), dtype=torch.bfloat16), torch.zeros(4)
+
+    def dims():
+        d = next(a._obj for a in recorded[-1][1] if hasattr(a, "_obj"))
+        return d.ldx, d.ldw, d.ldy
+    for cols in (48, 50, 63, 2 ** 21 + 100):
+        moe.linear_i8(40, row[:, :cols], s, row[:, :cols], s, bf[:, :1])
+        assert dims() == (48, 48, 1)
+        moe.grouped_linear_i8(40, row[:, :cols], s, s, row[None, :, :cols], s, bf[:, :1])
+        assert dims() == (48, 48, 1)
+        moe.quantize_rows(bf[:, :40], row[:, :cols], s)
+        assert recorded[-1][1][3] == 40 and recorded[-1][1][5] == 48
+    # several rows: as they lie, odd distances for the library to refuse
+    moe.linear_i8(40, torch.zeros((2, 50), dtype=torch.int8), s, torch.zeros((3, 80), dtype=torch.int8)[:, :48], s,
+                  torch.zeros((2, 7), dtype=torch.bfloat16)[:, :3])
+    assert dims() == (50, 80, 7)
