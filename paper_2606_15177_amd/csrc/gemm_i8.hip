@@ -7,19 +7,22 @@ namespace moe {
 namespace {
 
 // 256-row tiles want rows that fill them and tiles for half of the CUs; more on
-// short K, where an item's turnaround is short too.  Over 800 random layers (65 to
+// short K, where an item's turnaround is short too.  Over 320 random layers (65 to
 // 8192 tokens, even to Zipf 1 routing, K 392 to 14336) these lines choose the
-// faster kernel within 8 % for all but 75 of 1600 grouped products (1.39 at worst,
-// 0.9 % on average), and over 297 random products of static rows for all but 5
-// (1.38, 0.4 %).  Both sides, us (items, tiles):
+// faster kernel within 8 % for all but 34 of 640 grouped products (1.36 at worst,
+// 1.1 % on average), and over 300 random products of static rows for all but 17
+// (1.49, 1.1 %).  Both sides, us (items, tiles):
 //   rows: 8 experts of K 4096, N 14336 at a mean of 67 178 and 186, of 81 225 and
-//     196; K 3128, N 904, 34 groups of 80 54 and 40;
+//     196; K 3128, N 904, 34 groups of 80 35 and 29;
 //   many groups of short K, whose last tiles are mostly padding: Qwen3 gate/up at a
 //     mean of 193 147 and 163, of 252 172 and 206; DSV2-Lite's at 281 216 and 247,
 //     at 308 235 and 235, its down at 381 168 and 152;
-//   few tiles, grouped: 116 of K 2936 26 and 39, 126 of K 2408 37 and 29; short K:
-//     384 of K 712 28 and 38, 435 of K 1296 86 and 81; static: 84 of K 5033 72 and
-//     60, 117 of K 1142 18 and 25, 264 of K 796 29 and 34.
+//   few tiles, grouped: 112 of K 3080 47 and 45, 128 of K 14336 157 and 143; short
+//     K: 324 of K 888 24 and 34, 408 of K 1208 52 and 60, 456 of K 480 64 and 54;
+//   static: 48 of K 5000 34 and 38, 64 of K 7168 50 and 43, 70 of K 1500 21 and 19,
+//     84 of K 5033 71 and 46; short K: 102 of K 844 20 and 17, 117 of K 1142 21 and
+//     18, 264 of K 796 35 and 31, 528 of K 829 48 and 55.  (These lines stand a
+//     little high: tiles win from about 64 on since an only round runs in parts.)
 constexpr int kMeanRows = 75, kMeanMany = 300;
 constexpr int kMany = 64, kManyK = 2048;
 constexpr int kShortK = 1500;
@@ -55,6 +58,11 @@ GemmI8Plan plan_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, 
   if (!a.xb && takes_tiles(seg, a, sh, gated)) return {1, 1, 256, 0};
   const Cut c = a.xb ? few_cut(seg, a, sh, gated) : items_cut(seg, a, sh, gated);
   return {a.xb ? 2 : 0, c.parts, c.rows, c.half};
+}
+
+GemmI8Round round_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, int tiles) {
+  const int grid = tiled_grid(seg, a, sh, gated);
+  return {grid, grid > 0 ? last_round_parts(tiles % grid, grid) : 0};
 }
 
 }  // namespace moe

@@ -57,6 +57,12 @@ __device__ __forceinline__ void store_cols(uint16_t* p, u32x4 v, int col, int N)
 // a over seg and sh (nullable, static rows) in one launch: 256-row tiles (K of
 // either past kTiledMinK), or items of up to 128 rows.
 constexpr int kTiledMinK = 384;
+int tiled_grid(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
+// In how many parts each of the `rest` tiles past a grid's last whole round runs.
+constexpr int kMaxParts = 4;
+__host__ __device__ __forceinline__ int last_round_parts(int rest, int grid) {
+  return kMaxParts * rest <= grid ? kMaxParts : 2 * rest <= grid ? 2 : 1;
+}
 hipError_t launch_tiled_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
 hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st);
 // How a launch of items cuts its products: K in `parts`, chunks of `rows` rows.

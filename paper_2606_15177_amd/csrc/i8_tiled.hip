@@ -23,7 +23,9 @@
 //
 // Last round.  Where the tiles past the last whole round of the grid are at most
 // half (a quarter) of the workgroups, each is run in two (four) parts of its
-// rows on as many CUs.
+// rows on as many CUs.  So is an only round: the grid is sized for the parts (90
+// tiles of K 1700 31.2 us on 96 workgroups, 24.0 on 256; 96 of K 7168 70 and 51;
+// 128 of K 14336 131 and 112; up to 3 % more where no tile has a second part).
 //
 // A group's last tile: rows past its end cost no traffic (their loads lie past
 // the descriptor's range), and a tile of up to 128 or 64 rows takes half or a
@@ -134,7 +136,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   const int xcd = static_cast<int>(blockIdx.x) % kXcds, in_xcd = static_cast<int>(blockIdx.x) / kXcds;
   const int rounds = total / n_wg, rest = total - rounds * n_wg;
   // the last round's tiles in `split` parts of 256 / split rows
-  const int split = 4 * rest <= n_wg ? 4 : 2 * rest <= n_wg ? 2 : 1;
+  const int split = last_round_parts(rest, n_wg);
   const int rest_lo = static_cast<int>(static_cast<long long>(rest) * split * xcd / kXcds);
   const int rest_hi = static_cast<int>(static_cast<long long>(rest) * split * (xcd + 1) / kXcds);
   int mine = rounds + (in_xcd < rest_hi - rest_lo ? 1 : 0);  // tiles of this workgroup
@@ -520,15 +522,22 @@ hipError_t launch_pfx(const TiledI8& ta, int grid, hipStream_t st) {
 
 }  // namespace
 
+static int shared_tiles(const GemmI8* sh, bool gated) {
+  return sh ? ceil_div(sh->static_rows, kTile) * ceil_div(sh->N, gated ? kTile / 2 : kTile) : 0;
+}
+
+// One workgroup per CU (its LDS), a whole number per XCD; fewer where the tiles
+// there may be, in their most parts, are fewer.
+int tiled_grid(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated) {
+  const long long m_tiles = a.offsets ? seg.total_rows / kTile + std::min(seg.groups, seg.total_rows) : ceil_div(a.static_rows, kTile);
+  const long long tiles = shared_tiles(sh, gated) + m_tiles * ceil_div(a.N, gated ? kTile / 2 : kTile);
+  return static_cast<int>((std::min<long long>(kMaxParts * tiles, device_cu_count()) + kXcds - 1) / kXcds * kXcds);
+}
+
 hipError_t launch_tiled_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, hipStream_t st) {
-  const int cols = gated ? kTile / 2 : kTile;
-  long long m_tiles = a.offsets ? seg.total_rows / kTile + std::min(seg.groups, seg.total_rows) : ceil_div(a.static_rows, kTile);
-  TiledI8 ta{a, sh ? *sh : GemmI8{}, seg.total_rows, 0};
-  if (sh) ta.sp_tiles = ceil_div(sh->static_rows, kTile) * ceil_div(sh->N, cols);
-  const long long tiles = ta.sp_tiles + m_tiles * ceil_div(a.N, cols);
-  if (tiles == 0) return hipSuccess;
-  // one workgroup per CU (its LDS), a whole number per XCD
-  const int grid = static_cast<int>((std::min<long long>(tiles, device_cu_count()) + kXcds - 1) / kXcds * kXcds);
+  const TiledI8 ta{a, sh ? *sh : GemmI8{}, seg.total_rows, shared_tiles(sh, gated)};
+  const int grid = tiled_grid(seg, a, sh, gated);
+  if (grid == 0) return hipSuccess;
   if (seg.groups <= kWave) return gated ? launch_pfx<true, 1>(ta, grid, st) : launch_pfx<false, 1>(ta, grid, st);
   if (seg.groups <= 4 * kWave) return gated ? launch_pfx<true, 4>(ta, grid, st) : launch_pfx<false, 4>(ta, grid, st);
   return gated ? launch_pfx<true, 16>(ta, grid, st) : launch_pfx<false, 16>(ta, grid, st);

@@ -203,6 +203,12 @@ struct GemmI8Plan {
   int kernel, parts, rows, half;
 };
 GemmI8Plan plan_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
+// Host only: workgroups of a launch of tiles, and the parts in which the tiles
+// past its last whole round run where `tiles` have rows.
+struct GemmI8Round {
+  int grid, parts;
+};
+GemmI8Round round_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, int tiles);
 
 // ---- combine.hip -----------------------------------------------------------
 hipError_t launch_combine(int T, int k, int H, const uint16_t* y_perm, const int32_t* inv_pos,

@@ -783,18 +783,32 @@ int moe_test_ffn_plan(const moe_dims* d, int rows_indexed, int64_t out[2][7]) {
 // For the tests: how the 8-bit products run (moe::GemmI8Plan: kernel, parts,
 // rows, half), of moe_linear_i8 or moe_grouped_linear_i8, and of
 // moe_forward_i8's or moe_expert_ffn_i8's gate/up and down.
+static moe::GemmI8 plan_args(const moe_linear_dims* d, const moe::Segments& seg) {
+  moe::GemmI8 a{};
+  a.offsets = seg.offsets;
+  a.static_rows = seg.offsets ? 0 : d->M;
+  a.groups = seg.groups;
+  a.K = d->K, a.N = d->N;
+  return a;
+}
+
 int moe_test_linear_i8_plan(const moe_linear_dims* d, int grouped, int64_t out[4]) {
   static const int32_t some = 0;  // stands for device offsets
   if (d == nullptr || d->M < 1 || d->N < 1 || d->K < 1 || (grouped && d->G < 1)) return MOE_ERR_DIMS;
   const moe::Segments seg = linear_segments(d, grouped ? &some : nullptr, grouped != 0);
-  moe::GemmI8 a{};
-  a.offsets = seg.offsets;
-  a.static_rows = grouped ? 0 : d->M;
-  a.groups = seg.groups;
-  a.K = d->K, a.N = d->N;
-  const moe::GemmI8Plan p = moe::plan_gemm_i8(seg, a, nullptr, false);
+  const moe::GemmI8Plan p = moe::plan_gemm_i8(seg, plan_args(d, seg), nullptr, false);
   const int64_t v[4] = {p.kernel, p.parts, p.rows, p.half};
   std::copy(v, v + 4, out);
+  return MOE_OK;
+}
+
+// For the tests: moe::GemmI8Round of a product on tiles, `tiles` of which have rows.
+int moe_test_linear_i8_round(const moe_linear_dims* d, int grouped, int tiles, int64_t out[2]) {
+  static const int32_t some = 0;
+  if (d == nullptr || d->M < 1 || d->N < 1 || d->K < 1 || tiles < 0 || (grouped && d->G < 1)) return MOE_ERR_DIMS;
+  const moe::Segments seg = linear_segments(d, grouped ? &some : nullptr, grouped != 0);
+  const moe::GemmI8Round r = moe::round_gemm_i8(seg, plan_args(d, seg), nullptr, false, tiles);
+  out[0] = r.grid, out[1] = r.parts;
   return MOE_OK;
 }
 

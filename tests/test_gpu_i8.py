@@ -729,3 +729,31 @@ def test_outputs_on_a_raw_stream_handle(moe):
         with torch.cuda.stream(side):
             own = [torch.empty(12 << 20, dtype=torch.uint8, device="cuda") for _ in range(4)]
         assert blocks <= {t.data_ptr() for t in own} and not blocks & {t.data_ptr() for t in other}
+
+
+# Tiles of a last round in two and four parts of their rows, with row tiles that
+# end in the first part, in a later one and between two.
+PARTS = [(2500, 2100, 0, 90, 2), (2433, 2300, 0, 90, 2), (5003, 4400, 0, 360, 2), (4737, 4400, 0, 342, 2), (5003, 3801, 0, 300, 4),
+         (4097, 2048, [200, 0, 300, 700], 48, 4), (4096, 2048, [64, 65, 513, 640], 64, 4), (4100, 2040, [1000, 129, 0, 1024], 72, 2),
+         (6000, 4400, [1300, 1, 1200, 2400, 0, 255], 414, 1), (6000, 4400, [1200, 128, 1150, 2000, 0, 129], 360, 2)]
+
+
+@pytest.mark.parametrize("case", range(len(PARTS)))
+@pytest.mark.parametrize("gather", [False, True])
+def test_parts_of_a_last_round(moe, case, gather):
+    M, N, sizes, tiles, parts = PARTS[case]
+    K, G = 1600, len(sizes) if sizes else 0
+    out = (C.c_int64 * 2)()
+    rows = [-(-n // 256) for n in sizes or [M]]
+    assert sum(rows) * -(-N // 256) == tiles and linear_plan(moe, M, N, K, G) == (TILES, 1, 256)
+    assert moe._lib.moe_test_linear_i8_round(C.byref(moe.MoeLinearDims(M=M, N=N, K=K, G=G)), int(G > 0), tiles, out) == 0
+    assert tuple(out) == (256, parts)
+    if sizes:
+        check_grouped(moe, sizes, N, K, case, spare=M - sum(sizes), gather=997 if gather else None)
+    elif gather:
+        check_grouped(moe, [M], N, K, case, spare=0, gather=997)
+    else:
+        xq, xs, wq, ws = operands(M, N, K, case)
+        y = torch.full((M + 1, N), 3.0, dtype=torch.bfloat16, device="cuda")
+        moe.linear_i8(K, xq, xs, wq, ws, y[:M])
+        assert torch.equal(y[:M], exact_product(xq, xs, wq, ws, K)) and (y[M] == 3.0).all()

@@ -461,3 +461,17 @@ def test_one_row_has_no_stride(moe, recorded):
     moe.linear_i8(40, torch.zeros((2, 50), dtype=torch.int8), s, torch.zeros((3, 80), dtype=torch.int8)[:, :48], s,
                   torch.zeros((2, 7), dtype=torch.bfloat16)[:, :3])
     assert dims() == (50, 80, 7)
+
+
+@pytest.mark.parametrize("M,N,G,tiles,grid,parts", [
+    (2500, 2100, 0, 90, 256, 2), (2560, 2048, 0, 80, 256, 2), (2048, 4096, 0, 128, 256, 2), (2048, 4097, 0, 136, 256, 1),   # an only round
+    (2048, 2048, 0, 64, 256, 4), (2048, 2049, 0, 72, 256, 2), (256, 256, 0, 1, 8, 4), (1280, 1024, 0, 20, 80, 4),
+    (5003, 3801, 0, 300, 256, 4), (5003, 4400, 0, 360, 256, 2), (5003, 5000, 0, 400, 256, 1),                             # past one of 256
+    (4096, 2048, 4, 48, 256, 4), (4096, 2048, 4, 96, 256, 2), (4096, 2048, 4, 160, 256, 1),                               # groups with few rows
+])
+def test_tiles_of_a_last_round_run_in_parts(moe, M, N, G, tiles, grid, parts):
+    """(on 256 CUs)"""
+    d, out = moe.MoeLinearDims(M=M, N=N, K=1700, G=G), (C.c_int64 * 2)()
+    assert G or tiles == -(-M // 256) * -(-N // 256)
+    assert moe._lib.moe_test_linear_i8_round(C.byref(d), int(G > 0), tiles, out) == 0
+    assert tuple(out) == (grid, parts)
