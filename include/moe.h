@@ -377,6 +377,10 @@ int moe_quantize_rows(int32_t rows, int32_t cols, const moe_bf16 *x, int64_t ldx
  *   ldx, ldw  row strides of xq and wq in bytes: multiples of 16, at least K
  *             rounded up to 16, at most 2^21.
  *   ldy       row stride of y in values, at least N.
+ *   R         rows expected in all groups together, by which the grouped product
+ *             chooses its kernel; 0 (or anything outside 1..M): M.  For a y with
+ *             room for more rows than there will be, as on an expert-parallel
+ *             rank: T*k*E_local/E of M = T*k.  No result depends on it.
  * Limits (MOE_ERR_UNSUPPORTED beyond them): K < 2^17 (the int32 sums are then
  * exact for any int8 values), ldy (and so N) <= 2^21, M <= 2^31 - 256 and, with
  * x_rows, X*ldx < 2^31.  A product of short rows may need more workgroups than
@@ -385,6 +389,7 @@ int moe_quantize_rows(int32_t rows, int32_t cols, const moe_bf16 *x, int64_t ldx
 typedef struct moe_linear_dims {
     int32_t M, N, K, G, X;
     int64_t ldx, ldw, ldy;
+    int32_t R;
 } moe_linear_dims;
 
 /*

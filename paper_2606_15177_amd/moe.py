@@ -47,7 +47,7 @@ class MoeTaps(C.Structure):
 
 class MoeLinearDims(C.Structure):
     _fields_ = ([(n, C.c_int32) for n in ("M", "N", "K", "G", "X")] +
-                [(n, C.c_int64) for n in ("ldx", "ldw", "ldy")])
+                [(n, C.c_int64) for n in ("ldx", "ldw", "ldy")] + [("R", C.c_int32)])
 
 
 class MoeWeightsI8(C.Structure):
@@ -385,10 +385,12 @@ def linear_i8(K, xq, x_scale, wq, w_scale, y, stream=None):
           wp, _vec(w_scale, _F32, N, "w_scale"), yp, st)
 
 
-def grouped_linear_i8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stream=None):
+def grouped_linear_i8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stream=None, rows=None):
     """moe_grouped_linear_i8: rows offsets[g] .. offsets[g+1] of y [M, N] from
     those of xq (or xq[x_rows[r]]) and wq[g]; wq int8 [G, N, >= K padded to 16],
-    w_scale fp32 [G, N], offsets int32 [G+1], x_rows int32 [M]."""
+    w_scale fp32 [G, N], offsets int32 [G+1], x_rows int32 [M].  rows: how many of
+    the M are expected to be in groups where y has room for more (the kernel is
+    chosen by it; no result depends on it)."""
     yp, ldy = _rows(y, _BF16, 1, "y")
     M, N = y.shape
     if not isinstance(wq, torch.Tensor) or wq.dim() != 3 or wq.shape[1] != N:
@@ -398,9 +400,9 @@ def grouped_linear_i8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stre
     wp, ldw = _rows(wq.flatten(0, 1), _I8, _pad16(K), "wq")
     _need(wp == wq.data_ptr(), "wq: the groups must lie one behind the other")
     _need(x_rows is not None or xq.shape[0] == M, "expected as many rows of xq as of y")
-    _fits("moe_grouped_linear_i8", M, N, K, G, xq.shape[0])
+    _fits("moe_grouped_linear_i8", M, N, K, G, xq.shape[0], rows or 0)
     dev, st = _on_device(stream, xq, x_scale, offsets, wq, w_scale, y, x_rows)
-    _call(dev, "moe_grouped_linear_i8", C.byref(MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy)), xp,
+    _call(dev, "moe_grouped_linear_i8", C.byref(MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy, rows or 0)), xp,
           _vec(x_scale, _F32, xq.shape[0], "x_scale"), None if x_rows is None else _vec(x_rows, _I32, M, "x_rows"),
           _vec(offsets, _I32, G + 1, "offsets"), wp, _vec(w_scale, _F32, G * N, "w_scale"), yp, st)
 

@@ -757,3 +757,26 @@ def test_parts_of_a_last_round(moe, case, gather):
         y = torch.full((M + 1, N), 3.0, dtype=torch.bfloat16, device="cuda")
         moe.linear_i8(K, xq, xs, wq, ws, y[:M])
         assert torch.equal(y[:M], exact_product(xq, xs, wq, ws, K)) and (y[M] == 3.0).all()
+
+
+@pytest.mark.parametrize("gather", [None, 700])
+def test_expected_rows_change_no_result(moe, gather):
+    """Room for four times the rows: the expected number chooses the kernel (told
+    right, tiles are not for them; told wrong, all rows are computed), the bits
+    are the same and rows behind the last group stay as they were."""
+    sizes, N, K, M = ragged(24, 35, 6, 150), 1300, 1700, 4000
+    _, xq, xs, wq, ws, offsets, x_rows = grouped_case(sizes, N, K, 8, spare=M - sum(sizes), gather=gather)
+    kernels, ref = set(), None
+    for rows in (None, sum(sizes), 1, M, 24 * 75):
+        d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=24, R=rows or 0), (C.c_int64 * 4)()
+        assert moe._lib.moe_test_linear_i8_plan(C.byref(d), 1, out) == 0
+        kernels.add(tuple(out[:3]))
+        y = torch.full((M, N), 3.0, dtype=torch.bfloat16, device="cuda")
+        moe.grouped_linear_i8(K, xq, xs, offsets, wq, ws, y, x_rows=x_rows, rows=rows)
+        ref = y if ref is None else ref
+        assert torch.equal(y, ref) and (y[sum(sizes):] == 3.0).all(), rows
+    assert kernels == {(TILES, 1, 256), (ITEMS, 1, 128), (ITEMS, 4, 32)}
+    g = int(np.argmax(sizes))
+    r = slice(offsets[g].item(), offsets[g + 1].item())
+    src = r if x_rows is None else x_rows[r].long()
+    assert torch.equal(ref[r], exact_product(xq[src], xs[src], wq[g], ws[g], K))

@@ -475,3 +475,26 @@ def test_tiles_of_a_last_round_run_in_parts(moe, M, N, G, tiles, grid, parts):
     assert G or tiles == -(-M // 256) * -(-N // 256)
     assert moe._lib.moe_test_linear_i8_round(C.byref(d), int(G > 0), tiles, out) == 0
     assert tuple(out) == (grid, parts)
+
+
+@pytest.mark.parametrize("M,N,K,G,R,plan,as_m", [
+    (5120, 2048, 4096, 64, 1280, (ITEMS, 1, 128), (TILES, 1, 256)),     # a quarter of the experts hosted, 20 rows each
+    (5120, 2048, 4096, 64, 64 * 75, (TILES, 1, 256), (TILES, 1, 256)), (5120, 2048, 4096, 64, 64 * 74, (ITEMS, 1, 128), (TILES, 1, 256)),
+    (4096, 512, 1024, 64, 16, (ITEMS, 4, 64), (ITEMS, 1, 128)),         # most groups empty: fewer items than CUs
+])
+def test_grouped_products_take_the_kernel_of_their_expected_rows(moe, M, N, K, G, R, plan, as_m):
+    """y may have room for more rows than there will be (M); R says how many."""
+    for r, want in ((R, plan), (0, as_m), (M, as_m), (-1, as_m), (M + 1, as_m), (2 ** 31 - 1, as_m), (-2 ** 31, as_m)):
+        d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G, R=r), (C.c_int64 * 4)()
+        assert moe._lib.moe_test_linear_i8_plan(C.byref(d), 1, out) == 0
+        assert tuple(out[:3]) == want and not out[3], r
+    dense, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G, R=R), (C.c_int64 * 4)()
+    assert moe._lib.moe_test_linear_i8_plan(C.byref(dense), 0, out) == 0 and tuple(out[:3]) == linear_plan(moe, M, N, K)
+
+
+def test_binding_passes_the_expected_rows(moe, recorded):
+    y, w = torch.zeros((40, 8), dtype=torch.bfloat16), torch.zeros((2, 8, 48), dtype=torch.int8)
+    q, s, o = torch.zeros((40, 48), dtype=torch.int8), torch.zeros(40), torch.zeros(3, dtype=torch.int32)
+    for rows, r in ((None, 0), (7, 7), (0, 0)):
+        moe.grouped_linear_i8(40, q, s, o, w, s, y, rows=rows)
+        assert next(a._obj for a in recorded[-1][1] if hasattr(a, "_obj")).R == r
