@@ -314,9 +314,9 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _fits(where: str, *sizes: int) -> None:
-    """Sizes of 32 bits in the C interface, which ctypes would cut to them."""
-    if max(sizes) >= 1 << 31:
+def _fits(where: str, sizes: int) -> None:
+    """Sizes (or'ed) of 31 bits in the C interface, which ctypes would cut to 32."""
+    if sizes >> 31:
         raise MoeError(MOE_ERR_UNSUPPORTED, where)
 
 
@@ -358,7 +358,7 @@ def quantize_rows(x, q=None, scale=None, stream=None):
     Returns (q, scale)."""
     xp, ldx = _rows(x, _BF16, 1, "x")
     rows, cols = x.shape
-    _fits("moe_quantize_rows", rows, cols)
+    _fits("moe_quantize_rows", rows | cols)
     dev, st = _on_device(stream, x, q, scale)
     if q is None or scale is None:
         with _allocating_on(stream, dev):
@@ -379,7 +379,7 @@ def linear_i8(K, xq, x_scale, wq, w_scale, y, stream=None):
     xp, ldx = _rows(xq, _I8, _pad16(K), "xq")
     wp, ldw = _rows(wq, _I8, _pad16(K), "wq")
     _need(xq.shape[0] == M and wq.shape[0] == N, "expected as many rows of xq and wq as y has rows and columns")
-    _fits("moe_linear_i8", M, N, K)
+    _fits("moe_linear_i8", M | N)
     dev, st = _on_device(stream, xq, x_scale, wq, w_scale, y)
     _call(dev, "moe_linear_i8", C.byref(MoeLinearDims(M, N, K, 1, 0, ldx, ldw, ldy)), xp, _vec(x_scale, _F32, M, "x_scale"),
           wp, _vec(w_scale, _F32, N, "w_scale"), yp, st)
@@ -400,9 +400,9 @@ def grouped_linear_i8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stre
     wp, ldw = _rows(wq.flatten(0, 1), _I8, _pad16(K), "wq")
     _need(wp == wq.data_ptr(), "wq: the groups must lie one behind the other")
     _need(x_rows is not None or xq.shape[0] == M, "expected as many rows of xq as of y")
-    _fits("moe_grouped_linear_i8", M, N, K, G, xq.shape[0], rows or 0)
+    _fits("moe_grouped_linear_i8", M | N | G | xq.shape[0])
     dev, st = _on_device(stream, xq, x_scale, offsets, wq, w_scale, y, x_rows)
-    _call(dev, "moe_grouped_linear_i8", C.byref(MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy, rows or 0)), xp,
+    _call(dev, "moe_grouped_linear_i8", C.byref(MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy, min(rows or 0, M))), xp,
           _vec(x_scale, _F32, xq.shape[0], "x_scale"), None if x_rows is None else _vec(x_rows, _I32, M, "x_rows"),
           _vec(offsets, _I32, G + 1, "offsets"), wp, _vec(w_scale, _F32, G * N, "w_scale"), yp, st)
 
