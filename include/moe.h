@@ -441,7 +441,7 @@ typedef struct moe_weights_i8 {
  * moe_expert_ffn on int8 experts: rows are quantised as by moe_quantize_rows,
  * gate and up are products as above (in fp32, not rounded), h = silu(gate) * up
  * is rounded to bf16 and quantised by row again, and y_perm is the product of
- * that with down.  y_shared (bf16) is the shared FFN of x.
+ * that with down, rounded to bf16.  y_shared (bf16) is the shared FFN of x.
  * Arguments as moe_expert_ffn's, x_perm and x in bf16; rows of y_perm past
  * offsets[E_local] are left as they were.
  *   ws  MOE_ENTRY_EXPERT_FFN_I8 workspace.
@@ -453,8 +453,11 @@ int moe_expert_ffn_i8(const moe_dims *dims, const moe_bf16 *x_perm, const int32_
 
 /*
  * moe_forward on int8 experts: the layer as there, with moe_expert_ffn_i8's
- * networks (x is quantised once per token).  Stage MOE_STAGE_FFN_UP includes
- * the quantisation of x, MOE_STAGE_FFN_DOWN that of the hidden rows.
+ * networks (x is quantised once per token).  As there, an expert's output for a
+ * token and the shared experts' are each rounded to bf16 before the weighted sum,
+ * which is taken in fp32 and rounded once more: the layer's bits are those of
+ * moe_expert_ffn_i8 and moe_combine.  Stage MOE_STAGE_FFN_UP includes the
+ * quantisation of x, MOE_STAGE_FFN_DOWN that of the hidden rows.
  *   ws  MOE_ENTRY_FORWARD_I8 workspace.
  */
 int moe_forward_i8(const moe_dims *dims, const moe_gating *gating, const float *logits,

@@ -88,7 +88,12 @@ FfnWs carve_ffn(const moe_dims* d, void* base) {
 }
 size_t ffn_ws(const moe_dims* d) { return carve_ffn(d, nullptr).bytes; }
 
-// The forward workspace, carved in this order.
+// The forward workspace, carved in this order.  The experts' outputs wait for the
+// weighted sum in bf16, as moe_expert_ffn and moe_expert_ffn_i8 return them, so
+// that the layer's bits are its steps'.  On int8 experts the layer is 0.20 to
+// 0.23 % off the exact sum (norms) where one rounding at the end leaves 0.17 %;
+// in fp32 they would cost 4 more bytes per value, 0.2 to 0.3 ms by bytes of the
+// 1.6 to 2.3 ms that 16384 tokens of DSV3's 32 local experts take.
 struct ForwardWs {
   int32_t* topk_idx;
   float* topk_w;
