@@ -37,12 +37,14 @@ class MoeWeights(C.Structure):
 class MoeGating(C.Structure):
     _fields_ = [("bias", C.c_void_p), ("routed_scale", C.c_float), ("n_group", C.c_int32),
                 ("topk_group", C.c_int32)]
+    bias_tensor = None   # what gating() was given
 
 
 class MoeTaps(C.Structure):
     _fields_ = [("topk_idx", C.c_void_p), ("topk_w", C.c_void_p), ("expert_load", C.c_void_p),
                 ("offsets", C.c_void_p), ("perm_token", C.c_void_p), ("inv_pos", C.c_void_p),
                 ("events", C.c_void_p * (2 * len(STAGES)))]
+    tensors = {}   # by name, what make_taps was given
 
 
 class MoeLinearDims(C.Structure):
@@ -188,7 +190,9 @@ def workspace(d: MoeDims, entry: int, device="cuda") -> torch.Tensor:
 def gating(bias=None, routed_scale=1.0, n_group=0, topk_group=0) -> MoeGating:
     """Parameters of the gate function that moe_dims.flags selects; bias is a
     device fp32 [E] tensor (sigmoid gates only)."""
-    return MoeGating(_ptr(bias, _F32), float(routed_scale), int(n_group), int(topk_group))
+    g = MoeGating(_ptr(bias, _F32), float(routed_scale), int(n_group), int(topk_group))
+    g.bias_tensor = bias
+    return g
 
 
 def _gating_ref(g):
@@ -230,6 +234,8 @@ def make_taps(topk_idx=None, topk_w=None, expert_load=None, offsets=None, perm_t
               inv_pos=None, events=None) -> MoeTaps:
     t = MoeTaps(_ptr(topk_idx, _I32), _ptr(topk_w, _F32), _ptr(expert_load, _I32),
                 _ptr(offsets, _I32), _ptr(perm_token, _I32), _ptr(inv_pos, _I32))
+    t.tensors = {n: v for n, v in (("topk_idx", topk_idx), ("topk_w", topk_w), ("expert_load", expert_load),
+                                   ("offsets", offsets), ("perm_token", perm_token), ("inv_pos", inv_pos)) if v is not None}
     if events is not None:
         for i, e in enumerate(events):
             t.events[i] = e  # None leaves the slot empty: that stage is not recorded
@@ -478,7 +484,13 @@ def expert_ffn_i8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=N
 def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=None, stream=None, gating=None):
     """moe_forward_i8; weights as make_weights_i8 returns them, or its dict."""
     n = d.T * d.H
-    dev, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws)
+    tapped = {} if taps is None else taps.tensors
+    bias = None if gating is None else gating.bias_tensor
+    dev, st = _on_device(stream, logits, src, x, local_experts, counts, out, ws, bias, *tapped.values())
+    for name, t in tapped.items():
+        size = {"expert_load": d.E, "offsets": d.E_local + 1}.get(name, d.T * d.k)
+        _need(t.numel() >= size, f"taps: {name}: expected {size} values")
+    _need(bias is None or bias.numel() >= d.E, f"gating: bias: expected {d.E} values")
     weights = _weights_i8(d, weights, dev)
     _call(dev, "moe_forward_i8", C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"),
           _opt(src, _I32, 0 if counts is None else d.T, "src"), _vec(x, _BF16, n, "x"),

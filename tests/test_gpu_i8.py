@@ -780,3 +780,39 @@ def test_expected_rows_change_no_result(moe, gather):
     r = slice(offsets[g].item(), offsets[g + 1].item())
     src = r if x_rows is None else x_rows[r].long()
     assert torch.equal(ref[r], exact_product(xq[src], xs[src], wq[g], ws[g], K))
+
+
+@pytest.mark.parametrize("case", [1, 5])
+def test_taps_of_the_layer(moe, case):
+    """The extra outputs are those of the separate steps, the output that of the
+    layer without them; events of every stage are recorded in order."""
+    d = moe.dims(S=3, **FFN[case])
+    _, q = layer_weights(moe, d, case)
+    logits, x = torch.randn((d.T, d.E), generator=gen(case), device="cuda"), randn((d.T, d.H), case + 60)
+    src = torch.randint(0, 3, (d.T,), generator=gen(case), device="cuda", dtype=torch.int32)
+    local = torch.randperm(d.E, generator=gen(case), device="cuda")[:d.E_local].to(torch.int32)
+    rows, i32 = d.T * d.k, dict(dtype=torch.int32, device="cuda")
+
+    def outputs():
+        return dict(topk_idx=torch.full((d.T, d.k), -7, **i32), topk_w=torch.full((d.T, d.k), -7.0, device="cuda"),
+                    expert_load=torch.full((d.E,), -7, **i32), offsets=torch.full((d.E_local + 1,), -7, **i32),
+                    perm_token=torch.full((rows,), -7, **i32), inv_pos=torch.full((rows,), -7, **i32))
+    ref, got = outputs(), outputs()
+    counts = [torch.zeros((3, d.E), dtype=torch.int64, device="cuda") for _ in range(2)]
+    moe.route(d, logits, ref["topk_idx"], ref["topk_w"])
+    moe.route_stats(d, src, ref["topk_idx"], counts[0], ref["expert_load"])
+    moe.permute(d, ref["topk_idx"], local, None, ref["offsets"], ref["perm_token"], ref["inv_pos"], None,
+                moe.workspace(d, moe.ENTRY_PERMUTE))
+    events = [torch.cuda.Event(enable_timing=True) for _ in range(2 * len(moe.STAGES))]
+    for e in events:
+        e.record()   # (torch makes the handle with the first record)
+    layer = moe.MoeLayerI8(d, q, local)
+    plain = layer.forward(logits, src, x)
+    out = layer.forward(logits, src, x, counts=counts[1], taps=moe.make_taps(**got, events=[e.cuda_event for e in events]))
+    torch.cuda.synchronize()
+    assert torch.equal(out, plain) and torch.equal(*counts)
+    used = ref["offsets"][-1].item()
+    for name in got:
+        n = used if name == "perm_token" else None
+        assert torch.equal(got[name].flatten()[:n], ref[name].flatten()[:n]), name
+    assert all(a.elapsed_time(b) >= 0 for a, b in zip(events, events[1:]))

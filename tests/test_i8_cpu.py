@@ -498,3 +498,34 @@ def test_binding_passes_the_expected_rows(moe, recorded):
     for rows, r in ((None, 0), (7, 7), (0, 0)):
         moe.grouped_linear_i8(40, q, s, o, w, s, y, rows=rows)
         assert next(a._obj for a in recorded[-1][1] if hasattr(a, "_obj")).R == r
+
+
+TAPS = ("topk_idx", "topk_w", "expert_load", "offsets", "perm_token", "inv_pos")
+
+
+def test_forward_binding_checks_taps_and_bias(moe, recorded, monkeypatch):
+    """Extra outputs and the gate's bias are as long as the layer takes them to
+    be, live where it runs, and are kept as long as the structs that point at them."""
+    d, t = _host_layer(moe, 7, 0)
+    d.flags = moe.GATE_SIGMOID
+    w = moe.make_weights_i8(d, _host_weights(moe))
+    sizes = dict(topk_idx=14, topk_w=14, expert_load=8, offsets=6, perm_token=14, inv_pos=14)
+
+    def call(taps=None, gating=None):
+        moe.forward_i8(d, t["logits"], t["src"], t["x"], t["local_experts"], w, t["counts"], t["out"], None, taps=taps, gating=gating)
+    for name in TAPS:
+        dtype = torch.float32 if name == "topk_w" else torch.int32
+        tensor = torch.zeros(sizes[name], dtype=dtype)
+        call(moe.make_taps(**{name: tensor}))
+        assert moe.make_taps(**{name: tensor}).tensors[name] is tensor
+        with pytest.raises(ValueError, match=name):
+            call(moe.make_taps(**{name: tensor[:-1]}))
+    call(moe.make_taps(), moe.gating(torch.zeros(8)))
+    with pytest.raises(ValueError, match="bias"):
+        call(gating=moe.gating(torch.zeros(7)))
+    call(moe.MoeTaps(), moe.MoeGating(None, 1.0, 0, 0))   # filled in by hand
+    seen = []
+    monkeypatch.setattr(moe, "_on_device", lambda stream, *tensors: (seen.extend(tensors), (0, 0))[1])
+    bias, idx = torch.zeros(8), torch.zeros(14, dtype=torch.int32)
+    call(moe.make_taps(topk_idx=idx), moe.gating(bias))
+    assert any(s is bias for s in seen) and any(s is idx for s in seen)
