@@ -144,7 +144,9 @@ enum moe_entry {
     MOE_ENTRY_EXPERT_FFN = 2,
     MOE_ENTRY_FORWARD = 3,
     MOE_ENTRY_EXPERT_FFN_I8 = 4,
-    MOE_ENTRY_FORWARD_I8 = 5
+    MOE_ENTRY_FORWARD_I8 = 5,
+    MOE_ENTRY_EXPERT_FFN_F8 = 6,
+    MOE_ENTRY_FORWARD_F8 = 7
 };
 
 /* Stages of moe_forward, for the optional timing events of moe_taps. */
@@ -463,6 +465,174 @@ int moe_expert_ffn_i8(const moe_dims *dims, const moe_bf16 *x_perm, const int32_
 int moe_forward_i8(const moe_dims *dims, const moe_gating *gating, const float *logits,
                    const int32_t *src, const moe_bf16 *x, const int32_t *local_experts,
                    const moe_weights_i8 *weights, int64_t *counts, moe_bf16 *out,
+                   const moe_taps *taps, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * ---- Norms around the layer -----------------------------------------------
+ *
+ * The end of one block and the beginning of the next, row by row, for blocks
+ * that add to a residual stream h:
+ *   z  = y / sqrt(mean_c y^2 + eps) * (post_weight + weight_add), or y where
+ *        post_weight is NULL
+ *   h' = residual_scale * h + gate * z
+ *   x  = h' / sqrt(mean_c h'^2 + eps) * (weight + weight_add)
+ * in fp32; h' and x are rounded to bf16 once, on their way out, and the
+ * quantised x is made from the fp32 one (as moe_quantize_rows_f8 makes it from
+ * a bf16 one, the quotient rounded to fp32).
+ */
+typedef struct moe_norm {
+    int32_t H;                    /* columns, 1..32768 */
+    const moe_bf16 *weight;       /* [H], nullable: x without weights */
+    const moe_bf16 *post_weight;  /* [H], nullable: y is not normed */
+    float residual_scale, eps, weight_add;
+} moe_norm;
+
+/*
+ * The rows of a call; rows of bf16 may lie any number of values >= H apart and
+ * start anywhere.
+ *   h      [T][H] bf16: the residual stream.
+ *   h_out  [T][H] bf16 out, nullable: h'.  May be h (same stride).
+ *   x      [T][H] bf16 out, nullable: the next block's input.  May be y.
+ *   q, scale  nullable, both or none: x as moe_quantize_rows_f8 lays it out
+ *             (rows ldq bytes apart, a multiple of 16, padded with zeros to 16;
+ *             scale [T][ceil(H/128)] fp32).
+ *   gate   bf16, nullable (1): that of row t and column c at
+ *          gate[t*gate_row + c*gate_col]; gate_col 1 or 0, gate_row 0 where all
+ *          rows share a gate.
+ */
+typedef struct moe_norm_io {
+    const moe_bf16 *h;
+    moe_bf16 *h_out, *x;
+    uint8_t *q;
+    float *scale;
+    const moe_bf16 *gate;
+    int64_t ldh, ldh_out, ldx, ldq, gate_row, gate_col;
+} moe_norm_io;
+
+/*
+ * T rows of it.  y [T][H] bf16, rows ldy values apart; NULL: h' = residual_scale
+ * * h (a block's first norm).  At least one output; no output but those named
+ * above may overlap an input.  T = 0 is a no-op.
+ */
+int moe_norm_rows(const moe_norm *norm, const moe_norm_io *rows, int32_t T,
+                  const moe_bf16 *y, int64_t ldy, void *stream);
+
+/*
+ * ---- Experts in 8-bit floating point --------------------------------------
+ *
+ * The experts' matrices and their inputs in e4m3 (OCP: 4 exponent bits, 3 of the
+ * significand, largest value 448, no infinity), with one fp32 scale for each 128
+ * columns of a row (token) and for each 128 x 128 block of a matrix, counted
+ * from its first row and column; a matrix of N rows and K columns has
+ * ceil(N/128) x ceil(K/128) scales.  A value stands for q * scale; scales may be
+ * any fp32 values.
+ *
+ * Rows of e4m3 lie a multiple of 16 bytes apart and start 16-byte aligned.  A
+ * row of K values that is not a multiple of 16 long goes on with zeros up to
+ * the next multiple, as the quantisers write it (both operands: a NaN there
+ * would count).
+ */
+typedef uint8_t moe_f8;
+
+/*
+ * Rows to e4m3, for activations at every step: for each 128 columns of a row
+ *   a = max |x|;  scale = a / 448;  q = 448 x / a to the nearest e4m3, ties to
+ * even, exactly (no result depends on how fp32 rounds the quotient); scale 0 and
+ * q 0 where a = 0.  128 columns that hold a NaN or an infinity get scale NaN
+ * and q 0.
+ *   x      bf16, row r at x + r*ldx (ldx >= cols values, any alignment).
+ *   q      e4m3 out, row r at q + r*ldq (ldq >= cols, a multiple of 16),
+ *          written up to the next multiple of 16 of cols (zeros past cols).
+ *   scale  [rows][ceil(cols/128)] fp32 out.
+ * rows = 0 is a no-op.  x and q must not overlap.
+ */
+int moe_quantize_rows_f8(int32_t rows, int32_t cols, const moe_bf16 *x, int64_t ldx,
+                         moe_f8 *q, int64_t ldq, float *scale, void *stream);
+
+/*
+ * The same with a scale for each 128 x 128 block, for weights once: G matrices
+ * of `rows` rows one behind the other (row r of matrix g is row g*rows + r).
+ *   scale  [G][ceil(rows/128)][ceil(cols/128)] fp32 out.
+ * G = 0 is a no-op.
+ */
+int moe_quantize_blocks_f8(int32_t G, int32_t rows, int32_t cols, const moe_bf16 *x, int64_t ldx,
+                           moe_f8 *q, int64_t ldq, float *scale, void *stream);
+
+/*
+ * y[r][n] = sum_b x_scale[r][b] w_scale[n/128][b] (sum_c xq[r][c] wq[n][c] over
+ * the 128 columns c of b), in fp32, one rounding to bf16.
+ *   xq [M] rows, x_scale [M][ceil(K/128)], wq [N] rows, w_scale [ceil(N/128)]
+ *   [ceil(K/128)], y [M] rows out.
+ * Uses M, N, K and the strides of moe_linear_dims, within the limits named
+ * there.  M = 0 is a no-op.
+ */
+int moe_linear_f8(const moe_linear_dims *dims, const moe_f8 *xq, const float *x_scale,
+                  const moe_f8 *wq, const float *w_scale, moe_bf16 *y, void *stream);
+
+/*
+ * The same over ragged groups of rows, each with a weight matrix of its own:
+ * rows [offsets[g], offsets[g+1]) of y from those rows of xq, or from
+ * xq[x_rows[r]] (and its scales), and wq[g].  offsets, x_rows, rows outside the
+ * groups and R: as moe_grouped_linear_i8.
+ *   wq  [G][N] rows, w_scale [G][ceil(N/128)][ceil(K/128)].
+ */
+int moe_grouped_linear_f8(const moe_linear_dims *dims, const moe_f8 *xq, const float *x_scale,
+                          const int32_t *x_rows, const int32_t *offsets, const moe_f8 *wq,
+                          const float *w_scale, moe_bf16 *y, void *stream);
+
+/*
+ * Expert weights in e4m3, stacked by local slot as in moe_weights.  Hp, Ip and
+ * Wp are H, I and W = n_shared*I_shared rounded up to multiples of 16; HB, IB and
+ * WB are those in blocks of 128, the last of them maybe short.
+ *   w_gate, w_up   [E_local][I][Hp]    w_down   [E_local][H][Ip]
+ *   s_gate, s_up   [E_local][IB][HB]   s_down   [E_local][HB][IB]   fp32 scales
+ * The shared experts are one FFN of width W (their sum is that FFN): gate and
+ * up stacked, the rows of down side by side.
+ *   sh_gate, sh_up [W][Hp]             sh_down  [H][Wp]
+ *   sh_s_gate, sh_s_up [WB][HB]        sh_s_down [HB][WB]
+ * The shared pointers may be NULL when n_shared == 0.
+ */
+typedef struct moe_weights_f8 {
+    const moe_f8 *w_gate, *w_up, *w_down;
+    const float *s_gate, *s_up, *s_down;
+    const moe_f8 *sh_gate, *sh_up, *sh_down;
+    const float *sh_s_gate, *sh_s_up, *sh_s_down;
+} moe_weights_f8;
+
+/*
+ * moe_expert_ffn on e4m3 experts: rows are quantised as by moe_quantize_rows_f8,
+ * gate and up are products as above (in fp32, not rounded), h = silu(gate) * up
+ * is rounded to bf16 and quantised by row again, and y_perm is the product of
+ * that with down, rounded to bf16.  y_shared (bf16) is the shared FFN of x.
+ * Arguments as moe_expert_ffn's, x_perm and x in bf16; rows of y_perm past
+ * offsets[E_local] are left as they were.
+ *   ws  MOE_ENTRY_EXPERT_FFN_F8 workspace.
+ * Limits as moe_expert_ffn_i8's.
+ */
+int moe_expert_ffn_f8(const moe_dims *dims, const moe_bf16 *x_perm, const int32_t *offsets,
+                      const moe_weights_f8 *weights, const moe_bf16 *x, moe_bf16 *y_perm,
+                      moe_bf16 *y_shared, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * moe_forward on e4m3 experts, with the norms after it as its end: the layer as
+ * there, with moe_expert_ffn_f8's networks.
+ *   x      [T][H] bf16; or NULL, and
+ *   xq, x_scale  the same rows as moe_quantize_rows_f8 or moe_norm_rows leaves
+ *                them (rows H rounded up to 16 bytes apart).  Exactly one of x and
+ *                the pair is given.
+ *   out    [T][H] bf16 out: the weighted sum (an expert's output and the shared
+ *          experts' are each rounded to bf16 before it, as by
+ *          moe_expert_ffn_f8), rounded once.  May be NULL with norm.
+ *   norm, rows  nullable, both or none: moe_norm_rows of that sum, as it is in
+ *          fp32, with norm->H = H.
+ * Stage MOE_STAGE_FFN_UP includes the quantisation of x, MOE_STAGE_FFN_DOWN that of
+ * the hidden rows, MOE_STAGE_COMBINE the norms.
+ *   ws  MOE_ENTRY_FORWARD_F8 workspace.
+ */
+int moe_forward_f8(const moe_dims *dims, const moe_gating *gating, const float *logits,
+                   const int32_t *src, const moe_bf16 *x, const moe_f8 *xq, const float *x_scale,
+                   const int32_t *local_experts, const moe_weights_f8 *weights, int64_t *counts,
+                   moe_bf16 *out, const moe_norm *norm, const moe_norm_io *rows,
                    const moe_taps *taps, void *ws, size_t ws_bytes, void *stream);
 
 /*

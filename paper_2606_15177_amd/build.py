@@ -25,6 +25,8 @@ SOURCES = ["route.hip", "permute.hip", "combine.hip", "ffn_skinny.hip", "ffn_mid
            "moe_abi.hip"]
 # the 8-bit experts
 SOURCES_I8 = ["quant.hip", "gemm_i8.hip", "i8_few.hip", "i8_mid.hip", "i8_tiled.hip"]
+# the experts in 8-bit floating point, and the norms around the layer
+SOURCES_F8 = ["quant_f8.hip", "gemm_f8.hip", "norm.hip"]
 
 CXXFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -67,7 +69,7 @@ def _check_resolved(lib: str) -> None:
 def build(verbose: bool = False) -> str:
     """Compile and link the library; returns its path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
-    sources = SOURCES + SOURCES_I8
+    sources = SOURCES + SOURCES_I8 + SOURCES_F8
     with cf.ThreadPoolExecutor(max_workers=min(len(sources), os.cpu_count() or 1)) as ex:
         objs = list(ex.map(_compile, sources))
     tmp = LIB_PATH + ".tmp"

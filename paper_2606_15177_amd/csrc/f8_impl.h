@@ -1,0 +1,29 @@
+// Shared definitions of the e4m3 product kernels (gemm_f8.hip's launchers choose
+// among them).
+//
+// A product of 128 columns is one MFMA sum that starts from zero; it is scaled by
+// its row's and its matrix block's scales and added to the result in fp32 by
+// ordinary fused multiply-adds: 16 for each 32 x 32 results and 128 columns, beside
+// two MFMAs of 64 cycles.
+//
+// Precision: the f8f6f4 MFMA adds the products of eight neighbouring columns first,
+// aligned to the largest of them, and cuts off what lies 2^-13 below it (found with
+// +1, -1 and a small third product among the eight); those sums and everything after
+// are fp32.  That is 2^-9 of an e4m3 step.  The older fp8 MFMAs run at half its rate.
+#pragma once
+
+#include "i8_impl.h"
+#include "quant_f8_impl.h"
+
+namespace moe {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// Lane l holds 32 bytes of A's row l % 32 and of B's column l % 32, those of half l
+// / 32 of 64 columns (any order within them that is the same in both), and C[8 (i /
+// 4) + 4 (l / 32) + i % 4][l % 32] in element i.
+__device__ __forceinline__ f32x16 mfma_f8(i32x8 a, i32x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+}
+
+}  // namespace moe

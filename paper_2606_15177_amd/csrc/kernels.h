@@ -210,6 +210,78 @@ struct GemmI8Round {
 };
 GemmI8Round round_gemm_i8(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated, int tiles);
 
+// ---- quant_f8.hip ----------------------------------------------------------
+// e4m3 rows with a scale per 128 columns (see moe.h), for r < rows, or r <
+// *n_rows (device) when that is fewer.
+struct QuantF8Args {
+  const uint16_t* x;
+  uint8_t* q;
+  float* scale;
+  const int32_t* n_rows;  // nullable
+  long long ldx, ldq;
+  int rows, cols;
+};
+// a, and b (nullable) in the same launch.
+hipError_t launch_quantize_rows_f8(const QuantF8Args& a, const QuantF8Args* b, hipStream_t st);
+// G matrices of `rows` rows with a scale per 128 x 128 block.
+hipError_t launch_quantize_blocks_f8(int G, int rows, int cols, const uint16_t* x, long long ldx, uint8_t* q, long long ldq,
+                                     float* scale, hipStream_t st);
+bool quantize_blocks_f8_supported(int G, int rows, int cols);
+
+// ---- gemm_f8.hip -----------------------------------------------------------
+// out[r][n] = bf16(sum_b xs[r][b] ws0[g][n/128][b] (sum_{c in b} X[r][c] w0[g][n][c]))
+// for the rows r of group g, b the blocks of 128 columns; with w1, ws1 the
+// gated pair silu(.0) * (.1).  X[r] = x[r], or x[x_rows[r]] (x_count rows of x; an
+// entry outside them counts as a row of zeros), scales along.  Rows are ldx and
+// ldw bytes (multiples of 16) and ldo values apart, and hold zeros from K to the
+// next multiple of 16; groups of weights are N rows apart, scales dense.
+struct GemmF8 {
+  const uint8_t* x;
+  const float* x_scale;
+  const int32_t* x_rows;
+  int x_count;
+  const int32_t* offsets;
+  int static_rows;
+  int groups;
+  const uint8_t *w0, *w1;
+  const float *ws0, *ws1;
+  uint16_t* out;
+  int K, N;
+  long long ldx, ldw, ldo;
+};
+// a over seg (as the expert GEMMs above), and sh (nullable, static rows) in
+// the same launch.
+hipError_t launch_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
+// Host only: whether it accepts these sizes (the pointers are not looked at,
+// but for offsets being null or not).
+bool gemm_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+
+// ---- norm.hip --------------------------------------------------------------
+// The norms around a block (see moe.h): of y, or (inv_pos given) of the weighted
+// sum of expert outputs that launch_combine makes, which also goes to out
+// (nullable).
+struct NormArgs {
+  int T, H;
+  const uint16_t* y;  // nullable
+  long long ldy;
+  const uint16_t *weight, *post_weight;
+  float rho, eps, add;
+  const uint16_t* h;
+  uint16_t *h_out, *x;
+  uint8_t* q;
+  float* scale;
+  const uint16_t* gate;
+  long long ldh, ldho, ldx, ldq, gate_row, gate_col;
+  // the combine
+  int k;
+  const uint16_t *y_perm, *y_shared;
+  const int32_t* inv_pos;
+  const float* topk_w;
+  uint16_t* out;
+};
+constexpr int kNormMaxH = 32768;
+hipError_t launch_norm(const NormArgs& a, hipStream_t st);
+
 // ---- combine.hip -----------------------------------------------------------
 hipError_t launch_combine(int T, int k, int H, const uint16_t* y_perm, const int32_t* inv_pos,
                           const float* topk_w, const uint16_t* y_shared, uint16_t* out,

@@ -132,6 +132,7 @@ ForwardWs carve_forward(const moe_dims* d, size_t ffn_bytes, void* base) {
 }
 
 size_t ffn_i8_ws(const moe_dims* d, bool one_x);
+size_t ffn_f8_ws(const moe_dims* d, bool one_x);
 
 size_t entry_ws(const moe_dims* d, int entry) {
   switch (entry) {
@@ -145,6 +146,10 @@ size_t entry_ws(const moe_dims* d, int entry) {
       return ffn_i8_ws(d, false);
     case MOE_ENTRY_FORWARD_I8:
       return carve_forward(d, ffn_i8_ws(d, true), nullptr).bytes;
+    case MOE_ENTRY_EXPERT_FFN_F8:
+      return ffn_f8_ws(d, false);
+    case MOE_ENTRY_FORWARD_F8:
+      return carve_forward(d, ffn_f8_ws(d, true), nullptr).bytes;
     default:
       return 0;
   }
@@ -225,6 +230,7 @@ int check_ffn_limits(const moe_dims* d, bool rows_indexed) {
 }
 
 int check_ffn_i8_limits(const moe_dims* d, bool one_x);
+int check_ffn_f8_limits(const moe_dims* d, bool one_x);
 
 // The limits of one entry point (0: of every bf16 entry point).
 int check_entry(const moe_dims* d, int entry) {
@@ -233,6 +239,8 @@ int check_entry(const moe_dims* d, int entry) {
   if (s == MOE_OK && (entry == 0 || entry == MOE_ENTRY_FORWARD)) s = check_ffn_limits(d, true);
   if (entry == MOE_ENTRY_EXPERT_FFN_I8 || entry == MOE_ENTRY_FORWARD_I8)
     s = check_ffn_i8_limits(d, entry == MOE_ENTRY_FORWARD_I8);
+  if (entry == MOE_ENTRY_EXPERT_FFN_F8 || entry == MOE_ENTRY_FORWARD_F8)
+    s = check_ffn_f8_limits(d, entry == MOE_ENTRY_FORWARD_F8);
   return s;
 }
 
@@ -346,7 +354,9 @@ int check_ffn_i8_limits(const moe_dims* d, bool one_x) {
   return MOE_OK;
 }
 
-int weights_i8_ok(const moe_dims* d, const moe_weights_i8* w) {
+// Weights of 8 bits with their scales (either kind).
+template <class Weights>
+int weights_8bit_ok(const moe_dims* d, const Weights* w) {
   if (w == nullptr) return MOE_ERR_NULL;
   const void* routed[] = {w->w_gate, w->w_up, w->w_down, w->s_gate, w->s_up, w->s_down};
   const void* shared[] = {w->sh_gate, w->sh_up, w->sh_down, w->sh_s_gate, w->sh_s_up, w->sh_s_down};
@@ -408,6 +418,162 @@ int run_ffn_i8(const moe_dims* d, const uint16_t* x, const int32_t* x_rows, cons
   return MOE_OK;
 }
 
+// ---- the same on e4m3 experts ----
+
+int64_t blocks128(int64_t n) { return (n + 127) / 128; }
+
+// Workspace of the e4m3 expert FFN, as the int8 one's with a scale per 128 columns.
+struct FfnF8Ws {
+  uint8_t *xq, *xq_sh, *hq, *hq_sh;
+  float *xs, *xs_sh, *hs, *hs_sh;
+  uint16_t *h, *h_sh;
+  size_t bytes;
+};
+FfnF8Ws carve_ffn_f8(const moe_dims* d, bool one_x, void* base) {
+  FfnF8Ws w{};
+  unsigned char* p = static_cast<unsigned char*>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    unsigned char* r = p ? p + off : nullptr;
+    off += align_up(bytes);
+    return r;
+  };
+  const size_t T = d->T, rows = T * d->k, shw = sh_width(d);
+  const size_t x_rows = one_x ? T : rows, sh_x = one_x || shw == 0 ? 0 : T, sh_h = shw == 0 ? 0 : T;
+  auto q = [&](size_t r, size_t cols) { return take(r * pad16(cols)); };
+  auto scales = [&](size_t r, size_t cols) { return reinterpret_cast<float*>(take(r * blocks128(cols) * sizeof(float))); };
+  w.xq = q(x_rows, d->H);
+  w.xs = scales(x_rows, d->H);
+  w.xq_sh = q(sh_x, d->H);
+  w.xs_sh = scales(sh_x, d->H);
+  w.h = reinterpret_cast<uint16_t*>(take(rows * d->I * sizeof(uint16_t)));
+  w.hq = q(rows, d->I);
+  w.hs = scales(rows, d->I);
+  w.h_sh = reinterpret_cast<uint16_t*>(take(sh_h * shw * sizeof(uint16_t)));
+  w.hq_sh = q(sh_h, shw);
+  w.hs_sh = scales(sh_h, shw);
+  if (one_x) {
+    w.xq_sh = w.xq;
+    w.xs_sh = w.xs;
+  }
+  w.bytes = off;
+  return w;
+}
+
+size_t ffn_f8_ws(const moe_dims* d, bool one_x) { return carve_ffn_f8(d, one_x, nullptr).bytes; }
+
+// The experts' products, built the same way for the limit check (null
+// pointers) and for the launches.
+struct FfnF8Plan {
+  moe::Segments routed;
+  moe::GemmF8 up, sh_up, dn, sh_dn;
+  bool sh;
+};
+FfnF8Plan plan_ffn_f8(const moe_dims* d, const FfnF8Ws& fw, const int32_t* x_rows, const int32_t* offsets,
+                      const moe_weights_f8& w, uint16_t* y_perm, uint16_t* y_shared) {
+  const int shw = static_cast<int>(sh_width(d));
+  const long long hp = pad16(d->H), ip = pad16(d->I), wp = pad16(shw);
+  FfnF8Plan p{};
+  p.routed = routed_segments(d, offsets);
+  p.up = moe::GemmF8{fw.xq, fw.xs, x_rows, x_rows ? d->T : 0, offsets, 0, d->E_local, w.w_gate, w.w_up, w.s_gate, w.s_up,
+                     fw.h, d->H, d->I, hp, hp, d->I};
+  p.sh_up = moe::GemmF8{fw.xq_sh, fw.xs_sh, nullptr, 0, nullptr, d->T, 1, w.sh_gate, w.sh_up, w.sh_s_gate, w.sh_s_up,
+                        fw.h_sh, d->H, shw, hp, hp, shw};
+  p.dn = moe::GemmF8{fw.hq, fw.hs, nullptr, 0, offsets, 0, d->E_local, w.w_down, nullptr, w.s_down, nullptr,
+                     y_perm, d->I, d->H, ip, ip, d->H};
+  p.sh_dn = moe::GemmF8{fw.hq_sh, fw.hs_sh, nullptr, 0, nullptr, d->T, 1, w.sh_down, nullptr, w.sh_s_down, nullptr,
+                        y_shared, shw, d->H, wp, wp, d->H};
+  p.sh = d->n_shared > 0;
+  return p;
+}
+
+int check_ffn_f8_limits(const moe_dims* d, bool one_x) {
+  if (d->H > kMaxI8K || d->I > kMaxI8K || sh_width(d) > kMaxI8K) return MOE_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(d->T) * d->k > kMaxI8Rows) return MOE_ERR_UNSUPPORTED;
+  if (one_x && static_cast<int64_t>(d->T) * pad16(d->H) > kSpan) return MOE_ERR_UNSUPPORTED;
+  if (d->T == 0) return MOE_OK;
+  static const int32_t some = 0;  // stands for device offsets
+  const FfnF8Plan p = plan_ffn_f8(d, FfnF8Ws{}, nullptr, &some, moe_weights_f8{}, nullptr, nullptr);
+  if (!moe::gemm_f8_supported(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true) ||
+      !moe::gemm_f8_supported(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false))
+    return MOE_ERR_UNSUPPORTED;
+  return MOE_OK;
+}
+
+// The experts' networks on e4m3: x quantised (unless it came so: x NULL), gate/up on
+// it (through x_rows where x holds tokens), the hidden rows quantised, down.
+int run_ffn_f8(const moe_dims* d, const uint16_t* x, const uint8_t* xq, const float* xs, const int32_t* x_rows,
+               const int32_t* offsets, const moe_weights_f8* w, const uint16_t* x_sh, uint16_t* y_perm, uint16_t* y_shared,
+               void* ws, const moe_taps* taps, hipStream_t st) {
+  const bool one_x = x_rows != nullptr;
+  const FfnF8Ws fw = carve_ffn_f8(d, one_x, ws);
+  FfnF8Plan p = plan_ffn_f8(d, fw, x_rows, offsets, *w, y_perm, y_shared);
+  if (!x) {
+    p.up.x = p.sh_up.x = xq;
+    p.up.x_scale = p.sh_up.x_scale = xs;
+  }
+  const int shw = static_cast<int>(sh_width(d)), rows = d->T * d->k;
+  const int32_t* n_rows = offsets + d->E_local;
+  hipError_t e;
+
+  record(taps, 2 * MOE_STAGE_FFN_UP, st);
+  const moe::QuantF8Args qx{x, fw.xq, fw.xs, one_x ? nullptr : n_rows, d->H, p.up.ldx, one_x ? d->T : rows, d->H};
+  const moe::QuantF8Args qx_sh{x_sh, fw.xq_sh, fw.xs_sh, nullptr, d->H, p.up.ldx, d->T, d->H};
+  e = !x ? hipSuccess : moe::launch_quantize_rows_f8(qx, p.sh && !one_x ? &qx_sh : nullptr, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  e = moe::launch_gemm_f8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  record(taps, 2 * MOE_STAGE_FFN_UP + 1, st);
+
+  record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
+  const moe::QuantF8Args qh{fw.h, fw.hq, fw.hs, n_rows, d->I, p.dn.ldx, rows, d->I};
+  const moe::QuantF8Args qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, p.sh_dn.ldx, d->T, shw};
+  e = moe::launch_quantize_rows_f8(qh, p.sh ? &qh_sh : nullptr, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  e = moe::launch_gemm_f8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false, st);
+  if (e != hipSuccess) return MOE_ERR_DEVICE;
+  record(taps, 2 * MOE_STAGE_FFN_DOWN + 1, st);
+  return MOE_OK;
+}
+
+// ---- the norms ----
+
+bool aligned2(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 1u) == 0; }
+constexpr int64_t kMaxNormStride = int64_t{1} << 40;
+
+// The checks of a norm and its rows; T of them.
+int norm_ok(const moe_norm* n, const moe_norm_io* r, int32_t T) {
+  if (n == nullptr || r == nullptr) return MOE_ERR_NULL;
+  if (n->H < 1 || T < 0 || r->ldh < n->H || (r->h_out && r->ldh_out < n->H) || (r->x && r->ldx < n->H) ||
+      (r->q && r->ldq < n->H))
+    return MOE_ERR_DIMS;
+  if (r->gate && (r->gate_row < 0 || r->gate_col < 0 || r->gate_col > 1)) return MOE_ERR_DIMS;
+  if (r->gate && r->gate_row > 0 && r->gate_col == 1 && r->gate_row < n->H) return MOE_ERR_DIMS;
+  if (n->H > moe::kNormMaxH || r->ldh > kMaxNormStride || r->ldh_out > kMaxNormStride || r->ldx > kMaxNormStride ||
+      r->ldq > kMaxNormStride || r->gate_row > kMaxNormStride)
+    return MOE_ERR_UNSUPPORTED;
+  if (r->q && r->ldq % 16 != 0) return MOE_ERR_ALIGN;
+  if ((r->q == nullptr) != (r->scale == nullptr)) return MOE_ERR_NULL;
+  if (T == 0) return MOE_OK;
+  if (!r->h || (!r->h_out && !r->x && !r->q)) return MOE_ERR_NULL;
+  if (!aligned2(r->h) || !aligned2(r->h_out) || !aligned2(r->x) || !aligned2(r->gate) || !aligned2(n->weight) ||
+      !aligned2(n->post_weight) || !aligned16(r->q) || (reinterpret_cast<uintptr_t>(r->scale) & 3u) != 0)
+    return MOE_ERR_ALIGN;
+  return MOE_OK;
+}
+
+moe::NormArgs norm_args(const moe_norm* n, const moe_norm_io* r, int32_t T, const uint16_t* y, int64_t ldy) {
+  moe::NormArgs a{};
+  a.T = T, a.H = n->H;
+  a.y = y, a.ldy = ldy;
+  a.weight = n->weight, a.post_weight = n->post_weight;
+  a.rho = n->residual_scale, a.eps = n->eps, a.add = n->weight_add;
+  a.h = r->h, a.h_out = r->h_out, a.x = r->x, a.q = r->q, a.scale = r->scale, a.gate = r->gate;
+  a.ldh = r->ldh, a.ldho = r->ldh_out, a.ldx = r->ldx, a.ldq = r->ldq;
+  a.gate_row = r->gate_row, a.gate_col = r->gate_col;
+  return a;
+}
+
 // Up to M rows in all groups, R of them expected (where it is a number of rows),
 // evenly spread.  Room for four times the rows, with M and with R as the expected
 // number, us: 64 groups of 20, N 2048, K 4096 130 (tiles) and 84 (items); 32 of 20,
@@ -439,7 +605,7 @@ int linear_ok(const moe_linear_dims* d, bool grouped, bool gathered, const void*
   return MOE_OK;
 }
 
-int forward_io_ok(const moe_dims* d, const float* logits, const int32_t* src, const moe_bf16* x,
+int forward_io_ok(const moe_dims* d, const float* logits, const int32_t* src, const void* x,
                   const int64_t* counts, const moe_bf16* out) {
   if (d->T > 0 && (!logits || !x || !out)) return MOE_ERR_NULL;
   if (counts && d->T > 0 && !src) return MOE_ERR_NULL;
@@ -447,11 +613,12 @@ int forward_io_ok(const moe_dims* d, const float* logits, const int32_t* src, co
   return MOE_OK;
 }
 
-// The layer's launches, ffn(x_rows, offsets) being the experts' networks.
-template <class Ffn>
+// The layer's launches, ffn(x_rows, offsets) being the experts' networks and
+// end(inv_pos, topk_w) what makes the layer's output of theirs.
+template <class Ffn, class End>
 int run_forward(const moe_dims* d, const moe::RouteGating& rg, const float* logits, const int32_t* src,
-                const int32_t* local_experts, int64_t* counts, moe_bf16* out, const moe_taps* taps,
-                const ForwardWs& fw, hipStream_t st, Ffn ffn) {
+                const int32_t* local_experts, int64_t* counts, const moe_taps* taps,
+                const ForwardWs& fw, hipStream_t st, Ffn ffn, End end) {
   int32_t* topk_idx = (taps && taps->topk_idx) ? taps->topk_idx : fw.topk_idx;
   float* topk_w = (taps && taps->topk_w) ? taps->topk_w : fw.topk_w;
   int32_t* offsets = (taps && taps->offsets) ? taps->offsets : fw.offsets;
@@ -500,11 +667,21 @@ int run_forward(const moe_dims* d, const moe::RouteGating& rg, const float* logi
   }
 
   record(taps, 2 * MOE_STAGE_COMBINE, st);
-  e = moe::launch_combine(d->T, d->k, d->H, fw.y_perm, inv_pos, topk_w,
-                          d->n_shared > 0 ? fw.y_shared : nullptr, out, st);
+  e = end(inv_pos, topk_w);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   record(taps, 2 * MOE_STAGE_COMBINE + 1, st);
   return MOE_OK;
+}
+
+template <class Ffn>
+int run_forward(const moe_dims* d, const moe::RouteGating& rg, const float* logits, const int32_t* src,
+                const int32_t* local_experts, int64_t* counts, moe_bf16* out, const moe_taps* taps,
+                const ForwardWs& fw, hipStream_t st, Ffn ffn) {
+  return run_forward(d, rg, logits, src, local_experts, counts, taps, fw, st, ffn,
+                     [&](const int32_t* inv_pos, const float* topk_w) {
+                       return moe::launch_combine(d->T, d->k, d->H, fw.y_perm, inv_pos, topk_w,
+                                                  d->n_shared > 0 ? fw.y_shared : nullptr, out, st);
+                     });
 }
 
 // The workspace of moe_forward_noalloc: a library-owned device array, one
@@ -730,7 +907,7 @@ int moe_expert_ffn_i8(const moe_dims* d, const moe_bf16* x_perm, const int32_t* 
                       void* stream) {
   int s = check_dims(d);
   if (s != MOE_OK) return s;
-  s = weights_i8_ok(d, w);
+  s = weights_8bit_ok(d, w);
   if (s != MOE_OK) return s;
   if (!x_perm || !offsets || !y_perm) return MOE_ERR_NULL;
   if (d->n_shared > 0 && (!x || !y_shared)) return MOE_ERR_NULL;
@@ -753,7 +930,7 @@ int moe_forward_i8(const moe_dims* d, const moe_gating* gating, const float* log
   s = gating_ok(d, gating, &rg);
   if (s != MOE_OK) return s;
   if (!local_experts && d->E_local != d->E) return MOE_ERR_DIMS;
-  s = weights_i8_ok(d, w);
+  s = weights_8bit_ok(d, w);
   if (s != MOE_OK) return s;
   s = forward_io_ok(d, logits, src, x, counts, out);
   if (s != MOE_OK) return s;
@@ -768,6 +945,132 @@ int moe_forward_i8(const moe_dims* d, const moe_gating* gating, const float* log
                      [&](const int32_t* x_rows, const int32_t* offsets) {
                        return run_ffn_i8(d, x, x_rows, offsets, w, x, fw.y_perm, fw.y_shared, fw.ffn_ws, taps, st);
                      });
+}
+
+int moe_norm_rows(const moe_norm* n, const moe_norm_io* r, int32_t T, const moe_bf16* y, int64_t ldy, void* stream) {
+  const int s = norm_ok(n, r, T);
+  if (s != MOE_OK) return s;
+  if (y && ldy < n->H) return MOE_ERR_DIMS;
+  if (y && ldy > kMaxNormStride) return MOE_ERR_UNSUPPORTED;
+  if (!aligned2(y)) return MOE_ERR_ALIGN;
+  moe::NormArgs a = norm_args(n, r, T, y, ldy);
+  if (!y) a.post_weight = a.gate = nullptr;  // nothing to norm or to gate
+  return status(moe::launch_norm(a, static_cast<hipStream_t>(stream)));
+}
+
+int moe_quantize_rows_f8(int32_t rows, int32_t cols, const moe_bf16* x, int64_t ldx, moe_f8* q, int64_t ldq,
+                         float* scale, void* stream) {
+  if (rows < 0 || cols < 1 || ldx < cols || ldq < cols) return MOE_ERR_DIMS;
+  if (ldx > kMaxNormStride || ldq > kMaxNormStride || cols > kIntMax - 256) return MOE_ERR_UNSUPPORTED;
+  if (ldq % 16 != 0) return MOE_ERR_ALIGN;
+  if (rows == 0) return MOE_OK;
+  if (!x || !q || !scale) return MOE_ERR_NULL;
+  if (!aligned2(x) || !aligned16(q) || (reinterpret_cast<uintptr_t>(scale) & 3u) != 0) return MOE_ERR_ALIGN;
+  const moe::QuantF8Args a{x, q, scale, nullptr, ldx, ldq, rows, cols};
+  return status(moe::launch_quantize_rows_f8(a, nullptr, static_cast<hipStream_t>(stream)));
+}
+
+int moe_quantize_blocks_f8(int32_t G, int32_t rows, int32_t cols, const moe_bf16* x, int64_t ldx, moe_f8* q,
+                           int64_t ldq, float* scale, void* stream) {
+  if (G < 0 || rows < 1 || cols < 1 || ldx < cols || ldq < cols) return MOE_ERR_DIMS;
+  if (ldx > kMaxNormStride || ldq > kMaxNormStride || cols > kIntMax - 256 || rows > kIntMax - 256 ||
+      !moe::quantize_blocks_f8_supported(G, rows, cols))
+    return MOE_ERR_UNSUPPORTED;
+  if (ldq % 16 != 0) return MOE_ERR_ALIGN;
+  if (G == 0) return MOE_OK;
+  if (!x || !q || !scale) return MOE_ERR_NULL;
+  if (!aligned2(x) || !aligned16(q) || (reinterpret_cast<uintptr_t>(scale) & 3u) != 0) return MOE_ERR_ALIGN;
+  return status(moe::launch_quantize_blocks_f8(G, rows, cols, x, ldx, q, ldq, scale, static_cast<hipStream_t>(stream)));
+}
+
+int moe_linear_f8(const moe_linear_dims* d, const moe_f8* xq, const float* x_scale, const moe_f8* wq,
+                  const float* w_scale, moe_bf16* y, void* stream) {
+  const int s = linear_ok(d, false, false, xq, x_scale, wq, w_scale, y);
+  if (s != MOE_OK || d->M == 0) return s;
+  const moe::Segments seg = linear_segments(d, nullptr, false);
+  const moe::GemmF8 a{xq, x_scale, nullptr, 0, nullptr, d->M, 1, wq, nullptr, w_scale, nullptr, y,
+                      d->K, d->N, d->ldx, d->ldw, d->ldy};
+  if (!moe::gemm_f8_supported(seg, a, nullptr, false)) return MOE_ERR_UNSUPPORTED;
+  return status(moe::launch_gemm_f8(seg, a, nullptr, false, static_cast<hipStream_t>(stream)));
+}
+
+int moe_grouped_linear_f8(const moe_linear_dims* d, const moe_f8* xq, const float* x_scale, const int32_t* x_rows,
+                          const int32_t* offsets, const moe_f8* wq, const float* w_scale, moe_bf16* y, void* stream) {
+  const int s = linear_ok(d, true, x_rows != nullptr, xq, x_scale, wq, w_scale, y);
+  if (s != MOE_OK || d->M == 0) return s;
+  if (!offsets) return MOE_ERR_NULL;
+  if (((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(x_rows)) & 3u) != 0) return MOE_ERR_ALIGN;
+  const moe::Segments seg = linear_segments(d, offsets, true);
+  const moe::GemmF8 a{xq, x_scale, x_rows, x_rows ? d->X : 0, offsets, 0, d->G, wq, nullptr, w_scale, nullptr, y,
+                      d->K, d->N, d->ldx, d->ldw, d->ldy};
+  if (!moe::gemm_f8_supported(seg, a, nullptr, false)) return MOE_ERR_UNSUPPORTED;
+  return status(moe::launch_gemm_f8(seg, a, nullptr, false, static_cast<hipStream_t>(stream)));
+}
+
+int moe_expert_ffn_f8(const moe_dims* d, const moe_bf16* x_perm, const int32_t* offsets, const moe_weights_f8* w,
+                      const moe_bf16* x, moe_bf16* y_perm, moe_bf16* y_shared, void* ws, size_t ws_bytes,
+                      void* stream) {
+  int s = check_dims(d);
+  if (s != MOE_OK) return s;
+  s = weights_8bit_ok(d, w);
+  if (s != MOE_OK) return s;
+  if (!x_perm || !offsets || !y_perm) return MOE_ERR_NULL;
+  if (d->n_shared > 0 && (!x || !y_shared)) return MOE_ERR_NULL;
+  if (!aligned16(x_perm) || !aligned16(y_perm)) return MOE_ERR_ALIGN;
+  if (d->n_shared > 0 && (!aligned16(x) || !aligned16(y_shared))) return MOE_ERR_ALIGN;
+  s = check_entry(d, MOE_ENTRY_EXPERT_FFN_F8);
+  if (s != MOE_OK) return s;
+  s = check_ws(d, MOE_ENTRY_EXPERT_FFN_F8, ws, ws_bytes);
+  if (s != MOE_OK) return s;
+  if (d->T == 0) return MOE_OK;
+  return run_ffn_f8(d, x_perm, nullptr, nullptr, nullptr, offsets, w, x, y_perm, y_shared, ws, nullptr,
+                    static_cast<hipStream_t>(stream));
+}
+
+int moe_forward_f8(const moe_dims* d, const moe_gating* gating, const float* logits, const int32_t* src,
+                   const moe_bf16* x, const moe_f8* xq, const float* x_scale, const int32_t* local_experts,
+                   const moe_weights_f8* w, int64_t* counts, moe_bf16* out, const moe_norm* norm,
+                   const moe_norm_io* rows, const moe_taps* taps, void* ws, size_t ws_bytes, void* stream) {
+  int s = check_dims(d);
+  if (s != MOE_OK) return s;
+  moe::RouteGating rg;
+  s = gating_ok(d, gating, &rg);
+  if (s != MOE_OK) return s;
+  if (!local_experts && d->E_local != d->E) return MOE_ERR_DIMS;
+  s = weights_8bit_ok(d, w);
+  if (s != MOE_OK) return s;
+  // rows in one form; an output of the layer or its end
+  if ((xq == nullptr) != (x_scale == nullptr) || (norm == nullptr) != (rows == nullptr)) return MOE_ERR_NULL;
+  if (x && xq) return MOE_ERR_DIMS;
+  const void* some_x = x ? static_cast<const void*>(x) : xq;
+  s = forward_io_ok(d, logits, src, some_x, counts, out || !rows ? out : reinterpret_cast<const moe_bf16*>(kAlign));
+  if (s != MOE_OK) return s;
+  if ((reinterpret_cast<uintptr_t>(x_scale) & 3u) != 0) return MOE_ERR_ALIGN;
+  if (norm) {
+    if (norm->H != d->H) return MOE_ERR_DIMS;
+    s = norm_ok(norm, rows, d->T);
+    if (s != MOE_OK) return s;
+  }
+  s = check_entry(d, MOE_ENTRY_FORWARD_F8);
+  if (s != MOE_OK) return s;
+  s = check_ws(d, MOE_ENTRY_FORWARD_F8, ws, ws_bytes);
+  if (s != MOE_OK) return s;
+
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const ForwardWs fw = carve_forward(d, ffn_f8_ws(d, true), ws);
+  const uint16_t* y_shared = d->n_shared > 0 ? fw.y_shared : nullptr;
+  return run_forward(
+      d, rg, logits, src, local_experts, counts, taps, fw, st,
+      [&](const int32_t* x_rows, const int32_t* offsets) {
+        return run_ffn_f8(d, x, xq, x_scale, x_rows, offsets, w, x, fw.y_perm, fw.y_shared, fw.ffn_ws, taps, st);
+      },
+      [&](const int32_t* inv_pos, const float* topk_w) {
+        if (!norm) return moe::launch_combine(d->T, d->k, d->H, fw.y_perm, inv_pos, topk_w, y_shared, out, st);
+        moe::NormArgs a = norm_args(norm, rows, d->T, nullptr, 0);
+        a.k = d->k;
+        a.y_perm = fw.y_perm, a.y_shared = y_shared, a.inv_pos = inv_pos, a.topk_w = topk_w, a.out = out;
+        return moe::launch_norm(a, st);
+      });
 }
 
 // For the tests, which assert the kernel that a shape is meant for (not part

@@ -21,6 +21,7 @@ MOE_OK, MOE_ERR_NULL, MOE_ERR_DIMS, MOE_ERR_UNSUPPORTED = 0, -1, -2, -3
 MOE_ERR_WORKSPACE, MOE_ERR_DEVICE, MOE_ERR_ALIGN = -4, -5, -6
 ENTRY_PERMUTE, ENTRY_EXPERT_FFN, ENTRY_FORWARD = 1, 2, 3
 ENTRY_EXPERT_FFN_I8, ENTRY_FORWARD_I8 = 4, 5
+ENTRY_EXPERT_FFN_F8, ENTRY_FORWARD_F8 = 6, 7
 GATE_SOFTMAX_TOPK, GATE_SOFTMAX, GATE_SIGMOID = 0, 1, 2   # moe_dims.flags
 STAGES = ("route", "permute", "ffn_up", "ffn_down", "combine")
 
@@ -57,6 +58,24 @@ class MoeWeightsI8(C.Structure):
                                           "sh_down", "sh_s_gate", "sh_s_up", "sh_s_down")]
     # of a handle that make_weights_i8 made: its device, and its experts, H, I and shared width
     device_index = sizes = None
+
+
+class MoeWeightsF8(C.Structure):
+    _fields_ = MoeWeightsI8._fields_
+    # of a handle that make_weights_f8 made (see MoeWeightsI8)
+    device_index = sizes = None
+
+
+class MoeNorm(C.Structure):
+    _fields_ = ([("H", C.c_int32), ("weight", C.c_void_p), ("post_weight", C.c_void_p)] +
+                [(n, C.c_float) for n in ("residual_scale", "eps", "weight_add")])
+    tensors = ()   # what norm() was given
+
+
+class MoeNormIo(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("h", "h_out", "x", "q", "scale", "gate")] +
+                [(n, C.c_int64) for n in ("ldh", "ldh_out", "ldx", "ldq", "gate_row", "gate_col")])
+    tensors, shape = (), None   # what norm_io() was given, and (T, H)
 
 
 class MoePlaceDims(C.Structure):
@@ -101,6 +120,14 @@ def _load() -> C.CDLL:
         "moe_expert_ffn_i8": ([dp, vp, vp, C.POINTER(MoeWeightsI8), vp, vp, vp, vp, sz, vp], i32),
         "moe_forward_i8": ([dp, C.POINTER(MoeGating), vp, vp, vp, vp, C.POINTER(MoeWeightsI8), vp, vp,
                             C.POINTER(MoeTaps), vp, sz, vp], i32),
+        "moe_norm_rows": ([C.POINTER(MoeNorm), C.POINTER(MoeNormIo), C.c_int32, vp, C.c_int64, vp], i32),
+        "moe_quantize_rows_f8": ([C.c_int32, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, vp], i32),
+        "moe_quantize_blocks_f8": ([C.c_int32, C.c_int32, C.c_int32, vp, C.c_int64, vp, C.c_int64, vp, vp], i32),
+        "moe_linear_f8": ([C.POINTER(MoeLinearDims), vp, vp, vp, vp, vp, vp], i32),
+        "moe_grouped_linear_f8": ([C.POINTER(MoeLinearDims), vp, vp, vp, vp, vp, vp, vp, vp], i32),
+        "moe_expert_ffn_f8": ([dp, vp, vp, C.POINTER(MoeWeightsF8), vp, vp, vp, vp, sz, vp], i32),
+        "moe_forward_f8": ([dp, C.POINTER(MoeGating), vp, vp, vp, vp, vp, vp, C.POINTER(MoeWeightsF8), vp, vp,
+                            C.POINTER(MoeNorm), C.POINTER(MoeNormIo), C.POINTER(MoeTaps), vp, sz, vp], i32),
         "moe_place_slots": ([C.POINTER(MoePlaceDims), vp], sz),
         "moe_place_experts": ([C.POINTER(MoePlaceDims), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp], i32),
         "moe_window_stats": ([C.POINTER(MoeWindowDims), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp], i32),
@@ -342,8 +369,8 @@ def _rows(t, dtypes, cols: int, what: str):
         raise ValueError(f"{what}: expected rows of at least {cols} values, got {tuple(shape)}")
     if shape[1] != 1 and stride[1] != 1:
         raise ValueError(f"{what}: rows must be contiguous")
-    # one row has no stride to speak of: int8 rows are asked for in whole 16s
-    return t.data_ptr(), stride[0] if shape[0] > 1 else cols if t.dtype == torch.int8 else shape[1]
+    # one row has no stride to speak of: 8-bit rows are asked for in whole 16s
+    return t.data_ptr(), stride[0] if shape[0] > 1 else cols if t.element_size() == 1 else shape[1]
 
 
 def _vec(t, dtypes, n: int, what: str):
@@ -459,6 +486,10 @@ def _weights_i8(d: MoeDims, w, dev: int) -> MoeWeightsI8:
         w = make_weights_i8(d, w)
     elif not isinstance(w, MoeWeightsI8):
         raise TypeError(f"weights: expected int8 ones (make_weights_i8, quantize_weights), not a {type(w).__name__} or bf16 ones")
+    return _handle_fits(d, w, dev)
+
+
+def _handle_fits(d: MoeDims, w, dev: int):
     if w.sizes is not None:
         _need(w.device_index == dev, "weights live on another device")
         EL, H, I, width = w.sizes
@@ -496,6 +527,253 @@ def forward_i8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=
           _opt(src, _I32, 0 if counts is None else d.T, "src"), _vec(x, _BF16, n, "x"),
           _opt(local_experts, _I32, d.E_local, "local_experts"), C.byref(weights), _opt(counts, _I64, d.S * d.E, "counts"),
           _vec(out, _BF16, n, "out"),
+          None if taps is None else C.byref(taps), _ptr(ws), _bytes(ws), st)
+
+
+# ---- norms around the layer ----
+
+_F8 = (torch.float8_e4m3fn,)
+
+
+def _blocks128(n: int) -> int:
+    return (n + 127) // 128
+
+
+def _strided_rows(t, T: int, H: int, what: str):
+    """Pointer and row stride of a bf16 tensor [T, H]."""
+    p, ld = _rows(t, _BF16, H, what)
+    _need(tuple(t.shape) == (T, H), f"{what}: expected [{T}, {H}], got {tuple(t.shape)}")
+    # (rows that lie on one another, as a broadcast's, are none of an output's)
+    _need(ld >= H, f"{what}: rows overlap")
+    return p, ld
+
+
+def norm(H, weight=None, post_weight=None, residual_scale=1.0, eps=1e-6, weight_add=0.0) -> MoeNorm:
+    """The parameters of the norms around a block (moe_norm): bf16 [H] weights of
+    the norm before the next block (None: without weights) and of the one after
+    this block (None: no such norm).  The handle holds the tensors."""
+    n = MoeNorm(H, _opt(weight, _BF16, H, "weight"), _opt(post_weight, _BF16, H, "post_weight"), float(residual_scale), float(eps),
+                float(weight_add))
+    n.tensors = tuple(t for t in (weight, post_weight) if t is not None)
+    return n
+
+
+def norm_io(h, h_out=None, x=None, q=None, scale=None, gate=None) -> MoeNormIo:
+    """The rows of a call (moe_norm_io): h, h_out, x bf16 [T, H] (rows contiguous,
+    any row stride), q float8_e4m3fn [T, H rounded up to 16], scale fp32 [T,
+    ceil(H / 128)], gate bf16 [T or 1, H or 1].  It holds the tensors."""
+    if not isinstance(h, torch.Tensor) or h.dim() != 2:
+        raise ValueError("h: expected a tensor [T, H]")
+    T, H = h.shape
+    _fits("moe_norm_rows", T | H)
+    hp, ldh = _strided_rows(h, T, H, "h")
+    r = MoeNormIo(h=hp, ldh=ldh)
+    if h_out is not None:
+        r.h_out, r.ldh_out = _strided_rows(h_out, T, H, "h_out")
+    if x is not None:
+        r.x, r.ldx = _strided_rows(x, T, H, "x")
+    _need((q is None) == (scale is None), "q and scale: both or none")
+    if q is not None:
+        r.q, r.ldq = _rows(q, _F8, _pad16(H), "q")
+        _need(q.shape[0] == T, "q: expected as many rows as h has")
+        _need(r.ldq >= _pad16(H), "q: rows overlap")
+        r.scale = _vec(scale, _F32, T * _blocks128(H), "scale")
+    if gate is not None:
+        if gate.dtype not in _BF16:
+            raise TypeError(f"gate: dtype {gate.dtype} not in {_BF16}")
+        _need(gate.dim() == 2 and gate.shape[0] in (1, T) and gate.shape[1] in (1, H), f"gate: expected [1 or {T}, 1 or {H}]")
+        _need(gate.shape[1] == 1 or gate.stride(1) == 1, "gate: rows must be contiguous")
+        _need(gate.shape[0] == 1 or gate.shape[1] == 1 or gate.stride(0) >= H, "gate: rows overlap")
+        r.gate = gate.data_ptr()
+        r.gate_row = gate.stride(0) if gate.shape[0] > 1 else 0
+        r.gate_col = 1 if gate.shape[1] > 1 else 0
+    r.tensors = tuple(t for t in (h, h_out, x, q, scale, gate) if t is not None)
+    r.shape = (T, H)
+    return r
+
+
+def norm_rows(norm: MoeNorm, rows: MoeNormIo, y=None, stream=None):
+    """moe_norm_rows: the end of the block that computed y (bf16 [T, H], any row
+    stride; None: a block's first norm) and the beginning of the next."""
+    T, H = rows.shape
+    _need(norm.H == H, f"norm: made for {norm.H} columns, rows have {H}")
+    yp, ldy = (None, 0) if y is None else _strided_rows(y, T, H, "y")
+    dev, st = _on_device(stream, y, *rows.tensors, *norm.tensors)
+    _call(dev, "moe_norm_rows", C.byref(norm), C.byref(rows), T, yp, ldy, st)
+
+
+# ---- experts in 8-bit floating point ----
+
+
+def quantize_rows_f8(x, q=None, scale=None, stream=None):
+    """moe_quantize_rows_f8: e4m3 rows of x, bf16 [rows, cols] (rows contiguous,
+    any row stride), and fp32 scales [rows, ceil(cols / 128)].  q is float8_e4m3fn
+    [rows, cols rounded up to a multiple of 16], padded with zeros; both are
+    allocated when not given.  Returns (q, scale)."""
+    xp, ldx = _rows(x, _BF16, 1, "x")
+    rows, cols = x.shape
+    _fits("moe_quantize_rows_f8", rows | cols)
+    dev, st = _on_device(stream, x, q, scale)
+    if q is None or scale is None:
+        with _allocating_on(stream, dev):
+            q = torch.empty((rows, _pad16(cols)), dtype=_F8[0], device=x.device) if q is None else q
+            scale = torch.empty((rows, _blocks128(cols)), dtype=torch.float32, device=x.device) if scale is None else scale
+    qp, ldq = _rows(q, _F8, _pad16(cols), "q")
+    _need(q.shape[0] == rows, "q: expected as many rows as x has")
+    _call(dev, "moe_quantize_rows_f8", rows, cols, xp, ldx, qp, ldq, _vec(scale, _F32, rows * _blocks128(cols), "scale"), st)
+    return q, scale
+
+
+def _matrices(t, dtypes, G: int, rows: int, cols: int, what: str):
+    """Pointer and row stride of G matrices one behind the other."""
+    _need(tuple(t.shape[:2]) == (G, rows), f"{what}: expected [{G}, {rows}, ...]")
+    flat = t.flatten(0, 1)
+    p, ld = _rows(flat, dtypes, cols, what)
+    _need(p == t.data_ptr(), f"{what}: the matrices must lie one behind the other")
+    return p, ld
+
+
+def quantize_blocks_f8(x, q=None, scale=None, stream=None):
+    """moe_quantize_blocks_f8: e4m3 matrices of x, bf16 [rows, cols] or [G, rows,
+    cols], with an fp32 scale for each 128 x 128 block: [G,] ceil(rows / 128),
+    ceil(cols / 128).  q as quantize_rows_f8's.  Returns (q, scale)."""
+    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
+        raise ValueError("x: expected a tensor [rows, cols] or [G, rows, cols]")
+    one = x.dim() == 2
+    x3 = x.unsqueeze(0) if one else x
+    G, rows, cols = x3.shape
+    _fits("moe_quantize_blocks_f8", G | rows | cols)
+    xp, ldx = _matrices(x3, _BF16, G, rows, 1, "x")
+    dev, st = _on_device(stream, x, q, scale)
+    if q is None or scale is None:
+        with _allocating_on(stream, dev):
+            lead = () if one else (G,)
+            q = torch.empty((*lead, rows, _pad16(cols)), dtype=_F8[0], device=x.device) if q is None else q
+            scale = (torch.empty((*lead, _blocks128(rows), _blocks128(cols)), dtype=torch.float32, device=x.device)
+                     if scale is None else scale)
+    _need(q.dim() == x.dim(), "q: expected as many dimensions as x has")
+    qp, ldq = _matrices(q.unsqueeze(0) if one else q, _F8, G, rows, _pad16(cols), "q")
+    _call(dev, "moe_quantize_blocks_f8", G, rows, cols, xp, ldx, qp, ldq,
+          _vec(scale, _F32, G * _blocks128(rows) * _blocks128(cols), "scale"), st)
+    return q, scale
+
+
+def linear_f8(K, xq, x_scale, wq, w_scale, y, stream=None):
+    """moe_linear_f8: y [M, N] bf16 of xq [M, >= K padded to 16] and wq [N, the
+    same] e4m3 with fp32 scales [M, ceil(K / 128)] and [ceil(N / 128), ceil(K /
+    128)], as quantize_rows_f8 and quantize_blocks_f8 make them.  The rows of xq,
+    wq and y may lie apart."""
+    yp, ldy = _rows(y, _BF16, 1, "y")
+    M, N = y.shape
+    xp, ldx = _rows(xq, _F8, _pad16(K), "xq")
+    wp, ldw = _rows(wq, _F8, _pad16(K), "wq")
+    _need(xq.shape[0] == M and wq.shape[0] == N, "expected as many rows of xq and wq as y has rows and columns")
+    _fits("moe_linear_f8", M | N)
+    dev, st = _on_device(stream, xq, x_scale, wq, w_scale, y)
+    kb = _blocks128(K)
+    _call(dev, "moe_linear_f8", C.byref(MoeLinearDims(M, N, K, 1, 0, ldx, ldw, ldy)), xp, _vec(x_scale, _F32, M * kb, "x_scale"),
+          wp, _vec(w_scale, _F32, _blocks128(N) * kb, "w_scale"), yp, st)
+
+
+def grouped_linear_f8(K, xq, x_scale, offsets, wq, w_scale, y, x_rows=None, stream=None, rows=None):
+    """moe_grouped_linear_f8: rows offsets[g] .. offsets[g+1] of y [M, N] from those
+    of xq (or xq[x_rows[r]]) and wq[g]; wq e4m3 [G, N, >= K padded to 16], w_scale
+    fp32 [G, ceil(N / 128), ceil(K / 128)]; offsets, x_rows and rows as
+    grouped_linear_i8's."""
+    yp, ldy = _rows(y, _BF16, 1, "y")
+    M, N = y.shape
+    if not isinstance(wq, torch.Tensor) or wq.dim() != 3 or wq.shape[1] != N:
+        raise ValueError(f"wq: expected [groups, {N}, ...]")
+    G = wq.shape[0]
+    xp, ldx = _rows(xq, _F8, _pad16(K), "xq")
+    wp, ldw = _matrices(wq, _F8, G, N, _pad16(K), "wq")
+    _need(x_rows is not None or xq.shape[0] == M, "expected as many rows of xq as of y")
+    _fits("moe_grouped_linear_f8", M | N | G | xq.shape[0])
+    dev, st = _on_device(stream, xq, x_scale, offsets, wq, w_scale, y, x_rows)
+    kb = _blocks128(K)
+    _call(dev, "moe_grouped_linear_f8", C.byref(MoeLinearDims(M, N, K, G, xq.shape[0], ldx, ldw, ldy, min(rows or 0, M))), xp,
+          _vec(x_scale, _F32, xq.shape[0] * kb, "x_scale"), None if x_rows is None else _vec(x_rows, _I32, M, "x_rows"),
+          _vec(offsets, _I32, G + 1, "offsets"), wp, _vec(w_scale, _F32, G * _blocks128(N) * kb, "w_scale"), yp, st)
+
+
+def quantize_weights_f8(d: MoeDims, w: dict) -> dict:
+    """The e4m3 weights of a layer (moe_weights_f8's layout) from its bf16 ones
+    (moe_weights' layout), a scale per 128 x 128 block."""
+    EL, H, I = d.E_local, d.H, d.I
+    out = {}
+    for n, rows, cols in (("gate", I, H), ("up", I, H), ("down", H, I)):
+        out["w_" + n], out["s_" + n] = quantize_blocks_f8(w["w_" + n].reshape(EL, rows, cols))
+    if d.n_shared:
+        width = d.n_shared * d.I_shared
+        for n in ("gate", "up"):
+            out["sh_" + n], out["sh_s_" + n] = quantize_blocks_f8(w["sh_" + n].reshape(width, H))
+        down = w["sh_down"].reshape(d.n_shared, H, d.I_shared).permute(1, 0, 2).reshape(H, width)
+        out["sh_down"], out["sh_s_down"] = quantize_blocks_f8(down)
+    return out
+
+
+def make_weights_f8(d: MoeDims, w: dict) -> MoeWeightsF8:
+    """The handle of e4m3 weights (see quantize_weights_f8); it holds the tensors."""
+    EL, H, I, width = d.E_local, d.H, d.I, d.n_shared * d.I_shared
+    hp, ip, wp = _pad16(H), _pad16(I), _pad16(width)
+    hb, ib, wb = _blocks128(H), _blocks128(I), _blocks128(width)
+    need = {"w_gate": (_F8, EL * I * hp), "w_up": (_F8, EL * I * hp), "w_down": (_F8, EL * H * ip),
+            "s_gate": (_F32, EL * ib * hb), "s_up": (_F32, EL * ib * hb), "s_down": (_F32, EL * hb * ib)}
+    if d.n_shared:
+        need.update({"sh_gate": (_F8, width * hp), "sh_up": (_F8, width * hp), "sh_down": (_F8, H * wp),
+                     "sh_s_gate": (_F32, wb * hb), "sh_s_up": (_F32, wb * hb), "sh_s_down": (_F32, hb * wb)})
+    h = MoeWeightsF8(**{n: _vec(w.get(n), t, size, n) for n, (t, size) in need.items()})
+    h.tensors = {n: w[n] for n in need}
+    h.device_index = _on_device(None, *h.tensors.values())[0]
+    h.sizes = (EL, H, I, width)
+    return h
+
+
+def _weights_f8(d: MoeDims, w, dev: int) -> MoeWeightsF8:
+    """As _weights_i8."""
+    if isinstance(w, dict):
+        w = make_weights_f8(d, w)
+    elif not isinstance(w, MoeWeightsF8):
+        raise TypeError(f"weights: expected e4m3 ones (make_weights_f8, quantize_weights_f8), not a {type(w).__name__} or other ones")
+    return _handle_fits(d, w, dev)
+
+
+def expert_ffn_f8(d, x_perm, offsets, weights, x, y_perm, y_shared, ws, stream=None):
+    """moe_expert_ffn_f8; weights as make_weights_f8 returns them, or its dict."""
+    n, n_shared = d.T * d.k * d.H, d.T * d.H if d.n_shared else 0
+    dev, st = _on_device(stream, x_perm, offsets, x, y_perm, y_shared, ws)
+    weights = _weights_f8(d, weights, dev)
+    _call(dev, "moe_expert_ffn_f8", C.byref(d), _vec(x_perm, _BF16, n, "x_perm"), _vec(offsets, _I32, d.E_local + 1, "offsets"),
+          C.byref(weights), _opt(x, _BF16, n_shared, "x"), _vec(y_perm, _BF16, n, "y_perm"),
+          _opt(y_shared, _BF16, n_shared, "y_shared"), _ptr(ws), _bytes(ws), st)
+
+
+def forward_f8(d, logits, src, x, local_experts, weights, counts, out, ws, taps=None, stream=None, gating=None, xq=None,
+               x_scale=None, norm=None, rows=None):
+    """moe_forward_f8; weights as make_weights_f8 returns them, or its dict.  x is
+    bf16 [T, H], or None with the same rows quantised, xq and x_scale, as
+    quantize_rows_f8 and norm_rows leave them (dense).  norm and rows (see norm,
+    norm_io): the layer's output goes through moe_norm_rows; out may then be
+    None."""
+    n = d.T * d.H
+    tapped = {} if taps is None else taps.tensors
+    bias = None if gating is None else gating.bias_tensor
+    _need((norm is None) == (rows is None), "norm and rows: both or none")
+    _need((xq is None) == (x_scale is None) and (x is None) != (xq is None), "rows to the layer: x, or xq and x_scale")
+    ends = () if norm is None else (*norm.tensors, *rows.tensors)
+    dev, st = _on_device(stream, logits, src, x, xq, x_scale, local_experts, counts, out, ws, bias, *tapped.values(), *ends)
+    for name, t in tapped.items():
+        size = {"expert_load": d.E, "offsets": d.E_local + 1}.get(name, d.T * d.k)
+        _need(t.numel() >= size, f"taps: {name}: expected {size} values")
+    _need(bias is None or bias.numel() >= d.E, f"gating: bias: expected {d.E} values")
+    if norm is not None:
+        _need(rows.shape == (d.T, d.H), f"rows: expected [{d.T}, {d.H}], got {rows.shape}")
+    weights = _weights_f8(d, weights, dev)
+    _call(dev, "moe_forward_f8", C.byref(d), _gating_ref(gating), _vec(logits, _F32, d.T * d.E, "logits"),
+          _opt(src, _I32, 0 if counts is None else d.T, "src"), _opt(x, _BF16, n, "x"),
+          _opt(xq, _F8, d.T * _pad16(d.H), "xq"), _opt(x_scale, _F32, d.T * _blocks128(d.H), "x_scale"),
+          _opt(local_experts, _I32, d.E_local, "local_experts"), C.byref(weights), _opt(counts, _I64, d.S * d.E, "counts"),
+          _opt(out, _BF16, n, "out"), None if norm is None else C.byref(norm), None if rows is None else C.byref(rows),
           None if taps is None else C.byref(taps), _ptr(ws), _bytes(ws), st)
 
 
@@ -584,4 +862,31 @@ class MoeLayerI8:
                 out = torch.empty((self.d.T, self.d.H), dtype=torch.bfloat16, device=x.device)
         forward_i8(self.d, logits, src, x, self.local_experts, self._w, counts, out, self.ws if ws is None else ws, taps,
                    stream, gating=self.gating)
+        return out
+
+
+class MoeLayerF8:
+    """MoeLayer on e4m3 experts: the weights are quantised once (bf16 ones, in
+    MoeLayer's layout) or taken as they are (quantize_weights_f8's dict), and
+    forward calls moe_forward_f8.  With `norm` and `rows` the norms after the
+    layer are its end, and it returns None unless `out` is given.  Calls that may
+    overlap each need a workspace of their own: workspace(d, ENTRY_FORWARD_F8),
+    given to forward as `ws`."""
+
+    def __init__(self, d: MoeDims, weights: dict, local_experts=None, device="cuda", gating=None):
+        self.d = d
+        self.gating = gating
+        self.local_experts = local_experts
+        self._w = make_weights_f8(d, weights if "s_gate" in weights else quantize_weights_f8(d, weights))
+        self.ws = workspace(d, ENTRY_FORWARD_F8, device)
+        self.device = device
+
+    def forward(self, logits, src, x=None, counts=None, out=None, taps=None, stream=None, ws=None, xq=None, x_scale=None,
+                norm=None, rows=None):
+        if out is None and norm is None:
+            dev = _on_device(stream, x, xq)[0]
+            with _allocating_on(stream, dev):
+                out = torch.empty((self.d.T, self.d.H), dtype=torch.bfloat16, device=torch.device("cuda", dev))
+        forward_f8(self.d, logits, src, x, self.local_experts, self._w, counts, out, self.ws if ws is None else ws, taps,
+                   stream, gating=self.gating, xq=xq, x_scale=x_scale, norm=norm, rows=rows)
         return out
