@@ -26,7 +26,7 @@ SOURCES = ["route.hip", "permute.hip", "combine.hip", "ffn_skinny.hip", "ffn_mid
 # the 8-bit experts
 SOURCES_I8 = ["quant.hip", "gemm_i8.hip", "i8_few.hip", "i8_mid.hip", "i8_tiled.hip"]
 # the experts in 8-bit floating point, and the norms around the layer
-SOURCES_F8 = ["quant_f8.hip", "gemm_f8.hip", "norm.hip"]
+SOURCES_F8 = ["quant_f8.hip", "gemm_f8.hip", "f8_tiled.hip", "norm.hip"]
 
 CXXFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -38,6 +38,11 @@ CXXFLAGS = [
 ]
 
 
+# matrix instructions write ordinary registers, where the e4m3 products' scaled
+# additions read them (accumulation registers cost a move each)
+EXTRA_FLAGS = {"f8_tiled.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+
+
 def _hipcc() -> str:
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
     cand = os.path.join(rocm, "bin", "hipcc")
@@ -46,7 +51,7 @@ def _hipcc() -> str:
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD_DIR, os.path.splitext(src)[0] + ".o")
-    cmd = [_hipcc(), *CXXFLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [_hipcc(), *CXXFLAGS, *EXTRA_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{r.stdout}\n{r.stderr}")

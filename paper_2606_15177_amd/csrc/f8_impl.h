@@ -26,4 +26,9 @@ __device__ __forceinline__ f32x16 mfma_f8(i32x8 a, i32x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
 }
 
+// a over seg and sh (nullable, static rows) in one launch: tiles of 256 weight rows
+// by 192 rows (K of either past kTiledMinK).
+int tiled_f8_grid(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+hipError_t launch_tiled_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
+
 }  // namespace moe

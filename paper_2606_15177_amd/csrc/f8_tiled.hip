@@ -1,0 +1,531 @@
+// e4m3 products for prefill-sized batches: persistent tiles of 256 weight rows x 192
+// token rows on v_mfma_f32_32x32x64_f8f6f4, operands straight into LDS, one wave per
+// SIMD.
+//
+// TODO-COMMENT
+#include <algorithm>
+#include <type_traits>
+
+#include "f8_impl.h"
+
+namespace moe {
+namespace {
+
+constexpr int kTileW = 256, kTileX = 192;
+constexpr int kTiledThreads = 4 * kWave;
+constexpr int kRow = kF8Block;            // bytes of an LDS row: K per stage
+constexpr int kXPart = kTileX * kRow, kWPart = kTileW * kRow;
+constexpr int kXSlots = 2, kWSlots = 3;
+constexpr int kScaleSlot = 4 * kWave * 4;              // a stage's scales of the rows (the last wave's share unused)
+constexpr int kScales = kXSlots * kXPart + kWSlots * kWPart;
+constexpr int kTops = kScales + kXSlots * kScaleSlot;  // largest magnitudes of a gated tile's rows, by wave
+constexpr int kTiledLds = kTops + 4 * 96 * 4;
+constexpr int kXLoads = 6, kWLoads = 8;   // per part and wave: 8 rows each
+constexpr int kXRows = 8 * kXLoads;       // rows of a wave's X loads
+constexpr int kBlockM = 8;
+
+struct TiledF8 {
+  GemmF8 g, sp;
+  int rows;      // of g's result
+  int sp_tiles;  // tiles of sp, 0: none
+};
+
+// The lane id, recomputed behind a volatile asm: what is derived from it is
+// not hoisted out of the tile loop and holds no register across it.
+__device__ __forceinline__ int opaque_lane() {
+  int ln;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(ln));
+  return ln & 63;  // (known to be small and not negative)
+}
+
+// n / d for 0 <= n, 0 < d, n / d < 2^22 (tiles of a launch): the quotient in
+// fp32 is off by one at most.
+__device__ __forceinline__ int quotient(int n, int d) {
+  int q = static_cast<int>(static_cast<float>(n) * __builtin_amdgcn_rcpf(static_cast<float>(d)));
+  const int r = n - q * d;
+  q += r < 0 ? -1 : r >= d ? 1 : 0;
+  return q;
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+template <bool GATED, int PFX>
+__global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void tiled_f8_kernel(TiledF8 ta) {
+  constexpr int COLS = GATED ? kTileW / 2 : kTileW;  // output columns of a tile
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = lane_id();
+  const int wave = uniform(static_cast<int>(threadIdx.x) / kWave);
+  const int lrow = lane & 31, lhalf = lane >> 5;
+  const GemmF8& a = ta.g;
+
+  // ---- tiles ----
+  // lane L holds the end of the row tiles of groups L + 64 i
+  int mt_end[PFX];
+  int total_mt = 0;
+  if (a.offsets == nullptr) {
+    total_mt = ceil_div(a.static_rows, kTileX);
+#pragma unroll
+    for (int i = 0; i < PFX; ++i) mt_end[i] = 0x7fffffff;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PFX; ++i) {
+      const int g = i * kWave + lane;
+      int cnt = 0;
+      if (g < a.groups) cnt = ceil_div(max(row_at(a.offsets, g + 1, ta.rows) - row_at(a.offsets, g, ta.rows), 0), kTileX);
+      int inc = cnt;
+#pragma unroll
+      for (int off = 1; off < kWave; off <<= 1) {
+        const int o = __shfl_up(inc, off);
+        if (lane >= off) inc += o;
+      }
+      mt_end[i] = g < a.groups ? total_mt + inc : 0x7fffffff;
+      total_mt += __shfl(inc, kWave - 1);
+    }
+    total_mt = uniform(total_mt);
+  }
+  const int tiles_n = ceil_div(a.N, COLS);
+  const int total = ta.sp_tiles + total_mt * tiles_n;
+  const int n_wg = static_cast<int>(gridDim.x);  // a multiple of the XCDs
+  const int xcd = static_cast<int>(blockIdx.x) % kXcds, in_xcd = static_cast<int>(blockIdx.x) / kXcds;
+  const int rounds = total / n_wg, rest = total - rounds * n_wg;
+  // the last round's tiles in `split` parts of 192 / split rows
+  const int split = last_round_parts(rest, n_wg);
+  const int rest_lo = static_cast<int>(static_cast<long long>(rest) * split * xcd / kXcds);
+  const int rest_hi = static_cast<int>(static_cast<long long>(rest) * split * (xcd + 1) / kXcds);
+  int mine = rounds + (in_xcd < rest_hi - rest_lo ? 1 : 0);  // tiles of this workgroup
+
+  struct TileInfo {
+    int sp, g, row_base, m0, rows, nt;  // rows of the tile: m0 .. m0 + rows - 1 of the group
+  };
+  auto tile_info = [&](int i) {
+    const int part = rest_lo + in_xcd;  // (in the last round)
+    const int id = i < rounds ? i * n_wg + xcd * (n_wg / kXcds) + in_xcd : rounds * n_wg + part / split;
+    TileInfo ti;
+    ti.sp = id < ta.sp_tiles ? 1 : 0;
+    int local = id, mg, m, tn = tiles_n;
+    ti.g = 0;
+    ti.row_base = 0;
+    if (ti.sp) {
+      m = ta.sp.static_rows;
+      mg = ceil_div(m, kTileX);
+      tn = ceil_div(ta.sp.N, COLS);
+    } else if (a.offsets == nullptr) {
+      local -= ta.sp_tiles;
+      m = a.static_rows;
+      mg = total_mt;
+    } else {
+      local -= ta.sp_tiles;
+      const int at = quotient(local, tiles_n);  // row tile, of all groups
+      int cnt = 0, lo = 0;
+#pragma unroll
+      for (int k = 0; k < PFX; ++k) {
+        const uint64_t before = __ballot(mt_end[k] <= at);  // the groups that end before it: the first ones
+        const int n = __popcll(before);
+        cnt += n;
+        if (n > 0) lo = __builtin_amdgcn_readlane(mt_end[k], n - 1);
+      }
+      ti.g = cnt;
+      ti.row_base = min(max(load_scalar(a.offsets, cnt), 0), ta.rows);
+      m = min(max(load_scalar(a.offsets, cnt + 1), 0), ta.rows) - ti.row_base;
+      mg = ceil_div(m, kTileX);
+      local -= lo * tiles_n;
+    }
+    // blocks of kBlockM row tiles, the last block with the rest
+    const int b = quotient(local, kBlockM * tn), r = local - b * (kBlockM * tn);
+    const int bm = min(kBlockM, mg - b * kBlockM);
+    ti.nt = quotient(r, bm);
+    ti.m0 = (b * kBlockM + r - ti.nt * bm) * kTileX;
+    ti.rows = min(kTileX, m - ti.m0);
+    if (i == rounds && split > 1) {
+      const int at = part % split * (kTileX / split);
+      ti.m0 += at;
+      ti.rows = min(kTileX / split, ti.rows - at);
+    }
+    ti.sp = uniform(ti.sp);
+    ti.g = uniform(ti.g);
+    ti.row_base = uniform(ti.row_base);
+    ti.m0 = uniform(ti.m0);
+    ti.rows = uniform(ti.rows);
+    ti.nt = uniform(ti.nt);
+    return ti;
+  };
+  auto prob = [&](const TileInfo& ti) -> const GemmF8& { return ti.sp ? ta.sp : ta.g; };
+  auto stages = [&](const TileInfo& ti) { return ceil_div(prob(ti).K, kRow); };
+  auto full_tile = [](const TileInfo& ti) { return ti.rows > kTileX / 2; };
+
+  // (a part past the tile's rows is none)
+  if (mine > rounds && split > 1 && tile_info(rounds).rows <= 0) --mine;
+  if (mine == 0) return;
+
+  // ---- loads ----
+  // Wave w fills rows 48 w .. 48 w + 47 of an X part and 64 w .. 64 w + 63 of a W
+  // part; load i writes rows 8 i + lane / 8 of them, slot lane % 8, with the chunk
+  // that belongs there.  The scales of rows 64 w .. 64 w + 63 go along with X.
+  auto chunk_of = [&](int i, int ln) { return (ln % 8) ^ ((4 * i + ln / 16) % 8); };
+  const bool w_up = GATED && (wave & 1);  // the wave's 64 weight rows are all gate or all up rows
+  __amdgpu_buffer_rsrc_t rs_x, rs_w, rs_s;
+  uint32_t xoff[kXLoads], woff[kWLoads], soff;
+  // the stages to load next, of their tiles, and their slots
+  int x_kb = 0, w_kb = 0, x_nkb = 0, w_nkb = 0, x_bytes = 0, w_bytes = 0, x_slot = 0, w_slot = 0;
+  // Source rows of a tile: of the wave's rows of X and of its scales (read two
+  // tiles ahead: loads still in flight at the K loop's start, if it used them, would
+  // all be waited for there).
+  int xr = 0, xr_next = 0, sr = 0, sr_next = 0;
+  auto x_rows_of = [&](const TileInfo& ti, int row) {
+    const GemmF8& p = prob(ti);
+    int v = 0;
+    if (p.x_rows) v = p.x_rows[ti.row_base + ti.m0 + min(row, ti.rows - 1)];
+    return v;
+  };
+  auto read_rows = [&](const TileInfo& ti, int& xr_to, int& sr_to) {
+    const int ln = opaque_lane();
+    xr_to = x_rows_of(ti, kXRows * wave + ln);
+    sr_to = x_rows_of(ti, kWave * wave + ln);
+  };
+  auto x_setup = [&](const TileInfo& ti, bool live) {
+    const GemmF8& p = prob(ti);
+    const int ln = opaque_lane();
+    const int kb = ceil_div(p.K, kRow);
+    const long long first = p.x_rows ? 0 : ti.row_base + ti.m0;
+    rs_x = rsrc(p.x + first * p.ldx);
+    rs_s = rsrc(p.x_scale + first * kb);
+    auto source = [&](int row, int listed, int stride) {
+      const int own = p.x_rows ? listed : row;
+      const bool in = live && row < ti.rows && (!p.x_rows || static_cast<unsigned>(own) < static_cast<unsigned>(p.x_count));
+      return in ? own * stride : static_cast<int>(kPastEnd);
+    };
+    const int at = ln < kXRows ? source(kXRows * wave + ln, xr, static_cast<int>(p.ldx)) : static_cast<int>(kPastEnd);
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i)
+      xoff[i] = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(4 * (8 * i + ln / 8), at)) + chunk_of(i, ln) * 16;
+    soff = static_cast<uint32_t>(source(kWave * wave + ln, sr, 4 * kb));
+    x_kb = 0;
+    x_nkb = stages(ti);
+    x_bytes = ceil_div(p.K, 16) * 16;
+  };
+  auto w_setup = [&](const TileInfo& ti, bool live) {
+    const GemmF8& p = prob(ti);
+    const int ln = opaque_lane();
+    const int col0 = ti.nt * COLS;
+    rs_w = rsrc((w_up ? p.w1 : p.w0) + (static_cast<long long>(ti.g) * p.N + col0) * p.ldw);
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i) {
+      const int r = 8 * i + ln / 8, col = GATED ? 64 * (wave >> 1) + r : 64 * wave + r;
+      woff[i] = live && col0 + col < p.N ? static_cast<uint32_t>(col) * static_cast<uint32_t>(p.ldw) + chunk_of(i, ln) * 16 : kPastEnd;
+    }
+    w_kb = 0;
+    w_nkb = stages(ti);
+    w_bytes = ceil_div(p.K, 16) * 16;
+  };
+  // (the range check looks at the lane's offset, not at the scalar one)
+  auto load = [&](__amdgpu_buffer_rsrc_t rs, int at, uint32_t off, int kb) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(smem + at), 16, off, kb * kRow, 0, 0);
+  };
+  auto x_load = [&](int i) { load(rs_x, x_slot * kXPart + wave * (kXRows * kRow) + i * 1024, xoff[i], x_kb); };
+  auto s_load = [&]() {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rs_s, (__attribute__((address_space(3))) void*)(smem + kScales + x_slot * kScaleSlot + wave * (kWave * 4)), 4, soff, x_kb * 4, 0, 0);
+  };
+  auto w_load = [&](int i) { load(rs_w, kXSlots * kXPart + w_slot * kWPart + wave * (64 * kRow) + i * 1024, woff[i], w_kb); };
+  // The stream's last stage: chunks past K (the offsets are not used again)
+  auto mask_tail = [&](auto& off, int kb, int bytes) {
+    const int ln = opaque_lane();
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(off) / sizeof(off[0])); ++i)
+      if (kb * kRow + chunk_of(i, ln) * 16 >= bytes) off[i] = kPastEnd;
+  };
+
+  TileInfo cur = tile_info(0), nxt = cur, nn = cur;
+  bool more = false;
+  // (a product has at least four stages here, so the loads, up to three stages
+  // ahead, are on the current tile or the next one)
+  auto x_advance = [&]() {
+    x_slot ^= 1;
+    if (++x_kb == x_nkb) x_setup(nxt, more);
+    else if (x_kb == x_nkb - 1 && x_bytes % kRow != 0) mask_tail(xoff, x_kb, x_bytes);
+  };
+  auto w_advance = [&]() {
+    w_slot = w_slot == kWSlots - 1 ? 0 : w_slot + 1;
+    if (++w_kb == w_nkb) w_setup(nxt, more);
+    else if (w_kb == w_nkb - 1 && w_bytes % kRow != 0) mask_tail(woff, w_kb, w_bytes);
+  };
+
+  // ---- products ----
+  // A wave's block of a tile, in 32 x 32 results: four tiles of weights by three of
+  // rows, the waves two by two; in a tile of up to 96 (64) rows two by three (two),
+  // all waves along the weights.
+  f32x16 acc[4][3];
+  i32x8 xf[3][2], wf[4][2];  // [..][half of the stage's 128 columns]
+  // The lane's place in its row of a part: 32 bytes of a half, as two chunks.
+  int frag[2][2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) frag[h][c] = lrow * kRow + (((4 * h + 2 * lhalf + c) ^ ((lrow / 2) % 8)) << 4);
+  // bytes from a part's start to the block's rows, to its weight tiles and to
+  // the second half of them (gated: the up rows)
+  int x_at = 0, w_at[2] = {0, 0}, s_at = 0;
+  auto wave_row = [&](const TileInfo& ti) { return full_tile(ti) ? 96 * (wave & 1) : 0; };
+  auto place = [&](const TileInfo& ti) {
+    const bool full = full_tile(ti);
+    x_at = wave_row(ti) * kRow;
+    s_at = kScales + 4 * (wave_row(ti) + lrow);
+    w_at[0] = kXSlots * kXPart + kRow * (full ? 128 * (wave >> 1) : GATED ? 128 * (wave >> 1) + 32 * (wave & 1) : 64 * wave);
+    w_at[1] = w_at[0] + kRow * (full || GATED ? 64 : 32);
+  };
+  auto read16 = [&](i32x8& to, int c, int at) {
+    typedef int i32x4_ __attribute__((ext_vector_type(4)));
+    const i32x4_ v = *reinterpret_cast<const i32x4_*>(smem + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[4 * c + i] = v[i];
+  };
+  auto read_x = [&](int tm, int slot) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) read16(xf[tm][h], c, slot * kXPart + x_at + tm * 32 * kRow + frag[h][c]);
+  };
+  auto read_w = [&](auto tn_c, int t, int slot) {
+    constexpr int TN = decltype(tn_c)::value;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) read16(wf[t][h], c, slot * kWPart + w_at[t / (TN / 2)] + t % (TN / 2) * 32 * kRow + frag[h][c]);
+  };
+
+  // Scales of the matrix blocks: lane l holds those of stages l, l + 64, ... (gated:
+  // gate's and up's)
+  float cs[2] = {0.0f, 0.0f}, cs_next[2] = {0.0f, 0.0f};
+  auto read_scales = [&](const TileInfo& ti, int kb0, float (&to)[2]) {
+    const GemmF8& p = prob(ti);
+    const int ln = opaque_lane(), kb = ceil_div(p.K, kRow), nb = ceil_div(p.N, kF8Block);
+    const int block = GATED ? ti.nt : min(2 * ti.nt + (wave >> 1), nb - 1);
+    const long long at = (static_cast<long long>(ti.g) * nb + block) * kb + min(kb0 + ln, kb - 1);
+    to[0] = p.ws0[at];
+    if constexpr (GATED) to[1] = p.ws1[at];
+  };
+
+  auto epilogue = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w, unsigned char* scr) {
+    constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
+    constexpr int TILES = GATED ? TN / 2 : TN;      // of 32 output columns
+    constexpr int PASS = TILES < 2 ? TILES : 2;     // ... stored at a time
+    constexpr int CH = 4 * PASS;                    // 16-byte chunks of a row of them
+    const GemmF8& p = prob(ti);
+    const int row_w = wave_row(ti);
+    uint16_t* out = p.out + static_cast<long long>(ti.row_base + ti.m0 + row_w) * p.ldo;
+    const int rows = ti.rows - row_w;
+    const int ln = opaque_lane();
+    const int erow = ln & 31, eh = ln >> 5;
+    // 32 rows of CH chunks in one of two buffers, chunk c of row r rotated by the row
+    auto place = [&](int buf, int r, int c) { return scr + buf * 4096 + r * (16 * CH) + ((c ^ ((r / (8 / CH)) % CH)) << 4); };
+    auto emit = [&](auto inside) {
+      constexpr bool kInside = decltype(inside)::value;  // every row and column of the wave's block is a result
+#pragma unroll
+      for (int pass = 0; pass < TILES / PASS; ++pass) {
+        // a row tile's results go out while the next one's are computed
+        const int rr = ln / CH, cc = ln % CH;
+        const int col = col_w + 32 * PASS * pass + 8 * cc;
+        uint16_t* at = out + rr * p.ldo + col;
+        auto put = [&](int tm) {
+#pragma unroll
+          for (int q = 0; q < CH / 2; ++q) {
+            const int r = q * (kWave / CH) + rr;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(place(tm & 1, r, cc));
+            uint16_t* to = at + (32 * tm + q * (kWave / CH)) * p.ldo;
+            if constexpr (kInside) *reinterpret_cast<u32x4_a2*>(to) = v;
+            else if (32 * tm + r < rows && col < p.N) store_cols(to, v, col, p.N);
+          }
+        };
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) {
+#pragma unroll
+          for (int h = 0; h < PASS; ++h)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int tn = PASS * pass + h;
+              float o[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int e = 4 * v + i;
+                o[i] = acc[tn][tm][e];
+                if constexpr (GATED) o[i] = silu(o[i]) * acc[tn + TILES][tm][e];
+              }
+              *reinterpret_cast<u32x2*>(place(tm & 1, erow, 4 * h + v) + 8 * eh) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            }
+          if (tm > 0) put(tm - 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        put(TM - 1);
+      }
+    };
+    if (rows >= 32 * TM && col_w + 32 * TILES <= p.N) emit(std::true_type{});
+    else emit(std::false_type{});
+  };
+
+  // ---- the workgroup's tiles ----
+  read_rows(cur, xr, sr);
+  read_scales(cur, 0, cs_next);
+  if (mine > 1) {
+    nxt = tile_info(1);
+    read_rows(nxt, xr_next, sr_next);
+  }
+  x_setup(cur, true);
+  w_setup(cur, true);
+  auto load_part = [&](bool x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (x && i < kXLoads) x_load(i);
+      else if (!x) w_load(i);
+    }
+    if (x) s_load();
+  };
+  load_part(true);
+  x_advance();
+  load_part(false);
+  w_advance();
+  load_part(true);
+  x_advance();
+  load_part(false);
+  w_advance();
+  __builtin_amdgcn_s_waitcnt(wait_vm(kXLoads + 1 + kWLoads));  // own stage-0 loads landed
+  phase_barrier();
+  int xs = 0, ws = 0;  // slots of the stage that is computed
+  for (int i = 0; i < mine; ++i) {
+    const int nkb = stages(cur);
+    const bool full = full_tile(cur);
+    const int col_w = cur.nt * COLS + (full ? 2 * (wave >> 1) : wave) * (COLS / 4);
+    place(cur);
+    more = i + 1 < mine;
+    xr = xr_next;
+    sr = sr_next;
+    cs[0] = cs_next[0];
+    cs[1] = cs_next[1];
+    asm volatile("" : "+v"(xr), "+v"(sr), "+v"(cs[0]), "+v"(cs[1]));  // (waited for here, long after their loads, not in the loop)
+    if (more) read_scales(nxt, 0, cs_next);
+    if (i + 2 < mine) {
+      nn = tile_info(i + 2);
+      read_rows(nn, xr_next, sr_next);
+    }
+#pragma unroll
+    for (int tn = 0; tn < 4; ++tn)
+#pragma unroll
+      for (int tm = 0; tm < 3; ++tm) acc[tn][tm] = f32x16{};
+    auto tile = [&](auto tn_c, auto tm_c) {
+      constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
+      constexpr int TILES = TN * TM;
+#pragma unroll
+      for (int t = 0; t < TN; ++t) read_w(tn_c, t, ws);
+#pragma unroll
+      for (int t = 0; t < TM; ++t) read_x(t, xs);
+      float sx[3];
+#pragma unroll
+      for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs * kScaleSlot + 128 * t);
+      for (int kb = 0; kb < nkb; ++kb) {
+        const int xs1 = xs ^ 1, ws1 = ws == kWSlots - 1 ? 0 : ws + 1;
+        if ((kb & 63) == 0 && kb > 0) {
+          read_scales(cur, kb, cs);
+          asm volatile("" : "+v"(cs[0]), "+v"(cs[1]));  // (waited for here)
+        }
+        float s[2][3];
+        const float s0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(cs[0]), kb & 63));
+        const float s1 = GATED ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(cs[1]), kb & 63)) : s0;
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+          s[0][t] = sx[t] * s0;
+          s[1][t] = GATED ? sx[t] * s1 : s[0][t];
+        }
+        f32x16 part[2];
+        auto scale_add = [&](int t) {  // result t of the stage, in its order
+          const int tm = t / TN, tn = t % TN;
+          const float f = s[GATED && tn >= TN / 2 ? 1 : 0][tm];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[tn][tm][e] = fmaf(part[t & 1][e], f, acc[tn][tm][e]);
+          asm volatile("" : "+v"(acc[tn][tm]));  // (else the additions are gathered at the end of the stage)
+        };
+        constexpr int kTurn = TN * (TM - 1);  // the tiles from which on w fragments are used for the last time
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+          const int tm = t / TN, tn = t % TN;
+          if (t == kTurn) {
+            // The next stage has landed, for all; this one's fragments are in
+            // registers, for all: X of two stages on goes into its slot.
+            w_advance();
+            __builtin_amdgcn_s_waitcnt(wait_vm(kWLoads));
+            __builtin_amdgcn_s_waitcnt(kWaitLds);
+            phase_barrier();
+          }
+          f32x16 zero = {};
+          part[t & 1] = mfma_f8(wf[tn][0], xf[tm][0], zero);
+          part[t & 1] = mfma_f8(wf[tn][1], xf[tm][1], part[t & 1]);
+          if (t > 0) scale_add(t - 1);
+          if (t < kTurn) {
+#pragma unroll
+            for (int q = 0; q < kWLoads; ++q)
+              if (kTurn > 0 && q * kTurn / kWLoads == t) w_load(q);
+          } else {
+            const int u = t - kTurn;
+#pragma unroll
+            for (int q = 0; q < kXLoads; ++q)
+              if (q * TN / kXLoads == u) x_load(q);
+            if (u == 0) s_load();
+            read_w(tn_c, tn, ws1);
+            if (u < TM - 1) read_x(u, xs1);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        scale_add(TILES - 1);
+#pragma unroll
+        for (int u = TN < TM - 1 ? TN : TM - 1; u < TM; ++u) read_x(u, xs1);
+#pragma unroll
+        for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs1 * kScaleSlot + 128 * t);
+        x_advance();
+        xs = xs1;
+        ws = ws1;
+      }
+      epilogue(tn_c, tm_c, cur, col_w, smem + kXSlots * kXPart + (ws == 0 ? kWSlots - 1 : ws - 1) * kWPart + wave * (64 * kRow));
+    };
+    using Two = std::integral_constant<int, 2>;
+    using Three = std::integral_constant<int, 3>;
+    using Four = std::integral_constant<int, 4>;
+    if (full) tile(Four{}, Three{});
+    else if (cur.rows > 64) tile(Two{}, Three{});
+    else tile(Two{}, Two{});
+    cur = nxt;
+    nxt = nn;
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // the dead loads past the last tile: nothing may still write the LDS
+}
+
+template <bool GATED, int PFX>
+hipError_t launch_pfx(const TiledF8& ta, int grid, hipStream_t st) {
+  static unsigned long long lds_set = 0;  // devices with the LDS limit raised
+  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&tiled_f8_kernel<GATED, PFX>), kTiledLds, &lds_set);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((tiled_f8_kernel<GATED, PFX>), dim3(grid), dim3(kTiledThreads), kTiledLds, st, ta);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+static int shared_tiles(const GemmF8* sh, bool gated) {
+  return sh ? ceil_div(sh->static_rows, kTileX) * ceil_div(sh->N, gated ? kTileW / 2 : kTileW) : 0;
+}
+
+// One workgroup per CU (its LDS), a whole number per XCD; fewer where the tiles
+// there may be, in their most parts, are fewer.
+int tiled_f8_grid(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
+  const long long m_tiles = a.offsets ? seg.total_rows / kTileX + std::min(seg.groups, seg.total_rows) : ceil_div(a.static_rows, kTileX);
+  const long long tiles = shared_tiles(sh, gated) + m_tiles * ceil_div(a.N, gated ? kTileW / 2 : kTileW);
+  return static_cast<int>((std::min<long long>(kMaxParts * tiles, device_cu_count()) + kXcds - 1) / kXcds * kXcds);
+}
+
+hipError_t launch_tiled_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st) {
+  const TiledF8 ta{a, sh ? *sh : GemmF8{}, seg.total_rows, shared_tiles(sh, gated)};
+  const int grid = tiled_f8_grid(seg, a, sh, gated);
+  if (grid == 0) return hipSuccess;
+  if (seg.groups <= kWave) return gated ? launch_pfx<true, 1>(ta, grid, st) : launch_pfx<false, 1>(ta, grid, st);
+  if (seg.groups <= 4 * kWave) return gated ? launch_pfx<true, 4>(ta, grid, st) : launch_pfx<false, 4>(ta, grid, st);
+  return gated ? launch_pfx<true, 16>(ta, grid, st) : launch_pfx<false, 16>(ta, grid, st);
+}
+
+}  // namespace moe

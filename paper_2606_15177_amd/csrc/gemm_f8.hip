@@ -98,6 +98,15 @@ int simple_columns(const GemmF8& a, const GemmF8* sh, bool gated) {
   return ceil_div(std::max(a.N, sh ? sh->N : 0), gated ? 64 : 128);
 }
 
+bool takes_tiles(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
+  if (a.K <= kTiledMinK || (sh && sh->K <= kTiledMinK)) return false;
+  const int cols = gated ? 128 : 256;
+  auto tiles = [&](int rows, int N) { return static_cast<long long>(ceil_div(rows, 192)) * ceil_div(N, cols); };
+  if (!a.offsets) return tiles(a.static_rows, a.N) >= 80;
+  if (seg.groups * tiles(seg.mean_rows, a.N) + (sh ? tiles(sh->static_rows, sh->N) : 0) < 128) return false;
+  return seg.mean_rows >= 75;
+}
+
 }  // namespace
 
 bool gemm_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
@@ -105,6 +114,7 @@ bool gemm_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, b
 }
 
 hipError_t launch_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st) {
+  if (takes_tiles(seg, a, sh, gated)) return launch_tiled_f8(seg, a, sh, gated, st);
   PairF8 pa{a, sh ? *sh : GemmF8{}, seg.total_rows};
   if (!a.offsets) pa = PairF8{GemmF8{}, a, 0};  // a product of static rows alone
   const dim3 grid(static_cast<unsigned>(simple_chunks(seg, a, sh)), simple_columns(a, sh, gated));

@@ -604,3 +604,66 @@ def test_outputs_on_a_raw_stream_handle(moe):
         with torch.cuda.stream(side):
             own = [torch.empty(12 << 20, dtype=torch.uint8, device="cuda") for _ in range(4)]
         assert made <= {t.data_ptr() for t in own} and not made & {t.data_ptr() for t in other}
+
+
+# ------------------------------------------ shapes that reach each kernel ----
+
+
+KERNELS = [(2500, 2100, 1700), (5003, 3801, 1501), (5003, 2803, 1501), (16000, 1027, 385), (2600, 2049, 8200), (1900, 2304, 12288),
+           (4200, 2051, 380)]
+
+
+@pytest.mark.parametrize("M,N,K", KERNELS)
+def test_linear_kernels(moe, M, N, K):
+    xq, xs, wq, ws = operands(M, N, K, M + N + K)
+    y = torch.full((M + 1, N), 3.0, dtype=torch.bfloat16, device="cuda")
+    moe.linear_f8(K, xq, xs, wq, ws, y[:M])
+    assert_product(y[:M], xq, xs, wq, ws, K)
+    assert (y[M] == 3.0).all()
+
+
+# Groups: tiles of up to 64, 256 and 1024 groups with their last tiles in each of
+# their forms, empty groups and one that has most rows; items.
+GROUP_KERNELS = [(ragged(8, 350, 1), 2000, 1600), ([0, 64, 65, 96, 97, 192, 193, 2800, 0, 33, 32], 1999, 1603),
+                 (ragged(100, 120, 2, 1500), 513, 2100), (ragged(300, 120, 3), 260, 2100), (ragged(1000, 110, 4), 70, 2052),
+                 (ragged(30, 16, 5, 600), 1003, 900), ([5, 0, 70, 3], 3000, 700), ([2, 0, 1], 1000, 700), ([2, 30, 0, 9], 600, 900),
+                 ([2, 70, 0, 9, 33, 32, 8], 100, 900), ([3, 0, 4, 1], 2500, 500)]
+
+
+@pytest.mark.parametrize("case", range(len(GROUP_KERNELS)))
+@pytest.mark.parametrize("gather", [False, True])
+def test_grouped_kernels(moe, case, gather):
+    sizes, N, K = GROUP_KERNELS[case]
+    check_grouped(moe, sizes, N, K, case, spare=0, gather=max(1, sum(sizes) // 3) if gather else None)
+
+
+FFN_KERNELS = [dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_shared=520), dict(T=3300, H=2104, E=80, k=3, I=136, E_local=70),
+               dict(T=7200, H=2104, E=300, k=4, I=136, E_local=300), dict(T=3000, H=256, E=4, k=2, I=1536, E_local=4),
+               dict(T=2000, H=2048, E=4, k=2, I=1544, E_local=4, n_shared=1, I_shared=1600)]
+
+
+@pytest.mark.parametrize("case", range(len(FFN_KERNELS)))
+def test_ffn_kernels(moe, case):
+    """The layers that tiles and wide items are for, and their bits from one
+    entry point to the other."""
+    d = moe.dims(S=1, **FFN_KERNELS[case])
+    _, q = layer_weights(moe, d, case)
+    w = moe.make_weights_f8(d, q)
+    local = None if d.E_local == d.E else torch.arange(d.E_local, dtype=torch.int32, device="cuda")
+    logits, x = torch.randn((d.T, d.E), generator=gen(case), device="cuda"), randn((d.T, d.H), case)
+    out = moe.MoeLayerF8(d, q, local).forward(logits, None, x)
+    src, counts = torch.zeros(d.T, dtype=torch.int32, device="cuda"), torch.zeros((1, d.E), dtype=torch.int64, device="cuda")
+    assert torch.equal(out, run_steps(moe, d, logits, src, x, local, w, None, counts))
+    # and the experts' rows against 64 bits
+    o = dispatch(moe, d, case)
+    x_perm = randn((d.T * d.k, d.H), case + 50)
+    y = torch.full((d.T * d.k, d.H), 3.0, dtype=torch.bfloat16, device="cuda")
+    ysh = torch.empty((d.T, d.H), dtype=torch.bfloat16, device="cuda") if d.n_shared else None
+    moe.expert_ffn_f8(d, x_perm, torch.tensor(o, dtype=torch.int32, device="cuda"), w, x, y, ysh,
+                      moe.workspace(d, moe.ENTRY_EXPERT_FFN_F8).fill_(0xff))
+    for e in range(0, d.E_local, max(1, d.E_local // 8)):
+        if o[e] < o[e + 1]:
+            assert_ffn(y[o[e]:o[e + 1]], x_perm[o[e]:o[e + 1]], expert(q, e))
+    assert (y[o[-1]:] == 3.0).all()
+    if d.n_shared:
+        assert_ffn(ysh, x, expert(q, None, "sh_", "sh_s_"))
