@@ -165,8 +165,6 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   const bool w_up = GATED && (wave & 1);  // the wave's 64 weight rows are all gate or all up rows
   __amdgpu_buffer_rsrc_t rs_x, rs_w, rs_s;
   uint32_t xoff[kXLoads], woff[kWLoads], soff;
-  // the stages to load next, of their tiles, and their slots
-  int x_kb = 0, w_kb = 0, x_nkb = 0, w_nkb = 0, x_bytes = 0, w_bytes = 0, x_slot = 0, w_slot = 0;
   // Source rows of a tile: of the wave's rows of X and of its scales (read two
   // tiles ahead: loads still in flight at the K loop's start, if it used them, would
   // all be waited for there).
@@ -199,9 +197,6 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     for (int i = 0; i < kXLoads; ++i)
       xoff[i] = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(4 * (8 * i + ln / 8), at)) + chunk_of(i, ln) * 16;
     soff = static_cast<uint32_t>(source(kWave * wave + ln, sr, 4 * kb));
-    x_kb = 0;
-    x_nkb = stages(ti);
-    x_bytes = ceil_div(p.K, 16) * 16;
   };
   auto w_setup = [&](const TileInfo& ti, bool live) {
     const GemmF8& p = prob(ti);
@@ -213,21 +208,18 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
       const int r = 8 * i + ln / 8, col = GATED ? 64 * (wave >> 1) + r : 64 * wave + r;
       woff[i] = live && col0 + col < p.N ? static_cast<uint32_t>(col) * static_cast<uint32_t>(p.ldw) + chunk_of(i, ln) * 16 : kPastEnd;
     }
-    w_kb = 0;
-    w_nkb = stages(ti);
-    w_bytes = ceil_div(p.K, 16) * 16;
   };
   // (the range check looks at the lane's offset, not at the scalar one)
   auto load = [&](__amdgpu_buffer_rsrc_t rs, int at, uint32_t off, int kb) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(smem + at), 16, off, kb * kRow, 0, 0);
   };
-  auto x_load = [&](int i) { load(rs_x, x_slot * kXPart + wave * (kXRows * kRow) + i * 1024, xoff[i], x_kb); };
-  auto s_load = [&]() {
+  auto x_load = [&](int i, int kb, int slot) { load(rs_x, slot * kXPart + wave * (kXRows * kRow) + i * 1024, xoff[i], kb); };
+  auto s_load = [&](int kb, int slot) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        rs_s, (__attribute__((address_space(3))) void*)(smem + kScales + x_slot * kScaleSlot + wave * (kWave * 4)), 4, soff, x_kb * 4, 0, 0);
+        rs_s, (__attribute__((address_space(3))) void*)(smem + kScales + slot * kScaleSlot + wave * (kWave * 4)), 4, soff, kb * 4, 0, 0);
   };
-  auto w_load = [&](int i) { load(rs_w, kXSlots * kXPart + w_slot * kWPart + wave * (64 * kRow) + i * 1024, woff[i], w_kb); };
-  // The stream's last stage: chunks past K (the offsets are not used again)
+  auto w_load = [&](int i, int kb, int slot) { load(rs_w, kXSlots * kXPart + slot * kWPart + wave * (64 * kRow) + i * 1024, woff[i], kb); };
+  // A tile's last stage: chunks past K (the offsets are not used again)
   auto mask_tail = [&](auto& off, int kb, int bytes) {
     const int ln = opaque_lane();
 #pragma unroll
@@ -236,19 +228,6 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   };
 
   TileInfo cur = tile_info(0), nxt = cur, nn = cur;
-  bool more = false;
-  // (a product has at least four stages here, so the loads, up to three stages
-  // ahead, are on the current tile or the next one)
-  auto x_advance = [&]() {
-    x_slot ^= 1;
-    if (++x_kb == x_nkb) x_setup(nxt, more);
-    else if (x_kb == x_nkb - 1 && x_bytes % kRow != 0) mask_tail(xoff, x_kb, x_bytes);
-  };
-  auto w_advance = [&]() {
-    w_slot = w_slot == kWSlots - 1 ? 0 : w_slot + 1;
-    if (++w_kb == w_nkb) w_setup(nxt, more);
-    else if (w_kb == w_nkb - 1 && w_bytes % kRow != 0) mask_tail(woff, w_kb, w_bytes);
-  };
 
   // ---- products ----
   // A wave's block of a tile, in 32 x 32 results: four tiles of weights by three of
@@ -256,41 +235,37 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   // all waves along the weights.
   f32x16 acc[4][3];
   i32x8 xf[3][2], wf[4][2];  // [..][half of the stage's 128 columns]
-  // The lane's place in its row of a part: 32 bytes of a half, as two chunks.
-  int frag[2][2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) frag[h][c] = lrow * kRow + (((4 * h + 2 * lhalf + c) ^ ((lrow / 2) % 8)) << 4);
-  // bytes from a part's start to the block's rows, to its weight tiles and to
-  // the second half of them (gated: the up rows)
-  int x_at = 0, w_at[2] = {0, 0}, s_at = 0;
+  // Where the lane's 32 bytes of either half, two chunks each, lie in the stage that
+  // is read: of the block's first row and first weight row.
+  int x_at[4], w_at[4], s_at = 0;
   auto wave_row = [&](const TileInfo& ti) { return full_tile(ti) ? 96 * (wave & 1) : 0; };
-  auto place = [&](const TileInfo& ti) {
+  auto place = [&](const TileInfo& ti, int xs, int ws) {
     const bool full = full_tile(ti);
-    x_at = wave_row(ti) * kRow;
-    s_at = kScales + 4 * (wave_row(ti) + lrow);
-    w_at[0] = kXSlots * kXPart + kRow * (full ? 128 * (wave >> 1) : GATED ? 128 * (wave >> 1) + 32 * (wave & 1) : 64 * wave);
-    w_at[1] = w_at[0] + kRow * (full || GATED ? 64 : 32);
+    const int row = wave_row(ti), w_row = full ? 128 * (wave >> 1) : GATED ? 128 * (wave >> 1) + 32 * (wave & 1) : 64 * wave;
+    const int lds = static_cast<int>((uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
+    s_at = kScales + 4 * (row + lrow);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int at = lrow * kRow + (((4 * (c / 2) + 2 * lhalf + c % 2) ^ ((lrow / 2) % 8)) << 4);
+      x_at[c] = lds + at + row * kRow + xs * kXPart;
+      w_at[c] = lds + at + w_row * kRow + kXSlots * kXPart + ws * kWPart;
+    }
   };
   auto read16 = [&](i32x8& to, int c, int at) {
-    typedef int i32x4_ __attribute__((ext_vector_type(4)));
-    const i32x4_ v = *reinterpret_cast<const i32x4_*>(smem + at);
+    const i32x4 v = *(const __attribute__((address_space(3))) i32x4*)(static_cast<uintptr_t>(static_cast<uint32_t>(at)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) to[4 * c + i] = v[i];
   };
-  auto read_x = [&](int tm, int slot) {
+  auto read_x = [&](int tm) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) read16(xf[tm][h], c, slot * kXPart + x_at + tm * 32 * kRow + frag[h][c]);
+    for (int c = 0; c < 4; ++c) read16(xf[tm][c / 2], c % 2, x_at[c] + tm * 32 * kRow);
   };
-  auto read_w = [&](auto tn_c, int t, int slot) {
+  // (the second half of the weight tiles: gated the up rows)
+  auto read_w = [&](auto tn_c, int t) {
     constexpr int TN = decltype(tn_c)::value;
+    constexpr int kSecond = (TN == 4 || GATED ? 64 : 32) * kRow;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) read16(wf[t][h], c, slot * kWPart + w_at[t / (TN / 2)] + t % (TN / 2) * 32 * kRow + frag[h][c]);
+    for (int c = 0; c < 4; ++c) read16(wf[t][c / 2], c % 2, w_at[c] + t / (TN / 2) * kSecond + t % (TN / 2) * 32 * kRow);
   };
 
   // Scales of the matrix blocks: lane l holds those of stages l, l + 64, ... (gated:
@@ -371,31 +346,22 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   }
   x_setup(cur, true);
   w_setup(cur, true);
-  auto load_part = [&](bool x) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (x && i < kXLoads) x_load(i);
-      else if (!x) w_load(i);
-    }
-    if (x) s_load();
-  };
-  load_part(true);
-  x_advance();
-  load_part(false);
-  w_advance();
-  load_part(true);
-  x_advance();
-  load_part(false);
-  w_advance();
+  for (int j = 0; j < 2; ++j) {
+#pragma unroll
+    for (int i = 0; i < kXLoads; ++i) x_load(i, j, j);
+    s_load(j, j);
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i) w_load(i, j, j);
+  }
   __builtin_amdgcn_s_waitcnt(wait_vm(kXLoads + 1 + kWLoads));  // own stage-0 loads landed
   phase_barrier();
   int xs = 0, ws = 0;  // slots of the stage that is computed
   for (int i = 0; i < mine; ++i) {
-    const int nkb = stages(cur);
-    const bool full = full_tile(cur);
+    const int nkb = stages(cur), bytes = ceil_div(prob(cur).K, 16) * 16;
+    const bool full = full_tile(cur), more = i + 1 < mine;
     const int col_w = cur.nt * COLS + (full ? 2 * (wave >> 1) : wave) * (COLS / 4);
-    place(cur);
-    more = i + 1 < mine;
+    place(cur, xs, ws);
     xr = xr_next;
     sr = sr_next;
     cs[0] = cs_next[0];
@@ -410,78 +376,104 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     for (int tn = 0; tn < 4; ++tn)
 #pragma unroll
       for (int tm = 0; tm < 3; ++tm) acc[tn][tm] = f32x16{};
+    // Stage j: W of stage j + 2 goes out with its first results, X of stage j + 2
+    // with its last ones, past the barrier.
     auto tile = [&](auto tn_c, auto tm_c) {
       constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
       constexpr int TILES = TN * TM;
+      constexpr int kTurn = TN * (TM - 1);  // the results from which on weight fragments are used for the last time
 #pragma unroll
-      for (int t = 0; t < TN; ++t) read_w(tn_c, t, ws);
+      for (int t = 0; t < TN; ++t) read_w(tn_c, t);
 #pragma unroll
-      for (int t = 0; t < TM; ++t) read_x(t, xs);
-      float sx[3];
+      for (int t = 0; t < TM; ++t) read_x(t);
+      float sx[3], last = 0.0f;  // (last: the scale of the stage's last result)
+      f32x16 part[2] = {f32x16{}, f32x16{}};
 #pragma unroll
       for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs * kScaleSlot + 128 * t);
+      auto scale_add = [&](int t, float f) {  // result t of a stage, in its order
+        const int tm = t / TN, tn = t % TN;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[tn][tm][e] = fmaf(part[t & 1][e], f, acc[tn][tm][e]);
+        asm volatile("" : "+v"(acc[tn][tm]));  // (else the additions are gathered at the end of the stage)
+      };
+      int k2 = 2;  // the stage to load, of this tile or the next one
+#pragma clang loop unroll(disable)
       for (int kb = 0; kb < nkb; ++kb) {
-        const int xs1 = xs ^ 1, ws1 = ws == kWSlots - 1 ? 0 : ws + 1;
-        if ((kb & 63) == 0 && kb > 0) {
-          read_scales(cur, kb, cs);
-          asm volatile("" : "+v"(cs[0]), "+v"(cs[1]));  // (waited for here)
+        if (kb == nkb - 2) {
+          asm volatile("");  // (nothing of it is computed ahead)
+          x_setup(nxt, more);
+          w_setup(nxt, more);
+          k2 = 0;
+        } else if (kb == nkb - 3 && bytes % kRow != 0) {
+          asm volatile("");
+          mask_tail(xoff, k2, bytes);
+          mask_tail(woff, k2, bytes);
         }
-        float s[2][3];
+        const int to_w = ws == 0 ? kWSlots - 1 : ws - 1;
         const float s0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(cs[0]), kb & 63));
         const float s1 = GATED ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(cs[1]), kb & 63)) : s0;
+        float s[2][3];
 #pragma unroll
         for (int t = 0; t < TM; ++t) {
           s[0][t] = sx[t] * s0;
           s[1][t] = GATED ? sx[t] * s1 : s[0][t];
         }
-        f32x16 part[2];
-        auto scale_add = [&](int t) {  // result t of the stage, in its order
-          const int tm = t / TN, tn = t % TN;
-          const float f = s[GATED && tn >= TN / 2 ? 1 : 0][tm];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[tn][tm][e] = fmaf(part[t & 1][e], f, acc[tn][tm][e]);
-          asm volatile("" : "+v"(acc[tn][tm]));  // (else the additions are gathered at the end of the stage)
-        };
-        constexpr int kTurn = TN * (TM - 1);  // the tiles from which on w fragments are used for the last time
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
           const int tm = t / TN, tn = t % TN;
           if (t == kTurn) {
             // The next stage has landed, for all; this one's fragments are in
             // registers, for all: X of two stages on goes into its slot.
-            w_advance();
             __builtin_amdgcn_s_waitcnt(wait_vm(kWLoads));
             __builtin_amdgcn_s_waitcnt(kWaitLds);
             phase_barrier();
+            const int dx = xs == 0 ? kXPart : -kXPart, dw = ws == kWSlots - 1 ? -(kWSlots - 1) * kWPart : kWPart;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              x_at[c] += dx;
+              w_at[c] += dw;
+            }
           }
-          f32x16 zero = {};
-          part[t & 1] = mfma_f8(wf[tn][0], xf[tm][0], zero);
-          part[t & 1] = mfma_f8(wf[tn][1], xf[tm][1], part[t & 1]);
-          if (t > 0) scale_add(t - 1);
+          // the first product, loads and reads, the second one; the additions then
+          // run beside it
+          part[t & 1] = mfma_f8(wf[tn][0], xf[tm][0], f32x16{});
           if (t < kTurn) {
 #pragma unroll
             for (int q = 0; q < kWLoads; ++q)
-              if (kTurn > 0 && q * kTurn / kWLoads == t) w_load(q);
+              if (q * kTurn / kWLoads == t) w_load(q, k2, to_w);
           } else {
             const int u = t - kTurn;
 #pragma unroll
             for (int q = 0; q < kXLoads; ++q)
-              if (q * TN / kXLoads == u) x_load(q);
-            if (u == 0) s_load();
-            read_w(tn_c, tn, ws1);
-            if (u < TM - 1) read_x(u, xs1);
+              if (q * TN / kXLoads == u) x_load(q, k2, xs);
+            if (u == 0) s_load(k2, xs);
+            if (u < TM - 1) read_x(u);
           }
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_barrier(0);
+          part[t & 1] = mfma_f8(wf[tn][1], xf[tm][1], part[t & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+          if (t == 0) scale_add(TILES - 1, last);
+          else scale_add(t - 1, s[GATED && (t - 1) % TN >= TN / 2 ? 1 : 0][(t - 1) / TN]);
+          if (t >= kTurn) read_w(tn_c, tn);
           __builtin_amdgcn_sched_barrier(0);
         }
-        scale_add(TILES - 1);
+        last = s[GATED ? 1 : 0][TM - 1];
+        const int xs1 = xs ^ 1;
 #pragma unroll
-        for (int u = TN < TM - 1 ? TN : TM - 1; u < TM; ++u) read_x(u, xs1);
+        for (int u = TN < TM - 1 ? TN : TM - 1; u < TM; ++u) read_x(u);
 #pragma unroll
         for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs1 * kScaleSlot + 128 * t);
-        x_advance();
         xs = xs1;
-        ws = ws1;
+        ws = ws == kWSlots - 1 ? 0 : ws + 1;
+        ++k2;
+        if (((kb + 1) & 63) == 0 && kb + 1 < nkb) {
+          read_scales(cur, kb + 1, cs);
+          asm volatile("" : "+v"(cs[0]), "+v"(cs[1]));  // (waited for here)
+        }
       }
+      scale_add(TILES - 1, last);
       epilogue(tn_c, tm_c, cur, col_w, smem + kXSlots * kXPart + (ws == 0 ? kWSlots - 1 : ws - 1) * kWPart + wave * (64 * kRow));
     };
     using Two = std::integral_constant<int, 2>;
