@@ -29,6 +29,9 @@ __device__ __forceinline__ f32x16 mfma_f8(i32x8 a, i32x8 b, f32x16 c) {
 // a over seg and sh (nullable, static rows) in one launch: tiles of 256 weight rows
 // by 192 rows (K of either past kTiledMinK).
 int tiled_f8_grid(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+hipError_t launch_items_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
+Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+long long items_f8_blocks(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 hipError_t launch_tiled_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
 
 }  // namespace moe
