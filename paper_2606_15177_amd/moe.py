@@ -541,11 +541,13 @@ def _blocks128(n: int) -> int:
 
 def _strided_rows(t, T: int, H: int, what: str):
     """Pointer and row stride of a bf16 tensor [T, H]."""
-    p, ld = _rows(t, _BF16, H, what)
-    _need(tuple(t.shape) == (T, H), f"{what}: expected [{T}, {H}], got {tuple(t.shape)}")
-    # (rows that lie on one another, as a broadcast's, are none of an output's)
-    _need(ld >= H, f"{what}: rows overlap")
-    return p, ld
+    if isinstance(t, torch.Tensor) and t.dtype in _BF16 and t.shape == (T, H):
+        row, col = t.stride()
+        if (col == 1 or H == 1) and (row >= H or T == 1):
+            return t.data_ptr(), row if T > 1 else H
+    _rows(t, _BF16, H, what)   # (says what is wrong with its rows)
+    _need(t.shape == (T, H), f"{what}: expected [{T}, {H}], got {tuple(t.shape)}")
+    raise ValueError(f"{what}: rows overlap")
 
 
 def norm(H, weight=None, post_weight=None, residual_scale=1.0, eps=1e-6, weight_add=0.0) -> MoeNorm:
@@ -561,34 +563,45 @@ def norm(H, weight=None, post_weight=None, residual_scale=1.0, eps=1e-6, weight_
 def norm_io(h, h_out=None, x=None, q=None, scale=None, gate=None) -> MoeNormIo:
     """The rows of a call (moe_norm_io): h, h_out, x bf16 [T, H] (rows contiguous,
     any row stride), q float8_e4m3fn [T, H rounded up to 16], scale fp32 [T,
-    ceil(H / 128)], gate bf16 [T or 1, H or 1].  It holds the tensors."""
+    ceil(H / 128)], gate bf16 [T or 1, H or 1].  It holds the tensors; a caller whose
+    buffers stay keeps it."""
     if not isinstance(h, torch.Tensor) or h.dim() != 2:
         raise ValueError("h: expected a tensor [T, H]")
     T, H = h.shape
     _fits("moe_norm_rows", T | H)
     hp, ldh = _strided_rows(h, T, H, "h")
-    r = MoeNormIo(h=hp, ldh=ldh)
+    tensors = [h]
+    op = xp = qp = sp = gp = None
+    ldo = ldx = ldq = gate_row = gate_col = 0
     if h_out is not None:
-        r.h_out, r.ldh_out = _strided_rows(h_out, T, H, "h_out")
+        op, ldo = _strided_rows(h_out, T, H, "h_out")
+        tensors.append(h_out)
     if x is not None:
-        r.x, r.ldx = _strided_rows(x, T, H, "x")
-    _need((q is None) == (scale is None), "q and scale: both or none")
-    if q is not None:
-        r.q, r.ldq = _rows(q, _F8, _pad16(H), "q")
+        xp, ldx = _strided_rows(x, T, H, "x")
+        tensors.append(x)
+    if q is not None or scale is not None:
+        _need(q is not None and scale is not None, "q and scale: both or none")
+        qp, ldq = _rows(q, _F8, _pad16(H), "q")
         _need(q.shape[0] == T, "q: expected as many rows as h has")
-        _need(r.ldq >= _pad16(H), "q: rows overlap")
-        r.scale = _vec(scale, _F32, T * _blocks128(H), "scale")
+        _need(ldq >= _pad16(H), "q: rows overlap")
+        if not isinstance(scale, torch.Tensor) or scale.dtype not in _F32:
+            raise TypeError("scale: expected an fp32 tensor")
+        _need(scale.numel() >= T * _blocks128(H) and scale.is_contiguous(), "scale: expected [T, ceil(H / 128)], contiguous")
+        sp = scale.data_ptr()
+        tensors += (q, scale)
     if gate is not None:
-        if gate.dtype not in _BF16:
-            raise TypeError(f"gate: dtype {gate.dtype} not in {_BF16}")
-        _need(gate.dim() == 2 and gate.shape[0] in (1, T) and gate.shape[1] in (1, H), f"gate: expected [1 or {T}, 1 or {H}]")
-        _need(gate.shape[1] == 1 or gate.stride(1) == 1, "gate: rows must be contiguous")
-        _need(gate.shape[0] == 1 or gate.shape[1] == 1 or gate.stride(0) >= H, "gate: rows overlap")
-        r.gate = gate.data_ptr()
-        r.gate_row = gate.stride(0) if gate.shape[0] > 1 else 0
-        r.gate_col = 1 if gate.shape[1] > 1 else 0
-    r.tensors = tuple(t for t in (h, h_out, x, q, scale, gate) if t is not None)
-    r.shape = (T, H)
+        if not isinstance(gate, torch.Tensor) or gate.dtype not in _BF16:
+            raise TypeError("gate: expected a bf16 tensor")
+        if gate.dim() != 2 or gate.shape[0] not in (1, T) or gate.shape[1] not in (1, H):
+            raise ValueError(f"gate: expected [1 or {T}, 1 or {H}]")
+        rows, cols = gate.shape
+        row, col = gate.stride()
+        _need(cols == 1 or col == 1, "gate: rows must be contiguous")
+        _need(rows == 1 or cols == 1 or row >= H, "gate: rows overlap")
+        gp, gate_row, gate_col = gate.data_ptr(), row if rows > 1 else 0, 1 if cols > 1 else 0
+        tensors.append(gate)
+    r = MoeNormIo(hp, op, xp, qp, sp, gp, ldh, ldo, ldx, ldq, gate_row, gate_col)
+    r.tensors, r.shape = tensors, (T, H)
     return r
 
 
@@ -596,7 +609,8 @@ def norm_rows(norm: MoeNorm, rows: MoeNormIo, y=None, stream=None):
     """moe_norm_rows: the end of the block that computed y (bf16 [T, H], any row
     stride; None: a block's first norm) and the beginning of the next."""
     T, H = rows.shape
-    _need(norm.H == H, f"norm: made for {norm.H} columns, rows have {H}")
+    if norm.H != H:
+        raise ValueError(f"norm: made for {norm.H} columns, rows have {H}")
     yp, ldy = (None, 0) if y is None else _strided_rows(y, T, H, "y")
     dev, st = _on_device(stream, y, *rows.tensors, *norm.tensors)
     _call(dev, "moe_norm_rows", C.byref(norm), C.byref(rows), T, yp, ldy, st)

@@ -71,7 +71,8 @@ def check(moe, T, H, seed, post=True, gate="none", pre=True, quant=True, rho=1.0
 
 
 @pytest.mark.parametrize("T,H", [(1, 1), (1, 7), (3, 8), (2, 64), (5, 129), (4, 511), (4, 512), (3, 513), (2, 1000), (70, 2048), (3, 2049),
-                                 (1, 7168), (9, 4099), (3, 8192), (2, 8193), (1, 16384), (2, 20001), (2, 32768), (1500, 264)])
+                                 (1, 7168), (9, 4099), (3, 8192), (2, 8193), (1, 16384), (2, 20001), (2, 32768), (1500, 264),
+                                 (700, 4096), (700, 3001), (600, 7168), (530, 8190), (600, 16000)])
 def test_norm_sizes(moe, T, H):
     check(moe, T, H, T + H)
 
@@ -172,7 +173,8 @@ def test_norm_in_a_graph_and_on_streams(moe):
 
 
 ENDS = [dict(T=1, H=264, E=4, k=2, I=136, E_local=4), dict(T=9, H=1000, E=12, k=3, I=264, E_local=5, n_shared=1, I_shared=72),
-        dict(T=300, H=2056, E=8, k=8, I=136, E_local=8, n_shared=2, I_shared=136), dict(T=70, H=8200, E=4, k=1, I=64, E_local=1)]
+        dict(T=300, H=2056, E=8, k=8, I=136, E_local=8, n_shared=2, I_shared=136), dict(T=70, H=8200, E=4, k=1, I=64, E_local=1),
+        dict(T=600, H=7168, E=4, k=2, I=64, E_local=2), dict(T=7, H=20000, E=8, k=8, I=64, E_local=6), dict(T=520, H=2504, E=32, k=32, I=64, E_local=32)]
 
 
 def layer_of(moe, d, seed):
