@@ -26,6 +26,12 @@ __device__ __forceinline__ f32x16 mfma_f8(i32x8 a, i32x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
 }
 
+// Lane l holds 32 bytes of A's row l % 16 and of B's column l % 16, those of quarter l
+// / 16 of 128 columns, and C[4 (l / 16) + i][l % 16] in element i.
+__device__ __forceinline__ f32x4 mfma_f8_16(i32x8 a, i32x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+}
+
 // a over seg and sh (nullable, static rows) in one launch: tiles of 256 weight rows
 // by 192 rows (K of either past kTiledMinK).
 int tiled_f8_grid(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);

@@ -1,10 +1,11 @@
 // e4m3 products for prefill-sized batches: persistent tiles of 256 weight rows x 192
-// token rows on v_mfma_f32_32x32x64_f8f6f4, operands straight into LDS, one wave per
+// token rows on v_mfma_f32_16x16x128_f8f6f4, operands straight into LDS, one wave per
 // SIMD.
 //
 // TODO-COMMENT
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "f8_impl.h"
 
@@ -47,6 +48,12 @@ __device__ __forceinline__ int quotient(int n, int d) {
   return q;
 }
 
+// f(0), f(1), ...: a loop of more steps than the compiler unrolls.
+template <class F, int... I>
+__device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <bool GATED, int PFX>
@@ -55,7 +62,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = lane_id();
   const int wave = uniform(static_cast<int>(threadIdx.x) / kWave);
-  const int lrow = lane & 31, lhalf = lane >> 5;
+  const int lrow = lane & 15, lquad = lane >> 4;
   const GemmF8& a = ta.g;
 
   // ---- tiles ----
@@ -230,14 +237,16 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
   TileInfo cur = tile_info(0), nxt = cur, nn = cur;
 
   // ---- products ----
-  // A wave's block of a tile, in 32 x 32 results: four tiles of weights by three of
-  // rows, the waves two by two; in a tile of up to 96 (64) rows two by three (two),
+  // A wave's block of a tile, in 16 x 16 results: eight tiles of weights by six of
+  // rows, the waves two by two; in a tile of up to 96 (64) rows four by six (four),
   // all waves along the weights.
-  f32x16 acc[4][3];
-  i32x8 xf[3][2], wf[4][2];  // [..][half of the stage's 128 columns]
-  // Where the lane's 32 bytes of either half, two chunks each, lie in the stage that
-  // is read: of the block's first row and first weight row.
-  int x_at[4], w_at[4], s_at = 0;
+  f32x4 acc[8][6];
+  i32x8 xf[6], wf[8];
+  // Where the lane's 32 bytes, two chunks, lie in the stage that is read: of the
+  // block's first row and first weight row.  (Which columns a lane quarter takes is
+  // free, the same in both operands: with chunks q and q + 4 the 16 lanes of an LDS
+  // access touch all banks once, with 2 q and 2 q + 1 half of them twice.)
+  int x_at[2], w_at[2], s_at = 0;
   auto wave_row = [&](const TileInfo& ti) { return full_tile(ti) ? 96 * (wave & 1) : 0; };
   auto place = [&](const TileInfo& ti, int xs, int ws) {
     const bool full = full_tile(ti);
@@ -245,27 +254,26 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     const int lds = static_cast<int>((uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
     s_at = kScales + 4 * (row + lrow);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const int at = lrow * kRow + (((4 * (c / 2) + 2 * lhalf + c % 2) ^ ((lrow / 2) % 8)) << 4);
-      x_at[c] = lds + at + row * kRow + xs * kXPart;
-      w_at[c] = lds + at + w_row * kRow + kXSlots * kXPart + ws * kWPart;
+    for (int c = 0; c < 2; ++c) {
+      const int at = lds + lrow * kRow + (((lquad + 4 * c) ^ ((lrow / 2) % 8)) << 4);
+      x_at[c] = at + row * kRow + xs * kXPart;
+      w_at[c] = at + w_row * kRow + kXSlots * kXPart + ws * kWPart;
     }
   };
-  auto read16 = [&](i32x8& to, int c, int at) {
-    const i32x4 v = *(const __attribute__((address_space(3))) i32x4*)(static_cast<uintptr_t>(static_cast<uint32_t>(at)));
+  auto read32 = [&](i32x8& to, const int (&at)[2], int off) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) to[4 * c + i] = v[i];
-  };
-  auto read_x = [&](int tm) {
+    for (int c = 0; c < 2; ++c) {
+      const i32x4 v = *(const __attribute__((address_space(3))) i32x4*)(static_cast<uintptr_t>(static_cast<uint32_t>(at[c] + off)));
 #pragma unroll
-    for (int c = 0; c < 4; ++c) read16(xf[tm][c / 2], c % 2, x_at[c] + tm * 32 * kRow);
+      for (int i = 0; i < 4; ++i) to[4 * c + i] = v[i];
+    }
   };
+  auto read_x = [&](int tm) { read32(xf[tm], x_at, tm * 16 * kRow); };
   // (the second half of the weight tiles: gated the up rows)
   auto read_w = [&](auto tn_c, int t) {
     constexpr int TN = decltype(tn_c)::value;
-    constexpr int kSecond = (TN == 4 || GATED ? 64 : 32) * kRow;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) read16(wf[t][c / 2], c % 2, w_at[c] + t / (TN / 2) * kSecond + t % (TN / 2) * 32 * kRow);
+    constexpr int kSecond = (TN == 8 || GATED ? 64 : 32) * kRow;
+    read32(wf[t], w_at, t / (TN / 2) * kSecond + t % (TN / 2) * 16 * kRow);
   };
 
   // Scales of the matrix blocks: lane l holds those of stages l, l + 64, ... (gated:
@@ -282,58 +290,58 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
 
   auto epilogue = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w, unsigned char* scr) {
     constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
-    constexpr int TILES = GATED ? TN / 2 : TN;      // of 32 output columns
-    constexpr int PASS = TILES < 2 ? TILES : 2;     // ... stored at a time
-    constexpr int CH = 4 * PASS;                    // 16-byte chunks of a row of them
+    constexpr int TILES = GATED ? TN / 2 : TN;      // of 16 output columns
+    constexpr int PASS = TILES < 4 ? TILES : 4;     // ... stored at a time
+    constexpr int CH = 2 * PASS;                    // 16-byte chunks of a row of them
     const GemmF8& p = prob(ti);
     const int row_w = wave_row(ti);
     uint16_t* out = p.out + static_cast<long long>(ti.row_base + ti.m0 + row_w) * p.ldo;
     const int rows = ti.rows - row_w;
     const int ln = opaque_lane();
-    const int erow = ln & 31, eh = ln >> 5;
+    const int erow = ln & 15, eq = ln >> 4;
     // 32 rows of CH chunks in one of two buffers, chunk c of row r rotated by the row
     auto place = [&](int buf, int r, int c) { return scr + buf * 4096 + r * (16 * CH) + ((c ^ ((r / (8 / CH)) % CH)) << 4); };
     auto emit = [&](auto inside) {
       constexpr bool kInside = decltype(inside)::value;  // every row and column of the wave's block is a result
 #pragma unroll
       for (int pass = 0; pass < TILES / PASS; ++pass) {
-        // a row tile's results go out while the next one's are computed
+        // 32 rows' results go out while the next ones' are computed
         const int rr = ln / CH, cc = ln % CH;
-        const int col = col_w + 32 * PASS * pass + 8 * cc;
+        const int col = col_w + 16 * PASS * pass + 8 * cc;
         uint16_t* at = out + rr * p.ldo + col;
-        auto put = [&](int tm) {
+        auto put = [&](int m) {
 #pragma unroll
           for (int q = 0; q < CH / 2; ++q) {
             const int r = q * (kWave / CH) + rr;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(place(tm & 1, r, cc));
-            uint16_t* to = at + (32 * tm + q * (kWave / CH)) * p.ldo;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(place(m & 1, r, cc));
+            uint16_t* to = at + (32 * m + q * (kWave / CH)) * p.ldo;
             if constexpr (kInside) *reinterpret_cast<u32x4_a2*>(to) = v;
-            else if (32 * tm + r < rows && col < p.N) store_cols(to, v, col, p.N);
+            else if (32 * m + r < rows && col < p.N) store_cols(to, v, col, p.N);
           }
         };
 #pragma unroll
-        for (int tm = 0; tm < TM; ++tm) {
+        for (int m = 0; m < TM / 2; ++m) {
 #pragma unroll
-          for (int h = 0; h < PASS; ++h)
+          for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const int tn = PASS * pass + h;
+            for (int h = 0; h < PASS; ++h) {
+              const int tn = PASS * pass + h, tm = 2 * m + t;
               float o[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int e = 4 * v + i;
-                o[i] = acc[tn][tm][e];
-                if constexpr (GATED) o[i] = silu(o[i]) * acc[tn + TILES][tm][e];
+                o[i] = acc[tn][tm][i];
+                if constexpr (GATED) o[i] = silu(o[i]) * acc[tn + TILES][tm][i];
               }
-              *reinterpret_cast<u32x2*>(place(tm & 1, erow, 4 * h + v) + 8 * eh) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+              *reinterpret_cast<u32x2*>(place(m & 1, 16 * t + erow, 2 * h + eq / 2) + 8 * (eq % 2)) =
+                  u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
             }
-          if (tm > 0) put(tm - 1);
+          if (m > 0) put(m - 1);
           __builtin_amdgcn_sched_barrier(0);
         }
-        put(TM - 1);
+        put(TM / 2 - 1);
       }
     };
-    if (rows >= 32 * TM && col_w + 32 * TILES <= p.N) emit(std::true_type{});
+    if (rows >= 16 * TM && col_w + 16 * TILES <= p.N) emit(std::true_type{});
     else emit(std::false_type{});
   };
 
@@ -373,29 +381,36 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
       read_rows(nn, xr_next, sr_next);
     }
 #pragma unroll
-    for (int tn = 0; tn < 4; ++tn)
+    for (int tn = 0; tn < 8; ++tn)
 #pragma unroll
-      for (int tm = 0; tm < 3; ++tm) acc[tn][tm] = f32x16{};
+      for (int tm = 0; tm < 6; ++tm) acc[tn][tm] = f32x4{};
     // Stage j: W of stage j + 2 goes out with its first results, X of stage j + 2
     // with its last ones, past the barrier.
     auto tile = [&](auto tn_c, auto tm_c) {
       constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
       constexpr int TILES = TN * TM;
-      constexpr int kTurn = TN * (TM - 1);  // the results from which on weight fragments are used for the last time
+      // The results of a stage go row tile by row tile.  From kTurn on the next
+      // stage's fragments take the place of those that are done with: the rows' first,
+      // with the last row tile the weights'.
+      constexpr int kTurn = TN * (TM - 2), kLastRows = TN * (TM - 1);
+      constexpr int kLag = 3;  // a result is added so many after it was begun
 #pragma unroll
       for (int t = 0; t < TN; ++t) read_w(tn_c, t);
 #pragma unroll
       for (int t = 0; t < TM; ++t) read_x(t);
-      float sx[3], last = 0.0f;  // (last: the scale of the stage's last result)
-      f32x16 part[2] = {f32x16{}, f32x16{}};
+      f32x4 part[kLag + 1];
 #pragma unroll
-      for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs * kScaleSlot + 128 * t);
+      for (int t = 0; t <= kLag; ++t) part[t] = f32x4{};
+      float sx[TM], last[GATED ? 2 : 1] = {};  // (last: the scales of the stage's last results)
+#pragma unroll
+      for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs * kScaleSlot + 64 * t);
       auto scale_add = [&](int t, float f) {  // result t of a stage, in its order
         const int tm = t / TN, tn = t % TN;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[tn][tm][e] = fmaf(part[t & 1][e], f, acc[tn][tm][e]);
+        for (int e = 0; e < 4; ++e) acc[tn][tm][e] = fmaf(part[t % (kLag + 1)][e], f, acc[tn][tm][e]);
         asm volatile("" : "+v"(acc[tn][tm]));  // (else the additions are gathered at the end of the stage)
       };
+      auto is_up = [](int t) { return GATED && t % TN >= TN / 2 ? 1 : 0; };
       int k2 = 2;  // the stage to load, of this tile or the next one
 #pragma clang loop unroll(disable)
       for (int kb = 0; kb < nkb; ++kb) {
@@ -412,17 +427,11 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
         const int to_w = ws == 0 ? kWSlots - 1 : ws - 1;
         const float s0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(cs[0]), kb & 63));
         const float s1 = GATED ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(cs[1]), kb & 63)) : s0;
-        float s[2][3];
-#pragma unroll
-        for (int t = 0; t < TM; ++t) {
-          s[0][t] = sx[t] * s0;
-          s[1][t] = GATED ? sx[t] * s1 : s[0][t];
-        }
+        float s[2][TM];
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-          const int tm = t / TN, tn = t % TN;
-          if (t == kTurn) {
+        each([&](auto t_c) {
+          constexpr int t = decltype(t_c)::value, tm = t / TN, tn = t % TN;
+          if constexpr (t == kTurn) {
             // The next stage has landed, for all; this one's fragments are in
             // registers, for all: X of two stages on goes into its slot.
             __builtin_amdgcn_s_waitcnt(wait_vm(kWLoads));
@@ -430,41 +439,42 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
             phase_barrier();
             const int dx = xs == 0 ? kXPart : -kXPart, dw = ws == kWSlots - 1 ? -(kWSlots - 1) * kWPart : kWPart;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
               x_at[c] += dx;
               w_at[c] += dw;
             }
           }
-          // the first product, loads and reads, the second one; the additions then
-          // run beside it
-          part[t & 1] = mfma_f8(wf[tn][0], xf[tm][0], f32x16{});
+          part[t % (kLag + 1)] = mfma_f8_16(wf[tn], xf[tm], f32x4{});
+          __builtin_amdgcn_sched_barrier(0);
+          if (tn == 0) s[0][tm] = sx[tm] * s0;
+          if (GATED && tn == 0) s[1][tm] = sx[tm] * s1;
+          if constexpr (t < kLag) scale_add(TILES - kLag + t, last[is_up(TILES - kLag + t)]);
+          else scale_add(t - kLag, s[is_up(t - kLag)][(t - kLag) / TN]);
           if (t < kTurn) {
 #pragma unroll
             for (int q = 0; q < kWLoads; ++q)
               if (q * kTurn / kWLoads == t) w_load(q, k2, to_w);
-          } else {
+          } else if (t < kLastRows) {
             const int u = t - kTurn;
 #pragma unroll
             for (int q = 0; q < kXLoads; ++q)
               if (q * TN / kXLoads == u) x_load(q, k2, xs);
-            if (u == 0) s_load(k2, xs);
-            if (u < TM - 1) read_x(u);
+            if (u == TN - 1) s_load(k2, xs);
+#pragma unroll
+            for (int q = 0; q < TM - 2; ++q)
+              if (q * TN / (TM - 2) == u) read_x(q);
+          } else {
+            read_w(tn_c, tn);
+            if (tn == 0) read_x(TM - 2);
           }
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           __builtin_amdgcn_sched_barrier(0);
-          part[t & 1] = mfma_f8(wf[tn][1], xf[tm][1], part[t & 1]);
-          __builtin_amdgcn_sched_barrier(0);
-          if (t == 0) scale_add(TILES - 1, last);
-          else scale_add(t - 1, s[GATED && (t - 1) % TN >= TN / 2 ? 1 : 0][(t - 1) / TN]);
-          if (t >= kTurn) read_w(tn_c, tn);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        last = s[GATED ? 1 : 0][TM - 1];
+        }, std::make_integer_sequence<int, TILES>{});
+        last[0] = s[0][TM - 1];
+        if constexpr (GATED) last[1] = s[1][TM - 1];
         const int xs1 = xs ^ 1;
+        read_x(TM - 1);
 #pragma unroll
-        for (int u = TN < TM - 1 ? TN : TM - 1; u < TM; ++u) read_x(u);
-#pragma unroll
-        for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs1 * kScaleSlot + 128 * t);
+        for (int t = 0; t < TM; ++t) sx[t] = *reinterpret_cast<const float*>(smem + s_at + xs1 * kScaleSlot + 64 * t);
         xs = xs1;
         ws = ws == kWSlots - 1 ? 0 : ws + 1;
         ++k2;
@@ -473,15 +483,16 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
           asm volatile("" : "+v"(cs[0]), "+v"(cs[1]));  // (waited for here)
         }
       }
-      scale_add(TILES - 1, last);
+#pragma unroll
+      for (int t = 0; t < kLag; ++t) scale_add(TILES - kLag + t, last[is_up(TILES - kLag + t)]);
       epilogue(tn_c, tm_c, cur, col_w, smem + kXSlots * kXPart + (ws == 0 ? kWSlots - 1 : ws - 1) * kWPart + wave * (64 * kRow));
     };
-    using Two = std::integral_constant<int, 2>;
-    using Three = std::integral_constant<int, 3>;
     using Four = std::integral_constant<int, 4>;
-    if (full) tile(Four{}, Three{});
-    else if (cur.rows > 64) tile(Two{}, Three{});
-    else tile(Two{}, Two{});
+    using Six = std::integral_constant<int, 6>;
+    using Eight = std::integral_constant<int, 8>;
+    if (full) tile(Eight{}, Six{});
+    else if (cur.rows > 64) tile(Four{}, Six{});
+    else tile(Four{}, Four{});
     cur = nxt;
     nxt = nn;
   }
