@@ -21,6 +21,7 @@ constexpr int kScaleSlot = 4 * kWave * 4;              // a stage's scales of th
 constexpr int kScales = kXSlots * kXPart + kWSlots * kWPart;
 constexpr int kTops = kScales + kXSlots * kScaleSlot;  // largest magnitudes of a gated tile's rows, by wave
 constexpr int kTiledLds = kTops + 4 * 96 * 4;
+static_assert(kTiledLds <= 160 * 1024, "the rings fit");
 constexpr int kXLoads = 6, kWLoads = 8;   // per part and wave: 8 rows each
 constexpr int kXRows = 8 * kXLoads;       // rows of a wave's X loads
 constexpr int kBlockM = 8;
@@ -288,6 +289,65 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     if constexpr (GATED) to[1] = p.ws1[at];
   };
 
+  // A gated tile's hidden rows, quantised: its 128 columns share a scale, so the
+  // largest of a row is found over the waves that hold parts of it.
+  auto quantize = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w, unsigned char* scr) {
+    constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
+    constexpr int TILES = TN / 2;                    // of 16 columns
+    constexpr int PARTS = TN == 8 ? 2 : 4;           // waves that hold a row
+    const GemmF8& p = prob(ti);
+    const int row_w = wave_row(ti), rows = ti.rows - row_w;
+    const int ln = opaque_lane(), erow = ln & 15, eq = ln >> 4;
+    const int col_part = TN == 8 ? wave >> 1 : wave;
+    uint32_t* tops = reinterpret_cast<uint32_t*>(smem + kTops);  // [row of the tile][part]
+    uint32_t h[TM][TILES][2];                        // four columns of a row, as bf16
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) {
+      u16x2 top = {0, 0};
+#pragma unroll
+      for (int tn = 0; tn < TILES; ++tn) {
+        float o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = silu(acc[tn][tm][i]) * acc[tn + TILES][tm][i];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          h[tm][tn][i] = pack_bf16x2(o[2 * i], o[2 * i + 1]);
+          top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, h[tm][tn][i] & 0x7fff7fffu));
+        }
+      }
+      uint32_t t = max(static_cast<uint32_t>(top[0]), static_cast<uint32_t>(top[1]));
+      t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), 16)));
+      t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), 32)));
+      if (eq == 0) tops[(row_w + 16 * tm + erow) * PARTS + col_part] = t;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitLds);
+    phase_barrier();
+    const long long row0 = ti.row_base + ti.m0 + row_w;
+    const int blocks = ceil_div(p.N, kF8Block), padded = ceil_div(p.N, 16) * 16;
+    constexpr int CH = TILES;                        // 16-byte chunks of a row's part
+    auto place = [&](int buf, int r, int c) { return scr + buf * 1024 + r * (16 * CH) + ((c ^ ((r / (8 / CH)) % CH)) << 4); };
+    auto put = [&](int tm) {
+      const int r = ln / CH, c = ln % CH, col = col_w + 16 * c;
+      if (r >= 16) return;                           // (two chunks a row: half of the lanes)
+      const u32x4 v = *reinterpret_cast<const u32x4*>(place(tm & 1, r, c));
+      if (16 * tm + r < rows && col < padded) store16(p.outq + (row0 + 16 * tm + r) * p.ldq + col, v);
+    };
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) {
+      uint32_t t = 0;
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q) t = max(t, tops[(row_w + 16 * tm + erow) * PARTS + q]);
+      const F8Scale sc = f8_scale(t << 16);
+      if (eq == 0 && col_part == 0 && 16 * tm + erow < rows) p.outs[(row0 + 16 * tm + erow) * blocks + ti.nt] = sc.scale;
+#pragma unroll
+      for (int tn = 0; tn < TILES; ++tn)
+        *reinterpret_cast<uint32_t*>(place(tm & 1, erow, tn) + 4 * eq) = quantize_f8_4(h[tm][tn][0], h[tm][tn][1], sc);
+      if (tm > 0) put(tm - 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    put(TM - 1);
+  };
   auto epilogue = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w, unsigned char* scr) {
     constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
     constexpr int TILES = GATED ? TN / 2 : TN;      // of 16 output columns
@@ -341,8 +401,12 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
         put(TM / 2 - 1);
       }
     };
-    if (rows >= 16 * TM && col_w + 16 * TILES <= p.N) emit(std::true_type{});
-    else emit(std::false_type{});
+    if constexpr (GATED) {
+      quantize(tn_c, tm_c, ti, col_w, scr);
+    } else {
+      if (rows >= 16 * TM && col_w + 16 * TILES <= p.N) emit(std::true_type{});
+      else emit(std::false_type{});
+    }
   };
 
   // ---- the workgroup's tiles ----

@@ -29,6 +29,8 @@ hipError_t launch_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh
   return takes_tiles(seg, a, sh, gated) ? launch_tiled_f8(seg, a, sh, gated, st) : launch_items_f8(seg, a, sh, gated, st);
 }
 
+bool gemm_f8_quantizes(const Segments& seg, const GemmF8& a, const GemmF8* sh) { return takes_tiles(seg, a, sh, true); }
+
 bool gemm_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
   return items_f8_blocks(seg, a, sh, gated) <= kMaxItemBlocks || takes_tiles(seg, a, sh, gated);
 }

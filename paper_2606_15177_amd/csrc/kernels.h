@@ -234,7 +234,9 @@ bool quantize_blocks_f8_supported(int G, int rows, int cols);
 // gated pair silu(.0) * (.1).  X[r] = x[r], or x[x_rows[r]] (x_count rows of x; an
 // entry outside them counts as a row of zeros), scales along.  Rows are ldx and
 // ldw bytes (multiples of 16) and ldo values apart, and hold zeros from K to the
-// next multiple of 16; groups of weights are N rows apart, scales dense.
+// next multiple of 16; groups of weights are N rows apart, scales dense.  Where
+// gemm_f8_quantizes, the gated pair goes out as bf16 rows' e4m3 instead, to outq
+// (rows ldq bytes apart) and outs, as launch_quantize_rows_f8 makes them.
 struct GemmF8 {
   const uint8_t* x;
   const float* x_scale;
@@ -248,6 +250,9 @@ struct GemmF8 {
   uint16_t* out;
   int K, N;
   long long ldx, ldw, ldo;
+  uint8_t* outq = nullptr;
+  float* outs = nullptr;
+  long long ldq = 0;
 };
 // a over seg (as the expert GEMMs above), and sh (nullable, static rows) in
 // the same launch.
@@ -255,6 +260,8 @@ hipError_t launch_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh
 // Host only: whether it accepts these sizes (the pointers are not looked at,
 // but for offsets being null or not).
 bool gemm_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+// Host only: whether the gated product quantises its rows.
+bool gemm_f8_quantizes(const Segments& seg, const GemmF8& a, const GemmF8* sh);
 
 // ---- norm.hip --------------------------------------------------------------
 // The norms around a block (see moe.h): of y, or (inv_pos given) of the weighted

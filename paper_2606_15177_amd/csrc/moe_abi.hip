@@ -476,9 +476,9 @@ FfnF8Plan plan_ffn_f8(const moe_dims* d, const FfnF8Ws& fw, const int32_t* x_row
   FfnF8Plan p{};
   p.routed = routed_segments(d, offsets);
   p.up = moe::GemmF8{fw.xq, fw.xs, x_rows, x_rows ? d->T : 0, offsets, 0, d->E_local, w.w_gate, w.w_up, w.s_gate, w.s_up,
-                     fw.h, d->H, d->I, hp, hp, d->I};
+                     fw.h, d->H, d->I, hp, hp, d->I, fw.hq, fw.hs, ip};
   p.sh_up = moe::GemmF8{fw.xq_sh, fw.xs_sh, nullptr, 0, nullptr, d->T, 1, w.sh_gate, w.sh_up, w.sh_s_gate, w.sh_s_up,
-                        fw.h_sh, d->H, shw, hp, hp, shw};
+                        fw.h_sh, d->H, shw, hp, hp, shw, fw.hq_sh, fw.hs_sh, wp};
   p.dn = moe::GemmF8{fw.hq, fw.hs, nullptr, 0, offsets, 0, d->E_local, w.w_down, nullptr, w.s_down, nullptr,
                      y_perm, d->I, d->H, ip, ip, d->H};
   p.sh_dn = moe::GemmF8{fw.hq_sh, fw.hs_sh, nullptr, 0, nullptr, d->T, 1, w.sh_down, nullptr, w.sh_s_down, nullptr,
@@ -528,7 +528,9 @@ int run_ffn_f8(const moe_dims* d, const uint16_t* x, const uint8_t* xq, const fl
   record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
   const moe::QuantF8Args qh{fw.h, fw.hq, fw.hs, n_rows, d->I, p.dn.ldx, rows, d->I};
   const moe::QuantF8Args qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, p.sh_dn.ldx, d->T, shw};
-  e = moe::launch_quantize_rows_f8(qh, p.sh ? &qh_sh : nullptr, st);
+  // (tiles have quantised the hidden rows)
+  e = moe::gemm_f8_quantizes(p.routed, p.up, p.sh ? &p.sh_up : nullptr) ? hipSuccess
+                                                                       : moe::launch_quantize_rows_f8(qh, p.sh ? &qh_sh : nullptr, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   e = moe::launch_gemm_f8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;

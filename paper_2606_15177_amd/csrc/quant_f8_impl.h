@@ -56,16 +56,20 @@ __device__ __forceinline__ uint32_t pack_f8x4(float a, float b, float c, float d
   return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
 }
 
-// Eight bf16 values' e4m3 (zeros in a group that is not finite).
-__device__ __forceinline__ u32x2 quantize_f8_vec(u32x4 v, const F8Scale& s) {
-  if (!s.finite) return u32x2{0u, 0u};
-  float y[8];
+// Four bf16 values' e4m3 (zeros in a group that is not finite).
+__device__ __forceinline__ uint32_t quantize_f8_4(uint32_t lo, uint32_t hi, const F8Scale& s) {
+  if (!s.finite) return 0u;
+  float y[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = __uint_as_float((i & 1) ? (v[i / 2] & 0xffff0000u) : (v[i / 2] << 16));
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t v = i < 2 ? lo : hi;
+    const float x = __uint_as_float((i & 1) ? (v & 0xffff0000u) : (v << 16));
     y[i] = __uint_as_float((__float_as_uint((x * s.pre) * s.c) + 32u) & ~63u);
   }
-  return u32x2{pack_f8x4(y[0], y[1], y[2], y[3]), pack_f8x4(y[4], y[5], y[6], y[7])};
+  return pack_f8x4(y[0], y[1], y[2], y[3]);
+}
+__device__ __forceinline__ u32x2 quantize_f8_vec(u32x4 v, const F8Scale& s) {
+  return u32x2{quantize_f8_4(v[0], v[1], s), quantize_f8_4(v[2], v[3], s)};
 }
 
 // Largest magnitude of eight bf16 values, as fp32 bits.
