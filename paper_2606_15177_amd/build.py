@@ -26,7 +26,7 @@ SOURCES = ["route.hip", "permute.hip", "combine.hip", "ffn_skinny.hip", "ffn_mid
 # the 8-bit experts
 SOURCES_I8 = ["quant.hip", "gemm_i8.hip", "i8_few.hip", "i8_mid.hip", "i8_tiled.hip"]
 # the experts in 8-bit floating point, and the norms around the layer
-SOURCES_F8 = ["quant_f8.hip", "gemm_f8.hip", "f8_mid.hip", "f8_tiled.hip", "norm.hip"]
+SOURCES_F8 = ["quant_f8.hip", "gemm_f8.hip", "f8_few.hip", "f8_mid.hip", "f8_tiled.hip", "norm.hip"]
 
 CXXFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -40,7 +40,7 @@ CXXFLAGS = [
 
 # matrix instructions write ordinary registers, where the e4m3 products' scaled
 # additions read them (accumulation registers cost a move each)
-EXTRA_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for s in ("f8_mid.hip", "f8_tiled.hip")}
+EXTRA_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for s in ("f8_few.hip", "f8_mid.hip", "f8_tiled.hip")}
 
 
 def _hipcc() -> str:

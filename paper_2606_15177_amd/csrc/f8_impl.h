@@ -38,6 +38,11 @@ int tiled_f8_grid(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool g
 hipError_t launch_items_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
 Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 long long items_f8_blocks(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+// Bf16 rows (xb), few of them per group (any number is computed): each
+// workgroup quantises the rows that it multiplies.
+bool few_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+Cut few_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+hipError_t launch_few_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
 hipError_t launch_tiled_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
 
 }  // namespace moe

@@ -236,7 +236,9 @@ bool quantize_blocks_f8_supported(int G, int rows, int cols);
 // ldw bytes (multiples of 16) and ldo values apart, and hold zeros from K to the
 // next multiple of 16; groups of weights are N rows apart, scales dense.  Where
 // gemm_f8_quantizes, the gated pair goes out as bf16 rows' e4m3 instead, to outq
-// (rows ldq bytes apart) and outs, as launch_quantize_rows_f8 makes them.
+// (rows ldq bytes apart) and outs, as launch_quantize_rows_f8 makes them.  With xb
+// the rows are bf16, ldxb values apart, and the product quantises them itself (x
+// and x_scale are not read); only where gemm_f8_takes_bf16.
 struct GemmF8 {
   const uint8_t* x;
   const float* x_scale;
@@ -253,6 +255,8 @@ struct GemmF8 {
   uint8_t* outq = nullptr;
   float* outs = nullptr;
   long long ldq = 0;
+  const uint16_t* xb = nullptr;
+  long long ldxb = 0;
 };
 // a over seg (as the expert GEMMs above), and sh (nullable, static rows) in
 // the same launch.
@@ -262,6 +266,16 @@ hipError_t launch_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh
 bool gemm_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 // Host only: whether the gated product quantises its rows.
 bool gemm_f8_quantizes(const Segments& seg, const GemmF8& a, const GemmF8* sh);
+// Host only: whether these sizes take bf16 rows, and run faster so than after a
+// launch that quantises them.
+bool gemm_f8_takes_bf16(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+// Host only: how a launch runs.  The kernel (0 items, 1 tiles, 2 items that quantise
+// their rows), the parts of K, the rows of a tile or a chunk, and whether a wave takes
+// 16 weight rows instead of 32.
+struct GemmF8Plan {
+  int kernel, parts, rows, half;
+};
+GemmF8Plan plan_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 
 // ---- norm.hip --------------------------------------------------------------
 // The norms around a block (see moe.h): of y, or (inv_pos given) of the weighted

@@ -500,6 +500,20 @@ int check_ffn_f8_limits(const moe_dims* d, bool one_x) {
   return MOE_OK;
 }
 
+// Where there are few rows the products quantise them (x and x_sh: null where the
+// rows came quantised).
+void quantize_in_f8_products(const moe_dims* d, const FfnF8Ws& fw, const uint16_t* x, const uint16_t* x_sh, FfnF8Plan* p) {
+  if (x && moe::gemm_f8_takes_bf16(p->routed, p->up, p->sh ? &p->sh_up : nullptr, true)) {
+    p->up.xb = x, p->sh_up.xb = x_sh;
+    p->up.ldxb = p->sh_up.ldxb = d->H;
+  }
+  const bool up_quantises = !p->up.xb && moe::gemm_f8_quantizes(p->routed, p->up, p->sh ? &p->sh_up : nullptr);
+  if (!up_quantises && moe::gemm_f8_takes_bf16(p->routed, p->dn, p->sh ? &p->sh_dn : nullptr, false)) {
+    p->dn.xb = fw.h, p->sh_dn.xb = fw.h_sh;
+    p->dn.ldxb = d->I, p->sh_dn.ldxb = p->sh_dn.K;
+  }
+}
+
 // The experts' networks on e4m3: x quantised (unless it came so: x NULL), gate/up on
 // it (through x_rows where x holds tokens), the hidden rows quantised, down.
 int run_ffn_f8(const moe_dims* d, const uint16_t* x, const uint8_t* xq, const float* xs, const int32_t* x_rows,
@@ -512,6 +526,7 @@ int run_ffn_f8(const moe_dims* d, const uint16_t* x, const uint8_t* xq, const fl
     p.up.x = p.sh_up.x = xq;
     p.up.x_scale = p.sh_up.x_scale = xs;
   }
+  quantize_in_f8_products(d, fw, x, x_sh, &p);
   const int shw = static_cast<int>(sh_width(d)), rows = d->T * d->k;
   const int32_t* n_rows = offsets + d->E_local;
   hipError_t e;
@@ -519,7 +534,7 @@ int run_ffn_f8(const moe_dims* d, const uint16_t* x, const uint8_t* xq, const fl
   record(taps, 2 * MOE_STAGE_FFN_UP, st);
   const moe::QuantF8Args qx{x, fw.xq, fw.xs, one_x ? nullptr : n_rows, d->H, p.up.ldx, one_x ? d->T : rows, d->H};
   const moe::QuantF8Args qx_sh{x_sh, fw.xq_sh, fw.xs_sh, nullptr, d->H, p.up.ldx, d->T, d->H};
-  e = !x ? hipSuccess : moe::launch_quantize_rows_f8(qx, p.sh && !one_x ? &qx_sh : nullptr, st);
+  e = !x || p.up.xb ? hipSuccess : moe::launch_quantize_rows_f8(qx, p.sh && !one_x ? &qx_sh : nullptr, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   e = moe::launch_gemm_f8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
@@ -528,9 +543,9 @@ int run_ffn_f8(const moe_dims* d, const uint16_t* x, const uint8_t* xq, const fl
   record(taps, 2 * MOE_STAGE_FFN_DOWN, st);
   const moe::QuantF8Args qh{fw.h, fw.hq, fw.hs, n_rows, d->I, p.dn.ldx, rows, d->I};
   const moe::QuantF8Args qh_sh{fw.h_sh, fw.hq_sh, fw.hs_sh, nullptr, shw, p.sh_dn.ldx, d->T, shw};
-  // (tiles have quantised the hidden rows)
-  e = moe::gemm_f8_quantizes(p.routed, p.up, p.sh ? &p.sh_up : nullptr) ? hipSuccess
-                                                                       : moe::launch_quantize_rows_f8(qh, p.sh ? &qh_sh : nullptr, st);
+  // (unless gate/up's tiles have quantised the hidden rows, or down does)
+  const bool quantised = p.dn.xb || (!p.up.xb && moe::gemm_f8_quantizes(p.routed, p.up, p.sh ? &p.sh_up : nullptr));
+  e = quantised ? hipSuccess : moe::launch_quantize_rows_f8(qh, p.sh ? &qh_sh : nullptr, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
   e = moe::launch_gemm_f8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false, st);
   if (e != hipSuccess) return MOE_ERR_DEVICE;
@@ -1140,6 +1155,44 @@ int moe_test_ffn_i8_plan(const moe_dims* d, int64_t out[2][4]) {
   quantize_in_products(d, fw, &row, &row, &p);
   const moe::GemmI8Plan g[2] = {moe::plan_gemm_i8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true),
                                 moe::plan_gemm_i8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false)};
+  for (int i = 0; i < 2; ++i) {
+    const int64_t v[4] = {g[i].kernel, g[i].parts, g[i].rows, g[i].half};
+    std::copy(v, v + 4, out[i]);
+  }
+  return MOE_OK;
+}
+
+// For the tests: how the e4m3 products run (moe::GemmF8Plan), of moe_linear_f8 or
+// moe_grouped_linear_f8, and of the layer's gate/up and down (of rows that come
+// quantised or not).
+int moe_test_linear_f8_plan(const moe_linear_dims* d, int grouped, int64_t out[4]) {
+  static const int32_t some = 0;  // stands for device offsets
+  if (d == nullptr || d->M < 1 || d->N < 1 || d->K < 1 || (grouped && d->G < 1)) return MOE_ERR_DIMS;
+  const moe::Segments seg = linear_segments(d, grouped ? &some : nullptr, grouped != 0);
+  moe::GemmF8 a{};
+  a.offsets = seg.offsets;
+  a.static_rows = seg.offsets ? 0 : d->M;
+  a.groups = seg.groups;
+  a.K = d->K, a.N = d->N;
+  const moe::GemmF8Plan p = moe::plan_gemm_f8(seg, a, nullptr, false);
+  const int64_t v[4] = {p.kernel, p.parts, p.rows, p.half};
+  std::copy(v, v + 4, out);
+  return MOE_OK;
+}
+
+int moe_test_ffn_f8_plan(const moe_dims* d, int quantised, int64_t out[2][4]) {
+  const int s = check_dims(d);
+  if (s != MOE_OK) return s;
+  if (d->T == 0 || check_ffn_f8_limits(d, false) != MOE_OK) return MOE_ERR_UNSUPPORTED;
+  static const int32_t some = 0;
+  static const uint16_t row = 0;
+  FfnF8Ws fw{};
+  uint16_t h = 0;
+  fw.h = fw.h_sh = &h;
+  FfnF8Plan p = plan_ffn_f8(d, fw, nullptr, &some, moe_weights_f8{}, nullptr, nullptr);
+  quantize_in_f8_products(d, fw, quantised ? nullptr : &row, quantised ? nullptr : &row, &p);
+  const moe::GemmF8Plan g[2] = {moe::plan_gemm_f8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true),
+                                moe::plan_gemm_f8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false)};
   for (int i = 0; i < 2; ++i) {
     const int64_t v[4] = {g[i].kernel, g[i].parts, g[i].rows, g[i].half};
     std::copy(v, v + 4, out[i]);

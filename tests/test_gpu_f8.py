@@ -403,11 +403,34 @@ def placed(d, seed):
     return None if d.E_local == d.E else torch.randperm(d.E, generator=gen(seed), device="cuda")[:d.E_local].to(torch.int32)
 
 
+def assert_layer(moe, out, d, q, logits, x, local, gating):
+    """A layer's output against 64 bits, expert by expert: an expert's output is within
+    its bound and the sum adds k + 1 terms in fp32."""
+    idx, gates = torch.empty((d.T, d.k), dtype=torch.int32, device="cuda"), torch.empty((d.T, d.k), device="cuda")
+    moe.route(d, logits, idx, gates, gating=gating)
+    ref, bound = torch.zeros((2, d.T, d.H), dtype=torch.float64, device="cuda")
+    terms = torch.zeros_like(ref)
+    for slot, e in enumerate(range(d.E) if local is None else local.tolist()):
+        t, j = (idx == e).nonzero(as_tuple=True)
+        if len(t):
+            y, b = ffn_and_bound(x[t], *expert(q, slot))
+            g = gates[t, j].double()[:, None]
+            ref[t], bound[t], terms[t] = ref[t] + g * y, bound[t] + g * b, terms[t] + g * (y.abs() + b)
+    if d.n_shared:
+        y, b = ffn_and_bound(x, *expert(q, None, "sh_", "sh_s_"))
+        ref, bound, terms = ref + y, bound + b, terms + y.abs() + b
+    bound = bound + terms * (d.k + 2) * 2.0 ** -24
+    off = (out.double() - ref).abs()
+    bound = bound + (ref.abs() + bound) * BF16
+    assert (off <= bound).all(), (off / bound).max().item()
+
+
 @pytest.mark.parametrize("case", range(len(FFN)))
 def test_forward_is_its_steps(moe, case):
-    """forward_f8 gives the bits of route, permute, expert_ffn_f8 and combine, from
-    bf16 rows and from quantised ones, and the layer class those of forward_f8; the
-    counts are those of the steps."""
+    """forward_f8 gives the bits of route, permute, expert_ffn_f8 and combine, and
+    the layer class those of forward_f8; the counts are those of the steps.  From
+    quantised rows too, but that with up to 8 tokens other kernels add in another
+    order: those are held against 64 bits."""
     d = moe.dims(S=3, flags=case % 3, **FFN[case])
     _, q = layer_weights(moe, d, case)
     logits, x = torch.randn((d.T, d.E), generator=gen(case), device="cuda"), randn((d.T, d.H), case + 60)
@@ -421,7 +444,12 @@ def test_forward_is_its_steps(moe, case):
     assert torch.equal(out, ref) and torch.equal(counts[0], counts[1])
     xq, xs = moe.quantize_rows_f8(x)
     out = layer.forward(logits, src, counts=counts[2], xq=xq, x_scale=xs)
-    assert torch.equal(out, ref) and torch.equal(counts[0], counts[2])
+    assert torch.equal(counts[0], counts[2])
+    if d.T > 8:
+        assert torch.equal(out, ref)
+    else:
+        assert_layer(moe, out, d, q, logits, x, local, gating)
+        assert_layer(moe, ref, d, q, logits, x, local, gating)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     again = layer.forward(logits, src, x, stream=side, ws=moe.workspace(d, moe.ENTRY_FORWARD_F8).fill_(0xff))
@@ -513,6 +541,39 @@ def test_few_tokens_in_any_groups(moe, sizes):
             assert_ffn(y[o[e]:o[e + 1]], x_perm[o[e]:o[e + 1]], expert(q, e))
     assert (y[o[-1]:] == 3.0).all()
     assert_ffn(ysh, x, expert(q, None, "sh_", "sh_s_"))
+
+
+# Few tokens: the products quantise the rows themselves, K in four, two and one
+# parts, rows longer than the registers hold (down, 9000), rows of the last case too
+# long for it at 8 tokens, and a shared expert of its own width.
+FEW = [dict(H=512, E=16, k=2, I=256, E_local=16), dict(H=2048, E=32, k=4, I=768, E_local=24),
+       dict(H=1000, E=6, k=3, I=1544, E_local=6, n_shared=1, I_shared=344), dict(H=136, E=8, k=8, I=40, E_local=8),
+       dict(H=256, E=4, k=2, I=9000, E_local=4, n_shared=2, I_shared=1000), dict(H=4104, E=8, k=4, I=2056, E_local=8),
+       dict(H=8704, E=2, k=1, I=264, E_local=2)]
+
+
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_few_tokens(moe, case):
+    """Up to 9 tokens, from bf16 rows and from quantised ones; one row is zero and
+    one not finite."""
+    big = moe.dims(T=9, S=1, **FEW[case])
+    _, q = layer_weights(moe, big, case)
+    local = None if big.E_local == big.E else torch.arange(big.E_local, dtype=torch.int32, device="cuda")
+    logits, x = torch.randn((9, big.E), generator=gen(case), device="cuda"), randn((9, big.H), case)
+    x[1], x[4, 3] = 0.0, float("nan")
+    for T in (1, 2, 3, 5, 8, 9):
+        d = moe.dims(T=T, S=1, **FEW[case])
+        layer = moe.MoeLayerF8(d, q, local)
+        xq, xs = moe.quantize_rows_f8(x[:T])
+        for rows in (dict(x=x[:T]), dict(xq=xq, x_scale=xs)):
+            layer.ws.fill_(0xff)
+            out = layer.forward(logits[:T], None, **rows)
+            # (a token none of whose experts is hosted here, without shared ones, is zero)
+            keep = [t for t in range(T) if t != 4]
+            at = moe.dims(T=len(keep), S=1, **FEW[case])
+            assert_layer(moe, out[keep], at, q, logits[keep], x[keep], local, None)
+            if T > 4:
+                assert torch.isnan(out[4]).all() or (out[4] == 0).all()
 
 
 # --------------------------------------------- far offsets, calls at once ----
@@ -609,44 +670,83 @@ def test_outputs_on_a_raw_stream_handle(moe):
 # ------------------------------------------ shapes that reach each kernel ----
 
 
-KERNELS = [(2500, 2100, 1700), (5003, 3801, 1501), (5003, 2803, 1501), (16000, 1027, 385), (2600, 2049, 8200), (1900, 2304, 12288),
-           (4200, 2051, 380)]
+ITEMS, TILES, FEWS, HALF = 0, 1, 2, "half"
 
 
-@pytest.mark.parametrize("M,N,K", KERNELS)
-def test_linear_kernels(moe, M, N, K):
+def linear_plan(moe, M, N, K, G=0):
+    """(kernel, parts of K, rows of a tile or chunk), and HALF where a wave
+    takes 16 weight rows."""
+    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), (C.c_int64 * 4)()
+    assert moe._lib.moe_test_linear_f8_plan(C.byref(d), int(G > 0), out) == 0
+    return tuple(out[:3]) + ((HALF,) if out[3] else ())
+
+
+# Items: few rows with K in 2 and 4 parts, chunks of 64, 32 and 8, a wave with 32
+# and 16 weight rows; undivided, with 256 weight rows per item.  Tiles: last rounds in
+# parts and whole, K a byte past the items', more than 64 stages.
+KERNELS = [(7, 9001, 130, (ITEMS, 2, 8)), (8, 517, 1003, (ITEMS, 4, 8, HALF)), (50, 1003, 517, (ITEMS, 4, 32, HALF)),
+           (7, 5001, 1003, (ITEMS, 4, 8)), (50, 4001, 517, (ITEMS, 4, 32)), (30, 1999, 1700, (ITEMS, 4, 32, HALF)),
+           (260, 300, 3001, (ITEMS, 4, 32, HALF)), (50, 5003, 517, (ITEMS, 4, 64)), (60, 12003, 4100, (ITEMS, 2, 64)),
+           (777, 1003, 517, (ITEMS, 2, 64)), (4200, 2051, 380, (ITEMS, 1, 128)), (100, 33000, 8200, (ITEMS, 1, 128)),
+           (5, 8200, 34000, (ITEMS, 2, 8)), (3, 300, 130000, (ITEMS, 4, 8, HALF)),
+           (2500, 2100, 1700, (TILES, 1, 192)), (5003, 3801, 1501, (TILES, 1, 192)), (5003, 2803, 1501, (TILES, 1, 192)),
+           (16000, 1027, 385, (TILES, 1, 192)), (2600, 2049, 8200, (TILES, 1, 192)), (1900, 2304, 12288, (TILES, 1, 192)),
+           (1350, 1500, 16500, (TILES, 1, 192)), (193, 7300, 641, (TILES, 1, 192))]
+
+
+@pytest.mark.parametrize("M,N,K,plan", KERNELS)
+def test_linear_kernels(moe, M, N, K, plan):
+    assert linear_plan(moe, M, N, K) == plan
     xq, xs, wq, ws = operands(M, N, K, M + N + K)
     y = torch.full((M + 1, N), 3.0, dtype=torch.bfloat16, device="cuda")
     moe.linear_f8(K, xq, xs, wq, ws, y[:M])
-    assert_product(y[:M], xq, xs, wq, ws, K)
+    for a in range(0, M, 1000):
+        assert_product(y[a:min(M, a + 1000)], xq[a:a + 1000], xs[a:a + 1000], wq, ws, K)
     assert (y[M] == 3.0).all()
 
 
 # Groups: tiles of up to 64, 256 and 1024 groups with their last tiles in each of
 # their forms, empty groups and one that has most rows; items.
-GROUP_KERNELS = [(ragged(8, 350, 1), 2000, 1600), ([0, 64, 65, 96, 97, 192, 193, 2800, 0, 33, 32], 1999, 1603),
-                 (ragged(100, 120, 2, 1500), 513, 2100), (ragged(300, 120, 3), 260, 2100), (ragged(1000, 110, 4), 70, 2052),
-                 (ragged(30, 16, 5, 600), 1003, 900), ([5, 0, 70, 3], 3000, 700), ([2, 0, 1], 1000, 700), ([2, 30, 0, 9], 600, 900),
-                 ([2, 70, 0, 9, 33, 32, 8], 100, 900), ([3, 0, 4, 1], 2500, 500)]
+GROUP_KERNELS = [(ragged(8, 350, 1), 2000, 1600, (TILES, 1, 192)),
+                 ([0, 64, 65, 96, 97, 192, 193, 2800, 0, 33, 32], 1999, 1603, (TILES, 1, 192)),
+                 (ragged(100, 120, 2, 1500), 513, 2100, (TILES, 1, 192)), (ragged(300, 120, 3), 260, 2100, (TILES, 1, 192)),
+                 (ragged(1000, 110, 4), 70, 2052, (TILES, 1, 192)), (ragged(140, 36, 7), 1030, 900, (TILES, 1, 192)),
+                 (ragged(30, 16, 5, 600), 1003, 900, (ITEMS, 1, 128)), ([5, 0, 70, 3], 3000, 700, (ITEMS, 2, 64)),
+                 ([2, 0, 1], 1000, 700, (ITEMS, 4, 8, HALF)), ([2, 30, 0, 9], 600, 900, (ITEMS, 4, 32, HALF)),
+                 ([2, 70, 0, 9, 33, 32, 8], 100, 900, (ITEMS, 4, 32, HALF)), ([3, 0, 4, 1], 2500, 500, (ITEMS, 2, 8)),
+                 (ragged(40, 60, 9), 3000, 2300, (ITEMS, 1, 128))]
 
 
 @pytest.mark.parametrize("case", range(len(GROUP_KERNELS)))
 @pytest.mark.parametrize("gather", [False, True])
 def test_grouped_kernels(moe, case, gather):
-    sizes, N, K = GROUP_KERNELS[case]
+    sizes, N, K, plan = GROUP_KERNELS[case]
+    assert linear_plan(moe, sum(sizes), N, K, len(sizes)) == plan
     check_grouped(moe, sizes, N, K, case, spare=0, gather=max(1, sum(sizes) // 3) if gather else None)
 
 
-FFN_KERNELS = [dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_shared=520), dict(T=3300, H=2104, E=80, k=3, I=136, E_local=70),
-               dict(T=7200, H=2104, E=300, k=4, I=136, E_local=300), dict(T=3000, H=256, E=4, k=2, I=1536, E_local=4),
-               dict(T=2000, H=2048, E=4, k=2, I=1544, E_local=4, n_shared=1, I_shared=1600)]
+def ffn_plan(moe, d, quantised=False):
+    out = (C.c_int64 * 8)()
+    assert moe._lib.moe_test_ffn_f8_plan(C.byref(d), int(quantised), out) == 0
+    return tuple(out[:3]), tuple(out[4:7])
+
+
+FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_shared=520), (TILES, 1, 192), (ITEMS, 1, 128)),
+               (dict(T=3300, H=2104, E=80, k=3, I=136, E_local=70), (TILES, 1, 192), (ITEMS, 1, 128)),
+               (dict(T=7200, H=2104, E=300, k=4, I=136, E_local=300), (TILES, 1, 192), (ITEMS, 1, 128)),
+               (dict(T=3000, H=256, E=4, k=2, I=1536, E_local=4), (ITEMS, 1, 128), (ITEMS, 1, 128)),
+               (dict(T=2000, H=2048, E=4, k=2, I=1544, E_local=4, n_shared=1, I_shared=1600), (TILES, 1, 192), (TILES, 1, 192)),
+               (dict(T=5000, H=1160, E=16, k=3, I=904, E_local=16, n_shared=2, I_shared=456), (TILES, 1, 192), (TILES, 1, 192)),
+               (dict(T=8, H=1024, E=8, k=2, I=520, E_local=8, n_shared=1, I_shared=264), (FEWS, 2, 8), (FEWS, 2, 8))]
 
 
 @pytest.mark.parametrize("case", range(len(FFN_KERNELS)))
 def test_ffn_kernels(moe, case):
     """The layers that tiles and wide items are for, and their bits from one
     entry point to the other."""
-    d = moe.dims(S=1, **FFN_KERNELS[case])
+    conf, up, down = FFN_KERNELS[case]
+    d = moe.dims(S=1, **conf)
+    assert ffn_plan(moe, d) == (up, down)
     _, q = layer_weights(moe, d, case)
     w = moe.make_weights_f8(d, q)
     local = None if d.E_local == d.E else torch.arange(d.E_local, dtype=torch.int32, device="cuda")
