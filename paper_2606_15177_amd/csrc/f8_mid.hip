@@ -16,6 +16,7 @@ constexpr int kSplitChunk = 64;     // ... of any item where K is split (32 wher
 constexpr int kFewHalf = 32;        // items (of 32 token rows) up to which they are halved once more, K in 4 parts
 constexpr int kBriefChunk = 8;      // ... where no group has more rows
 constexpr int kWideRows = 64;       // groups of more rows take wide items
+constexpr int kWideMean = 44;       // ... which an uneven batch of so many rows per group has
 constexpr int kItemRows = 128;      // weight rows of a narrow item
 constexpr int kFewWide = 128;       // fewer wide items than this take 128 weight rows: half the CUs' worth
 constexpr int kOneWide = 256;       // ... or fewer than this, one per CU, in a launch of fewer items than
@@ -536,16 +537,20 @@ hipError_t launch_kp(long long blocks, const ItemsF8& ma, hipStream_t st) {
 
 // With the sums of few items (64 rows x 128 weight rows each, of an evenly
 // routed batch) most CUs would idle, and an item runs through its whole K
-// alone.  Time with K undivided, in 2 and in 4 parts, us (products of static
-// rows): 64 items, 64 x 8192 x 4096 19.9, 14.8, 12.7; 112, 64 x 14336 x 4096
-// 22.8, 17.2, 23.8; 189, 396 x 3391 x 12416 78, 55, 67; 256 of short K, 1000 x
-// 2048 x 768 10.6, 12.8, 22.4; 392, 849 x 3534 x 4367 35, 52, 71.
+// alone: K in parts.  Up to two per CU, two parts still win where groups have more than
+// 64 rows, whose wide items of 128 rows would leave CUs idle; where every item has a
+// chunk of its own the undivided K does, whose workgroups share a CU.  Weights from HBM,
+// K undivided, in 2 and in 4 parts, us:
+//   static rows: 64 items, 64 x 4096 x 14336 68.5, 43.8, 25.5; 128, 64 x 16384 x 4096
+//     25.4, 18.9, 28.7; 157, 64 x 20000 x 8192 44.9, 56.0, 62.2; 158, 96 x 10000 x 4096 40.8,
+//     26.7, 28.6; 189, 396 x 3391 x 12416 121, 68, 79; 256, 96 x 16384 x 2048 23.3, 18.2, 27.7,
+//     1000 x 2048 x 768 12.2, 12.0, 21.1; 392, 849 x 3534 x 4367 47, 56, 79;
+//   groups at a mean of 40 and 48 rows: 6 of N 4096, K 7168 (192 items) 41, 52, 60 and 68, 52,
+//     73; 8 of K 14336 (256) 86, 105, 144 and 131, 139, 161; gated at 60, 2 of N 7168, K 7168
+//     (224) 43, 55, 78.
 //
 // In 4 parts and still at most half a chip of workgroups, a wave takes 16 weight
 // rows instead of 32: half of an MFMA's rows go unused, twice as many CUs read.
-// Weights from HBM, us, 32 rows and 16: 1 x 2048 x 7168 9.9 and 8.2, 16 x 4096 x
-// 14336 22.4 and 17.0, 128 x 1024 x 4096 8.8 and 7.4; with more workgroups than CUs
-// (1 x 5120 x 4096) 8.7 and 9.1.
 Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
   const int cols = gated ? kItemRows / 2 : kItemRows;
   // items of 128 weight rows and so many token rows
@@ -555,9 +560,10 @@ Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool ga
            (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
   };
   const long long items = count(kSplitChunk);
+  const bool wide = a.offsets ? !gated && seg.mean_rows > kWideMean : a.static_rows > kWideRows;
   Cut c{1, kChunk, false};
   if (items <= 64) c.parts = 4;
-  else if (items <= 128 || (items <= 256 && a.K >= 4096)) c.parts = 2;
+  else if (items <= 128 || (wide && items <= (a.offsets ? 192 : 256))) c.parts = 2;
   if (c.parts > 1) c.rows = seg.max_rows <= kBriefChunk ? kBriefChunk : items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
   c.half = !gated && c.parts == 4 && count(32) <= kFewHalf;
   if (c.half && c.rows > 32) c.rows = 32;
