@@ -478,7 +478,8 @@ int moe_forward_i8(const moe_dims *dims, const moe_gating *gating, const float *
  *   x  = h' / sqrt(mean_c h'^2 + eps) * (weight + weight_add)
  * in fp32; h' and x are rounded to bf16 once, on their way out, and the
  * quantised x is made from the fp32 one (as moe_quantize_rows_f8 makes it from
- * a bf16 one, the quotient rounded to fp32).
+ * a bf16 one, the quotient rounded to fp32).  The sums of squares are fp32 too: a row
+ * whose sum passes 3.4e38 is normed to zeros.
  */
 typedef struct moe_norm {
     int32_t H;                    /* columns, 1..32768 */
@@ -492,7 +493,8 @@ typedef struct moe_norm {
  * start anywhere.
  *   h      [T][H] bf16: the residual stream.
  *   h_out  [T][H] bf16 out, nullable: h'.  May be h (same stride).
- *   x      [T][H] bf16 out, nullable: the next block's input.  May be y.
+ *   x      [T][H] bf16 out, nullable: the next block's input.  May be y (same
+ *          stride).
  *   q, scale  nullable, both or none: x as moe_quantize_rows_f8 lays it out
  *             (rows ldq bytes apart, a multiple of 16, padded with zeros to 16;
  *             scale [T][ceil(H/128)] fp32).
@@ -559,7 +561,7 @@ int moe_quantize_blocks_f8(int32_t G, int32_t rows, int32_t cols, const moe_bf16
                            moe_f8 *q, int64_t ldq, float *scale, void *stream);
 
 /*
- * y[r][n] = sum_b x_scale[r][b] w_scale[n/128][b] (sum_c xq[r][c] wq[n][c] over
+ * y[r][n] = sum_b (x_scale[r][b] w_scale[n/128][b]) (sum_c xq[r][c] wq[n][c] over
  * the 128 columns c of b), in fp32, one rounding to bf16.
  *   xq [M] rows, x_scale [M][ceil(K/128)], wq [N] rows, w_scale [ceil(N/128)]
  *   [ceil(K/128)], y [M] rows out.
@@ -624,7 +626,8 @@ int moe_expert_ffn_f8(const moe_dims *dims, const moe_bf16 *x_perm, const int32_
  *          experts' are each rounded to bf16 before it, as by
  *          moe_expert_ffn_f8), rounded once.  May be NULL with norm.
  *   norm, rows  nullable, both or none: moe_norm_rows of that sum, as it is in
- *          fp32, with norm->H = H.
+ *          fp32, with norm->H = H.  rows->x may be x, and rows->q and scale may be
+ *          xq and x_scale: they are written after the layer has read its rows.
  * Stage MOE_STAGE_FFN_UP includes the quantisation of x, MOE_STAGE_FFN_DOWN that of
  * the hidden rows, MOE_STAGE_COMBINE the norms.
  *   ws  MOE_ENTRY_FORWARD_F8 workspace.

@@ -569,6 +569,7 @@ int norm_ok(const moe_norm* n, const moe_norm_io* r, int32_t T) {
   if (n->H > moe::kNormMaxH || r->ldh > kMaxNormStride || r->ldh_out > kMaxNormStride || r->ldx > kMaxNormStride ||
       r->ldq > kMaxNormStride || r->gate_row > kMaxNormStride)
     return MOE_ERR_UNSUPPORTED;
+  if (T > 1 && r->h && r->h_out == r->h && r->ldh_out != r->ldh) return MOE_ERR_DIMS;  // rows over other rows
   if (r->q && r->ldq % 16 != 0) return MOE_ERR_ALIGN;
   if ((r->q == nullptr) != (r->scale == nullptr)) return MOE_ERR_NULL;
   if (T == 0) return MOE_OK;
@@ -969,6 +970,7 @@ int moe_norm_rows(const moe_norm* n, const moe_norm_io* r, int32_t T, const moe_
   if (s != MOE_OK) return s;
   if (y && ldy < n->H) return MOE_ERR_DIMS;
   if (y && ldy > kMaxNormStride) return MOE_ERR_UNSUPPORTED;
+  if (y && T > 1 && r->x == y && r->ldx != ldy) return MOE_ERR_DIMS;
   if (!aligned2(y)) return MOE_ERR_ALIGN;
   moe::NormArgs a = norm_args(n, r, T, y, ldy);
   if (!y) a.post_weight = a.gate = nullptr;  // nothing to norm or to gate

@@ -144,6 +144,7 @@ def test_layer_entry_points_refuse_before_launch(moe):
     (dict(x=17, ldx=64), 4, -6), (dict(gate=16, gate_row=-1), 4, -2), (dict(gate=16, gate_col=2), 4, -2),
     (dict(gate=16, gate_row=63, gate_col=1), 4, -2), (dict(gate=17), 4, -6), (dict(ldh=2 ** 41), 4, -3),
     (dict(gate=16, gate_row=2 ** 41), 4, -3), (dict(h=None), 0, 0),
+    (dict(ldh_out=72), 4, -2), (dict(ldh=72), 2, -2), (dict(h_out=32, x=16, ldx=72), 4, -2),  # in place, but rows over other rows
 ])
 def test_norm_refusals(moe, change, T, code):
     n = moe.MoeNorm(64, 16, None, 1.0, 1e-6, 0.0)

@@ -614,6 +614,16 @@ def test_grouped_past_32_bit_offsets(moe, rows):
         assert_product(y[r], xq[r], xs[r], wq[e], ws[e], K)
 
 
+def test_quantize_more_rows_than_workgroups(moe):
+    """Workgroups that take several lots of rows in turn."""
+    rows = 2 ** 26 + 3
+    x = torch.empty((rows, 8), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(5))
+    q, scale = moe.quantize_rows_f8(x)
+    for r in (slice(0, 70), slice(rows - 70, rows), slice(2 ** 26 - 70, 2 ** 26)):
+        ref, ref_s = rows_exactly(x[r])
+        assert torch.equal(q[r, :8].double(), ref) and torch.equal(scale[r], ref_s) and (raw(q)[r, 8:] == 0).all()
+
+
 def test_quantize_past_32_bit_offsets(moe):
     rows, cols = 140001, 16400
     x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(5))
@@ -624,6 +634,67 @@ def test_quantize_past_32_bit_offsets(moe):
     q, scale = moe.quantize_blocks_f8(x)
     ref, ref_s = blocks_exactly(x[None, rows - rows % 128:])
     assert torch.equal(q[rows - rows % 128:].double(), ref[0]) and torch.equal(scale[-1], ref_s[0, 0])
+
+
+@pytest.mark.parametrize("gather", [False, True])
+def test_expected_rows_move_no_result(moe, gather):
+    """Room for four times the rows: the expected number chooses the kernel (told
+    nothing, that of all the room); rows behind the last group stay as they were."""
+    sizes, N, K = ragged(24, 75, 3), 1100, 1600
+    M, xq, xs, wq, ws, offsets, x_rows = grouped_case(sizes, N, K, 7, spare=4 * sum(sizes), gather=500 if gather else None)
+    o, kernels = offsets.tolist(), set()
+    for rows in (None, sum(sizes), 1, M, 24 * 75, -3):
+        d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=24, R=rows or 0), (C.c_int64 * 4)()
+        assert moe._lib.moe_test_linear_f8_plan(C.byref(d), 1, out) == 0
+        kernels.add(out[0])
+        y = torch.full((M, N), 3.0, dtype=torch.bfloat16, device="cuda")
+        moe.grouped_linear_f8(K, xq, xs, offsets, wq, ws, y, x_rows=x_rows, rows=rows)
+        assert (y[o[-1]:] == 3.0).all(), rows
+        for g in range(24):
+            if o[g] < o[g + 1]:
+                assert_product(y[o[g]:o[g + 1]], xq, xs, wq[g], ws[g], K, slice(o[g], o[g + 1]) if x_rows is None else x_rows[o[g]:o[g + 1]].long())
+    assert kernels == {ITEMS, TILES}
+
+
+@pytest.mark.parametrize("case", [1, 5])
+def test_taps_of_the_layer(moe, case):
+    """The extra outputs are those of the separate steps, the output that of the
+    layer without them; events of every stage are recorded in order."""
+    d = moe.dims(S=3, **FFN[case])
+    _, q = layer_weights(moe, d, case)
+    logits, x = torch.randn((d.T, d.E), generator=gen(case), device="cuda"), randn((d.T, d.H), case + 60)
+    src = torch.randint(0, 3, (d.T,), generator=gen(case), device="cuda", dtype=torch.int32)
+    local = torch.randperm(d.E, generator=gen(case), device="cuda")[:d.E_local].to(torch.int32)
+    rows, i32 = d.T * d.k, dict(dtype=torch.int32, device="cuda")
+
+    def outputs():
+        return dict(topk_idx=torch.full((d.T, d.k), -7, **i32), topk_w=torch.full((d.T, d.k), -7.0, device="cuda"),
+                    expert_load=torch.full((d.E,), -7, **i32), offsets=torch.full((d.E_local + 1,), -7, **i32),
+                    perm_token=torch.full((rows,), -7, **i32), inv_pos=torch.full((rows,), -7, **i32))
+    ref, got = outputs(), outputs()
+    counts = [torch.zeros((3, d.E), dtype=torch.int64, device="cuda") for _ in range(2)]
+    moe.route(d, logits, ref["topk_idx"], ref["topk_w"])
+    moe.route_stats(d, src, ref["topk_idx"], counts[0], ref["expert_load"])
+    moe.permute(d, ref["topk_idx"], local, None, ref["offsets"], ref["perm_token"], ref["inv_pos"], None,
+                moe.workspace(d, moe.ENTRY_PERMUTE))
+    events = [torch.cuda.Event(enable_timing=True) for _ in range(2 * len(moe.STAGES))]
+    for e in events:
+        e.record()   # (torch makes the handle with the first record)
+    layer = moe.MoeLayerF8(d, q, local)
+    plain = layer.forward(logits, src, x)
+    h, norm = randn((d.T, d.H), 3), moe.norm(d.H)
+    ends = [torch.empty_like(h) for _ in range(2)]
+    layer.forward(logits, src, x, norm=norm, rows=moe.norm_io(h, ends[0]))
+    out = torch.empty_like(plain)
+    layer.forward(logits, src, x, counts=counts[1], out=out, norm=norm, rows=moe.norm_io(h, ends[1]),
+                  taps=moe.make_taps(**got, events=[e.cuda_event for e in events]))
+    torch.cuda.synchronize()
+    assert torch.equal(out, plain) and torch.equal(*ends) and torch.equal(*counts)
+    used = ref["offsets"][-1].item()
+    for name in got:
+        n = used if name == "perm_token" else None
+        assert torch.equal(got[name].flatten()[:n], ref[name].flatten()[:n]), name
+    assert all(a.elapsed_time(b) >= 0 for a, b in zip(events, events[1:]))
 
 
 @pytest.mark.parametrize("T", [3, 200])

@@ -135,6 +135,30 @@ def test_norm_no_rows(moe):
     moe.norm_rows(moe.norm(40), moe.norm_io(e, e, x=torch.empty_like(e)), y=e)
 
 
+def test_layer_end_without_rows(moe):
+    d = moe.dims(T=0, S=1, H=64, E=4, k=2, I=64, E_local=4)
+    layer = layer_of(moe, d, 1)
+    e = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
+    q, s = torch.empty((0, 64), dtype=F8, device="cuda"), torch.empty((0, 1), device="cuda")
+    io = moe.norm_io(e, e, x=torch.empty_like(e), q=q, scale=s)
+    assert layer.forward(torch.empty((0, 4), device="cuda"), None, e, norm=moe.norm(64), rows=io) is None
+    assert layer.forward(torch.empty((0, 4), device="cuda"), None, xq=q, x_scale=s, norm=moe.norm(64), rows=io) is None
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T,H", [(4 * 2 ** 20 + 5, 8), (2 ** 20 + 3, 1032)])
+def test_norm_more_rows_than_workgroups(moe, T, H):
+    """Workgroups that take several rows in turn."""
+    y, h = (torch.empty((T, H), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(s)) for s in (1, 2))
+    w, pw = randn((H,), 3), randn((H,), 4)
+    out, x = torch.empty_like(h), torch.empty_like(h)
+    moe.norm_rows(moe.norm(H, w, pw, 0.5), moe.norm_io(h, out, x=x), y=y)
+    for r in (slice(0, 70), slice(T - 70, T), slice(T // 2, T // 2 + 70)):
+        (rh, bh), (rx, bx, _) = norm_and_bounds(y[r], h[r], pw, None, w, 0.5, 1e-6, 0.0)
+        within(out[r], rh, bh)
+        within(x[r], rx, bx)
+
+
 def test_norm_past_32_bit_offsets(moe):
     T, H = 140001, 16400
     h = torch.empty((T, H), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(5))
@@ -174,7 +198,8 @@ def test_norm_in_a_graph_and_on_streams(moe):
 
 ENDS = [dict(T=1, H=264, E=4, k=2, I=136, E_local=4), dict(T=9, H=1000, E=12, k=3, I=264, E_local=5, n_shared=1, I_shared=72),
         dict(T=300, H=2056, E=8, k=8, I=136, E_local=8, n_shared=2, I_shared=136), dict(T=70, H=8200, E=4, k=1, I=64, E_local=1),
-        dict(T=600, H=7168, E=4, k=2, I=64, E_local=2), dict(T=7, H=20000, E=8, k=8, I=64, E_local=6), dict(T=520, H=2504, E=32, k=32, I=64, E_local=32)]
+        dict(T=600, H=7168, E=4, k=2, I=64, E_local=2), dict(T=7, H=20000, E=8, k=8, I=64, E_local=6), dict(T=520, H=2504, E=32, k=32, I=64, E_local=32),
+        dict(T=2100, H=4104, E=4, k=2, I=64, E_local=3)]
 
 
 def layer_of(moe, d, seed):
