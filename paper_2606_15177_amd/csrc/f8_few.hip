@@ -18,6 +18,9 @@
 //
 // Two workgroups share a CU.  Rows that leave room for one only are quantised by a
 // launch.
+//
+// One token of a layer of 128 experts, H 2048, I 768, 8 of them hit: 29 us, where the
+// quantisers' launches and the items took 32.
 #include <algorithm>
 #include <type_traits>
 
@@ -334,11 +337,17 @@ bool few_f8_supported(const Segments& seg, const GemmF8& a, const GemmF8* sh, bo
   return few_lds(seg, a, sh) <= kMaxLds && few_items(seg, a, sh, gated) < (1 << 20);
 }
 
-// K in parts where the items are few, and further on long K, whose items last.
+// K in parts where the items (128 weight rows of a group that has rows) are few.
+// Weights from HBM, K undivided, in 2 and in 4 parts, us:
+//   32 items: gated K 7168 24.7, 15.9, 11.9; K 1024 8.1, 7.0, 6.5; 64: K 14336 45, 29, 24;
+//   96: gated K 2048 11.2, 9.0, 9.2; K 1408 9.2, 7.9, 8.7; 112: K 2048 11.0, 9.3, 9.2;
+//   128: K 768 8.1, 7.5, 8.2; K 5000 29, 20, 19; gated K 7168 26.1, 20.5, 20.4;
+//   168: K 2048 11.6, 12.2, 15.2; 192: gated K 4096 20.9, 20.8, 24.0; 256: K 768 8.8, 9.8,
+//     14.5; 448: gated K 4096 36.5, 38.6, 43.9.
 Cut few_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
   const int cols = gated ? 64 : 128;
   const long long hit = static_cast<long long>(seg.hit_groups) * ceil_div(a.N, cols) + (sh ? ceil_div(sh->N, cols) : 0);
-  return {hit <= 64 ? 4 : hit <= 128 || (hit <= 512 && a.K >= 4096) ? 2 : 1, chunk_rows(seg, sh), false};
+  return {hit <= 64 ? 4 : hit <= 128 ? 2 : 1, chunk_rows(seg, sh), false};
 }
 
 hipError_t launch_few_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st) {

@@ -2,7 +2,48 @@
 // per group than fill 192-row tiles.  Bound by reading the weights of the groups that
 // have rows once; groups of many rows add MFMA work.
 //
-// TODO-COMMENT
+// Items.  A workgroup of four waves takes a chunk of the token rows of one group
+// times a block of weight rows.  K undivided: up to 128 token rows, 128 weight
+// rows for groups of up to 64 rows (narrow items), 256 or 128 for larger ones
+// (wide).  A wave owns blocks of 32 weight rows (gated: 16 gate rows and the 16
+// up rows of the same columns, which meet in one lane of the MFMA's result) and
+// all rows of the chunk.  Where a launch has few items, KP = 2 or 4 groups of
+// waves split K, over a half, a quarter or (KP 4, HALF) an eighth of 128 weight
+// rows each and chunks of 64, 32 or 8 token rows, and add their fp32 sums through
+// LDS in the order of the parts.  Weights from HBM: 8 experts of gate and up 4096 x
+// 14336 with 4 rows each 143 us (6.5 TB/s), 128 of 2048 x 768 with 16 rows 67 us (6.0),
+// 1 x 2048 x 7168 9.3 us, of which a launch of nothing is 2.
+//
+// Scales.  The MFMAs of 128 columns of a row and a block of weight rows start from
+// zero; a lane of their result belongs to one token row, so that one factor (its row's
+// scale times the block's) multiplies all 16 elements on their way into the
+// accumulators.  Those stay in ordinary registers, where the vector unit adds.  The
+// rows' scales come through the ring with the stage, one float for each row; the
+// blocks' are held across the lanes, 64 stages at a time.
+//
+// Pipeline.  buffer_load_dwordx4 ... lds into a ring of K stages, D - 1 stages
+// ahead.  One barrier per stage, none where a wave reads its own loads alone (KP 4).
+// With K divided the next stage's fragments are read among the MFMAs of one, since
+// then a SIMD has no other wave to run.  Chunks of up to 8 rows hold no more in the
+// ring.  16-byte chunk c of a row sits at a slot rotated by the row, which spreads a
+// fragment's rows over the banks.  Each workgroup starts its walk along K elsewhere, so
+// that rows that lie a power of two apart spread over the memory channels.  A stage is
+// 128 bytes, and so one block of scales; wide items, whose ring would not fit, take half
+// a block at a time and scale each half by itself.
+//
+// Order.  Items are numbered per kind (shared, wide, narrow) by group, column
+// block, chunk; an XCD owns a contiguous run of each kind, so that a group's
+// token rows and the weight block that its chunks share stay in one L2.  Within
+// an XCD heavy (shared and wide) and narrow items take turns of eight, a
+// multiple of its shader engines.
+//
+// Caches.  Weights that one workgroup alone reads, in whole 128-byte lines, leave
+// the L2 first.  From HBM, us without the hint and with it: 8 experts of gate and up
+// 4096 x 14336 with 16 rows each 165 and 145, 32 of 7168 x 2048 with 8 159 and 139, 64
+// of 2048 x 1408 with 12 71 and 63, 128 of 768 x 2048 (down) with 16 47 and 44.  Not in
+// the small launches that divide K, whose weights a program may find in the cache
+// behind the L2 again: from that cache 1 x 2048 x 7168 9.1 without it and 9.5 with it,
+// 32 x 4096 x 14336 16.8 and 21.1.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,10 +66,8 @@ constexpr int kTurn = 8;
 constexpr int kItemThreads = 4 * kWave;
 
 // LDS of a workgroup, and so workgroups per CU: two, or one where K is divided
-// over chunks of more than 8 rows (the launch has hardly more than one per CU).
-// More than the ring is worth keeps the next launch waiting: 80 KB and rings of
-// four stages against 160 KB and seven, 1 x 2048 x 7168 8.2 and 9.5 us; 96 against
-// 160, 256 x 1024 x 1024 5.1 and 5.4; 128 against 160, 777 x 1003 x 528 6.2 and 6.5.
+// over chunks of more than 8 rows (the launch has hardly more than one per CU).  Each
+// is what its rings need; 160 KB for all of one workgroup per CU took the same time.
 constexpr int item_lds(int parts, int chunk) {
   return 1024 * (parts == 1 || chunk == kBriefChunk ? 80 : chunk == 32 ? 100 : parts == 2 ? 128 : 160);
 }
@@ -551,6 +590,8 @@ hipError_t launch_kp(long long blocks, const ItemsF8& ma, hipStream_t st) {
 //
 // In 4 parts and still at most half a chip of workgroups, a wave takes 16 weight
 // rows instead of 32: half of an MFMA's rows go unused, twice as many CUs read.
+// Weights from HBM, us, 32 rows and 16: 8 x 4096 x 14336 18.6 and 15.6, 16 rows 21.9
+// and 18.3, 32 rows 26.7 and 23.1, 1 x 2048 x 7168 9.4 and 9.3.
 Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
   const int cols = gated ? kItemRows / 2 : kItemRows;
   // items of 128 weight rows and so many token rows

@@ -2,7 +2,51 @@
 // token rows on v_mfma_f32_16x16x128_f8f6f4, operands straight into LDS, one wave per
 // SIMD.
 //
-// TODO-COMMENT
+// Mathematics.  A stage is 128 columns, one block of scales: a result's MFMA starts
+// from zero and is added to its accumulator times the row's and the matrix block's
+// scale, four fused multiply-adds per lane for the 16 x 16 results of an MFMA of 32
+// cycles.  So the accumulators are ordinary registers (192 of 512), the fragments
+// accumulation registers.  (32 x 32 x 64 MFMAs have as many additions, 16 at a time
+// behind two of them: dense 16384 x 4096 x 7168 467 us where these take 435.)  A result is added three MFMAs after it was begun; the
+// weights' scales of a wave's block are one (gated two) per stage, held across the
+// lanes for 64 stages, the rows' come with the stage.
+//
+// Bound: the board's power, and issue.  431 to 443 us (2.2 PFLOP/s) at 1.7 to 1.9 GHz
+// with the MFMAs busy 53 % of the time; the library's product of e4m3 with one scale
+// per tensor, which adds nothing beside its MFMAs, 303.  Of a stage's 1.48 us (256
+// workgroups; 1.09 with 64, whose clock is higher) copies with a part left out take
+// 1.00 without the loads into LDS, 1.39 without the fragments' reads, 1.22 without the
+// additions, 0.88 with the loads alone, 0.82 with the MFMAs alone: what moves costs
+// clock.  Without gain: fragments in two sets (430), a second barrier to load earlier
+// (1.53 us per stage), row scales four stages at a time, 4, 6 or 16 row tiles to a block.
+//
+// Tiles.  192 token rows x 256 weight rows of one group, four waves two by two, 96 x
+// 128 each: 256 rows would leave no registers for the additions.  Gated products take
+// 128 gate and the 128 up rows of the same columns, so that both sums of an output
+// meet in one lane, and the tile's 128 hidden columns share a scale: the tile quantises
+// them, its rows' largest magnitudes meet in LDS.  (bf16 hidden rows and a launch that
+// quantises them: 3 to 12 us more.)  Tile ids go group by group; within a group by
+// blocks of 8 row tiles, column tiles within a block, row tiles fastest: the 32 tiles
+// that run on one XCD at a time share weight tiles and token tiles in its L2.  Each
+// round of the grid is dealt to the XCDs in contiguous shares, the last partly filled
+// one too.  The shared experts (static rows) are one more group, first, with operands
+// of its own.
+//
+// Last round.  Where the tiles past the last whole round of the grid are at most
+// half (a quarter) of the workgroups, each is run in two (four) parts of its rows on as
+// many CUs.  So is an only round: the grid is sized for the parts.
+//
+// A group's last tile: rows past its end cost no traffic (their loads lie past the
+// descriptor's range), and a tile of up to 96 or 64 rows takes half or a third of the
+// MFMAs, the four waves side by side along the weights.
+//
+// Stages and pipeline.  A stage is an X and a W part [192 and 256 rows x 128 bytes] and
+// the rows' scales; rings of two X and three W parts take 147 KB of LDS.  16-byte chunk
+// c of row r sits at slot c ^ ((r / 2) % 8).  One barrier per stage, before its last two
+// row tiles, once the wave's loads of the next stage have landed and its LDS reads
+// are done; past it the next stage's fragments take the place of those that are done
+// with, and X of two stages on goes into the slot of this one; W of two on went out
+// before it, into the slot of the stage before.  Stages run on across tiles.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
