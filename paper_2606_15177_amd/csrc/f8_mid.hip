@@ -576,17 +576,21 @@ hipError_t launch_kp(long long blocks, const ItemsF8& ma, hipStream_t st) {
 
 // With the sums of few items (64 rows x 128 weight rows each, of an evenly
 // routed batch) most CUs would idle, and an item runs through its whole K
-// alone: K in parts.  Up to two per CU, two parts still win where groups have more than
-// 64 rows, whose wide items of 128 rows would leave CUs idle; where every item has a
-// chunk of its own the undivided K does, whose workgroups share a CU.  Weights from HBM,
-// K undivided, in 2 and in 4 parts, us:
+// alone: K in parts.  Up to two per CU (on short K less, for what uneven groups add)
+// two parts still win where groups have more than 64 rows, whose wide items of 128
+// rows would leave CUs idle; where every item has a chunk of its own the undivided K
+// does, whose workgroups share a CU.  Weights from HBM, K undivided, in 2 and in 4
+// parts, us:
 //   static rows: 64 items, 64 x 4096 x 14336 68.5, 43.8, 25.5; 128, 64 x 16384 x 4096
 //     25.4, 18.9, 28.7; 157, 64 x 20000 x 8192 44.9, 56.0, 62.2; 158, 96 x 10000 x 4096 40.8,
 //     26.7, 28.6; 189, 396 x 3391 x 12416 121, 68, 79; 256, 96 x 16384 x 2048 23.3, 18.2, 27.7,
 //     1000 x 2048 x 768 12.2, 12.0, 21.1; 392, 849 x 3534 x 4367 47, 56, 79;
 //   groups at a mean of 40 and 48 rows: 6 of N 4096, K 7168 (192 items) 41, 52, 60 and 68, 52,
 //     73; 8 of K 14336 (256) 86, 105, 144 and 131, 139, 161; gated at 60, 2 of N 7168, K 7168
-//     (224) 43, 55, 78.
+//     (224) 43, 55, 78; at 130, 16 of N 520, K 4096 (240) 41, 28, 32; at 190, 6 of N 1400, K
+//     2048 (198) 24, 20, 32, 5 of N 2048, K 1408 (240) 19, 25, 35, 16 of N 512, K 1000 (192)
+//     15.6, 16.0, 26.7; 10 of N 517, K 1003 with room for 260 each (250) and half of it
+//     full 15.8, 9.4, 14.5.
 //
 // In 4 parts and still at most half a chip of workgroups, a wave takes 16 weight
 // rows instead of 32: half of an MFMA's rows go unused, twice as many CUs read.
@@ -604,7 +608,7 @@ Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool ga
   const bool wide = a.offsets ? !gated && seg.mean_rows > kWideMean : a.static_rows > kWideRows;
   Cut c{1, kChunk, false};
   if (items <= 64) c.parts = 4;
-  else if (items <= 128 || (wide && items <= (a.offsets ? 192 : 256))) c.parts = 2;
+  else if (items <= 128 || (wide && items <= (!a.offsets ? 256 : a.K >= kLongK ? 255 : 208))) c.parts = 2;
   if (c.parts > 1) c.rows = seg.max_rows <= kBriefChunk ? kBriefChunk : items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
   c.half = !gated && c.parts == 4 && count(32) <= kFewHalf;
   if (c.half && c.rows > 32) c.rows = 32;
