@@ -333,9 +333,22 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     if constexpr (GATED) to[1] = p.ws1[at];
   };
 
+  // Quantised results leave the registers without LDS (1 to 3 % of a launch; bf16 ones,
+  // whose rows are twice as long, lose as much so).  A lane holds columns 4 q .. 4 q + 3 (q
+  // its quarter of the wave) of row lane % 16 of each 16 x 16 tile; swaps of neighbouring
+  // quarters and of halves between two tiles' registers gather 16 bytes of a row.
+  auto swap16 = [](uint32_t& x, uint32_t& y) {  // even quarters x and the next one's, odd ones the last one's y and y
+    const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = r[0], y = r[1];
+  };
+  auto swap32 = [](uint32_t& x, uint32_t& y) {  // the same of halves
+    const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    x = r[0], y = r[1];
+  };
+
   // A gated tile's hidden rows, quantised: its 128 columns share a scale, so the
   // largest of a row is found over the waves that hold parts of it.
-  auto quantize = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w, unsigned char* scr) {
+  auto quantize = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w) {
     constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
     constexpr int TILES = TN / 2;                    // of 16 columns
     constexpr int PARTS = TN == 8 ? 2 : 4;           // waves that hold a row
@@ -359,43 +372,49 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
           top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, h[tm][tn][i] & 0x7fff7fffu));
         }
       }
-      uint32_t t = max(static_cast<uint32_t>(top[0]), static_cast<uint32_t>(top[1]));
-      t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), 16)));
-      t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), 32)));
-      if (eq == 0) tops[(row_w + 16 * tm + erow) * PARTS + col_part] = t;
+      uint32_t t = max(static_cast<uint32_t>(top[0]), static_cast<uint32_t>(top[1])), u = t;
+      swap16(t, u);
+      u = t = max(t, u);
+      swap32(t, u);
+      if (eq == 0) tops[(row_w + 16 * tm + erow) * PARTS + col_part] = max(t, u);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_waitcnt(kWaitLds);
     phase_barrier();
     const long long row0 = ti.row_base + ti.m0 + row_w;
     const int blocks = ceil_div(p.N, kF8Block), padded = ceil_div(p.N, 16) * 16;
-    constexpr int CH = TILES;                        // 16-byte chunks of a row's part
-    auto place = [&](int buf, int r, int c) { return scr + buf * 1024 + r * (16 * CH) + ((c ^ ((r / (8 / CH)) % CH)) << 4); };
-    auto put = [&](int tm) {
-      const int r = ln / CH, c = ln % CH, col = col_w + 16 * c;
-      if (r >= 16) return;                           // (two chunks a row: half of the lanes)
-      const u32x4 v = *reinterpret_cast<const u32x4*>(place(tm & 1, r, c));
-      if (16 * tm + r < rows && col < padded) store16(p.outq + (row0 + 16 * tm + r) * p.ldq + col, v);
-    };
+    uint32_t top[TM];
 #pragma unroll
     for (int tm = 0; tm < TM; ++tm) {
-      uint32_t t = 0;
+      top[tm] = 0;
 #pragma unroll
-      for (int q = 0; q < PARTS; ++q) t = max(t, tops[(row_w + 16 * tm + erow) * PARTS + q]);
-      const F8Scale sc = f8_scale(t << 16);
-      if (eq == 0 && col_part == 0 && 16 * tm + erow < rows) p.outs[(row0 + 16 * tm + erow) * blocks + ti.nt] = sc.scale;
-#pragma unroll
-      for (int tn = 0; tn < TILES; ++tn)
-        *reinterpret_cast<uint32_t*>(place(tm & 1, erow, tn) + 4 * eq) = quantize_f8_4(h[tm][tn][0], h[tm][tn][1], sc);
-      if (tm > 0) put(tm - 1);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int q = 0; q < PARTS; ++q) top[tm] = max(top[tm], tops[(row_w + 16 * tm + erow) * PARTS + q]);
     }
-    put(TM - 1);
+    const int col = col_w + (TILES == 4 ? 16 * eq : 16 * (eq & 1) + 8 * (eq >> 1));
+    uint8_t* to = p.outq + (row0 + erow) * p.ldq + col;
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) {
+      const F8Scale sc = f8_scale(top[tm] << 16);
+      const bool in = 16 * tm + erow < rows;
+      if (eq == 0 && col_part == 0 && in) p.outs[(row0 + 16 * tm + erow) * blocks + ti.nt] = sc.scale;
+      uint32_t v[TILES];
+#pragma unroll
+      for (int tn = 0; tn < TILES; ++tn) v[tn] = quantize_f8_4(h[tm][tn][0], h[tm][tn][1], sc);
+      if constexpr (TILES == 4) {
+        swap32(v[0], v[2]);
+        swap32(v[1], v[3]);
+        swap16(v[0], v[1]);
+        swap16(v[2], v[3]);
+        if (in && col < padded) store16(to + 16 * tm * p.ldq, u32x4{v[0], v[1], v[2], v[3]});
+      } else {
+        swap16(v[0], v[1]);
+        if (in && col < padded) *reinterpret_cast<u32x2*>(to + 16 * tm * p.ldq) = u32x2{v[0], v[1]};
+      }
+    }
   };
   auto epilogue = [&](auto tn_c, auto tm_c, const TileInfo& ti, int col_w, unsigned char* scr) {
     constexpr int TN = decltype(tn_c)::value, TM = decltype(tm_c)::value;
-    constexpr int TILES = GATED ? TN / 2 : TN;      // of 16 output columns
-    constexpr int PASS = TILES < 4 ? TILES : 4;     // ... stored at a time
+    constexpr int PASS = 4;                         // tiles of 16 columns stored at a time
     constexpr int CH = 2 * PASS;                    // 16-byte chunks of a row of them
     const GemmF8& p = prob(ti);
     const int row_w = wave_row(ti);
@@ -408,7 +427,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
     auto emit = [&](auto inside) {
       constexpr bool kInside = decltype(inside)::value;  // every row and column of the wave's block is a result
 #pragma unroll
-      for (int pass = 0; pass < TILES / PASS; ++pass) {
+      for (int pass = 0; pass < TN / PASS; ++pass) {
         // 32 rows' results go out while the next ones' are computed
         const int rr = ln / CH, cc = ln % CH;
         const int col = col_w + 16 * PASS * pass + 8 * cc;
@@ -430,12 +449,7 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
 #pragma unroll
             for (int h = 0; h < PASS; ++h) {
               const int tn = PASS * pass + h, tm = 2 * m + t;
-              float o[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                o[i] = acc[tn][tm][i];
-                if constexpr (GATED) o[i] = silu(o[i]) * acc[tn + TILES][tm][i];
-              }
+              const f32x4 o = acc[tn][tm];
               *reinterpret_cast<u32x2*>(place(m & 1, 16 * t + erow, 2 * h + eq / 2) + 8 * (eq % 2)) =
                   u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
             }
@@ -446,9 +460,9 @@ __global__ __launch_bounds__(kTiledThreads) __attribute__((amdgpu_waves_per_eu(1
       }
     };
     if constexpr (GATED) {
-      quantize(tn_c, tm_c, ti, col_w, scr);
+      quantize(tn_c, tm_c, ti, col_w);
     } else {
-      if (rows >= 16 * TM && col_w + 16 * TILES <= p.N) emit(std::true_type{});
+      if (rows >= 16 * TM && col_w + 16 * TN <= p.N) emit(std::true_type{});
       else emit(std::false_type{});
     }
   };
