@@ -7,9 +7,10 @@
 // scale, four fused multiply-adds per lane for the 16 x 16 results of an MFMA of 32
 // cycles.  So the accumulators are ordinary registers (192 of 512), the fragments
 // accumulation registers.  (32 x 32 x 64 MFMAs have as many additions, 16 at a time
-// behind two of them: dense 16384 x 4096 x 7168 467 us where these take 435.)  A result is added three MFMAs after it was begun; the
-// weights' scales of a wave's block are one (gated two) per stage, held across the
-// lanes for 64 stages, the rows' come with the stage.
+// behind two of them: dense 16384 x 4096 x 7168 467 us where these take 435.)  A result
+// is added three MFMAs after it was begun; the weights' scales of a wave's block are one
+// (gated two) per stage, held across the lanes for 64 stages, the rows' come with the
+// stage.
 //
 // Bound: the board's power, and issue.  431 to 443 us (2.2 PFLOP/s) at 1.7 to 1.9 GHz
 // with the MFMAs busy 53 % of the time; the library's product of e4m3 with one scale
@@ -18,7 +19,10 @@
 // 1.00 without the loads into LDS, 1.39 without the fragments' reads, 1.22 without the
 // additions, 0.88 with the loads alone, 0.82 with the MFMAs alone: what moves costs
 // clock.  Without gain: fragments in two sets (430), a second barrier to load earlier
-// (1.53 us per stage), row scales four stages at a time, 4, 6 or 16 row tiles to a block.
+// (1.53 us per stage), row scales four stages at a time, 4, 6 or 16 row tiles to a block,
+// weights a stage earlier, all loads behind the barrier (32 experts of gate and up 7168 x
+// 2048 with 1000 rows each 925 us, 1040).  A gated tile's end, of vector work alone, is
+// 4 to 5 us (a launch without it: 64 experts of 2048 x 1408 with 96 rows 103 and 89).
 //
 // Tiles.  192 token rows x 256 weight rows of one group, four waves two by two, 96 x
 // 128 each: 256 rows would leave no registers for the additions.  Gated products take
