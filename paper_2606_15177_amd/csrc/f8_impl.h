@@ -9,7 +9,10 @@
 // Precision: the f8f6f4 MFMA adds the products of eight neighbouring columns first,
 // aligned to the largest of them, and cuts off what lies 2^-13 below it (found with
 // +1, -1 and a small third product among the eight); those sums and everything after
-// are fp32.  That is 2^-9 of an e4m3 step.  The older fp8 MFMAs run at half its rate.
+// are fp32.  That is 2^-9 of an e4m3 step.  (The older fp8 MFMAs cut off the same, at
+// half the rate.)  Where it moves a hidden value over the border between two e4m3 values,
+// that value is an e4m3 step off: the experts' outputs lie 0.0022 to 0.0027 of their norm
+// from 64 bits, where products in fp32, rounded once, leave 0.0017.
 #pragma once
 
 #include "i8_impl.h"
