@@ -40,6 +40,8 @@ __device__ __forceinline__ f32x4 mfma_f8_16(i32x8 a, i32x8 b, f32x4 c) {
 int tiled_f8_grid(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 hipError_t launch_items_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated, hipStream_t st);
 Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
+// Whether items with K in two parts are at most two per CU.
+bool items_f8_fit(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 long long items_f8_blocks(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 // Bf16 rows (xb), few of them per group (any number is computed): each
 // workgroup quantises the rows that it multiplies.

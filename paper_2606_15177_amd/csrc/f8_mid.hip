@@ -57,7 +57,8 @@ constexpr int kSplitChunk = 64;     // ... of any item where K is split (32 wher
 constexpr int kFewHalf = 32;        // items (of 32 token rows) up to which they are halved once more, K in 4 parts
 constexpr int kBriefChunk = 8;      // ... where no group has more rows
 constexpr int kWideRows = 64;       // groups of more rows take wide items
-constexpr int kWideMean = 44;       // ... which an uneven batch of so many rows per group has
+constexpr int kWideMean = 44;       // ... which an uneven batch of so many rows per group has,
+constexpr int kUneven = 192;        // ... and then more items than this many even ones stand for
 constexpr int kItemRows = 128;      // weight rows of a narrow item
 constexpr int kFewWide = 128;       // fewer wide items than this take 128 weight rows: half the CUs' worth
 constexpr int kOneWide = 256;       // ... or fewer than this, one per CU, in a launch of fewer items than
@@ -65,11 +66,12 @@ constexpr int kSlots = 512;         // workgroups fit the chip
 constexpr int kTurn = 8;
 constexpr int kItemThreads = 4 * kWave;
 
-// LDS of a workgroup, and so workgroups per CU: two, or one where K is divided
-// over chunks of more than 8 rows (the launch has hardly more than one per CU).  Each
-// is what its rings need; 160 KB for all of one workgroup per CU took the same time.
-constexpr int item_lds(int parts, int chunk) {
-  return 1024 * (parts == 1 || chunk == kBriefChunk ? 80 : chunk == 32 ? 100 : parts == 2 ? 128 : 160);
+// LDS of a workgroup, and so workgroups per CU: two, or one where K is divided over
+// chunks of more than 8 rows and the launch has no more than one per CU (unless PAIR:
+// two, whose rings are shorter).  Each is what its rings need; 160 KB for all of one
+// workgroup per CU took the same time.
+constexpr int item_lds(int parts, int chunk, bool pair) {
+  return 1024 * (parts == 1 || chunk == kBriefChunk || pair ? 80 : chunk == 32 ? 100 : parts == 2 ? 128 : 160);
 }
 
 struct ItemsF8 {
@@ -95,7 +97,7 @@ __device__ __forceinline__ void wait_stage(int j) {
   }
 }
 
-template <bool GATED, int KP, int CHUNK, bool HALF>
+template <bool GATED, int KP, int CHUNK, bool HALF, bool PAIR>
 __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void items_f8_kernel(ItemsF8 ma) {
   constexpr int FULL_COLS = GATED ? kItemRows / 2 : kItemRows;  // output columns of 128 weight rows
   constexpr int OUT_COLS = FULL_COLS / KP / (HALF ? 2 : 1);     // ... of a narrow item
@@ -276,7 +278,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int WL = WB * WR / RPI;              // weight loads per wave and stage
     constexpr int LOADS = XL + 1 + WL;
     constexpr int KS = BK / 64;                    // MFMA K-steps per stage
-    static_assert(D * STAGE <= item_lds(KP, CHUNK), "the ring fits");
+    static_assert(D * STAGE <= item_lds(KP, CHUNK, PAIR), "the ring fits");
     static_assert(FEW ? RPI == 8 : XL * RPI * WN == XR, "whole loads fill the token rows");
     const int lr = lane / CPR;                     // row of a load
     const int wn = wave % WN, wk = wave / WN;
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     }
     __builtin_amdgcn_s_waitcnt(wait_vm(0));  // the loads past the last stage: nothing may still write the LDS
     if constexpr (NK > 1) {
-      static_assert((NK - 1) * WN * WB * NSUB * 16 * kWave * 4 <= item_lds(KP, CHUNK), "the partial sums fit the LDS");
+      static_assert((NK - 1) * WN * WB * NSUB * 16 * kWave * 4 <= item_lds(KP, CHUNK, PAIR), "the partial sums fit the LDS");
       float* red = reinterpret_cast<float*>(smem);
       __syncthreads();  // every wave is past its last stage
       if (wk > 0) {
@@ -537,7 +539,6 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   using C2 = integral_constant<int, 2>;
   using C3 = integral_constant<int, 3>;
   using C4 = integral_constant<int, 4>;
-  using C5 = integral_constant<int, 5>;
   using K64 = integral_constant<int, 64>;
   using K128 = integral_constant<int, 128>;
   constexpr std::false_type whole{};
@@ -550,8 +551,8 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   } else if constexpr (CHUNK == kBriefChunk) {
     body(C1{}, C1{}, integral_constant<int, KP>{}, K128{}, integral_constant<int, HALF ? 6 : KP == 2 ? 4 : 3>{}, few);
   } else if constexpr (KP == 2) {
-    if (rows > 32) body(C2{}, C1{}, C2{}, K128{}, C3{}, whole);
-    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, C5{}, whole);
+    if (rows > 32) body(C2{}, C1{}, C2{}, K128{}, integral_constant<int, PAIR ? 2 : 3>{}, whole);
+    else if (rows > 8) body(C1{}, C1{}, C2{}, K128{}, integral_constant<int, PAIR ? 3 : 5>{}, whole);
     else body(C1{}, C1{}, C2{}, K128{}, C4{}, few);
   } else {
     if constexpr (CHUNK > 32) {
@@ -562,35 +563,51 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
   }
 }
 
-template <bool GATED, int KP, int CHUNK, bool HALF = false>
+template <bool GATED, int KP, int CHUNK, bool HALF = false, bool PAIR = false>
 hipError_t launch_kp(long long blocks, const ItemsF8& ma, hipStream_t st) {
-  constexpr int lds = item_lds(KP, CHUNK);
+  constexpr int lds = item_lds(KP, CHUNK, PAIR);
   static unsigned long long lds_set = 0;  // devices with the LDS limit raised
-  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_f8_kernel<GATED, KP, CHUNK, HALF>), lds, &lds_set);
+  const hipError_t e = set_max_dynamic_lds(reinterpret_cast<const void*>(&items_f8_kernel<GATED, KP, CHUNK, HALF, PAIR>), lds, &lds_set);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((items_f8_kernel<GATED, KP, CHUNK, HALF>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), lds, st, ma);
+  hipLaunchKernelGGL((items_f8_kernel<GATED, KP, CHUNK, HALF, PAIR>), dim3(static_cast<unsigned>(blocks)), dim3(kItemThreads), lds, st, ma);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Items of 64 rows by `cols` columns, of an evenly routed batch.
+static long long count_items(const Segments& seg, const GemmF8& a, const GemmF8* sh, int rows, int cols) {
+  auto chunks = [&](int n) { return std::max(1, ceil_div(n, rows)); };
+  return (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +
+         (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
+}
+
+// K in two parts is for at most two workgroups per CU.
+bool items_f8_fit(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
+  return count_items(seg, a, sh, kSplitChunk, gated ? kItemRows / 4 : kItemRows / 2) <= kSlots;
+}
+
 // With the sums of few items (64 rows x 128 weight rows each, of an evenly
 // routed batch) most CUs would idle, and an item runs through its whole K
-// alone: K in parts.  Up to two per CU (on short K less, for what uneven groups add)
-// two parts still win where groups have more than 64 rows, whose wide items of 128
-// rows would leave CUs idle; where every item has a chunk of its own the undivided K
-// does, whose workgroups share a CU.  Weights from HBM, K undivided, in 2 and in 4
-// parts, us:
-//   static rows: 64 items, 64 x 4096 x 14336 68.5, 43.8, 25.5; 128, 64 x 16384 x 4096
-//     25.4, 18.9, 28.7; 157, 64 x 20000 x 8192 44.9, 56.0, 62.2; 158, 96 x 10000 x 4096 40.8,
-//     26.7, 28.6; 189, 396 x 3391 x 12416 121, 68, 79; 256, 96 x 16384 x 2048 23.3, 18.2, 27.7,
-//     1000 x 2048 x 768 12.2, 12.0, 21.1; 392, 849 x 3534 x 4367 47, 56, 79;
-//   groups at a mean of 40 and 48 rows: 6 of N 4096, K 7168 (192 items) 41, 52, 60 and 68, 52,
-//     73; 8 of K 14336 (256) 86, 105, 144 and 131, 139, 161; gated at 60, 2 of N 7168, K 7168
-//     (224) 43, 55, 78; at 130, 16 of N 520, K 4096 (240) 41, 28, 32; at 190, 6 of N 1400, K
-//     2048 (198) 24, 20, 32, 5 of N 2048, K 1408 (240) 19, 25, 35, 16 of N 512, K 1000 (192)
-//     15.6, 16.0, 26.7; 10 of N 517, K 1003 with room for 260 each (250) and half of it
-//     full 15.8, 9.4, 14.5.
+// alone: K in parts.  In two parts a workgroup takes 64 weight rows, up to one per CU
+// with the longer ring, up to two per CU in pairs with the shorter one, which still wins
+// where groups have more than 64 rows, whose wide items of 128 rows would leave CUs
+// idle.  Where every item has a chunk of its own, or an uneven batch of some 60 rows a
+// group more than the count says, the undivided K does.  Weights from HBM, us: K in 2
+// parts with a workgroup per CU, in 2 with two, undivided, in tiles (f8_tiled.hip):
+//   static rows: 112 items, 400 x 2048 x 7168 22.2, 22.9, 68, 41; 128, 500 x 2048 x 14336
+//     39, 46, 128, 75; 152, 1200 x 1003 x 2000 18.3, 12.9, 24.5, 18.4; 224, 400 x 4096 x 4096
+//     26.4, 18.6, 41, 26.7, 256 x 7168 x 2048 17.4, 12.1, 23, 17; 250, 128 x 16000 x 7168 50,
+//     46, 70, 55; 264, 2100 x 1024 x 1408 22.2, 15.4, 18.0, 14.0; 304, 1200 x 2048 x 7168 62,
+//     62, 68, 42; 392, 400 x 7168 x 2048 30, 20.7, 23.7, 18.5; a chunk of its own, 157, 64 x
+//     20000 x 8192 58, 54, 45, 65;
+//   groups: 100, 10 of N 517, K 1003 with 90 rows 9.3, 8.8, 15.9, 14.5; 160, 16 of N 520, K
+//     4096 with 90 29, 19, 41, 29; 192, 12 of N 2048, K 2048 with 60 23, 16, 25, 22; 240, 5 of
+//     N 2048, K 1408 with 190 25, 18, 19, 15; 256, 8 of N 4096, K 14336 with 30 105, 104, 84,
+//     119, with 60 144, 176, 134, 126; gated, 192, 3 of N 4096, K 4096 with 60 36, 30, 43, 41;
+//     256, 4 of N 2048, K 7168 with 90 53, 48, 70, 59.
+// In four parts: 64 items, 64 x 4096 x 14336 25.5 (in two 43.8, undivided 68.5), 128 x 4096
+// x 4096 12.3; 128, 64 x 16384 x 4096 28.7 (18.9, 25.4).
 //
 // In 4 parts and still at most half a chip of workgroups, a wave takes 16 weight
 // rows instead of 32: half of an MFMA's rows go unused, twice as many CUs read.
@@ -598,19 +615,15 @@ hipError_t launch_kp(long long blocks, const ItemsF8& ma, hipStream_t st) {
 // and 18.3, 32 rows 26.7 and 23.1, 1 x 2048 x 7168 9.4 and 9.3.
 Cut items_f8_cut(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
   const int cols = gated ? kItemRows / 2 : kItemRows;
-  // items of 128 weight rows and so many token rows
-  auto count = [&](int rows) {
-    auto chunks = [&](int n) { return std::max(1, ceil_div(n, rows)); };
-    return (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +
-           (sh ? static_cast<long long>(chunks(sh->static_rows)) * ceil_div(sh->N, cols) : 0);
-  };
-  const long long items = count(kSplitChunk);
-  const bool wide = a.offsets ? !gated && seg.mean_rows > kWideMean : a.static_rows > kWideRows;
+  const long long items = count_items(seg, a, sh, kSplitChunk, cols), halves = count_items(seg, a, sh, kSplitChunk, cols / 2);
+  const int rows = a.offsets ? seg.mean_rows : a.static_rows;
+  const bool several = rows > kWideRows || (a.offsets && rows > kWideMean && items <= kUneven);
   Cut c{1, kChunk, false};
   if (items <= 64) c.parts = 4;
-  else if (items <= 128 || (wide && items <= (!a.offsets ? 256 : a.K >= kLongK ? 255 : 208))) c.parts = 2;
+  else if (items <= 128 || (several && halves <= kSlots)) c.parts = 2;
   if (c.parts > 1) c.rows = seg.max_rows <= kBriefChunk ? kBriefChunk : items <= 32 && seg.max_rows > 32 ? 32 : kSplitChunk;
-  c.half = !gated && c.parts == 4 && count(32) <= kFewHalf;
+  c.pair = c.parts == 2 && c.rows == kSplitChunk && halves > kSlots / 2;
+  c.half = !gated && c.parts == 4 && count_items(seg, a, sh, 32, cols) <= kFewHalf;
   if (c.half && c.rows > 32) c.rows = 32;
   return c;
 }
@@ -628,6 +641,7 @@ long long items_f8_blocks(const Segments& seg, const GemmF8& a, const GemmF8* sh
 template <bool GATED>
 static hipError_t launch_cut(const Cut& c, long long blocks, const ItemsF8& ma, hipStream_t st) {
   if (c.parts == 1) return launch_kp<GATED, 1, kChunk>(blocks, ma, st);
+  if (c.parts == 2 && c.pair) return launch_kp<GATED, 2, kSplitChunk, false, true>(blocks, ma, st);
   if (c.parts == 2)
     return c.rows == kBriefChunk ? launch_kp<GATED, 2, kBriefChunk>(blocks, ma, st) : launch_kp<GATED, 2, kSplitChunk>(blocks, ma, st);
   if constexpr (!GATED)

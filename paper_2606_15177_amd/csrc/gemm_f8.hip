@@ -6,35 +6,35 @@
 namespace moe {
 namespace {
 
-// Tiles want rows that fill them, and enough of them; on short K, where an item's
-// turnaround is short too, more.  A gated tile also saves the launch that quantises
-// the hidden rows (3 to 12 us).  Both sides, us (items, tiles):
+// Tiles want rows that fill them, and more of them than items with K in two parts run at
+// once (both sides of that in f8_mid.hip); where rows fill them less, on short K, many.  A
+// gated tile also saves the launch that quantises the hidden rows (3 to 12 us).  Both
+// sides, us (items, tiles):
 //   rows of a group: 8 experts of K 4096, N 14336 gated at a mean of 64 179 and 190, of
 //     80 233 and 196; 32 of K 7168, N 2048 gated at 80 222 and 227, at 96 299 and 229;
 //     64 of K 2048, N 1408 gated at 96 87 and 104, at 128 112 and 107; 128 of K 2048, N
 //     768 gated at 96 104 and 106; 32 of K 2048, N 7168 at 80 102 and 111, at 96 130 and 114;
+//   past two items per CU: 16 of K 4096, N 520 at 260 43 and 32; 3 of K 7168, N 3000 at 260 70
+//     and 56; 24 of K 700, N 1024 at 90 14.4 and 13.7; 4 of K 7168, N 2048 gated at 130 71 and
+//     58; 8 of K 1000, N 1000 gated at 130 15.5 and 17.2;
 //   short K, many tiles, not gated: 128 of K 768, N 2048 at 24 53 and 48, at 96 62 and 57,
 //     at 256 130 and 97; 64 of K 1408, N 2048 at 64 46 and 47, at 96 58 and 48;
-//   few tiles: 24 of K 1000, N 520 gated, 120 tiles at a mean of 96 16 and 21; 24 of K
-//     520, N 1000, 96 tiles 12 and 12;
-//   static: 32 tiles of K 7168 23 and 42, 48 44 and 43, 64 71 and 44; 22 of K 4096 17 and
-//     26, 44 32 and 28; shorter K: 24 of K 1408 9 and 14, 32 18 and 14; 24 of K 517 8 and
-//     11, 32 13 and 11; 28 of K 2048 at 192 rows 23 and 17, at 128 (one chunk) 10 and 17.
+//   static: 64 x 30000 x 4096 31 and 40; 70 x 30000 x 4096 46 and 41, 100 x 33000 x 8200 173
+//     and 109, 80 x 40000 x 1000 21 and 17.
 constexpr int kMeanRows = 85, kMeanShort = 24;
 constexpr int kShortK = 1500;
-constexpr long long kFewTiles = 128, kFewShort = 400, kFewStatic = 44, kFewStaticShort = 28;
-constexpr int kOneChunk = 128;
+constexpr long long kFewShort = 400;
+constexpr int kOneChunk = 64;
 
 bool takes_tiles(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
   if (a.K <= kTiledMinK || (sh && sh->K <= kTiledMinK)) return false;
   if (items_f8_blocks(seg, a, sh, gated) > kMaxItemBlocks) return true;
-  const int cols = gated ? 128 : 256;
-  const bool brief = a.K < kShortK;
-  auto tiles = [&](int rows, int N) { return static_cast<long long>(ceil_div(rows, 192)) * ceil_div(N, cols); };
-  if (!a.offsets)
-    return a.static_rows > kOneChunk && tiles(a.static_rows, a.N) >= (a.K < kLongK ? kFewStaticShort : kFewStatic);
-  if (seg.groups * tiles(seg.mean_rows, a.N) + (sh ? tiles(sh->static_rows, sh->N) : 0) < (brief ? kFewShort : kFewTiles)) return false;
-  return seg.mean_rows >= (brief && !gated ? kMeanShort : kMeanRows);
+  const bool many = !items_f8_fit(seg, a, sh, gated);
+  if (!a.offsets) return a.static_rows > kOneChunk && many;
+  if (seg.mean_rows >= kMeanRows) return many;
+  auto tiles = [&](int rows, int N) { return static_cast<long long>(ceil_div(rows, 192)) * ceil_div(N, 256); };
+  return !gated && a.K < kShortK && seg.mean_rows >= kMeanShort &&
+         seg.groups * tiles(seg.mean_rows, a.N) + (sh ? tiles(sh->static_rows, sh->N) : 0) >= kFewShort;
 }
 
 }  // namespace

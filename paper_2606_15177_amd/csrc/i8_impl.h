@@ -69,6 +69,7 @@ hipError_t launch_items_i8(const Segments& seg, const GemmI8& a, const GemmI8* s
 struct Cut {
   int parts, rows;
   bool half;  // 16 weight rows per wave, not 32
+  bool pair = false;  // two workgroups per CU
 };
 Cut items_cut(const Segments& seg, const GemmI8& a, const GemmI8* sh, bool gated);
 // Bf16 rows (xb), few of them per group (any number is computed): each

@@ -758,11 +758,12 @@ def linear_plan(moe, M, N, K, G=0):
 KERNELS = [(7, 9001, 130, (ITEMS, 2, 8)), (8, 517, 1003, (ITEMS, 4, 8, HALF)), (50, 1003, 517, (ITEMS, 4, 32, HALF)),
            (7, 5001, 1003, (ITEMS, 4, 8)), (50, 4001, 517, (ITEMS, 4, 32)), (30, 1999, 1700, (ITEMS, 4, 32, HALF)),
            (260, 300, 3001, (ITEMS, 4, 32, HALF)), (50, 5003, 517, (ITEMS, 4, 64)), (60, 12003, 4100, (ITEMS, 2, 64)),
-           (777, 1003, 517, (ITEMS, 2, 64)), (4200, 2051, 380, (ITEMS, 1, 128)), (100, 33000, 8200, (ITEMS, 1, 128)),
+           (777, 1003, 517, (ITEMS, 2, 64)), (4200, 2051, 380, (ITEMS, 1, 128)), (100, 33000, 8200, (TILES, 1, 192)),
            (50, 17000, 517, (ITEMS, 1, 128)), (150, 6001, 1300, (ITEMS, 2, 64)), (5, 8200, 34000, (ITEMS, 2, 8)), (3, 300, 130000, (ITEMS, 4, 8, HALF)),
            (2500, 2100, 1700, (TILES, 1, 192)), (5003, 3801, 1501, (TILES, 1, 192)), (5003, 2803, 1501, (TILES, 1, 192)),
            (16000, 1027, 385, (TILES, 1, 192)), (2600, 2049, 8200, (TILES, 1, 192)), (1900, 2304, 12288, (TILES, 1, 192)),
-           (1350, 1500, 16500, (TILES, 1, 192)), (193, 7300, 641, (TILES, 1, 192))]
+           (1350, 1500, 16500, (TILES, 1, 192)), (193, 7300, 641, (ITEMS, 2, 64)),
+           (300, 14600, 641, (TILES, 1, 192)), (400, 4100, 700, (ITEMS, 2, 64)), (16000, 60, 500, (ITEMS, 2, 64))]
 
 
 @pytest.mark.parametrize("M,N,K,plan", KERNELS)
@@ -785,7 +786,7 @@ GROUP_KERNELS = [(ragged(8, 350, 1), 2000, 1600, (TILES, 1, 192)),
                  (ragged(30, 16, 5, 600), 1003, 900, (ITEMS, 1, 128)), ([5, 0, 70, 3], 3000, 700, (ITEMS, 2, 64)),
                  ([2, 0, 1], 1000, 700, (ITEMS, 4, 8, HALF)), ([2, 30, 0, 9], 600, 900, (ITEMS, 4, 32, HALF)),
                  ([2, 70, 0, 9, 33, 32, 8], 100, 900, (ITEMS, 4, 32, HALF)), ([3, 0, 4, 1], 2500, 500, (ITEMS, 2, 8)),
-                 (ragged(12, 60, 5), 1500, 1100, (ITEMS, 2, 64)), (ragged(24, 30, 6), 1003, 1100, (ITEMS, 1, 128)),
+                 (ragged(12, 60, 5), 1500, 1100, (ITEMS, 2, 64)), (ragged(24, 30, 6), 1003, 1100, (ITEMS, 1, 128)), (ragged(9, 200, 8), 700, 1500, (ITEMS, 2, 64)),
                  (ragged(40, 60, 9), 3000, 2300, (ITEMS, 1, 128))]
 
 
@@ -803,7 +804,7 @@ def ffn_plan(moe, d, quantised=False):
     return tuple(out[:3]), tuple(out[4:7])
 
 
-FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_shared=520), (TILES, 1, 192), (ITEMS, 1, 128)),
+FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_shared=520), (TILES, 1, 192), (TILES, 1, 192)),
                (dict(T=3300, H=2104, E=80, k=3, I=136, E_local=70), (TILES, 1, 192), (ITEMS, 1, 128)),
                (dict(T=7200, H=2104, E=300, k=4, I=136, E_local=300), (TILES, 1, 192), (ITEMS, 1, 128)),
                (dict(T=3000, H=256, E=4, k=2, I=1536, E_local=4), (ITEMS, 1, 128), (ITEMS, 2, 64)),
