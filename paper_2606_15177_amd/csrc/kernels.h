@@ -302,6 +302,9 @@ struct NormArgs {
 };
 constexpr int kNormMaxH = 32768;
 hipError_t launch_norm(const NormArgs& a, hipStream_t st);
+// Host only: workgroups that take `rows` of T rows at a time, up to `most` of them
+// (T up to 2^31 - 1).
+int norm_blocks(int T, int rows, int most);
 
 // ---- combine.hip -----------------------------------------------------------
 hipError_t launch_combine(int T, int k, int H, const uint16_t* y_perm, const int32_t* inv_pos,

@@ -1202,6 +1202,9 @@ int moe_test_ffn_f8_plan(const moe_dims* d, int quantised, int64_t out[2][4]) {
   return MOE_OK;
 }
 
+// For the tests: workgroups of the norms (moe::norm_blocks).
+int moe_test_norm_blocks(int T, int rows, int most) { return moe::norm_blocks(T, rows, most); }
+
 // For the tests: pairs per thread in moe_route_stats.
 int moe_test_stats_per(int n_pairs, int S, int E) { return moe::stats_per(n_pairs, S, E); }
 

@@ -229,7 +229,7 @@ constexpr int kFewRowsNorm = 512;    // rows that run at once with 1024 threads 
 template <int THREADS, int V>
 hipError_t launch_rows(const NormArgs& a, int blocks, hipStream_t st) {
   constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
-  const int grid = std::min(ceil_div(a.T, ROWS), blocks);
+  const int grid = norm_blocks(a.T, ROWS, blocks);
   const dim3 threads(ROWS * THREADS);
   if (a.inv_pos) hipLaunchKernelGGL((norm_kernel<THREADS, V, true>), dim3(grid), threads, 0, st, a);
   else hipLaunchKernelGGL((norm_kernel<THREADS, V, false>), dim3(grid), threads, 0, st, a);
@@ -237,6 +237,10 @@ hipError_t launch_rows(const NormArgs& a, int blocks, hipStream_t st) {
 }
 
 }  // namespace
+
+int norm_blocks(int T, int rows, int most) {
+  return static_cast<int>(std::min<long long>((static_cast<long long>(T) + rows - 1) / rows, most));
+}
 
 // A wave per row up to 1024 columns, 256 threads past that, more past 8192; where
 // there are few rows, as many threads as a row has vectors (us, 1 row of 7168: 4.9

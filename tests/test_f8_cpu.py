@@ -151,6 +151,15 @@ def test_norm_refusals(moe, change, T, code):
     assert moe._lib.moe_norm_rows(C.byref(n), C.byref(_io(moe, **change)), T, 16, 64, None) == code
 
 
+@pytest.mark.parametrize("T,rows,most,blocks", [
+    (1, 4, 2 ** 20, 1), (4, 4, 2 ** 20, 1), (5, 4, 2 ** 20, 2), (5, 1, 2 ** 20, 5), (2 ** 22 - 1, 4, 2 ** 20, 2 ** 20), (7, 1, 3, 3),
+    (2 ** 31 - 4, 4, 2 ** 20, 2 ** 20), (2 ** 31 - 3, 4, 2 ** 20, 2 ** 20), (2 ** 31 - 1, 4, 2 ** 20, 2 ** 20), (2 ** 31 - 1, 1, 2 ** 20, 2 ** 20),
+    (2 ** 31 - 1, 4, 2 ** 31 - 1, 2 ** 29)])
+def test_norm_workgroups(moe, T, rows, most, blocks):
+    """Up to the most rows that 31 bits hold."""
+    assert moe._lib.moe_test_norm_blocks(T, rows, most) == blocks
+
+
 def test_norm_parameter_refusals(moe):
     f, ok = moe._lib.moe_norm_rows, moe.MoeNorm(64, 16, 16, 1.0, 1e-6, 0.0)
     io = _io(moe)

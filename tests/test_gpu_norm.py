@@ -159,6 +159,21 @@ def test_norm_more_rows_than_workgroups(moe, T, H):
         within(x[r], rx, bx)
 
 
+def test_norm_of_the_most_rows(moe):
+    """2^31 - 1 rows, four of them a workgroup at a time; every row is looked at."""
+    T = 2 ** 31 - 1
+    few = randn((65537, 1), 1, 2.0)   # (no power of two repeats with it)
+    h = few.repeat(T // len(few) + 1, 1)[:T]
+    x, w = torch.empty_like(h), randn((1,), 2)
+    moe.norm_rows(moe.norm(1, w, eps=0.5), moe.norm_io(h, x=x))
+    _, (rx, bx, _) = norm_and_bounds(None, few, None, None, w, 1.0, 0.5, 0.0)
+    lot = 256 * len(few)
+    rx, bx = rx.repeat(256, 1), bx.repeat(256, 1)
+    for a in range(0, T, lot):
+        n = min(lot, T - a)
+        within(x[a:a + n], rx[:n], bx[:n])
+
+
 def test_norm_past_32_bit_offsets(moe):
     T, H = 140001, 16400
     h = torch.empty((T, H), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(5))
