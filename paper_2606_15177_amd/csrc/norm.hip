@@ -206,14 +206,16 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_kernel(Nor
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(z[i][e]) & 0x7fffffffu);
-        const F8Scale s = f8_scale(group_max(top));
+        top = group_max(top);
+        const F8Scale s = f8_scale(top);
         if (tid % kF8Lanes == 0 && v < nvec) a.scale[t * ceil_div(a.H, kF8Block) + v / kF8Lanes] = s.scale;
         if (v * kVec < ceil_div(a.H, 16) * 16) {
           u32x2 o = {0u, 0u};
           if (s.finite) {
+            const float rest = f8_rest(top, s);
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = z[i][e] * s.pre * s.c;
+            for (int e = 0; e < 8; ++e) y[e] = f8_quotient(z[i][e], rest, s);
             o = u32x2{pack_f8x4(y[0], y[1], y[2], y[3]), pack_f8x4(y[4], y[5], y[6], y[7])};
           }
           *reinterpret_cast<u32x2*>(a.q + t * a.ldq + v * kVec) = o;

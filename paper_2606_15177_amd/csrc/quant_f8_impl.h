@@ -49,6 +49,19 @@ __device__ __forceinline__ F8Scale f8_scale(uint32_t top) {
   return s;
 }
 
+// Of any fp32 values 448 x / a is rounded to fp32 once, and then to e4m3: c is 448 / a
+// rounded, f8_rest what that leaves of it, and x c + x rest, added in one operation,
+// lies within 2^-47 of the quotient before it is rounded (2^-29 for a past 2^100, whose
+// rest is subnormal).  So ties between e4m3 values stay ties, which x c alone, rounded
+// twice, leaves in either direction.
+__device__ __forceinline__ float f8_rest(uint32_t top, const F8Scale& s) {
+  return fmaf(-s.c, __uint_as_float(top) * s.pre, kF8Max) * (s.c * (1.0f / kF8Max));
+}
+__device__ __forceinline__ float f8_quotient(float x, float rest, const F8Scale& s) {
+  const float v = x * s.pre;
+  return fmaf(v, s.c, v * rest);
+}
+
 // Four scaled values to e4m3.  (A value past 448 by fp32's rounding is still
 // nearest to 448: no clamp is needed.)
 __device__ __forceinline__ uint32_t pack_f8x4(float a, float b, float c, float d) {

@@ -3,7 +3,7 @@ against their definitions in 64 bits (bounds: f8_util.py)."""
 import pytest
 import torch
 
-from tests.f8_util import BF16, F8, FP32, blocks, by_column, e4m3_step, gen, norm_and_bounds, pad16, randn
+from tests.f8_util import BF16, F8, FP32, blocks, by_column, e4m3_step, gen, norm_and_bounds, pad16, randn, rows_exactly
 
 pytestmark = pytest.mark.gpu
 
@@ -91,6 +91,56 @@ def test_first_norm_and_unit_weights(moe, H):
     check(moe, 6, H, 1, with_y=False, post=True, gate="both")   # (neither is looked at)
     check(moe, 6, H, 2, unit=True, pad=8)
     check(moe, 6, H, 3, post=False, unit=True, with_y=False, eps=0.5)
+
+
+def quantised_of(moe, h, w):
+    """(x, q, scale) of the norm of h with weights w, eps 1 and values whose mean of
+    squares is below 2^-25: the root is 1, so that x is h w in fp32, which holds the
+    product of two bf16 values exactly."""
+    T, H = h.shape
+    assert h.double().square().mean(dim=1).max() < 2.0 ** -25
+    x, q = torch.empty_like(h), torch.zeros((T, pad16(H)), dtype=torch.uint8, device="cuda").view(F8)
+    s = torch.empty((T, blocks(H)), device="cuda")
+    moe.norm_rows(moe.norm(H, w, eps=1.0), moe.norm_io(h, x=x, q=q, scale=s))
+    return x, q, s
+
+
+def assert_quotients(moe, h, w):
+    x, q, s = quantised_of(moe, h, w)
+    exact = h.double() if w is None else h.double() * w.double()
+    assert torch.equal(x, exact.float().to(torch.bfloat16))
+    # x and its largest a have 16 significant bits at most and a tie of e4m3 has 5, so 448 x / a is a tie or 2^-22 of it
+    # away: rounded to fp32 (2^-24) it lies on the side of every tie that it is on in exact arithmetic
+    rq, rs = rows_exactly(exact)
+    assert torch.equal(s, rs)
+    off = q[:, :h.shape[1]].double() != rq
+    assert not off.any(), off.sum().item()
+
+
+@pytest.mark.parametrize("H", [128, 1000, 4100, 16400])
+def test_norm_quantises_the_rounded_quotient(moe, H):
+    """q is 448 x / a rounded to fp32 once and then to e4m3: products of 16 bits."""
+    for seed in range(3):
+        for small, large in ((2.0 ** -20, 1.0), (2.0 ** -60, 1.0), (2.0 ** -60, 2.0 ** -40), (2.0 ** -15, 2.0 ** 125)):
+            assert_quotients(moe, randn((40, H), seed, small), randn((H,), seed + 9, large))
+    assert_quotients(moe, randn((600, H), 5, 2.0 ** -20), None)
+
+
+def test_norm_quantises_ties(moe):
+    """Every tie between e4m3 values, against maxima of 448 j for odd j: x = m j has
+    448 x / a = m exactly, which goes to the even neighbour.  (m j times 448 / a rounded
+    to fp32 is m for most j only.)"""
+    ties = [(8 + m + 0.5) * 2.0 ** (e - 3) for e in range(-6, 9) for m in range(8)]
+    ties = [v for v in ties if v < 448.0] + [(m + 0.5) * 2.0 ** -9 for m in range(8)]
+    assert len(ties) == 126
+    row = torch.tensor(ties + [448.0, -448.0], dtype=torch.float64, device="cuda") * 2.0 ** -30
+    h = torch.stack([row, -row]).to(torch.bfloat16)
+    assert torch.equal(h[0].double(), row)
+    j = torch.arange(1, 256, 2, device="cuda")
+    for wide in (1, 9):   # (a wave per row, 256 threads)
+        for k in j.tolist():
+            w = torch.full((128 * wide,), float(k), dtype=torch.bfloat16, device="cuda")
+            assert_quotients(moe, h.repeat(1, wide), w)
 
 
 @pytest.mark.parametrize("T,H", [(1, 264), (300, 1000), (3, 9001)])
