@@ -283,3 +283,39 @@ def test_binding_refuses_sizes_of_31_bits(moe):
         with pytest.raises(moe.MoeError) as e:
             f(wide)
         assert e.value.status == moe.MOE_ERR_UNSUPPORTED
+
+
+# ------------------------------------------------ which kernel a layer takes ----
+
+
+ITEMS, TILES = 0, 1
+
+
+def ffn_plan(moe, conf, T, quantised=0):
+    out = (C.c_int64 * 8)()
+    assert moe._lib.moe_test_ffn_f8_plan(C.byref(moe.dims(T=T, S=1, **conf)), quantised, out) == 0
+    return out[0], out[4]
+
+
+SHARE = dict(H=7168, E=256, k=8, I=2048, E_local=32)
+LITE = dict(H=2048, E=64, k=6, I=1408, E_local=64, n_shared=2, I_shared=1408)
+WIDE = dict(H=7168, E=256, k=1, I=2048, E_local=8, n_shared=1, I_shared=8192)
+
+
+@pytest.mark.parametrize("conf,T,up,down", [
+    # routed rows alone: their mean, 85
+    (SHARE, 2719, ITEMS, ITEMS), (SHARE, 2720, TILES, TILES),
+    # a shared expert beside them: half of the rows are in one matrix of 33
+    (dict(SHARE, n_shared=1, I_shared=2048), 1000, ITEMS, ITEMS), (dict(SHARE, n_shared=1, I_shared=2048), 1500, TILES, TILES),
+    (dict(SHARE, n_shared=1, I_shared=2048), 2700, TILES, TILES), (dict(SHARE, n_shared=1, I_shared=2048), 3300, TILES, TILES),
+    # almost all of the work is shared
+    (WIDE, 200, ITEMS, ITEMS), (WIDE, 1000, TILES, TILES), (WIDE, 8000, TILES, TILES),
+    (dict(H=2048, E=64, k=4, I=1024, E_local=8, n_shared=1, I_shared=4096), 800, TILES, TILES),
+    # a quarter is; the shared experts' K is not short
+    (LITE, 400, ITEMS, ITEMS), (LITE, 600, ITEMS, ITEMS), (LITE, 900, TILES, TILES),
+    # (short K of both)
+    (dict(LITE, n_shared=1), 600, ITEMS, TILES),
+])
+def test_shared_rows_count_in_the_choice_of_kernel(moe, conf, T, up, down):
+    for quantised in (0, 1):
+        assert ffn_plan(moe, conf, T, quantised) == (up, down)

@@ -810,7 +810,9 @@ FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_
                (dict(T=3000, H=256, E=4, k=2, I=1536, E_local=4), (ITEMS, 1, 128), (ITEMS, 2, 64)),
                (dict(T=2000, H=2048, E=4, k=2, I=1544, E_local=4, n_shared=1, I_shared=1600), (TILES, 1, 192), (TILES, 1, 192)),
                (dict(T=5000, H=1160, E=16, k=3, I=904, E_local=16, n_shared=2, I_shared=456), (TILES, 1, 192), (TILES, 1, 192)),
-               (dict(T=8, H=1024, E=8, k=2, I=520, E_local=8, n_shared=1, I_shared=264), (FEWS, 2, 8), (FEWS, 2, 8))]
+               (dict(T=8, H=1024, E=8, k=2, I=520, E_local=8, n_shared=1, I_shared=264), (FEWS, 2, 8), (FEWS, 2, 8)),
+               # few routed rows beside a wide shared network
+               (dict(T=2000, H=1032, E=64, k=2, I=520, E_local=4, n_shared=1, I_shared=2056), (TILES, 1, 192), (TILES, 1, 192))]
 
 
 @pytest.mark.parametrize("case", range(len(FFN_KERNELS)))
