@@ -69,9 +69,9 @@ bool gemm_f8_takes_bf16(const Segments& seg, const GemmF8& a, const GemmF8* sh, 
 }
 
 GemmF8Plan plan_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated) {
-  if (!a.xb && takes_tiles(seg, a, sh, gated)) return {1, 1, 192, 0};
+  if (!a.xb && takes_tiles(seg, a, sh, gated)) return {1, 1, 192, 0, 0};
   const Cut c = a.xb ? few_f8_cut(seg, a, sh, gated) : items_f8_cut(seg, a, sh, gated);
-  return {a.xb ? 2 : 0, c.parts, c.rows, c.half};
+  return {a.xb ? 2 : 0, c.parts, c.rows, c.half, c.pair};
 }
 
 }  // namespace moe

@@ -270,10 +270,10 @@ bool gemm_f8_quantizes(const Segments& seg, const GemmF8& a, const GemmF8* sh);
 // launch that quantises them.
 bool gemm_f8_takes_bf16(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 // Host only: how a launch runs.  The kernel (0 items, 1 tiles, 2 items that quantise
-// their rows), the parts of K, the rows of a tile or a chunk, and whether a wave takes
-// 16 weight rows instead of 32.
+// their rows), the parts of K, the rows of a tile or a chunk, whether a wave takes
+// 16 weight rows instead of 32, and whether two workgroups share a CU by shorter rings.
 struct GemmF8Plan {
-  int kernel, parts, rows, half;
+  int kernel, parts, rows, half, pair;
 };
 GemmF8Plan plan_gemm_f8(const Segments& seg, const GemmF8& a, const GemmF8* sh, bool gated);
 

@@ -1166,23 +1166,21 @@ int moe_test_ffn_i8_plan(const moe_dims* d, int64_t out[2][4]) {
 
 // For the tests: how the e4m3 products run (moe::GemmF8Plan), of moe_linear_f8 or
 // moe_grouped_linear_f8, and of the layer's gate/up and down (of rows that come
-// quantised or not).
-int moe_test_linear_f8_plan(const moe_linear_dims* d, int grouped, int64_t out[4]) {
+// quantised or not); apart from that, whether two workgroups share a CU.
+static int linear_f8_plan(const moe_linear_dims* d, bool grouped, moe::GemmF8Plan* out) {
   static const int32_t some = 0;  // stands for device offsets
   if (d == nullptr || d->M < 1 || d->N < 1 || d->K < 1 || (grouped && d->G < 1)) return MOE_ERR_DIMS;
-  const moe::Segments seg = linear_segments(d, grouped ? &some : nullptr, grouped != 0);
+  const moe::Segments seg = linear_segments(d, grouped ? &some : nullptr, grouped);
   moe::GemmF8 a{};
   a.offsets = seg.offsets;
   a.static_rows = seg.offsets ? 0 : d->M;
   a.groups = seg.groups;
   a.K = d->K, a.N = d->N;
-  const moe::GemmF8Plan p = moe::plan_gemm_f8(seg, a, nullptr, false);
-  const int64_t v[4] = {p.kernel, p.parts, p.rows, p.half};
-  std::copy(v, v + 4, out);
+  *out = moe::plan_gemm_f8(seg, a, nullptr, false);
   return MOE_OK;
 }
 
-int moe_test_ffn_f8_plan(const moe_dims* d, int quantised, int64_t out[2][4]) {
+static int ffn_f8_plan(const moe_dims* d, bool quantised, moe::GemmF8Plan out[2]) {
   const int s = check_dims(d);
   if (s != MOE_OK) return s;
   if (d->T == 0 || check_ffn_f8_limits(d, false) != MOE_OK) return MOE_ERR_UNSUPPORTED;
@@ -1193,12 +1191,43 @@ int moe_test_ffn_f8_plan(const moe_dims* d, int quantised, int64_t out[2][4]) {
   fw.h = fw.h_sh = &h;
   FfnF8Plan p = plan_ffn_f8(d, fw, nullptr, &some, moe_weights_f8{}, nullptr, nullptr);
   quantize_in_f8_products(d, fw, quantised ? nullptr : &row, quantised ? nullptr : &row, &p);
-  const moe::GemmF8Plan g[2] = {moe::plan_gemm_f8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true),
-                                moe::plan_gemm_f8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false)};
+  out[0] = moe::plan_gemm_f8(p.routed, p.up, p.sh ? &p.sh_up : nullptr, true);
+  out[1] = moe::plan_gemm_f8(p.routed, p.dn, p.sh ? &p.sh_dn : nullptr, false);
+  return MOE_OK;
+}
+
+int moe_test_linear_f8_plan(const moe_linear_dims* d, int grouped, int64_t out[4]) {
+  moe::GemmF8Plan p;
+  const int s = linear_f8_plan(d, grouped != 0, &p);
+  if (s != MOE_OK) return s;
+  const int64_t v[4] = {p.kernel, p.parts, p.rows, p.half};
+  std::copy(v, v + 4, out);
+  return MOE_OK;
+}
+
+int moe_test_linear_f8_pair(const moe_linear_dims* d, int grouped, int64_t* out) {
+  moe::GemmF8Plan p;
+  const int s = linear_f8_plan(d, grouped != 0, &p);
+  if (s == MOE_OK) *out = p.pair;
+  return s;
+}
+
+int moe_test_ffn_f8_plan(const moe_dims* d, int quantised, int64_t out[2][4]) {
+  moe::GemmF8Plan g[2];
+  const int s = ffn_f8_plan(d, quantised != 0, g);
+  if (s != MOE_OK) return s;
   for (int i = 0; i < 2; ++i) {
     const int64_t v[4] = {g[i].kernel, g[i].parts, g[i].rows, g[i].half};
     std::copy(v, v + 4, out[i]);
   }
+  return MOE_OK;
+}
+
+int moe_test_ffn_f8_pair(const moe_dims* d, int quantised, int64_t out[2]) {
+  moe::GemmF8Plan g[2];
+  const int s = ffn_f8_plan(d, quantised != 0, g);
+  if (s != MOE_OK) return s;
+  for (int i = 0; i < 2; ++i) out[i] = g[i].pair;
   return MOE_OK;
 }
 

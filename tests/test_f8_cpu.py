@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2606_15177_amd import workloads as W
+from tests.test_gpu_f8 import FEW, FFN_KERNELS
 
 F8 = torch.float8_e4m3fn
 
@@ -319,3 +320,43 @@ WIDE = dict(H=7168, E=256, k=1, I=2048, E_local=8, n_shared=1, I_shared=8192)
 def test_shared_rows_count_in_the_choice_of_kernel(moe, conf, T, up, down):
     for quantised in (0, 1):
         assert ffn_plan(moe, conf, T, quantised) == (up, down)
+
+
+@pytest.mark.parametrize("M,N,K,G,pair", [
+    # from the longer ring, a workgroup per CU, to the shorter one, two of them: 256 items of 64 weight rows
+    (60, 12003, 4100, 0, 0), (777, 1003, 517, 0, 0), (16000, 60, 500, 0, 0), (256, 4096, 4096, 0, 0), (256, 4097, 4096, 0, 1),
+    (150, 6001, 1300, 0, 1), (193, 7300, 641, 0, 1), (400, 4100, 700, 0, 1), (64, 16384, 4096, 0, 0), (64, 16385, 4096, 0, 0),
+    (78, 3000, 700, 4, 0), (720, 1500, 1100, 12, 1), (1800, 700, 1500, 9, 1), (2500, 2100, 1700, 0, 0), (8, 517, 1003, 0, 0)])
+def test_pairs_of_items_on_a_cu(moe, M, N, K, G, pair):
+    d, out = moe.MoeLinearDims(M=M, N=N, K=K, G=G), C.c_int64(-1)
+    assert moe._lib.moe_test_linear_f8_pair(C.byref(d), int(G > 0), C.byref(out)) == 0 and out.value == pair
+
+
+def ffn_pairs(moe, conf, quantised=0):
+    out = (C.c_int64 * 2)(-1, -1)
+    assert moe._lib.moe_test_ffn_f8_pair(C.byref(moe.dims(S=1, **conf)), quantised, out) == 0
+    return tuple(out)
+
+
+def test_pairs_of_the_experts(moe):
+    """Both sides are among the layers that the GPU tests hold against 64 bits."""
+    pairs = {conf["T"]: ffn_pairs(moe, conf) for conf, up, down in FFN_KERNELS if (ITEMS, 2, 64) in (up, down)}
+    assert pairs == {3000: (0, 1), 60: (0, 0), 300: (0, 0), 150: (0, 0), 400: (1, 1)}
+
+
+# Parts of K of the products that quantise up to 8 tokens' rows (none: items), of
+# gate/up and down, by tokens.
+FEW_PARTS = [{1: (4, 4), 8: (4, 4)}, {1: (4, 4), 2: (2, 2), 3: (2, 2), 5: (1, 1), 8: (1, 1)}, {1: (2, 4), 2: (1, 4), 8: (1, 4)},
+             {1: (4, 4), 8: (4, 4)}, {1: (1, 4), 3: (1, 4), 5: (1, None), 8: (1, None)}, {1: (1, 1), 5: (1, 1), 8: (None, 1)},
+             {1: (4, 2), 2: (4, 1), 3: (4, 1), 5: (None, 1), 8: (None, 1)}]
+
+
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_parts_of_few_tokens(moe, case):
+    """The layers of few tokens that the GPU tests run reach every cut."""
+    assert len(FEW) == len(FEW_PARTS)
+    for T, want in FEW_PARTS[case].items():
+        out = (C.c_int64 * 8)()
+        assert moe._lib.moe_test_ffn_f8_plan(C.byref(moe.dims(T=T, S=1, **FEW[case])), 0, out) == 0
+        assert tuple(out[i + 1] if out[i] == 2 else None for i in (0, 4)) == want, T
+    assert ffn_plan(moe, FEW[case], 9)[0] == ITEMS

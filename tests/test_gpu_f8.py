@@ -812,7 +812,15 @@ FFN_KERNELS = [(dict(T=1500, H=1600, E=4, k=2, I=1032, E_local=4, n_shared=1, I_
                (dict(T=5000, H=1160, E=16, k=3, I=904, E_local=16, n_shared=2, I_shared=456), (TILES, 1, 192), (TILES, 1, 192)),
                (dict(T=8, H=1024, E=8, k=2, I=520, E_local=8, n_shared=1, I_shared=264), (FEWS, 2, 8), (FEWS, 2, 8)),
                # few routed rows beside a wide shared network
-               (dict(T=2000, H=1032, E=64, k=2, I=520, E_local=4, n_shared=1, I_shared=2056), (TILES, 1, 192), (TILES, 1, 192))]
+               (dict(T=2000, H=1032, E=64, k=2, I=520, E_local=4, n_shared=1, I_shared=2056), (TILES, 1, 192), (TILES, 1, 192)),
+               # gate and up in every cut of the items: K in two parts, a workgroup per CU and two, in four, whole
+               (dict(T=60, H=1032, E=4, k=2, I=1160, E_local=4), (ITEMS, 2, 64), (ITEMS, 4, 64)),
+               (dict(T=300, H=1032, E=4, k=2, I=520, E_local=4), (ITEMS, 2, 64), (ITEMS, 2, 64)),
+               (dict(T=150, H=520, E=2, k=1, I=72, E_local=2, n_shared=1, I_shared=1288), (ITEMS, 2, 64), (ITEMS, 4, 64)),
+               (dict(T=400, H=1032, E=4, k=2, I=904, E_local=4), (ITEMS, 2, 64), (ITEMS, 2, 64)),
+               (dict(T=100, H=1032, E=4, k=1, I=264, E_local=4), (ITEMS, 4, 32), (ITEMS, 4, 64)),
+               (dict(T=100, H=1032, E=4, k=1, I=776, E_local=4), (ITEMS, 4, 64), (ITEMS, 4, 64)),
+               (dict(T=100, H=1032, E=16, k=2, I=1032, E_local=16), (ITEMS, 1, 128), (ITEMS, 1, 128))]
 
 
 @pytest.mark.parametrize("case", range(len(FFN_KERNELS)))
@@ -842,3 +850,24 @@ def test_ffn_kernels(moe, case):
     assert (y[o[-1]:] == 3.0).all()
     if d.n_shared:
         assert_ffn(ysh, x, expert(q, None, "sh_", "sh_s_"))
+
+
+# Rows of up to 8 tokens that come quantised: gate and up in chunks of 8, K in four,
+# two and one parts, and the kernel that down has.
+QUANTISED = [(dict(T=8, H=1032, E=4, k=2, I=264, E_local=4), (ITEMS, 4, 8), (FEWS, 4, 8)),
+             (dict(T=8, H=1032, E=4, k=2, I=1160, E_local=4), (ITEMS, 2, 8), (FEWS, 4, 8)),
+             (dict(T=5, H=1000, E=6, k=3, I=1544, E_local=6, n_shared=1, I_shared=344), (ITEMS, 1, 128), (FEWS, 4, 5)),
+             (dict(T=5, H=256, E=4, k=2, I=9000, E_local=4), (ITEMS, 1, 128), (ITEMS, 4, 8))]
+
+
+@pytest.mark.parametrize("case", range(len(QUANTISED)))
+def test_quantised_rows_of_few_tokens(moe, case):
+    conf, up, down = QUANTISED[case]
+    d = moe.dims(S=1, **conf)
+    assert ffn_plan(moe, d, quantised=True) == (up, down)
+    _, q = layer_weights(moe, d, case)
+    logits, x = torch.randn((d.T, d.E), generator=gen(case), device="cuda"), randn((d.T, d.H), case)
+    xq, xs = moe.quantize_rows_f8(x)
+    layer = moe.MoeLayerF8(d, q)
+    layer.ws.fill_(0xff)
+    assert_layer(moe, layer.forward(logits, None, xq=xq, x_scale=xs), d, q, logits, x, None, None)
