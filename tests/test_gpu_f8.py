@@ -871,3 +871,41 @@ def test_quantised_rows_of_few_tokens(moe, case):
     layer = moe.MoeLayerF8(d, q)
     layer.ws.fill_(0xff)
     assert_layer(moe, layer.forward(logits, None, xq=xq, x_scale=xs), d, q, logits, x, None, None)
+
+
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_few_tokens_not_finite(moe, case):
+    """A token with a NaN or an infinity is NaN wherever an expert of its picks is hosted
+    or there is a shared one, and zero elsewhere; no other token changes."""
+    big = moe.dims(T=9, S=1, **FEW[case])
+    _, q = layer_weights(moe, big, case)
+    local = None if big.E_local == big.E else torch.arange(big.E_local, dtype=torch.int32, device="cuda")
+    x = randn((9, big.H), case)
+    bad = x.clone()
+    bad[1, big.H - 1], bad[4, 3] = float("inf"), float("nan")
+    for seed in range(3):
+        logits = torch.randn((9, big.E), generator=gen(seed), device="cuda")
+        if seed == 2:
+            logits[1, big.E - big.k:] += 40.0   # (token 1 picks the last experts)
+        for T in (2, 5, 8, 9):
+            d = moe.dims(T=T, S=1, **FEW[case])
+            idx, gates = torch.empty((T, d.k), dtype=torch.int32, device="cuda"), torch.empty((T, d.k), device="cuda")
+            moe.route(d, logits[:T], idx, gates)
+            hosted = (idx < d.E_local).any(dim=1) | (d.n_shared > 0)
+            layer = moe.MoeLayerF8(d, q, local)
+            for quantised in (False, True):
+                def run(rows):
+                    layer.ws.fill_(0xff)
+                    if not quantised:
+                        return layer.forward(logits[:T], None, rows[:T])
+                    xq, xs = moe.quantize_rows_f8(rows[:T])
+                    return layer.forward(logits[:T], None, xq=xq, x_scale=xs)
+                out, ref = run(bad), run(x)
+                for t in range(T):
+                    if t not in (1, 4):
+                        assert torch.equal(out[t], ref[t]), (T, quantised, t)
+                    elif hosted[t]:
+                        assert torch.isnan(out[t]).all(), (T, quantised, t)
+                    else:
+                        assert (out[t] == 0).all(), (T, quantised, t)
+    assert hosted[1] == (big.E_local == big.E)   # (both were seen where experts are missing)
