@@ -282,8 +282,10 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     static_assert(FEW ? RPI == 8 : XL * RPI * WN == XR, "whole loads fill the token rows");
     const int lr = lane / CPR;                     // row of a load
     const int wn = wave % WN, wk = wave / WN;
-    // What waits for nothing goes out first: the source rows of the token loads
-    // and of the results, then the weights of the first stages; the rest follows.
+    // The source rows of the token loads go out first, then the weights of the first
+    // stages, then the token loads.  (Those wait for all but the last of these stages'
+    // weights: the compiler counts one pass of the loop that issues them, and where there
+    // is no list of rows it waits as well.)
     auto x_row = [&](int q) { return FEW ? lr : RPI * (WN * q + wn) + lr; };  // (few rows: every wave of a K part loads them)
     int xsrc[XL];
 #pragma unroll
@@ -448,6 +450,8 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     int slot = 0;
     if constexpr (PIPE) {
       // stage j + D goes into the slot of stage j, whose fragments are in registers
+      // (the first wait does not count stage D - 1 and holds for token loads of later
+      // stages too)
       issue_x(D - 1, D - 1);
       issue_w(D - 1, D - 1);
       arrive(0);
@@ -575,7 +579,7 @@ hipError_t launch_kp(long long blocks, const ItemsF8& ma, hipStream_t st) {
 
 }  // namespace
 
-// Items of 64 rows by `cols` columns, of an evenly routed batch.
+// Items of `rows` rows by `cols` columns, of an evenly routed batch.
 static long long count_items(const Segments& seg, const GemmF8& a, const GemmF8* sh, int rows, int cols) {
   auto chunks = [&](int n) { return std::max(1, ceil_div(n, rows)); };
   return (a.offsets ? static_cast<long long>(seg.hit_groups) * chunks(seg.mean_rows) : chunks(a.static_rows)) * ceil_div(a.N, cols) +

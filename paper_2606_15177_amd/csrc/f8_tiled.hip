@@ -12,9 +12,10 @@
 // (gated two) per stage, held across the lanes for 64 stages, the rows' come with the
 // stage.
 //
-// Bound: the board's power, and issue.  431 to 443 us (2.2 PFLOP/s) at 1.7 to 1.9 GHz
-// with the MFMAs busy 53 % of the time; the library's product of e4m3 with one scale
-// per tensor, which adds nothing beside its MFMAs, 303.  Of a stage's 1.48 us (256
+// Bound: the board's power, and issue.  In a row (12000 of them, 5 s) 401 to 411 us (2.4
+// PFLOP/s); the first 30 after the card idled up to 575, in turn with other work 425
+// to 443 at 1.7 to 1.9 GHz, with the MFMAs busy 53 % of the time; the library's product
+// of e4m3 with one scale per tensor, which adds nothing beside its MFMAs, 303.  Of a stage's 1.48 us (256
 // workgroups; 1.09 with 64, whose clock is higher) copies with a part left out take
 // 1.00 without the loads into LDS, 1.39 without the fragments' reads, 1.22 without the
 // additions, 0.88 with the loads alone, 0.82 with the MFMAs alone: what moves costs

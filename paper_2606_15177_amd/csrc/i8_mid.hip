@@ -271,8 +271,9 @@ __global__ __launch_bounds__(kItemThreads) __attribute__((amdgpu_waves_per_eu(2,
     static_assert(FEW ? RPI == 8 : XL * RPI * WN == XR, "whole loads fill the token rows");
     const int lr = lane / CPR;                     // row of a load
     const int wn = wave % WN, wk = wave / WN;
-    // What waits for nothing goes out first: the source rows of the token loads
-    // and of the results, then the weights of the first stages; the rest follows.
+    // The source rows of the token loads and of the results go out first, then the
+    // weights of the first stages, then the rest, which waits for all but the last of
+    // these stages' weights: the compiler counts one pass of the loop that issues them.
     auto x_row = [&](int q) { return FEW ? lr : RPI * (WN * q + wn) + lr; };  // (few rows: every wave of a K part loads them)
     int xsrc[XL], src[NSUB];
 #pragma unroll
