@@ -32,6 +32,8 @@ namespace {
 //     229 and 189; 20 of K 2056, N 776, shared 2320, at 110 93 and 84;
 //   short K of the routed rows alone (items, down in tiles): 64 of K 1408 with a shared K of
 //     2816 at 48 161 and 161, with uneven rows 162 and 168, at 73 175 and 180, 174 and 187.
+//   Of 475 random layers with shared experts the routed rows alone chose another kernel for
+//   44; by all rows 43 of those are faster, 9 % on average, and one 1 % slower.
 constexpr int kMeanRows = 85, kMeanShort = 24;
 constexpr int kShortK = 1500;
 constexpr long long kFewShort = 400;
